@@ -19,6 +19,8 @@ GCN_OK, GCN_EINVAL, GCN_ESHAPE, GCN_EWORKSPACE, GCN_EHIP, GCN_EUNSUPPORTED = 0, 
 GCN_F32, GCN_BF16 = 0, 1
 GCN_AGGREGATE_FIRST, GCN_TRANSFORM_FIRST = 0, 1
 GCN_SOFTMAX_CE, GCN_SIGMOID_BCE = 0, 1
+GCN_ROWS_F32, GCN_ROWS_BF16 = 0, 1
+ROWS8_BLOCK = 128                         # columns under one scale of 8-bit rows
 LOSS_KIND = {"ce": GCN_SOFTMAX_CE, "bce": GCN_SIGMOID_BCE}
 GCN_NOALLOC_SCRATCH_BYTES = 64 << 20      # the static scratch array of gcn_aggregate_noalloc
 PREC = {"f32": GCN_F32, "fp32": GCN_F32, "bf16": GCN_BF16}
@@ -34,6 +36,17 @@ class gcn_csr(ctypes.Structure):
     _fields_ = [("n_rows", ctypes.c_int32), ("n_cols", ctypes.c_int32), ("nnz", ctypes.c_int32),
                 ("indptr", ctypes.c_void_p), ("indices", ctypes.c_void_p), ("vals", ctypes.c_void_p),
                 ("indices16", ctypes.c_void_p)]
+
+
+class gcn_rows8(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("f", ctypes.c_int32), ("ldq", ctypes.c_int32), ("ldscale", ctypes.c_int32),
+                ("q", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+
+
+class gcn_weights8(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_int32), ("N", ctypes.c_int32), ("ldq", ctypes.c_int32), ("ldqT", ctypes.c_int32),
+                ("ldscale", ctypes.c_int32), ("q", ctypes.c_void_p), ("qT", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p)]
 
 
 class gcn_sampler_params(ctypes.Structure):
@@ -64,6 +77,8 @@ _I32 = ctypes.c_int32
 _I64 = ctypes.c_int64
 _SZ = ctypes.c_size_t
 _CSRP = ctypes.POINTER(gcn_csr)
+_R8P = ctypes.POINTER(gcn_rows8)
+_W8P = ctypes.POINTER(gcn_weights8)
 
 _SIGNATURES = {
     "gcn_last_error": (ctypes.c_char_p, []),
@@ -110,6 +125,20 @@ _SIGNATURES = {
                                             _P, _SZ, _P]),
     "gcn_csr_pattern_symmetric_host": (ctypes.c_int, [_I32, _P, _P]),
     "gcn_gather_rows": (ctypes.c_int, [_P, _I32, _I32, _I64, _P, _I32, _P, _I64, _P]),
+    # gcn_rows8.h
+    "gcn_rows8_pack": (ctypes.c_int, [_P, ctypes.c_int, _I32, _R8P, _P]),
+    "gcn_rows8_unpack": (ctypes.c_int, [_R8P, _P, ctypes.c_int, _I32, _P]),
+    "gcn_weights8_pack": (ctypes.c_int, [_P, ctypes.c_int, _I32, _W8P, _P]),
+    "gcn_rows8_product_workspace_bytes": (_SZ, [_I32, _I32, _I32]),
+    "gcn_rows8_product": (ctypes.c_int, [_R8P, _W8P, ctypes.c_int, _P, ctypes.c_int, _P, ctypes.c_int, _I32, _P, _SZ,
+                                         _P]),
+    "gcn_rows8_weight_grad_workspace_bytes": (_SZ, [_I32, _I32, _I32]),
+    "gcn_rows8_weight_grad": (ctypes.c_int, [_R8P, _P, _I32, _P, ctypes.c_int, _I32, _I32, _P, _I32, _P, _R8P, _P, _SZ,
+                                             _P]),
+    # gcn_classes.h
+    "gcn_class_loss_workspace_bytes": (_SZ, [_I32, _I32, _I32, ctypes.c_int, ctypes.c_int]),
+    "gcn_class_loss": (ctypes.c_int, [_P, _I32, _I32, _I32, _P, _P, _I32, _P, ctypes.c_int, _P, _P, _P, _I32, _P, _P,
+                                      _P, _SZ, _P]),
     # gcn_optim.h
     "gcn_adam_update": (ctypes.c_int, [_P, _P, _P, _P, _I64, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                                        ctypes.c_double, _I32, _P]),
@@ -520,6 +549,186 @@ def gcn_gather_rows(X: torch.Tensor, rows: torch.Tensor, count: int, out: torch.
     _check(lib().gcn_gather_rows(_ptr(X2), int(X2.shape[0]), width, _ld(X2), _ptr(rows), int(count), _ptr(o2),
                                  _ld(o2), _stream(stream)), "gcn_gather_rows")
     return out
+
+
+# ---------------------------------------------------------------- 8-bit rows
+def _rows_type(t: torch.Tensor, name: str) -> int:
+    if not t.is_cuda or t.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"{name} must be a float32 or bfloat16 CUDA/HIP tensor")
+    return GCN_ROWS_F32 if t.dtype == torch.float32 else GCN_ROWS_BF16
+
+
+def _want(t: torch.Tensor, name: str, dtype, shape):
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise TypeError(f"{name} must be a {dtype} CUDA/HIP tensor of shape {tuple(shape)}")
+    return t
+
+
+def _blocks8(f: int) -> int:
+    return (f + ROWS8_BLOCK - 1) // ROWS8_BLOCK
+
+
+def _kept8(rows: int, cols: int, device) -> torch.Tensor:
+    """Zeroed e4m3 rows of whole blocks, as a view of their first `cols` columns."""
+    kept = torch.zeros((max(rows, 1), _blocks8(cols) * ROWS8_BLOCK), dtype=torch.uint8, device=device)
+    return kept.view(torch.float8_e4m3fn)[:rows, :cols]
+
+
+def _ld8(t: torch.Tensor, name: str) -> int:
+    if t.dim() != 2 or t.dtype != torch.float8_e4m3fn or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise TypeError(f"{name} must be a row-major float8_e4m3fn CUDA/HIP tensor")
+    return int(t.stride(0))
+
+
+class Rows8:
+    """n x f activations in 8 bits: `values` (float8_e4m3fn, n x f, in rows of
+    whole 128-column blocks) and `scale` (uint8, n x ceil(f / 128)); an element
+    stands for values * 2^(scale - 127)."""
+
+    def __init__(self, n: int, f: int, device="cuda"):
+        d = torch.device(device)
+        self._set(_kept8(n, f, d), torch.empty((n, _blocks8(f)), dtype=torch.uint8, device=d))
+
+    @classmethod
+    def of(cls, values: torch.Tensor, scale: torch.Tensor) -> "Rows8":
+        """Rows kept elsewhere: `values` a view of rows of whole blocks whose
+        columns past f are zero (their stride tells the length of a row)."""
+        self = cls.__new__(cls)
+        self._set(values, scale)
+        return self
+
+    def _set(self, values, scale):
+        self.n, self.f = int(values.shape[0]), int(values.shape[1])
+        self.values, self.scale = values, scale
+        if scale.dtype != torch.uint8 or tuple(scale.shape) != (self.n, _blocks8(self.f)) or not scale.is_cuda \
+                or (self.n and not scale.is_contiguous()):
+            raise TypeError("scale must be a contiguous uint8 CUDA/HIP tensor, n x ceil(f / 128)")
+        self.struct = gcn_rows8(self.n, self.f, _ld8(values, "values"), _blocks8(self.f), values.data_ptr(),
+                                scale.data_ptr())
+
+
+class Weights8:
+    """K x N weights in 8 bits, one scale per 128 x 128 block: `values` (K x N)
+    and `values_t` (N x K), float8_e4m3fn in rows of whole blocks, and `scale`
+    (uint8, ceil(K / 128) x ceil(N / 128))."""
+
+    def __init__(self, K: int, N: int, device="cuda"):
+        d = torch.device(device)
+        self._set(_kept8(K, N, d), _kept8(N, K, d),
+                  torch.empty((_blocks8(K), _blocks8(N)), dtype=torch.uint8, device=d))
+
+    @classmethod
+    def of(cls, values: torch.Tensor, values_t: torch.Tensor, scale: torch.Tensor) -> "Weights8":
+        self = cls.__new__(cls)
+        self._set(values, values_t, scale)
+        return self
+
+    def _set(self, values, values_t, scale):
+        self.K, self.N = int(values.shape[0]), int(values.shape[1])
+        self.values, self.values_t, self.scale = values, values_t, scale
+        if tuple(values_t.shape) != (self.N, self.K):
+            raise ValueError("values_t must be N x K")
+        _want(scale, "scale", torch.uint8, (_blocks8(self.K), _blocks8(self.N)))
+        if not scale.is_contiguous():
+            raise ValueError("scale must be contiguous")
+        self.struct = gcn_weights8(self.K, self.N, _ld8(values, "values"), _ld8(values_t, "values_t"),
+                                   _blocks8(self.N), values.data_ptr(), values_t.data_ptr(), scale.data_ptr())
+
+
+def gcn_rows8_pack(X: torch.Tensor, out: Rows8, stream=None) -> Rows8:
+    if tuple(X.shape) != (out.n, out.f):
+        raise ValueError("X and the 8-bit rows differ in shape")
+    _check(lib().gcn_rows8_pack(_ptr(X), _rows_type(X, "X"), _ld(X), ctypes.byref(out.struct), _stream(stream)),
+           "gcn_rows8_pack")
+    return out
+
+
+def gcn_rows8_unpack(rows: Rows8, out: torch.Tensor, stream=None) -> torch.Tensor:
+    if tuple(out.shape) != (rows.n, rows.f):
+        raise ValueError("out and the 8-bit rows differ in shape")
+    _check(lib().gcn_rows8_unpack(ctypes.byref(rows.struct), _ptr(out), _rows_type(out, "out"), _ld(out),
+                                  _stream(stream)), "gcn_rows8_unpack")
+    return out
+
+
+def gcn_weights8_pack(W: torch.Tensor, out: Weights8, stream=None) -> Weights8:
+    if tuple(W.shape) != (out.K, out.N):
+        raise ValueError("W and the 8-bit weights differ in shape")
+    _check(lib().gcn_weights8_pack(_ptr(W), _rows_type(W, "W"), _ld(W), ctypes.byref(out.struct), _stream(stream)),
+           "gcn_weights8_pack")
+    return out
+
+
+def gcn_rows8_product(X8: Rows8, W8: Weights8, Y: torch.Tensor, ws: Workspace, bias: Optional[torch.Tensor] = None,
+                      relu: bool = False, transpose: bool = False, stream=None) -> torch.Tensor:
+    """Y = act(X8 W8 + bias), or act(X8 W8^T + bias) with transpose."""
+    L = lib()
+    cols = W8.K if transpose else W8.N
+    if tuple(Y.shape) != (X8.n, cols):
+        raise ValueError("Y's shape does not fit the operands")
+    if bias is not None:
+        _dev_f32(bias, "bias")
+        if bias.numel() != cols or not bias.is_contiguous():
+            raise ValueError("bias needs one contiguous element per column of Y")
+    w, wb = ws.args(L.gcn_rows8_product_workspace_bytes(X8.n, W8.K, W8.N))
+    _check(L.gcn_rows8_product(ctypes.byref(X8.struct), ctypes.byref(W8.struct), int(bool(transpose)), _ptr(bias),
+                               int(bool(relu)), _ptr(Y), _rows_type(Y, "Y"), _ld(Y), w, wb, _stream(stream)),
+           "gcn_rows8_product")
+    return Y
+
+
+def gcn_rows8_weight_grad(X8: Rows8, dY: torch.Tensor, dW: torch.Tensor, ws: Workspace,
+                          db: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                          dZ8: Optional[Rows8] = None, stream=None):
+    """dW = X8^T dZ, db = sum_i dZ_i, dZ8 = the 8-bit rows of dZ, with dZ = dY
+    where mask (the values of the layer output's Rows8, or a column range of
+    them) is positive, or everywhere without a mask."""
+    L = lib()
+    N = int(dY.shape[1])
+    if dY.shape[0] != X8.n or tuple(dW.shape) != (X8.f, N):
+        raise ValueError("dY and dW must be n x N and f x N")
+    _dev_f32(dW, "dW")
+    if db is not None:
+        _want(db, "db", torch.float32, (N,))
+        if not db.is_contiguous():
+            raise ValueError("db must be contiguous")
+    ldm = 0
+    if mask is not None:
+        if tuple(mask.shape) != (X8.n, N):
+            raise ValueError("mask and dY differ in shape")
+        ldm = max(_ld8(mask, "mask"), N)
+    w, wb = ws.args(L.gcn_rows8_weight_grad_workspace_bytes(X8.n, X8.f, N))
+    _check(L.gcn_rows8_weight_grad(ctypes.byref(X8.struct), _ptr(mask), ldm, _ptr(dY), _rows_type(dY, "dY"), _ld(dY), N,
+                                   _ptr(dW), _ld(dW), _ptr(db), None if dZ8 is None else ctypes.byref(dZ8.struct), w,
+                                   wb, _stream(stream)), "gcn_rows8_weight_grad")
+
+
+# ------------------------------------------------------------- many classes
+def gcn_class_loss(HL: torch.Tensor, W_pred: torch.Tensor, b_pred: Optional[torch.Tensor], labels: torch.Tensor,
+                   loss: torch.Tensor, ws: Workspace, row_loss: Optional[torch.Tensor] = None,
+                   dHL: Optional[torch.Tensor] = None, dW_pred: Optional[torch.Tensor] = None,
+                   db_pred: Optional[torch.Tensor] = None, stream=None):
+    """Softmax cross entropy over many classes without keeping the logits; the
+    gradients are written when dHL, dW_pred and db_pred are given."""
+    L = lib()
+    t = _rows_type(HL, "HL")
+    n, f, C = int(HL.shape[0]), int(HL.shape[1]), int(W_pred.shape[1])
+    _want(W_pred, "W_pred", HL.dtype, (f, C))
+    _want(labels, "labels", torch.int32, (n,))
+    _want(loss, "loss", torch.float32, (1,))
+    for x, nm, dt, shape in ((b_pred, "b_pred", torch.float32, (C,)), (row_loss, "row_loss", torch.float32, (n,)),
+                             (dHL, "dHL", HL.dtype, (n, f)), (dW_pred, "dW_pred", HL.dtype, (f, C)),
+                             (db_pred, "db_pred", torch.float32, (C,))):
+        if x is not None:
+            _want(x, nm, dt, shape)
+    for x, nm in ((W_pred, "W_pred"), (labels, "labels"), (b_pred, "b_pred"), (row_loss, "row_loss"),
+                  (dW_pred, "dW_pred"), (db_pred, "db_pred")):
+        if x is not None and not x.is_contiguous():
+            raise ValueError(f"{nm} must be contiguous")
+    w, wb = ws.args(L.gcn_class_loss_workspace_bytes(n, f, C, t, int(dW_pred is not None)))
+    _check(L.gcn_class_loss(_ptr(HL), n, f, _ld(HL), _ptr(W_pred), _ptr(b_pred), C, _ptr(labels), t, _ptr(loss),
+                            _ptr(row_loss), _ptr(dHL), 0 if dHL is None else _ld(dHL), _ptr(dW_pred), _ptr(db_pred), w,
+                            wb, _stream(stream)), "gcn_class_loss")
 
 
 # ---------------------------------------------------------------- optimiser

@@ -1,0 +1,485 @@
+// PREDICT and softmax cross entropy over many classes in pieces of the
+// classes, without keeping the logits (gcn_classes.h).
+//
+//   pass 1, per piece: logits of the piece in the product's registers; per row
+//     and column tile their maximum and the sum of exponentials relative to
+//     it, joined into the row's running maximum and sum
+//   loss: row_loss = max + log(sum) - label's logit
+//   pass 2, per piece: the logits again, G = (softmax - onehot) / n_l in the
+//     same registers, written as bfloat16 rows and transposed rows; then
+//     dHL += G W_piece^T and dW_piece = HL^T G.
+// Every product is C = A B^T of operands contiguous along the contraction, so
+// W's piece is transposed once a pass and HL once a call.
+#include <algorithm>
+
+#include "gcn_classes.h"
+#include "rows8.h"
+
+namespace gcn {
+namespace {
+
+constexpr int kTB = 256;
+
+__device__ __forceinline__ bool has_label(int32_t l, int32_t C) { return l >= 0 && l < C; }
+
+// inv_count = 1 / max(1, rows with a label), by one workgroup
+__global__ __launch_bounds__(1024) void count_kernel(int32_t n, int32_t C, const int32_t *labels, float *inv_count) {
+    __shared__ int32_t part[16];
+    int32_t k = 0;
+    for (int32_t i = threadIdx.x; i < n; i += 1024) k += has_label(labels[i], C);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) k += __shfl_xor(k, d);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = k;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int32_t t = 0;
+        for (int w = 0; w < 16; ++w) t += part[w];
+        inv_count[0] = (float)(1.0 / (double)max(t, 1));
+    }
+}
+
+// dst [rows x ldd] = src [rows x cols] (lds), zero past cols and in rows
+// without a label
+template <class T>
+__global__ __launch_bounds__(kTB) void copy_rows_kernel(int32_t rows, int32_t cols, const T *src, int64_t lds, T *dst,
+                                                        int64_t ldd, const int32_t *labels, int32_t C) {
+    const int64_t total = (int64_t)rows * ldd;
+    for (int64_t i = (int64_t)blockIdx.x * kTB + threadIdx.x; i < total; i += (int64_t)gridDim.x * kTB) {
+        const int64_t r = i / ldd;
+        const int32_t c = (int32_t)(i - r * ldd);
+        dst[i] = c < cols && (!labels || has_label(labels[r], C)) ? src[r * lds + c] : (T)0;
+    }
+}
+
+// dst [cols x ldd] = src^T, src [rows x cols] (lds) bfloat16; columns rows ..
+// ldd - 1 of dst zero, and those of rows without a label
+__global__ __launch_bounds__(kTB) void transpose_kernel(int32_t rows, int32_t cols, const uint16_t *src, int64_t lds,
+                                                        uint16_t *dst, int64_t ldd, const int32_t *labels, int32_t C) {
+    __shared__ uint16_t t[64][66];
+    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
+    for (int i = threadIdx.x; i < 64 * 64; i += kTB) {
+        const int64_t r = r0 + i / 64, c = c0 + i % 64;
+        t[i / 64][i % 64] = r < rows && c < cols && (!labels || has_label(labels[r], C)) ? src[r * lds + c] : (uint16_t)0;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 64 * 64; i += kTB) {
+        const int64_t c = c0 + i / 64, r = r0 + i % 64;
+        if (c < cols && r < ldd) dst[c * ldd + r] = t[i % 64][i / 64];
+    }
+}
+
+// the tiles' maxima and sums of one piece joined into the running ones
+__global__ __launch_bounds__(kTB) void join_kernel(int32_t n, int32_t tiles, const float *tile_max,
+                                                   const float *tile_sum, float *run_max, float *run_sum, int first) {
+    const int32_t i = blockIdx.x * kTB + threadIdx.x;
+    if (i >= n) return;
+    float m = first ? -INFINITY : run_max[i], s = first ? 0.0f : run_sum[i];
+    for (int32_t t = 0; t < tiles; ++t) {
+        const float q = tile_max[(int64_t)t * n + i], u = tile_sum[(int64_t)t * n + i];
+        const float b = fmaxf(m, q);
+        s = (m == b ? s : s * __expf(m - b)) + (q == b ? u : u * __expf(q - b));
+        m = b;
+    }
+    run_max[i] = m;
+    run_sum[i] = s;
+}
+
+// logits of one piece (float32 rows) joined into the running maximum and sum,
+// a workgroup a row
+__global__ __launch_bounds__(kTB) void stats_rows_kernel(int32_t P, const float *X, int64_t ldx, const int32_t *labels,
+                                                         int32_t class0, int32_t C, float *run_max, float *run_sum,
+                                                         float *label_logit, int first) {
+    __shared__ float sm[kTB / 64], ss[kTB / 64];
+    const int32_t row = blockIdx.x;
+    const float *x = X + row * ldx;
+    float m = -INFINITY, s = 0.0f;
+    for (int32_t c = threadIdx.x; c < P; c += kTB) {
+        const float v = x[c], b = fmaxf(m, v);
+        if (!(v <= m)) {   // a new maximum (or NaN, which the sum keeps)
+            s = (m == -INFINITY ? 0.0f : s * expf(m - b)) + expf(v - (b == -INFINITY ? 0.0f : b));
+            m = b;
+        } else {
+            s += m == -INFINITY ? 0.0f : expf(v - m);
+        }
+    }
+    auto join = [](float &m, float &s, float q, float u) {
+        const float b = fmaxf(m, q);
+        s = (m == b ? s : s * expf(m - b)) + (q == b ? u : u * expf(q - b));
+        m = b;
+    };
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const float q = __shfl_xor(m, d), u = __shfl_xor(s, d);
+        join(m, s, q, u);
+    }
+    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m, ss[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < kTB / 64; ++w) join(m, s, sm[w], ss[w]);
+    if (!first) join(m, s, run_max[row], run_sum[row]);
+    run_max[row] = m;
+    run_sum[row] = s;
+    const int32_t l = labels[row];
+    if (has_label(l, C) && l >= class0 && l - class0 < P) label_logit[row] = x[l - class0];
+}
+
+__global__ __launch_bounds__(kTB) void grad_rows_kernel(int32_t P, float *X, int64_t ldx, const int32_t *labels,
+                                                        int32_t class0, int32_t C, const float *lse,
+                                                        const float *inv_count) {
+    const int32_t row = blockIdx.x;
+    float *x = X + row * ldx;
+    const int32_t l = labels[row];
+    const bool has = has_label(l, C);
+    const float z = lse[row], inv = inv_count[0];
+    for (int32_t c = threadIdx.x; c < P; c += kTB)
+        x[c] = has ? (expf(x[c] - z) - (class0 + c == l ? 1.0f : 0.0f)) * inv : 0.0f;
+}
+
+// lse, the rows' losses and their mean, by one workgroup in a fixed order
+__global__ __launch_bounds__(1024) void loss_kernel(int32_t n, int32_t C, const int32_t *labels, const float *run_max,
+                                                    const float *run_sum, const float *label_logit, float *lse,
+                                                    float *row_loss, const float *inv_count, float *loss) {
+    __shared__ double part[16];
+    double t = 0.0;
+    for (int32_t i = threadIdx.x; i < n; i += 1024) {
+        const float z = run_max[i] + logf(run_sum[i]);
+        lse[i] = z;
+        const bool has = has_label(labels[i], C);
+        const float v = has ? z - label_logit[i] : 0.0f;
+        if (row_loss) row_loss[i] = v;
+        t += v;
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) t += __shfl_xor(t, d);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = t;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double a = 0.0;
+        for (int w = 0; w < 16; ++w) a += part[w];
+        loss[0] = (float)(a * (double)inv_count[0]);
+    }
+}
+
+__global__ __launch_bounds__(kTB) void add_kernel(int32_t rows, int32_t cols, const float *x, float *y, int64_t ldy) {
+    const int64_t total = (int64_t)rows * cols;
+    for (int64_t i = (int64_t)blockIdx.x * kTB + threadIdx.x; i < total; i += (int64_t)gridDim.x * kTB)
+        y[i / cols * ldy + i % cols] += x[i];
+}
+
+__global__ __launch_bounds__(kTB) void zero_kernel(uint16_t *x, int64_t rows, int64_t cols, int64_t ld) {
+    for (int64_t i = (int64_t)blockIdx.x * kTB + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * kTB)
+        x[i / cols * ld + i % cols] = 0;
+}
+
+unsigned grid_of(int64_t work, int64_t most = 8192) {
+    return (unsigned)std::max<int64_t>(1, std::min(most, (work + kTB - 1) / kTB));
+}
+int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+// How a call is cut and what of the workspace it uses.
+struct Plan {
+    int64_t fp, np;            // f and n in whole 64-column pieces (bfloat16)
+    int32_t piece, pieces;     // classes per piece
+    int32_t split_h, split_w;  // parts of the two gradient products
+    size_t total;
+};
+struct Buffers {
+    float *inv_count, *run_max, *run_sum, *label_logit, *lse, *tile_max, *tile_sum, *colpart, *acc, *part, *X, *tmp;
+    uint16_t *H, *HT, *WT, *W, *G, *GT;
+    float *Hz;
+    void *gemm_ws, *col_ws;
+    size_t gemm_bytes, col_bytes;
+};
+
+GemmProblem dw_f32(int32_t f, int32_t P, int32_t n) {
+    GemmProblem w{};
+    w.M = f;
+    w.N = P;
+    w.seg[0].K = n;
+    return w;
+}
+
+// The elements of a piece: bfloat16 G and its transpose take 4 bytes each
+// together, float32 logits 4.
+constexpr int64_t kPieceElems = (int64_t)1 << 28, kPieceElemsF32 = (int64_t)1 << 26;
+
+Plan plan_of(int32_t n, int32_t f, int32_t C, bool bf, bool grad, void *ws, size_t ws_bytes, Buffers &b) {
+    Plan p{};
+    Arena ar(ws, ws_bytes);
+    const int64_t rows = std::max(n, 1);
+    p.fp = up(f, 64);
+    p.np = up(rows, 64);
+    int64_t piece = std::max<int64_t>(256, (bf ? kPieceElems / p.np : kPieceElemsF32 / rows) / 256 * 256);
+    piece = std::min<int64_t>(piece, up(C, 256));
+    p.pieces = (int32_t)((C + piece - 1) / piece);
+    p.piece = (int32_t)std::min<int64_t>(piece, C);
+    b = Buffers{};
+    b.inv_count = ar.take<float>(1);
+    b.run_max = ar.take<float>(rows);
+    b.run_sum = ar.take<float>(rows);
+    b.label_logit = ar.take<float>(rows);
+    b.lse = ar.take<float>(rows);
+    if (bf) {
+        const TileShape t = tile_shape(TILE_BF16, TILE_STATS, n, p.piece, (int32_t)(p.fp / 64));
+        const int64_t tn = (p.piece + t.n - 1) / t.n;
+        b.tile_max = ar.take<float>(tn * rows);
+        b.tile_sum = ar.take<float>(tn * rows);
+        b.H = ar.take<uint16_t>(rows * p.fp);
+        b.WT = ar.take<uint16_t>((size_t)p.piece * p.fp);
+        if (grad) {
+            const int64_t pp = up(p.piece, 64);
+            const TileShape tg = tile_shape(TILE_BF16, TILE_GRAD, n, p.piece, (int32_t)(p.fp / 64));
+            b.HT = ar.take<uint16_t>(f * p.np);
+            b.W = ar.take<uint16_t>(f * pp);
+            b.G = ar.take<uint16_t>(rows * pp);
+            b.GT = ar.take<uint16_t>((size_t)p.piece * p.np);
+            b.colpart = ar.take<float>((rows + tg.m - 1) / tg.m * p.piece);
+            p.split_h = tile_splits(TILE_BF16, n, f, (int32_t)(pp / 64));
+            p.split_w = tile_splits(TILE_BF16, f, p.piece, (int32_t)(p.np / 64));
+            b.acc = ar.take<float>((size_t)p.split_h * rows * f);
+            if (p.split_w > 1) b.part = ar.take<float>((size_t)p.split_w * f * p.piece);
+        }
+    } else {
+        b.Hz = ar.take<float>(rows * f);
+        b.X = ar.take<float>(rows * p.piece);
+        if (grad) {
+            const GemmProblem w = dw_f32(f, p.piece, n);
+            p.split_w = gemm_pick_split(1, &w, true);
+            b.gemm_bytes = gemm_workspace_bytes(1, &w, p.split_w);
+            b.gemm_ws = b.gemm_bytes ? ar.take<char>(b.gemm_bytes) : nullptr;
+            b.col_bytes = std::max(colsum_workspace_bytes(n, p.piece),
+                                   colsum_workspace_bytes(n, C - (p.pieces - 1) * p.piece));
+            b.col_ws = ar.take<char>(b.col_bytes);
+            if (p.pieces > 1) b.tmp = ar.take<float>(rows * f);
+        }
+    }
+    p.total = ar.used + 256;
+    return p;
+}
+
+int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, int32_t f, int64_t ldhl, const uint16_t *W,
+              const float *bias, int32_t C, const int32_t *labels, float *loss, float *row_loss, uint16_t *dHL,
+              int64_t lddhl, uint16_t *dW, float *db, hipStream_t s) {
+    int rc;
+    {
+        ProfScope prof(K_CLASS_PREP, s, 0.0, 4.0 * n * f);
+        hipLaunchKernelGGL(count_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, b.inv_count);
+        hipLaunchKernelGGL(copy_rows_kernel<uint16_t>, dim3(grid_of(n * p.fp)), dim3(kTB), 0, s, n, f, HL, ldhl, b.H,
+                           p.fp, labels, C);
+        if (dHL)
+            hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)(p.np / 64), (unsigned)((f + 63) / 64)), dim3(kTB), 0, s,
+                               n, f, HL, ldhl, b.HT, p.np, labels, C);
+        GCN_LAUNCH_CHECK("class_prep");
+    }
+    auto logits = [&](int32_t c0, int32_t P) {
+        ProfScope prof(K_CLASS_PREP, s, 0.0, 4.0 * f * P);
+        hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)(p.fp / 64), (unsigned)((P + 63) / 64)), dim3(kTB), 0, s, f, P,
+                           W + c0, (int64_t)C, b.WT, p.fp, (const int32_t *)nullptr, 0);
+        TileProduct t{};
+        t.A = (const uint8_t *)b.H;
+        t.lda = 2 * p.fp;
+        t.B = (const uint8_t *)b.WT;
+        t.ldb = 2 * p.fp;
+        t.M = n;
+        t.N = P;
+        t.kt = (int32_t)(p.fp / 64);
+        t.splits = 1;
+        t.bias = bias ? bias + c0 : nullptr;
+        t.labels = labels;
+        t.class0 = c0;
+        t.classes = C;
+        return t;
+    };
+    for (int32_t i = 0; i < p.pieces; ++i) {
+        const int32_t c0 = i * p.piece, P = std::min(p.piece, C - c0);
+        TileProduct t = logits(c0, P);
+        t.tile_max = b.tile_max;
+        t.tile_sum = b.tile_sum;
+        t.label_logit = b.label_logit;
+        {
+            ProfScope prof(K_CLASS_STATS, s, 2.0 * n * f * P, 2.0 * ((double)n + P) * f);
+            if ((rc = tile_product(TILE_BF16, TILE_STATS, t, s))) return rc;
+        }
+        const TileShape sh = tile_shape(TILE_BF16, TILE_STATS, n, P, t.kt);
+        ProfScope prof(K_CLASS_PREP, s, 0.0, 8.0 * n * ((P + sh.n - 1) / sh.n));
+        hipLaunchKernelGGL(join_kernel, dim3((unsigned)((n + kTB - 1) / kTB)), dim3(kTB), 0, s, n, (P + sh.n - 1) / sh.n,
+                           b.tile_max, b.tile_sum, b.run_max, b.run_sum, i == 0);
+        GCN_LAUNCH_CHECK("join_kernel");
+    }
+    hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, b.run_max, b.run_sum, b.label_logit, b.lse,
+                       row_loss, b.inv_count, loss);
+    GCN_LAUNCH_CHECK("loss_kernel");
+    if (!dHL) return GCN_OK;
+    for (int32_t i = 0; i < p.pieces; ++i) {
+        const int32_t c0 = i * p.piece, P = std::min(p.piece, C - c0);
+        const int64_t pp = up(P, 64);
+        TileProduct t = logits(c0, P);
+        t.lse = b.lse;
+        t.inv_count = b.inv_count;
+        t.G = b.G;
+        t.ldg = pp;
+        t.GT = b.GT;
+        t.ldgt = p.np;
+        t.colpart = b.colpart;
+        {
+            ProfScope prof(K_CLASS_GRAD, s, 2.0 * n * f * P, 2.0 * ((double)n + P) * f + 4.0 * n * P);
+            if ((rc = tile_product(TILE_BF16, TILE_GRAD, t, s))) return rc;
+        }
+        const TileShape sh = tile_shape(TILE_BF16, TILE_GRAD, n, P, t.kt);
+        if ((rc = colsum_reduce_rows((n + sh.m - 1) / sh.m, P, b.colpart, db + c0, s))) return rc;
+        hipLaunchKernelGGL(copy_rows_kernel<uint16_t>, dim3(grid_of(f * pp)), dim3(kTB), 0, s, f, P, W + c0, (int64_t)C,
+                           b.W, pp, (const int32_t *)nullptr, 0);
+        GCN_LAUNCH_CHECK("copy_rows_kernel");
+        ProfScope prof(K_CLASS_PRODUCT, s, 4.0 * n * f * P, 4.0 * n * P);
+        TileProduct h{};
+        h.A = (const uint8_t *)b.G;
+        h.lda = 2 * pp;
+        h.B = (const uint8_t *)b.W;
+        h.ldb = 2 * pp;
+        h.M = n;
+        h.N = f;
+        h.kt = (int32_t)(pp / 64);
+        h.splits = p.split_h;
+        h.acc = b.acc;
+        h.accumulate = i > 0;
+        if ((rc = tile_product(TILE_BF16, TILE_PARTIAL, h, s))) return rc;
+        TileProduct w{};
+        w.A = (const uint8_t *)b.HT;
+        w.lda = 2 * p.np;
+        w.B = (const uint8_t *)b.GT;
+        w.ldb = 2 * p.np;
+        w.M = f;
+        w.N = P;
+        w.kt = (int32_t)(p.np / 64);
+        w.splits = p.split_w;
+        if (p.split_w > 1) {
+            w.acc = b.part;
+            if ((rc = tile_product(TILE_BF16, TILE_PARTIAL, w, s))) return rc;
+            if ((rc = tile_reduce(p.split_w, f, P, b.part, dW + c0, 1, C, s))) return rc;
+        } else {
+            w.C = dW + c0;
+            w.ldc = C;
+            w.c_bf16 = 1;
+            if ((rc = tile_product(TILE_BF16, TILE_STORE, w, s))) return rc;
+        }
+    }
+    return tile_reduce(p.split_h, n, f, b.acc, dHL, 1, lddhl, s);
+}
+
+int loss_f32(const Plan &p, const Buffers &b, const float *HL, int32_t n, int32_t f, int64_t ldhl, const float *W,
+             const float *bias, int32_t C, const int32_t *labels, float *loss, float *row_loss, float *dHL, int64_t lddhl,
+             float *dW, float *db, hipStream_t s) {
+    int rc;
+    hipLaunchKernelGGL(count_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, b.inv_count);
+    hipLaunchKernelGGL(copy_rows_kernel<float>, dim3(grid_of((int64_t)n * f)), dim3(kTB), 0, s, n, f, HL, ldhl, b.Hz,
+                       (int64_t)f, labels, C);
+    GCN_LAUNCH_CHECK("class_prep");
+    auto logits = [&](int32_t c0, int32_t P) {
+        GemmProblem g{};
+        g.M = n;
+        g.N = P;
+        g.C = b.X;
+        g.ldc = P;
+        g.bias = bias ? bias + c0 : nullptr;
+        g.seg[0] = GemmSeg{b.Hz, f, W + c0, C, f};
+        return gemm(L_NN, 1, &g, 0, 1, nullptr, 0, s);
+    };
+    for (int32_t i = 0; i < p.pieces; ++i) {
+        const int32_t c0 = i * p.piece, P = std::min(p.piece, C - c0);
+        if ((rc = logits(c0, P))) return rc;
+        ProfScope prof(K_CLASS_STATS, s, 0.0, 4.0 * n * P);
+        hipLaunchKernelGGL(stats_rows_kernel, dim3((unsigned)n), dim3(kTB), 0, s, P, b.X, (int64_t)P, labels, c0, C,
+                           b.run_max, b.run_sum, b.label_logit, i == 0);
+        GCN_LAUNCH_CHECK("stats_rows_kernel");
+    }
+    hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, b.run_max, b.run_sum, b.label_logit, b.lse,
+                       row_loss, b.inv_count, loss);
+    GCN_LAUNCH_CHECK("loss_kernel");
+    if (!dHL) return GCN_OK;
+    for (int32_t i = 0; i < p.pieces; ++i) {
+        const int32_t c0 = i * p.piece, P = std::min(p.piece, C - c0);
+        // (a single piece's logits are still in place)
+        if (p.pieces > 1 && (rc = logits(c0, P))) return rc;
+        {
+            ProfScope prof(K_CLASS_GRAD, s, 0.0, 8.0 * n * P);
+            hipLaunchKernelGGL(grad_rows_kernel, dim3((unsigned)n), dim3(kTB), 0, s, P, b.X, (int64_t)P, labels, c0, C,
+                               b.lse, b.inv_count);
+            GCN_LAUNCH_CHECK("grad_rows_kernel");
+        }
+        if ((rc = colsum(n, P, b.X, P, db + c0, b.col_ws, b.col_bytes, s))) return rc;
+        GemmProblem w = dw_f32(f, P, n);
+        w.C = dW + c0;
+        w.ldc = C;
+        w.seg[0] = GemmSeg{b.Hz, f, b.X, P, n};
+        const int split = std::min(p.split_w, gemm_pick_split(1, &w, true));
+        if ((rc = gemm(L_TN, 1, &w, 0, split, b.gemm_ws, b.gemm_bytes, s))) return rc;
+        GemmProblem d{};
+        d.M = n;
+        d.N = f;
+        d.C = i ? b.tmp : dHL;
+        d.ldc = i ? f : lddhl;
+        d.seg[0] = GemmSeg{b.X, P, W + c0, C, P};
+        if ((rc = gemm(L_NT, 1, &d, 0, 1, nullptr, 0, s))) return rc;
+        if (i) {
+            hipLaunchKernelGGL(add_kernel, dim3(grid_of((int64_t)n * f)), dim3(kTB), 0, s, n, f, b.tmp, dHL, lddhl);
+            GCN_LAUNCH_CHECK("add_kernel");
+        }
+    }
+    return GCN_OK;
+}
+
+}  // namespace
+}  // namespace gcn
+
+using namespace gcn;
+
+extern "C" {
+
+size_t gcn_class_loss_workspace_bytes(int32_t n, int32_t f, int32_t C, gcn_rows_type type, int need_grad) {
+    if (n < 0 || f <= 0 || C <= 0) return 0;
+    Buffers b;
+    return plan_of(n, f, C, type == GCN_ROWS_BF16, need_grad != 0, nullptr, 0, b).total;
+}
+
+int gcn_class_loss(const void *HL, int32_t n, int32_t f, int32_t ldhl, const void *W_pred, const float *b_pred,
+                   int32_t C, const int32_t *labels, gcn_rows_type type, float *loss, float *row_loss, void *dHL,
+                   int32_t lddhl, void *dW_pred, float *db_pred, void *ws, size_t ws_bytes, void *stream) {
+    GCN_REQUIRE(n >= 0 && f > 0 && C > 0, GCN_ESHAPE, "gcn_class_loss: n=%d f=%d C=%d", n, f, C);
+    GCN_REQUIRE(type == GCN_ROWS_F32 || type == GCN_ROWS_BF16, GCN_EINVAL, "gcn_class_loss: bad element type %d",
+                (int)type);
+    const bool grad = dW_pred != nullptr, bf = type == GCN_ROWS_BF16;
+    GCN_REQUIRE((db_pred != nullptr) == grad && (dHL != nullptr || (grad && n == 0) || !grad) && (grad || !dHL), GCN_EINVAL,
+                "gcn_class_loss: dHL, dW_pred and db_pred are given together or not at all");
+    GCN_REQUIRE(ldhl >= f && (!grad || lddhl >= f), GCN_ESHAPE, "gcn_class_loss: ldhl=%d lddhl=%d < f=%d", ldhl, lddhl, f);
+    GCN_REQUIRE(W_pred && loss, GCN_EINVAL, "gcn_class_loss: null pointer");
+    GCN_REQUIRE(n == 0 || (HL && labels), GCN_EINVAL, "gcn_class_loss: null HL or labels");
+    const uintptr_t el = bf ? 1 : 3;
+    GCN_REQUIRE((((uintptr_t)HL | (uintptr_t)W_pred | (uintptr_t)dHL | (uintptr_t)dW_pred) & el) == 0, GCN_EINVAL,
+                "gcn_class_loss: misaligned operand");
+    Buffers b;
+    const Plan p = plan_of(n, f, C, bf, grad, ws, ws_bytes, b);
+    GCN_REQUIRE(ws && ((uintptr_t)ws & 255) == 0 && ws_bytes >= p.total, GCN_EWORKSPACE,
+                "gcn_class_loss: workspace %zu < %zu bytes, or not 256-byte aligned", ws_bytes, p.total);
+    hipStream_t s = (hipStream_t)stream;
+    if (n == 0) {
+        int rc = fill_zero(loss, 1, s);
+        if (!rc && grad) rc = fill_zero(db_pred, C, s);
+        if (!rc && grad) {
+            if (bf) {
+                hipLaunchKernelGGL(zero_kernel, dim3(grid_of((int64_t)f * C)), dim3(kTB), 0, s, (uint16_t *)dW_pred,
+                                   (int64_t)f, (int64_t)C, (int64_t)C);
+                GCN_LAUNCH_CHECK("zero_kernel");
+            } else {
+                rc = fill_zero((float *)dW_pred, (int64_t)f * C, s);
+            }
+        }
+        return rc;
+    }
+    if (bf)
+        return loss_bf16(p, b, (const uint16_t *)HL, n, f, ldhl, (const uint16_t *)W_pred, b_pred, C, labels, loss,
+                         row_loss, (uint16_t *)dHL, lddhl, (uint16_t *)dW_pred, db_pred, s);
+    return loss_f32(p, b, (const float *)HL, n, f, ldhl, (const float *)W_pred, b_pred, C, labels, loss, row_loss,
+                    (float *)dHL, lddhl, (float *)dW_pred, db_pred, s);
+}
+
+}  // extern "C"

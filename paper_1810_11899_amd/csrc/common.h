@@ -49,6 +49,15 @@ int hip_fail(hipError_t e, const char *what);
         if (e_ != hipSuccess) return ::gcn::hip_fail(e_, what); \
     } while (0)
 
+// argument checks of the entry points
+#define GCN_REQUIRE(cond, code, ...)     \
+    do {                                 \
+        if (!(cond)) {                   \
+            ::gcn::set_error(__VA_ARGS__); \
+            return (code);               \
+        }                                \
+    } while (0)
+
 // ---------------------------------------------------------------- profiling
 enum KernelClass {
     K_SPMM = 0,
@@ -80,6 +89,14 @@ enum KernelClass {
     K_GEMM_NT_BF16_BIG,         // the bfloat16 large-tile kernel
     K_GEMM_NT_BF16_BIG_MASKED,  // the same with the ReLU-derivative epilogue
     K_GEMM_TN_BF16_BIG,         // the large-tile kernel on k-major operands (weight gradients)
+    K_ROWS8_PACK,               // 8-bit rows and weights: packing, unpacking
+    K_ROWS8_PRODUCT,
+    K_ROWS8_MASK,               // the ReLU derivative and the bias gradient of the 8-bit backward pass
+    K_ROWS8_WEIGHT_GRAD,
+    K_CLASS_PREP,               // many-class loss: operand copies, counts, reductions
+    K_CLASS_STATS,              // logits of a piece joined into the running maximum and sum
+    K_CLASS_GRAD,               // logits of a piece to their gradient
+    K_CLASS_PRODUCT,            // the gradient's two products
     K_CLASS_COUNT
 };
 const char *class_name(int cls);

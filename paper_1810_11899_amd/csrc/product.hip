@@ -1,0 +1,514 @@
+// Products C = A B^T of bfloat16 or 8-bit rows on the matrix cores, with the
+// epilogues of the 8-bit layer products and of the many-class loss.
+//
+// Both operands come in rows of 128-byte pieces (64 bfloat16 or 128 e4m3
+// values), so one tile loop serves both types: a piece of each tile row is
+// copied from global memory straight into LDS (16 bytes a lane), and a lane's
+// share of a fragment is the two 16-byte chunks g and g + 4 of a row (g = lane
+// / 16): two k-steps of v_mfma_f32_16x16x32_bf16, or the one of
+// v_mfma_scale_f32_16x16x128_f8f6f4.  Which 16 of the 128 columns a chunk holds
+// does not matter as long as both operands agree.  LDS rows are 128 bytes with
+// their chunks XOR-swizzled by row, so that the 16 lanes of a fragment read
+// spread over the banks.
+//
+// The instructions are issued with B's fragment first, which leaves a lane
+// with four consecutive columns of one row of C.
+#include <algorithm>
+
+#include "rows8.h"
+
+namespace gcn {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16v8 __attribute__((ext_vector_type(8)));
+
+constexpr int kPiece = 128;   // bytes of a row in one stage
+
+struct Args {
+    TileProduct p;
+    int32_t tiles_m, tiles_n, kt_per_split, band;
+    int64_t total, per_xcd;
+};
+
+// Workgroups go round-robin over the 8 XCDs (workgroup b runs on XCD b % 8);
+// logical tiles are numbered XCD-major, and within that in bands of `band` row
+// tiles, row tile fastest, so that the tiles running at once on an XCD share
+// operand panels in its L2.
+struct Coord {
+    int split, tm, tn;
+};
+__device__ __forceinline__ bool coord_of(const Args &a, Coord &c) {
+    const int64_t L = (int64_t)(blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
+    if (L >= a.total) return false;
+    const int64_t per_split = (int64_t)a.tiles_m * a.tiles_n;
+    c.split = (int)(L / per_split);
+    const int64_t r = L % per_split;
+    const int64_t in_band = (int64_t)a.band * a.tiles_n;
+    const int b = (int)(r / in_band);
+    const int64_t q = r % in_band;
+    const int h = min(a.band, a.tiles_m - b * a.band);
+    c.tm = b * a.band + (int)(q % h);
+    c.tn = (int)(q / h);
+    return true;
+}
+
+struct Frag {
+    uint4 lo, hi;
+};
+
+template <int TYPE>
+__device__ __forceinline__ void mma(f32x4 &acc, const Frag &a, const Frag &b, int sa, int sb) {
+    if constexpr (TYPE == TILE_BF16) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16v8, b.lo),
+                                                      __builtin_bit_cast(bf16v8, a.lo), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16v8, b.hi),
+                                                      __builtin_bit_cast(bf16v8, a.hi), acc, 0, 0, 0);
+    } else if constexpr (TYPE == TILE_FP8) {
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i32x8, b),
+                                                               __builtin_bit_cast(i32x8, a), acc, 0, 0, 0, sb, 0, sa);
+    }
+}
+
+// eight e4m3 values as bfloat16, exactly
+typedef __bf16 bf16v2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ bf16v8 widen8(uint32_t x, uint32_t y) {
+    uint4 r;
+    r.x = __builtin_bit_cast(uint32_t, (bf16v2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false));
+    r.y = __builtin_bit_cast(uint32_t, (bf16v2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true));
+    r.z = __builtin_bit_cast(uint32_t, (bf16v2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, 1.0f, false));
+    r.w = __builtin_bit_cast(uint32_t, (bf16v2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, 1.0f, true));
+    return __builtin_bit_cast(bf16v8, r);
+}
+
+// the column of row's label, maybe outside this product's; kNoLabel without one
+constexpr int kNoLabel = -0x7FFFFFFF - 1;
+__device__ __forceinline__ int label_of(const TileProduct &p, int row) {
+    const int l = row < p.M ? p.labels[row] : -1;
+    return l >= 0 && l < p.classes ? l - p.class0 : kNoLabel;
+}
+
+// a softmax gradient's value; x - lse <= 0 up to rounding
+__device__ __forceinline__ float prob(float x, float lse) { return __expf(x - lse); }
+
+// ------------------------------------------------------------- epilogues
+// acc[i][j]: row m0 + 16 i + lane % 16 of C, columns n0 + 16 j + 4 (lane / 16)
+// .. + 3; `scratch`: the idle operand LDS, at least 8 KB.
+template <int EPI, int BM, int BN, int WM, int WN, int FM, int FN>
+__device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&acc)[FM][FN], char *scratch) {
+    const TileProduct &p = a.p;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wm = wave / WN, wn = wave % WN;
+    const int r0 = c.tm * BM + wm * (BM / WM) + (lane & 15);
+    const int c0 = c.tn * BN + wn * (BN / WN) + 4 * (lane >> 4);
+    if constexpr (EPI == TILE_STORE) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int col = c0 + 16 * j;
+            f32x4 bv = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (p.bias)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) bv[e] = col + e < p.N ? p.bias[col + e] : 0.0f;
+            const bool whole = col + 4 <= p.N && p.ldc % 4 == 0 && ((uintptr_t)p.C & (p.c_bf16 ? 7 : 15)) == 0;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const int row = r0 + 16 * i;
+                if (row >= p.M) continue;
+                f32x4 v = acc[i][j] + bv;
+                if (p.relu)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = v[e] < 0.0f ? 0.0f : v[e];   // (NaN stays)
+                const int64_t at = (int64_t)row * p.ldc + col;
+                if (p.c_bf16) {
+                    uint16_t *d = (uint16_t *)p.C + at;
+                    if (whole) {
+                        *(uint2 *)d = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (col + e < p.N) d[e] = to_bf16(v[e]);
+                    }
+                } else {
+                    float *d = (float *)p.C + at;
+                    if (whole) {
+                        *(f32x4 *)d = v;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (col + e < p.N) d[e] = v[e];
+                    }
+                }
+            }
+        }
+    } else if constexpr (EPI == TILE_PARTIAL) {
+        float *base = p.acc + (int64_t)c.split * p.M * p.N;
+        const bool vec = p.N % 4 == 0;
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const int row = r0 + 16 * i, col = c0 + 16 * j;
+                if (row >= p.M || col >= p.N) continue;
+                float *d = base + (int64_t)row * p.N + col;
+                if (vec) {
+                    f32x4 v = acc[i][j];
+                    if (p.accumulate) v += *(const f32x4 *)d;
+                    *(f32x4 *)d = v;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (col + e < p.N) d[e] = p.accumulate ? d[e] + acc[i][j][e] : acc[i][j][e];
+                }
+            }
+    } else {
+        // bias, and columns past the last class to minus infinity
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int col = c0 + 16 * j + e;
+                const float b = col < p.N ? (p.bias ? p.bias[col] : 0.0f) : -INFINITY;
+#pragma unroll
+                for (int i = 0; i < FM; ++i) acc[i][j][e] = col < p.N ? acc[i][j][e] + b : b;
+            }
+        if constexpr (EPI == TILE_STATS) {
+            // a row's columns lie in 4 lanes of WN wavefronts: maximum and sum
+            // over the lane's own, two exchanges, then LDS across wavefronts
+            float2 *part = (float2 *)scratch;   // [WN][BM]
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const int row = r0 + 16 * i;
+                float m = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[i][j][e]);
+                m = fmaxf(m, __shfl_xor(m, 16));
+                m = fmaxf(m, __shfl_xor(m, 32));
+                const float base = m == -INFINITY ? 0.0f : m;   // no finite logit yet: the sum stays 0
+                float s = 0.0f;
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s += __expf(acc[i][j][e] - base);
+                s += __shfl_xor(s, 16);
+                s += __shfl_xor(s, 32);
+                if (lane < 16) part[wn * BM + row - c.tm * BM] = make_float2(m, s);
+                const int lab = label_of(p, row);
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (c0 + 16 * j + e == lab && lab < p.N) p.label_logit[row] = acc[i][j][e];
+            }
+            __syncthreads();
+            for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) {
+                const int row = c.tm * BM + r;
+                if (row >= p.M) continue;
+                float m = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < WN; ++w) m = fmaxf(m, part[w * BM + r].x);
+                float s = 0.0f;
+#pragma unroll
+                for (int w = 0; w < WN; ++w) {
+                    const float2 q = part[w * BM + r];
+                    s += q.x == -INFINITY ? q.y : q.y * __expf(q.x - m);
+                }
+                p.tile_max[(int64_t)c.tn * p.M + row] = m;
+                p.tile_sum[(int64_t)c.tn * p.M + row] = s;
+            }
+        } else {
+            float cs[FN][4];
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) cs[j][e] = 0.0f;
+            const float inv = p.inv_count[0];
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const int row = r0 + 16 * i;
+                const bool in = row < p.M;
+                const float lse = in ? p.lse[row] : 0.0f;
+                const int lab = label_of(p, row);
+                const bool has = lab != kNoLabel;   // a row without a label has no gradient
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    const int col = c0 + 16 * j;
+                    f32x4 g;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        g[e] = has ? (prob(acc[i][j][e], lse) - (col + e == lab && lab < p.N ? 1.0f : 0.0f)) * inv : 0.0f;
+                        cs[j][e] += g[e];
+                    }
+                    if (in && col < p.ldg)
+                        *(uint2 *)(p.G + (int64_t)row * p.ldg + col) =
+                            make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]));
+                    if (row < p.ldgt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (col + e < p.N) p.GT[(int64_t)(col + e) * p.ldgt + row] = to_bf16(g[e]);
+                }
+            }
+            // column sums: 16 lanes of a wavefront, then the WM wavefronts
+            float *part = (float *)scratch;   // [WM][BN]
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float v = cs[j][e];
+#pragma unroll
+                    for (int d = 1; d < 16; d *= 2) v += __shfl_xor(v, d);
+                    if ((lane & 15) == 0) part[wm * BN + c0 - c.tn * BN + 16 * j + e] = v;
+                }
+            __syncthreads();
+            for (int k = threadIdx.x; k < BN; k += 64 * WM * WN) {
+                const int col = c.tn * BN + k;
+                if (col >= p.N) continue;
+                float v = 0.0f;
+#pragma unroll
+                for (int w = 0; w < WM; ++w) v += part[w * BN + k];
+                p.colpart[(int64_t)c.tm * p.N + col] = v;
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------ small tiles
+// WM x WN wavefronts, two LDS stages: the next piece is copied while one is
+// multiplied, and several blocks a CU cover each other's waits.
+template <int TYPE, int EPI, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
+    constexpr int FM = BM / WM / 16, FN = BN / WN / 16, T = 64 * WM * WN;
+    constexpr int kStage = (BM + BN) * kPiece;
+    constexpr int LA = BM * kPiece / 16 / T, LB = BN * kPiece / 16 / T;
+    static_assert(LA * T * 16 == BM * kPiece && LB * T * 16 == BN * kPiece, "whole chunks per lane");
+    __shared__ __attribute__((aligned(16))) char lds[2 * kStage];
+    Coord c;
+    if (!coord_of(a, c)) return;
+    const TileProduct &p = a.p;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wm = wave / WN, wn = wave % WN;
+    const int m0 = c.tm * BM, n0 = c.tn * BN;
+    const int kt0 = c.split * a.kt_per_split, kt1 = min(kt0 + a.kt_per_split, p.kt);
+    // lane of copy u: tile row (u T + thread) / 8, stored chunk thread % 8,
+    // which holds the row's chunk (thread % 8) ^ (row % 8); rows past the
+    // extent are clamped (their products are dropped)
+    const int lr = threadIdx.x >> 3, chunk = ((threadIdx.x & 7) ^ (lr & 7)) * 16;
+    const uint8_t *ga[LA], *gb[LB];
+#pragma unroll
+    for (int u = 0; u < LA; ++u) ga[u] = p.A + (int64_t)min(m0 + u * (T / 8) + lr, p.M - 1) * p.lda + chunk;
+#pragma unroll
+    for (int u = 0; u < LB; ++u) gb[u] = p.B + (int64_t)min(n0 + u * (T / 8) + lr, p.N - 1) * p.ldb + chunk;
+    auto copy = [&](int kt, int stage) {
+        char *d = lds + stage * kStage + wave * 1024;
+#pragma unroll
+        for (int u = 0; u < LA; ++u)
+            __builtin_amdgcn_global_load_lds((const void *)(ga[u] + (int64_t)kt * kPiece),
+                                             (void __attribute__((address_space(3))) *)(d + u * T * 16), 16, 0, 0);
+#pragma unroll
+        for (int u = 0; u < LB; ++u)
+            __builtin_amdgcn_global_load_lds((const void *)(gb[u] + (int64_t)kt * kPiece),
+                                             (void __attribute__((address_space(3))) *)(d + BM * kPiece + u * T * 16), 16,
+                                             0, 0);
+    };
+    f32x4 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int fr = lane & 15, g = lane >> 4;
+    const int o0 = (g ^ (fr & 7)) * 16, o1 = ((g + 4) ^ (fr & 7)) * 16;   // (a fragment's rows start at multiples of 16)
+    auto frag = [&](const char *tile, int row) {
+        const char *q = tile + (row + fr) * kPiece;
+        return Frag{*(const uint4 *)(q + o0), *(const uint4 *)(q + o1)};
+    };
+    if (kt0 < kt1) copy(kt0, 0);
+    __syncthreads();
+    for (int kt = kt0; kt < kt1; ++kt) {
+        const int st = (kt - kt0) & 1;
+        if (kt + 1 < kt1) copy(kt + 1, st ^ 1);
+        const char *ta = lds + st * kStage, *tb = ta + BM * kPiece;
+        int sa[FM], sb[FN];
+        if constexpr (TYPE != TILE_BF16) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+                sa[i] = p.sa[(int64_t)min(m0 + wm * (BM / WM) + 16 * i + fr, p.M - 1) * p.ldsa + kt];
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+                sb[j] = p.sb[(int64_t)(min(n0 + wn * (BN / WN) + 16 * j, p.N - 1) / kRows8Block) * p.sb_n + kt * p.sb_k];
+        }
+        Frag fb[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) fb[j] = frag(tb, wn * (BN / WN) + 16 * j);
+        if constexpr (TYPE == TILE_FP8_EXACT) {
+            bf16v8 wb[FN][4];
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                wb[j][0] = widen8(fb[j].lo.x, fb[j].lo.y);
+                wb[j][1] = widen8(fb[j].lo.z, fb[j].lo.w);
+                wb[j][2] = widen8(fb[j].hi.x, fb[j].hi.y);
+                wb[j][3] = widen8(fb[j].hi.z, fb[j].hi.w);
+            }
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const Frag fa = frag(ta, wm * (BM / WM) + 16 * i);
+                const bf16v8 wa[4] = {widen8(fa.lo.x, fa.lo.y), widen8(fa.lo.z, fa.lo.w), widen8(fa.hi.x, fa.hi.y),
+                                      widen8(fa.hi.z, fa.hi.w)};
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][k], wa[k], z, 0, 0, 0);
+                    const int e = sa[i] + sb[j] - 254;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[i][j][q] += __builtin_amdgcn_ldexpf(z[q], e);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const Frag fa = frag(ta, wm * (BM / WM) + 16 * i);
+#pragma unroll
+                for (int j = 0; j < FN; ++j) mma<TYPE>(acc[i][j], fa, fb[j], TYPE == TILE_FP8 ? sa[i] : 0, TYPE == TILE_FP8 ? sb[j] : 0);
+            }
+        }
+        __syncthreads();   // (also waits for the copies of the next piece)
+    }
+    finish<EPI, BM, BN, WM, WN, FM, FN>(a, c, acc, lds);
+}
+
+__global__ __launch_bounds__(256) void reduce_kernel(int32_t splits, int64_t count, int32_t N, const float *acc,
+                                                     void *out, int out_bf16, int64_t ldo) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
+        float v = acc[i];
+        for (int s = 1; s < splits; ++s) v += acc[(int64_t)s * count + i];
+        const int64_t at = i / N * ldo + i % N;
+        if (out_bf16) ((uint16_t *)out)[at] = to_bf16(v);
+        else ((float *)out)[at] = v;
+    }
+}
+
+template <int TYPE, int EPI>
+void launch_small(const Args &a, unsigned grid, hipStream_t s) {
+    hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 128, 128, 2, 2>), dim3(grid), dim3(256), 0, s, a);
+}
+
+}  // namespace
+
+TileShape tile_shape(TileType, TileEpilogue, int32_t, int32_t, int32_t) { return TileShape{128, 128}; }
+
+int32_t tile_splits(TileType type, int32_t M, int32_t N, int32_t kt) {
+    const TileShape t = tile_shape(type, TILE_PARTIAL, M, N, kt);
+    const int64_t tiles = (int64_t)((M + t.m - 1) / t.m) * ((N + t.n - 1) / t.n);
+    const int64_t sp = std::min<int64_t>(512 / std::max<int64_t>(1, tiles), kt / 8);
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(sp, 64));
+}
+
+int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStream_t s) {
+    if (p.M <= 0 || p.N <= 0) return GCN_OK;
+    const TileShape t = tile_shape(type, epi, p.M, p.N, p.kt);
+    Args a;
+    a.p = p;
+    a.tiles_m = (p.M + t.m - 1) / t.m;
+    a.tiles_n = (p.N + t.n - 1) / t.n;
+    const int32_t splits = std::max(1, p.splits);
+    a.kt_per_split = (p.kt + splits - 1) / splits;
+    a.band = 8;
+    a.total = (int64_t)splits * a.tiles_m * a.tiles_n;
+    a.per_xcd = (a.total + 7) / 8;
+    if (8 * a.per_xcd > 0x7FFFFFFF) {
+        set_error("tile_product: %d x %d is too large", p.M, p.N);
+        return GCN_EUNSUPPORTED;
+    }
+    const unsigned grid = (unsigned)(8 * a.per_xcd);
+    if (type == TILE_BF16) {
+        if (epi == TILE_STORE) launch_small<TILE_BF16, TILE_STORE>(a, grid, s);
+        else if (epi == TILE_PARTIAL) launch_small<TILE_BF16, TILE_PARTIAL>(a, grid, s);
+        else if (epi == TILE_STATS) launch_small<TILE_BF16, TILE_STATS>(a, grid, s);
+        else launch_small<TILE_BF16, TILE_GRAD>(a, grid, s);
+    } else if (type == TILE_FP8) {
+        if (epi == TILE_STORE) launch_small<TILE_FP8, TILE_STORE>(a, grid, s);
+        else launch_small<TILE_FP8, TILE_PARTIAL>(a, grid, s);
+    } else {
+        if (epi == TILE_STORE) launch_small<TILE_FP8_EXACT, TILE_STORE>(a, grid, s);
+        else launch_small<TILE_FP8_EXACT, TILE_PARTIAL>(a, grid, s);
+    }
+    GCN_LAUNCH_CHECK("tile_kernel");
+    return GCN_OK;
+}
+
+int tile_reduce(int32_t splits, int32_t M, int32_t N, const float *acc, void *out, int out_bf16, int64_t ldo,
+                hipStream_t s) {
+    const int64_t count = (int64_t)M * N;
+    if (count == 0) return GCN_OK;
+    const unsigned g = (unsigned)std::min<int64_t>((count + 255) / 256, 8192);
+    hipLaunchKernelGGL(reduce_kernel, dim3(g), dim3(256), 0, s, splits, count, N, acc, out, out_bf16, ldo);
+    GCN_LAUNCH_CHECK("reduce_kernel");
+    return GCN_OK;
+}
+
+}  // namespace gcn
+
+using namespace gcn;
+
+extern "C" {
+
+size_t gcn_rows8_product_workspace_bytes(int32_t n, int32_t K, int32_t N) {
+    (void)n, (void)K, (void)N;
+    return 256;
+}
+
+int gcn_rows8_product(const gcn_rows8 *X8, const gcn_weights8 *W8, int transpose, const float *bias, int relu, void *Y,
+                      gcn_rows_type type, int32_t ldy, void *ws, size_t ws_bytes, void *stream) {
+    int rc = check_rows8(X8, "gcn_rows8_product");
+    if (rc) return rc;
+    GCN_REQUIRE(W8, GCN_EINVAL, "gcn_rows8_product: null 8-bit weights");
+    GCN_REQUIRE(W8->K > 0 && W8->N > 0, GCN_ESHAPE, "gcn_rows8_product: 8-bit weights of %d x %d", W8->K, W8->N);
+    GCN_REQUIRE(type == GCN_ROWS_F32 || type == GCN_ROWS_BF16, GCN_EINVAL, "gcn_rows8_product: bad element type %d",
+                (int)type);
+    const int32_t K = transpose ? W8->N : W8->K, N = transpose ? W8->K : W8->N;   // contraction, columns of Y
+    const uint8_t *w = transpose ? W8->q : W8->qT;
+    const int32_t ldw = transpose ? W8->ldq : W8->ldqT;
+    GCN_REQUIRE(X8->f == K, GCN_ESHAPE, "gcn_rows8_product: rows of %d columns against %d", X8->f, K);
+    GCN_REQUIRE(w && W8->scale, GCN_EINVAL, "gcn_rows8_product: the weights' %s orientation is missing",
+                transpose ? "q" : "qT");
+    GCN_REQUIRE(ldw % 16 == 0 && ldw >= kRows8Block * blocks8(K) && (uintptr_t)w % 16 == 0, GCN_ESHAPE,
+                "gcn_rows8_product: weight rows need 16-byte alignment and a stride (%d) that is a multiple of 16 of at "
+                "least %lld", ldw, (long long)(kRows8Block * blocks8(K)));
+    GCN_REQUIRE(W8->ldscale >= blocks8(W8->N), GCN_ESHAPE, "gcn_rows8_product: ldscale=%d < %lld", W8->ldscale,
+                (long long)blocks8(W8->N));
+    GCN_REQUIRE(ldy >= N, GCN_ESHAPE, "gcn_rows8_product: ldy=%d < %d", ldy, N);
+    GCN_REQUIRE(X8->n == 0 || Y, GCN_EINVAL, "gcn_rows8_product: null Y");
+    GCN_REQUIRE(ws && ws_bytes >= gcn_rows8_product_workspace_bytes(X8->n, W8->K, W8->N), GCN_EWORKSPACE,
+                "gcn_rows8_product: workspace %zu bytes too small", ws_bytes);
+    if (X8->n == 0) return GCN_OK;
+    TileProduct p{};
+    p.A = X8->q;
+    p.lda = X8->ldq;
+    p.B = w;
+    p.ldb = ldw;
+    p.M = X8->n;
+    p.N = N;
+    p.kt = (int32_t)blocks8(K);
+    p.splits = 1;
+    p.sa = X8->scale;
+    p.ldsa = X8->ldscale;
+    p.sb = W8->scale;
+    p.sb_n = transpose ? W8->ldscale : 1;
+    p.sb_k = transpose ? 1 : W8->ldscale;
+    p.C = Y;
+    p.ldc = ldy;
+    p.c_bf16 = type == GCN_ROWS_BF16;
+    p.relu = relu;
+    p.bias = bias;
+    hipStream_t s = (hipStream_t)stream;
+    ProfScope prof(K_ROWS8_PRODUCT, s, 2.0 * p.M * N * K,
+                   (double)p.M * K + (double)N * K + (double)p.M * N * (p.c_bf16 ? 2.0 : 4.0));
+    return tile_product(p.c_bf16 ? TILE_FP8 : TILE_FP8_EXACT, TILE_STORE, p, s);
+}
+
+}  // extern "C"

@@ -1,0 +1,72 @@
+// Internal declarations of the 8-bit rows (rows8.hip) and the tile products
+// (product.hip) shared by the entry points that use them.
+#pragma once
+
+#include "common.h"
+#include "gcn_rows8.h"
+
+namespace gcn {
+
+constexpr int kRows8Block = 128;   // columns (and, for weights, rows) under one scale
+inline int64_t blocks8(int64_t f) { return (f + kRows8Block - 1) / kRows8Block; }
+
+// ---------------------------------------------------------------- products
+// C[M x N] = A B^T on the matrix cores, A [M x K] and B [N x K] in rows of kt
+// 128-byte pieces (64 bfloat16 or 128 e4m3 values), 16-byte aligned, the
+// columns past K zero in at least one of them and finite in the other.
+enum TileType {
+    TILE_BF16 = 0,       // bfloat16 operands
+    TILE_FP8 = 1,        // e4m3 operands with scales, 8-bit matrix instructions
+    TILE_FP8_EXACT = 2   // the same, as bfloat16 products (exact), one float32 sum per 128 columns
+};
+enum TileEpilogue {
+    TILE_STORE = 0,    // C (float32 or bfloat16), bias, ReLU
+    TILE_PARTIAL = 1,  // split s's sums to acc + s M N (float32), or added to what is there
+    TILE_STATS = 2,    // per row and column tile: maximum and sum of exponentials
+    TILE_GRAD = 3      // softmax gradient rows, transposed rows, column sums
+};
+struct TileProduct {
+    const uint8_t *A, *B;
+    int64_t lda, ldb;        // bytes
+    int32_t M, N, kt;
+    int32_t splits;          // TILE_PARTIAL only, else 1
+    // scales of 8-bit operands: A's of row i, piece k at sa[i * ldsa + k]; B's
+    // of row j, piece k at sb[(j / 128) * sb_n + k * sb_k]
+    const uint8_t *sa, *sb;
+    int64_t ldsa, sb_n, sb_k;
+    // TILE_STORE
+    void *C;
+    int64_t ldc;             // elements
+    int c_bf16, relu;
+    const float *bias;       // [N] or null (also TILE_STATS and TILE_GRAD)
+    // TILE_PARTIAL
+    float *acc;
+    int accumulate;
+    // TILE_STATS, TILE_GRAD: column j of C is class class0 + j
+    // of `classes`; a row whose label is none of them has no gradient
+    const int32_t *labels;
+    int32_t class0, classes;
+    float *tile_max, *tile_sum;     // [tiles_n x M]
+    float *label_logit;             // [M]
+    const float *lse, *inv_count;   // [M], [1]
+    uint16_t *G, *GT;               // [M x ldg], [N x ldgt] bfloat16
+    int64_t ldg, ldgt;
+    float *colpart;                 // [tiles_m x N]
+};
+// rows and columns of the tiles that this product runs on
+struct TileShape { int32_t m, n; };
+TileShape tile_shape(TileType type, TileEpilogue epi, int32_t M, int32_t N, int32_t kt);
+int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStream_t s);
+// out (float32, or bfloat16 rows of ldo) = the sum of `splits` partials M x N, in order
+int tile_reduce(int32_t splits, int32_t M, int32_t N, const float *acc, void *out, int out_bf16, int64_t ldo,
+                hipStream_t s);
+
+// how many parts to split `kt` pieces over, for a product with few tiles
+int32_t tile_splits(TileType type, int32_t M, int32_t N, int32_t kt);
+
+// ------------------------------------------------------------ 8-bit rows
+int check_rows8(const gcn_rows8 *r, const char *who);
+int rows8_pack(int32_t n, int32_t f, const void *X, int x_bf16, int64_t ldx, uint8_t *q, int64_t ldq,
+               uint8_t *scale, int64_t lds, hipStream_t s);
+
+}  // namespace gcn

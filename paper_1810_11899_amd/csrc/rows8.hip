@@ -1,0 +1,438 @@
+// 8-bit rows: e4m3 values with one power-of-two scale for each block of 128
+// columns (weights: of 128 x 128), and the elementwise pass of the backward
+// pass that reads them.
+#include <algorithm>
+
+#include "rows8.h"
+
+namespace gcn {
+namespace {
+
+constexpr int kTB = 256;
+constexpr int kBlk = kRows8Block;
+
+// The scale exponent of a block from the bits of its largest finite magnitude
+// a = m 2^k: k - 8 where m <= 1.75 (448 = 1.75 * 2^8 is the largest e4m3
+// value), k - 7 above, within -126 .. 127; 0 for a block of zeros.
+__device__ __forceinline__ int block_exponent(uint32_t a) {
+    const int k = (int)(a >> 23) - 127;
+    const int e = k - 8 + ((a & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return a == 0u ? 0 : max(e, -126);   // (a subnormal a has k = -127: the bound holds it)
+}
+__device__ __forceinline__ uint32_t finite_magnitude(float x) {
+    const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
+    return u < 0x7F800000u ? u : 0u;
+}
+// 2^-e, e in -126 .. 120
+__device__ __forceinline__ float inverse_scale(int e) { return __uint_as_float((uint32_t)(127 - e) << 23); }
+
+// four values to four e4m3 bytes: the hardware's rounding (nearest even), and
+// the two departures: no value but zero becomes zero, not finite becomes NaN
+__device__ __forceinline__ uint32_t held4(const float (&x)[4], float inv) {
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, r, true);
+    uint32_t q = (uint32_t)r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t u = __float_as_uint(x[i]) & 0x7FFFFFFFu;
+        if (u != 0u && (q & (0x7Fu << (8 * i))) == 0u) q |= 1u << (8 * i) | ((__float_as_uint(x[i]) >> 31) << (8 * i + 7));
+        if (u >= 0x7F800000u) q = (q & ~(0xFFu << (8 * i))) | (0x7Fu << (8 * i));
+    }
+    return q;
+}
+
+// eight consecutive elements from column c of a row (zeros past f)
+template <bool BF, bool VEC>
+__device__ __forceinline__ void load8(const void *row, int c, int f, float (&x)[8]) {
+    if (VEC && c + 8 <= f) {
+        if (BF) {
+            const uint4 v = *(const uint4 *)((const uint16_t *)row + c);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[2 * i] = __uint_as_float(w[i] << 16);
+                x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            }
+        } else {
+            const float4 a = *(const float4 *)((const float *)row + c), b = *(const float4 *)((const float *)row + c + 4);
+            x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            x[i] = c + i < f ? (BF ? __uint_as_float((uint32_t)((const uint16_t *)row)[c + i] << 16)
+                                   : ((const float *)row)[c + i])
+                             : 0.0f;
+    }
+}
+
+// Packs the 16 lanes' 128 values (8 a lane) and writes them; every lane of the
+// 16 calls it.  The largest magnitude by four exchanges between the lanes.
+__device__ __forceinline__ void pack_block(const float (&x)[8], uint8_t *q, uint8_t *scale, bool write) {
+    uint32_t a = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a = max(a, finite_magnitude(x[i]));
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) a = max(a, (uint32_t)__shfl_xor((int)a, d));
+    const int e = block_exponent(a);
+    const float inv = inverse_scale(e);
+    const float lo[4] = {x[0], x[1], x[2], x[3]}, hi[4] = {x[4], x[5], x[6], x[7]};
+    if (write) {
+        *(uint2 *)(q + 8 * (threadIdx.x & 15)) = make_uint2(held4(lo, inv), held4(hi, inv));
+        if ((threadIdx.x & 15) == 0) *scale = (uint8_t)(e + 127);
+    }
+}
+
+// One block of 128 columns to 16 lanes, the lanes of a wavefront along the row
+// (whole lines both ways).
+template <bool BF, bool VEC>
+__global__ __launch_bounds__(kTB) void pack_kernel(int64_t blocks, int32_t per_row, int32_t f, const void *X,
+                                                   int64_t ldx, uint8_t *q, int64_t ldq, uint8_t *scale,
+                                                   int64_t lds) {
+    const int64_t stride = (int64_t)gridDim.x * (kTB / 16);
+    for (int64_t b = (int64_t)blockIdx.x * (kTB / 16) + threadIdx.x / 16; b < ((blocks + 3) & ~(int64_t)3); b += stride) {
+        const bool in = b < blocks;    // (the 64 lanes of a wavefront stay together)
+        const int64_t row = in ? b / per_row : 0;
+        const int32_t bc = in ? (int32_t)(b - row * per_row) : 0;
+        float x[8];
+        load8<BF, VEC>((const char *)X + row * ldx * (BF ? 2 : 4), bc * kBlk + 8 * (int)(threadIdx.x & 15), f, x);
+        pack_block(x, q + row * ldq + bc * kBlk, scale + row * lds + bc, in);
+    }
+}
+
+__device__ __forceinline__ float e4m3_value(uint32_t b) {
+    return __builtin_amdgcn_cvt_f32_fp8((int)b, 0);
+}
+
+template <bool BF>
+__global__ __launch_bounds__(kTB) void unpack_kernel(int32_t n, int32_t f, const uint8_t *q, int64_t ldq,
+                                                     const uint8_t *scale, int64_t lds, void *X, int64_t ldx) {
+    const int64_t total = (int64_t)n * f;
+    for (int64_t i = (int64_t)blockIdx.x * kTB + threadIdx.x; i < total; i += (int64_t)gridDim.x * kTB) {
+        const int64_t row = i / f;
+        const int32_t c = (int32_t)(i - row * f);
+        const float v = ldexpf(e4m3_value(q[row * ldq + c]), (int)scale[row * lds + c / kBlk] - 127);
+        if (BF) ((uint16_t *)X)[row * ldx + c] = to_bf16(v);
+        else ((float *)X)[row * ldx + c] = v;
+    }
+}
+
+// One 128 x 128 block of the weights to a workgroup: the largest magnitude in
+// a first pass over it, the values to both orientations in a second (through
+// LDS, so that both are written along their rows).
+template <bool BF>
+__global__ __launch_bounds__(kTB) void pack_weights_kernel(int32_t K, int32_t N, const void *W, int64_t ldw, uint8_t *q,
+                                                           int64_t ldq, uint8_t *qT, int64_t ldqT, uint8_t *scale,
+                                                           int64_t lds) {
+    __shared__ uint8_t tile[kBlk][kBlk + 4];
+    __shared__ uint32_t top[kTB / 64];
+    const int k0 = blockIdx.y * kBlk, n0 = blockIdx.x * kBlk;
+    auto at = [&](int k, int n) {
+        if (k >= K || n >= N) return 0.0f;
+        const int64_t i = (int64_t)k * ldw + n;
+        return BF ? __uint_as_float((uint32_t)((const uint16_t *)W)[i] << 16) : ((const float *)W)[i];
+    };
+    uint32_t a = 0u;
+    for (int i = threadIdx.x; i < kBlk * kBlk; i += kTB) a = max(a, finite_magnitude(at(k0 + i / kBlk, n0 + i % kBlk)));
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) a = max(a, (uint32_t)__shfl_xor((int)a, d));
+    if ((threadIdx.x & 63) == 0) top[threadIdx.x / 64] = a;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kTB / 64; ++w) a = max(a, top[w]);
+    const int e = block_exponent(a);
+    const float inv = inverse_scale(e);
+    if (threadIdx.x == 0) scale[blockIdx.y * lds + blockIdx.x] = (uint8_t)(e + 127);
+    for (int i = threadIdx.x; i < kBlk * kBlk / 4; i += kTB) {
+        const int k = i / (kBlk / 4), n = i % (kBlk / 4) * 4;
+        const float x[4] = {at(k0 + k, n0 + n), at(k0 + k, n0 + n + 1), at(k0 + k, n0 + n + 2), at(k0 + k, n0 + n + 3)};
+        const uint32_t v = held4(x, inv);
+        *(uint32_t *)&tile[k][n] = v;
+        if (q && k0 + k < K) *(uint32_t *)(q + (int64_t)(k0 + k) * ldq + n0 + n) = v;
+    }
+    if (!qT) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBlk * kBlk / 4; i += kTB) {
+        const int n = i / (kBlk / 4), k = i % (kBlk / 4) * 4;
+        if (n0 + n >= N) continue;
+        *(uint32_t *)(qT + (int64_t)(n0 + n) * ldqT + k0 + k) =
+            (uint32_t)tile[k][n] | (uint32_t)tile[k + 1][n] << 8 | (uint32_t)tile[k + 2][n] << 16 | (uint32_t)tile[k + 3][n] << 24;
+    }
+}
+
+// The elementwise half of the backward pass: dZ = bf16(dY) where the mask byte
+// is a positive e4m3 value (1 .. 0x7E), zero elsewhere, as bfloat16 rows; the
+// column sums of a strip of rows; and, when wanted, dZ's 8-bit rows.  One
+// block of 128 columns and a strip of rows to a workgroup, 16 lanes a row, so
+// that one pass over dY and the mask serves all three.
+template <bool BF, bool VEC>
+__global__ __launch_bounds__(kTB) void mask_kernel(int32_t n, int32_t N, int32_t rows_per_strip, const void *dY,
+                                                   int64_t lddy, const uint8_t *mask, int64_t ldm, uint16_t *dZ,
+                                                   int64_t lddz, float *part, uint8_t *q, int64_t ldq, uint8_t *scale,
+                                                   int64_t lds) {
+    __shared__ float red[kTB / 16][kBlk];
+    const int c = blockIdx.x * kBlk + 8 * (int)(threadIdx.x & 15);
+    const int64_t r0 = (int64_t)blockIdx.y * rows_per_strip;
+    const int64_t r1 = min(r0 + rows_per_strip, (int64_t)n);
+    float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    // (the strip's rows in steps of 16; the lanes past its end stay for the
+    // exchanges of pack_block)
+    for (int64_t b = r0; b < r1; b += kTB / 16) {
+        const int64_t r = b + threadIdx.x / 16;
+        const bool in = r < r1;
+        float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        if (in) {
+            load8<BF, VEC>((const char *)dY + r * lddy * (BF ? 2 : 4), c, N, x);
+            uint32_t m[2] = {0x01010101u, 0x01010101u};
+            if (mask) {
+                const uint8_t *mp = mask + r * ldm + c;
+                if (VEC && c + 8 <= N) {
+                    const uint2 v = *(const uint2 *)mp;
+                    m[0] = v.x, m[1] = v.y;
+                } else {
+                    m[0] = m[1] = 0u;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (c + i < N) m[i / 4] |= (uint32_t)mp[i] << (8 * (i & 3));
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t byte = (m[i / 4] >> (8 * (i & 3))) & 0xFFu;
+                const float v = BF ? x[i] : __uint_as_float((uint32_t)to_bf16(x[i]) << 16);
+                x[i] = byte - 1u < 0x7Eu ? v : 0.0f;
+                sum[i] += x[i];
+            }
+            if (c < lddz)
+                *(uint4 *)(dZ + r * lddz + c) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                                           pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+        }
+        if (q) pack_block(x, q + (in ? r : r0) * ldq + blockIdx.x * kBlk, scale + (in ? r : r0) * lds + blockIdx.x, in);
+    }
+    if (!part) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) red[threadIdx.x / 16][8 * (threadIdx.x & 15) + i] = sum[i];
+    __syncthreads();
+    const int k = blockIdx.x * kBlk + threadIdx.x;
+    if (threadIdx.x < kBlk && k < N) {
+        float t = 0.0f;
+#pragma unroll
+        for (int g = 0; g < kTB / 16; ++g) t += red[g][threadIdx.x];
+        part[(int64_t)blockIdx.y * N + k] = t;
+    }
+}
+
+int check_type(gcn_rows_type t, const char *who) {
+    GCN_REQUIRE(t == GCN_ROWS_F32 || t == GCN_ROWS_BF16, GCN_EINVAL, "%s: bad element type %d", who, (int)t);
+    return GCN_OK;
+}
+
+bool aligned(const void *p, uintptr_t b) { return (uintptr_t)p % b == 0; }
+
+unsigned grid_of(int64_t work, int64_t per_block, int64_t most) {
+    return (unsigned)std::max<int64_t>(1, std::min(most, (work + per_block - 1) / per_block));
+}
+
+}  // namespace
+
+int check_rows8(const gcn_rows8 *r, const char *who) {
+    GCN_REQUIRE(r, GCN_EINVAL, "%s: null 8-bit rows", who);
+    GCN_REQUIRE(r->n >= 0 && r->f > 0, GCN_ESHAPE, "%s: 8-bit rows of %d x %d", who, r->n, r->f);
+    GCN_REQUIRE(r->ldq % 16 == 0 && r->ldq >= kBlk * blocks8(r->f), GCN_ESHAPE,
+                "%s: ldq=%d is not a multiple of 16 of at least %lld", who, r->ldq, (long long)(kBlk * blocks8(r->f)));
+    GCN_REQUIRE(r->ldscale >= blocks8(r->f), GCN_ESHAPE, "%s: ldscale=%d < %lld", who, r->ldscale,
+                (long long)blocks8(r->f));
+    GCN_REQUIRE(r->n == 0 || (r->q && r->scale), GCN_EINVAL, "%s: null 8-bit rows", who);
+    GCN_REQUIRE(aligned(r->q, 16), GCN_EINVAL, "%s: 8-bit rows must be 16-byte aligned", who);
+    return GCN_OK;
+}
+
+int rows8_pack(int32_t n, int32_t f, const void *X, int x_bf16, int64_t ldx, uint8_t *q, int64_t ldq,
+               uint8_t *scale, int64_t lds, hipStream_t s) {
+    if (n == 0) return GCN_OK;
+    const int32_t per_row = (int32_t)blocks8(f);
+    const int64_t blocks = (int64_t)n * per_row;
+    ProfScope prof(K_ROWS8_PACK, s, 0.0, (double)n * f * (x_bf16 ? 3.0 : 5.0) + (double)blocks);
+    const unsigned g = grid_of(blocks, kTB / 16, 16384);
+    const bool vec = aligned(X, 16) && ldx % (x_bf16 ? 8 : 4) == 0;
+#define GCN_PACK(BF, VEC) \
+    hipLaunchKernelGGL((pack_kernel<BF, VEC>), dim3(g), dim3(kTB), 0, s, blocks, per_row, f, X, ldx, q, ldq, scale, lds)
+    if (x_bf16) {
+        if (vec) GCN_PACK(true, true);
+        else GCN_PACK(true, false);
+    } else {
+        if (vec) GCN_PACK(false, true);
+        else GCN_PACK(false, false);
+    }
+#undef GCN_PACK
+    GCN_LAUNCH_CHECK("pack_kernel");
+    return GCN_OK;
+}
+
+}  // namespace gcn
+
+using namespace gcn;
+
+extern "C" {
+
+int gcn_rows8_pack(const void *X, gcn_rows_type type, int32_t ldx, const gcn_rows8 *out, void *stream) {
+    int rc = check_rows8(out, "gcn_rows8_pack");
+    if (rc) return rc;
+    if ((rc = check_type(type, "gcn_rows8_pack"))) return rc;
+    GCN_REQUIRE(ldx >= out->f, GCN_ESHAPE, "gcn_rows8_pack: ldx=%d < f=%d", ldx, out->f);
+    GCN_REQUIRE(out->n == 0 || X, GCN_EINVAL, "gcn_rows8_pack: null pointer");
+    return rows8_pack(out->n, out->f, X, type == GCN_ROWS_BF16, ldx, out->q, out->ldq, out->scale, out->ldscale,
+                      (hipStream_t)stream);
+}
+
+int gcn_rows8_unpack(const gcn_rows8 *r, void *X, gcn_rows_type type, int32_t ldx, void *stream) {
+    int rc = check_rows8(r, "gcn_rows8_unpack");
+    if (rc) return rc;
+    if ((rc = check_type(type, "gcn_rows8_unpack"))) return rc;
+    GCN_REQUIRE(ldx >= r->f, GCN_ESHAPE, "gcn_rows8_unpack: ldx=%d < f=%d", ldx, r->f);
+    GCN_REQUIRE(r->n == 0 || X, GCN_EINVAL, "gcn_rows8_unpack: null pointer");
+    if (r->n == 0) return GCN_OK;
+    hipStream_t s = (hipStream_t)stream;
+    const int64_t total = (int64_t)r->n * r->f;
+    ProfScope prof(K_ROWS8_PACK, s, 0.0, (double)total * (type == GCN_ROWS_BF16 ? 3.0 : 5.0));
+    const unsigned g = grid_of(total, kTB, 16384);
+    if (type == GCN_ROWS_BF16)
+        hipLaunchKernelGGL(unpack_kernel<true>, dim3(g), dim3(kTB), 0, s, r->n, r->f, r->q, (int64_t)r->ldq, r->scale,
+                           (int64_t)r->ldscale, X, (int64_t)ldx);
+    else
+        hipLaunchKernelGGL(unpack_kernel<false>, dim3(g), dim3(kTB), 0, s, r->n, r->f, r->q, (int64_t)r->ldq, r->scale,
+                           (int64_t)r->ldscale, X, (int64_t)ldx);
+    GCN_LAUNCH_CHECK("unpack_kernel");
+    return GCN_OK;
+}
+
+int gcn_weights8_pack(const void *W, gcn_rows_type type, int32_t ldw, const gcn_weights8 *out, void *stream) {
+    GCN_REQUIRE(out && W, GCN_EINVAL, "gcn_weights8_pack: null pointer");
+    const int32_t K = out->K, N = out->N;
+    GCN_REQUIRE(K > 0 && N > 0, GCN_ESHAPE, "gcn_weights8_pack: K=%d N=%d", K, N);
+    int rc = check_type(type, "gcn_weights8_pack");
+    if (rc) return rc;
+    GCN_REQUIRE(ldw >= N, GCN_ESHAPE, "gcn_weights8_pack: ldw=%d < N=%d", ldw, N);
+    GCN_REQUIRE((out->q || out->qT) && out->scale, GCN_EINVAL, "gcn_weights8_pack: null 8-bit weights");
+    GCN_REQUIRE(!out->q || (out->ldq % 16 == 0 && out->ldq >= kBlk * blocks8(N) && aligned(out->q, 16)), GCN_ESHAPE,
+                "gcn_weights8_pack: q needs 16-byte alignment and ldq=%d a multiple of 16 of at least %lld", out->ldq,
+                (long long)(kBlk * blocks8(N)));
+    GCN_REQUIRE(!out->qT || (out->ldqT % 16 == 0 && out->ldqT >= kBlk * blocks8(K) && aligned(out->qT, 16)), GCN_ESHAPE,
+                "gcn_weights8_pack: qT needs 16-byte alignment and ldqT=%d a multiple of 16 of at least %lld",
+                out->ldqT, (long long)(kBlk * blocks8(K)));
+    GCN_REQUIRE(out->ldscale >= blocks8(N), GCN_ESHAPE, "gcn_weights8_pack: ldscale=%d < %lld", out->ldscale,
+                (long long)blocks8(N));
+    GCN_REQUIRE(blocks8(K) <= 65535, GCN_EUNSUPPORTED, "gcn_weights8_pack: K=%d", K);
+    hipStream_t s = (hipStream_t)stream;
+    ProfScope prof(K_ROWS8_PACK, s, 0.0,
+                   (double)K * N * ((type == GCN_ROWS_BF16 ? 2.0 : 4.0) + (out->q ? 1 : 0) + (out->qT ? 1 : 0)));
+    const dim3 g((unsigned)blocks8(N), (unsigned)blocks8(K));
+    if (type == GCN_ROWS_BF16)
+        hipLaunchKernelGGL(pack_weights_kernel<true>, g, dim3(kTB), 0, s, K, N, W, (int64_t)ldw, out->q,
+                           (int64_t)out->ldq, out->qT, (int64_t)out->ldqT, out->scale, (int64_t)out->ldscale);
+    else
+        hipLaunchKernelGGL(pack_weights_kernel<false>, g, dim3(kTB), 0, s, K, N, W, (int64_t)ldw, out->q,
+                           (int64_t)out->ldq, out->qT, (int64_t)out->ldqT, out->scale, (int64_t)out->ldscale);
+    GCN_LAUNCH_CHECK("pack_weights_kernel");
+    return GCN_OK;
+}
+
+namespace {
+struct GradPlan {
+    int32_t Np, fp, split, strip, strips;
+    size_t gemm, total;
+};
+GemmProblem grad_problem(int32_t f, int32_t N, int32_t n) {
+    GemmProblem w{};
+    w.M = f;
+    w.N = N;
+    w.seg[0].K = n;
+    return w;
+}
+GradPlan plan_grad(int32_t n, int32_t f, int32_t N) {
+    GradPlan p{};
+    p.Np = (N + 7) / 8 * 8;
+    p.fp = (f + 7) / 8 * 8;
+    const GemmProblem w = grad_problem(f, N, n);
+    p.split = gemm_pick_split(1, &w, true);
+    p.gemm = gemm_workspace_bytes(1, &w, p.split);
+    // strips: about 2048 workgroups, at least 16 rows each
+    const int64_t most = std::max<int64_t>(1, 2048 / blocks8(N));
+    p.strip = (int32_t)std::max<int64_t>(16, ((n + most - 1) / most + 15) / 16 * 16);
+    p.strips = std::max(1, (n + p.strip - 1) / p.strip);
+    Arena ar(nullptr, 0);
+    ar.take<uint16_t>((size_t)n * p.Np);
+    ar.take<uint16_t>((size_t)n * p.fp);
+    ar.take<float>((size_t)p.strips * N);
+    ar.take<char>(p.gemm);
+    p.total = ar.used + 256;
+    return p;
+}
+}  // namespace
+
+size_t gcn_rows8_weight_grad_workspace_bytes(int32_t n, int32_t f, int32_t N) {
+    if (n < 0 || f <= 0 || N <= 0) return 0;
+    return plan_grad(n, f, N).total;
+}
+
+int gcn_rows8_weight_grad(const gcn_rows8 *X8, const uint8_t *mask, int32_t ldmask, const void *dY, gcn_rows_type type,
+                          int32_t lddy, int32_t N, float *dW, int32_t lddw, float *db, const gcn_rows8 *dZ8, void *ws,
+                          size_t ws_bytes, void *stream) {
+    int rc = check_rows8(X8, "gcn_rows8_weight_grad");
+    if (rc) return rc;
+    if ((rc = check_type(type, "gcn_rows8_weight_grad"))) return rc;
+    const int32_t n = X8->n, f = X8->f;
+    GCN_REQUIRE(N > 0, GCN_ESHAPE, "gcn_rows8_weight_grad: N=%d", N);
+    GCN_REQUIRE(lddy >= N && lddw >= N && (!mask || ldmask >= N), GCN_ESHAPE,
+                "gcn_rows8_weight_grad: lddy=%d lddw=%d ldmask=%d < N=%d", lddy, lddw, ldmask, N);
+    GCN_REQUIRE(dW && (n == 0 || dY), GCN_EINVAL, "gcn_rows8_weight_grad: null pointer");
+    if (dZ8) {
+        if ((rc = check_rows8(dZ8, "gcn_rows8_weight_grad"))) return rc;
+        GCN_REQUIRE(dZ8->n == n && dZ8->f == N, GCN_ESHAPE, "gcn_rows8_weight_grad: dZ8 is %d x %d, not %d x %d", dZ8->n,
+                    dZ8->f, n, N);
+    }
+    const GradPlan p = plan_grad(n, f, N);
+    GCN_REQUIRE(ws && aligned(ws, 256) && ws_bytes >= p.total, GCN_EWORKSPACE,
+                "gcn_rows8_weight_grad: workspace %zu < %zu bytes, or not 256-byte aligned", ws_bytes, p.total);
+    hipStream_t s = (hipStream_t)stream;
+    if (n == 0) {
+        for (int32_t i = 0; i < f; ++i)
+            if ((rc = fill_zero(dW + (int64_t)i * lddw, N, s))) return rc;
+        return db ? fill_zero(db, N, s) : GCN_OK;
+    }
+    Arena ar(ws, ws_bytes);
+    uint16_t *dZ = ar.take<uint16_t>((size_t)n * p.Np), *X = ar.take<uint16_t>((size_t)n * p.fp);
+    float *part = ar.take<float>((size_t)p.strips * N);
+    void *gw = p.gemm ? ar.take<char>(p.gemm) : nullptr;
+    {
+        const bool bf = type == GCN_ROWS_BF16;
+        ProfScope prof(K_ROWS8_MASK, s, 0.0, (double)n * N * ((bf ? 4.0 : 6.0) + (mask ? 1.0 : 0.0) + (dZ8 ? 1.0 : 0.0)));
+        const bool vec = aligned(dY, 16) && lddy % (bf ? 8 : 4) == 0 && (!mask || (aligned(mask, 8) && ldmask % 8 == 0));
+        const dim3 g((unsigned)blocks8(N), (unsigned)p.strips);
+#define GCN_MASK(BF, VEC)                                                                                              \
+    hipLaunchKernelGGL((mask_kernel<BF, VEC>), g, dim3(kTB), 0, s, n, N, p.strip, dY, (int64_t)lddy, mask,             \
+                       (int64_t)ldmask, dZ, (int64_t)p.Np, db ? part : nullptr, dZ8 ? dZ8->q : nullptr,                \
+                       dZ8 ? (int64_t)dZ8->ldq : 0, dZ8 ? dZ8->scale : nullptr, dZ8 ? (int64_t)dZ8->ldscale : 0)
+        if (bf) {
+            if (vec) GCN_MASK(true, true);
+            else GCN_MASK(true, false);
+        } else {
+            if (vec) GCN_MASK(false, true);
+            else GCN_MASK(false, false);
+        }
+#undef GCN_MASK
+        GCN_LAUNCH_CHECK("mask_kernel");
+    }
+    if (db && (rc = colsum_reduce_rows(p.strips, N, part, db, s))) return rc;
+    ProfScope prof(K_ROWS8_WEIGHT_GRAD, s, 2.0 * n * f * N, (double)n * f + 2.0 * n * N + 4.0 * f * N);
+    hipLaunchKernelGGL(unpack_kernel<true>, dim3(grid_of((int64_t)n * f, kTB, 16384)), dim3(kTB), 0, s, n, f, X8->q,
+                       (int64_t)X8->ldq, X8->scale, (int64_t)X8->ldscale, (void *)X, (int64_t)p.fp);
+    GCN_LAUNCH_CHECK("unpack_kernel");
+    GemmProblem w = grad_problem(f, N, n);
+    w.C = dW;
+    w.ldc = lddw;
+    w.seg[0] = GemmSeg{X, p.fp, dZ, p.Np, n};
+    return gemm(L_TN, 1, &w, 1, p.split, gw, p.gemm, s);
+}
+
+}  // extern "C"
