@@ -19,6 +19,7 @@ namespace gcn {
 namespace {
 
 constexpr int kTB = 256;
+constexpr int kSmallTile = 128;   // rows and columns of the smallest tiles
 
 __device__ __forceinline__ bool has_label(int32_t l, int32_t C) { return l >= 0 && l < C; }
 
@@ -220,20 +221,19 @@ Plan plan_of(int32_t n, int32_t f, int32_t C, bool bf, bool grad, void *ws, size
     b.label_logit = ar.take<float>(rows);
     b.lse = ar.take<float>(rows);
     if (bf) {
-        const TileShape t = tile_shape(TILE_BF16, TILE_STATS, n, p.piece, (int32_t)(p.fp / 64));
-        const int64_t tn = (p.piece + t.n - 1) / t.n;
+        // (sized for the smallest tiles: a last, smaller piece may run on them)
+        const int64_t tn = (p.piece + kSmallTile - 1) / kSmallTile;
         b.tile_max = ar.take<float>(tn * rows);
         b.tile_sum = ar.take<float>(tn * rows);
         b.H = ar.take<uint16_t>(rows * p.fp);
         b.WT = ar.take<uint16_t>((size_t)p.piece * p.fp);
         if (grad) {
             const int64_t pp = up(p.piece, 64);
-            const TileShape tg = tile_shape(TILE_BF16, TILE_GRAD, n, p.piece, (int32_t)(p.fp / 64));
             b.HT = ar.take<uint16_t>(f * p.np);
             b.W = ar.take<uint16_t>(f * pp);
             b.G = ar.take<uint16_t>(rows * pp);
             b.GT = ar.take<uint16_t>((size_t)p.piece * p.np);
-            b.colpart = ar.take<float>((rows + tg.m - 1) / tg.m * p.piece);
+            b.colpart = ar.take<float>((rows + kSmallTile - 1) / kSmallTile * p.piece);
             p.split_h = tile_splits(TILE_BF16, n, f, (int32_t)(pp / 64));
             p.split_w = tile_splits(TILE_BF16, f, p.piece, (int32_t)(p.np / 64));
             b.acc = ar.take<float>((size_t)p.split_h * rows * f);
@@ -300,7 +300,7 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
             ProfScope prof(K_CLASS_STATS, s, 2.0 * n * f * P, 2.0 * ((double)n + P) * f);
             if ((rc = tile_product(TILE_BF16, TILE_STATS, t, s))) return rc;
         }
-        const TileShape sh = tile_shape(TILE_BF16, TILE_STATS, n, P, t.kt);
+        const TileShape sh = tile_shape(TILE_BF16, t);
         ProfScope prof(K_CLASS_PREP, s, 0.0, 8.0 * n * ((P + sh.n - 1) / sh.n));
         hipLaunchKernelGGL(join_kernel, dim3((unsigned)((n + kTB - 1) / kTB)), dim3(kTB), 0, s, n, (P + sh.n - 1) / sh.n,
                            b.tile_max, b.tile_sum, b.run_max, b.run_sum, i == 0);
@@ -325,7 +325,7 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
             ProfScope prof(K_CLASS_GRAD, s, 2.0 * n * f * P, 2.0 * ((double)n + P) * f + 4.0 * n * P);
             if ((rc = tile_product(TILE_BF16, TILE_GRAD, t, s))) return rc;
         }
-        const TileShape sh = tile_shape(TILE_BF16, TILE_GRAD, n, P, t.kt);
+        const TileShape sh = tile_shape(TILE_BF16, t);
         if ((rc = colsum_reduce_rows((n + sh.m - 1) / sh.m, P, b.colpart, db + c0, s))) return rc;
         hipLaunchKernelGGL(copy_rows_kernel<uint16_t>, dim3(grid_of(f * pp)), dim3(kTB), 0, s, f, P, W + c0, (int64_t)C,
                            b.W, pp, (const int32_t *)nullptr, 0);

@@ -14,6 +14,7 @@
 // The instructions are issued with B's fragment first, which leaves a lane
 // with four consecutive columns of one row of C.
 #include <algorithm>
+#include <type_traits>
 
 #include "rows8.h"
 
@@ -381,6 +382,228 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
     finish<EPI, BM, BN, WM, WN, FM, FN>(a, c, acc, lds);
 }
 
+// ------------------------------------------------------------ large tiles
+// 256 x 256 tiles of 8 wavefronts (2 along M, 4 along N; 128 x 64 each), one
+// workgroup a CU, two wavefronts a SIMD that take turns: while one multiplies a
+// quarter of its tile, the other reads fragments and issues copies, and a
+// barrier every quarter swaps them.  The wavefronts of the second row start one
+// barrier late, which keeps the two halves apart for the whole loop.
+//
+// A piece of the tile is four regions of 128 rows: A's and B's rows that the
+// first and the second quarter of every wavefront reads.  Quarters of piece t:
+//   0: A-lo x B-lo (reads A-lo)      1: A-lo x B-hi (reads B-hi)
+//   2: A-hi x B-hi (reads A-hi)      3: A-hi x B-lo (reads B-lo of t + 1)
+// Two pieces are in LDS (128 KB); a region is refilled two quarters after it
+// was read, with the rows of two pieces later, which are read six quarters
+// after that: copies have about 3000 cycles to land, and no wait is ever for
+// the newest ones.
+//
+// Order of events.  Call a stretch between barriers a turn: the first half of
+// the wavefronts reads in quarter q at turn 2q and multiplies at 2q + 1, the
+// second one a turn later.  Reads of quarter q have returned to their
+// wavefront by the end of its multiplication, turn 2q + 2 at the latest, and
+// copies over them go out in quarter q + 2, turn 2q + 4 at the earliest.  A
+// wavefront waits for its own copies of what quarter q + 1 reads in quarter q,
+// turn 2q + 1 at the latest; quarter q + 1 reads at turn 2q + 2 at the earliest.
+constexpr int kBigT = 256, kBigThreads = 512;
+constexpr int kRegion = 128 * kPiece, kBuffer = 4 * kRegion;
+constexpr int kBigPieces = 120;                          // pieces whose scales fit in LDS
+constexpr int kScaleA = kBigPieces * 64 * 4, kScaleB = kBigPieces * 2;
+
+// 16 bytes a lane from base + off straight to LDS at dst + 16 lane (base, dst
+// uniform).  In assembly because the compiler, which sees only that both touch
+// LDS, puts a wait for every outstanding copy before each LDS read, and this
+// kernel keeps five quarters of copies in flight.  The instruction has no
+// register result that could be taken for written, its operands are read as it
+// is issued, and the kernel waits by wait_copies and a barrier.
+__device__ __forceinline__ void copy_to_lds(const uint8_t *base, uint32_t off, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void turn() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+template <int TYPE, int I, int J>
+__device__ __forceinline__ void mma_big(f32x4 &acc, const Frag &a, const Frag &b, int sa, int sb) {
+    if constexpr (TYPE == TILE_FP8)
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i32x8, b),
+                                                               __builtin_bit_cast(i32x8, a), acc, 0, 0, 0, sb, I, sa);
+    else
+        mma<TYPE>(acc, a, b, 0, 0);
+}
+
+template <int TYPE, int EPI>
+__global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void big_kernel(Args a) {
+    __shared__ __attribute__((aligned(16))) char lds[2 * kBuffer + (TYPE == TILE_FP8 ? kScaleA + kScaleB : 0)];
+    Coord c;
+    if (!coord_of(a, c)) return;
+    const TileProduct &p = a.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 2, wn = wave & 3;
+    const int m0 = c.tm * kBigT, n0 = c.tn * kBigT;
+    const int kt0 = c.split * a.kt_per_split;
+    const int nt = min(a.kt_per_split, p.kt - kt0);
+
+    // Copies: region row (8 u + wave) 8 + lane / 8, stored chunk lane % 8 with
+    // the row's chunk (lane % 8) ^ (row % 8); rows past the extent are clamped.
+    const uint8_t *const ba = p.A + (int64_t)m0 * p.lda + (int64_t)kt0 * kPiece;
+    const uint8_t *const bb = p.B + (int64_t)n0 * p.ldb + (int64_t)kt0 * kPiece;
+    uint32_t oa[2][2], ob[2][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int rr = (8 * u + wave) * 8 + (lane >> 3);
+        const uint32_t ch = (uint32_t)(((lane & 7) ^ (rr & 7)) * 16);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            oa[h][u] = (uint32_t)min((rr >> 6) * 128 + (rr & 63) + 64 * h, p.M - 1 - m0) * (uint32_t)p.lda + ch;
+            ob[h][u] = (uint32_t)min((rr >> 5) * 64 + (rr & 31) + 32 * h, p.N - 1 - n0) * (uint32_t)p.ldb + ch;
+        }
+    }
+    // region 0, 1: A-lo, A-hi; 2, 3: B-lo, B-hi
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * 1024;
+    auto copy = [&](int region, int t) {
+        const uint8_t *g = (region < 2 ? ba : bb) + (int64_t)t * kPiece;
+        const uint32_t d = lds0 + (t & 1) * kBuffer + region * kRegion;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) copy_to_lds(g, region < 2 ? oa[region & 1][u] : ob[region & 1][u], d + u * 8192);
+    };
+
+    f32x4 acc[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int fr = lane & 15, g = lane >> 4;
+    const int o0 = (g ^ (fr & 7)) * 16, o1 = ((g + 4) ^ (fr & 7)) * 16;
+    const char *const la = lds + (wm * 64 + fr) * kPiece, *const lb = lds + 2 * kRegion + (wn * 32 + fr) * kPiece;
+    auto read_a = [&](Frag (&f)[4], int t, int h) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const char *q = la + (t & 1) * kBuffer + h * kRegion + i * 16 * kPiece;
+            f[i] = Frag{*(const uint4 *)(q + o0), *(const uint4 *)(q + o1)};
+        }
+    };
+    auto read_b = [&](Frag (&f)[2], int t, int h) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const char *q = lb + (t & 1) * kBuffer + h * kRegion + j * 16 * kPiece;
+            f[j] = Frag{*(const uint4 *)(q + o0), *(const uint4 *)(q + o1)};
+        }
+    };
+    // Scales: for a piece, 16 lanes' words of four row blocks' bytes (the
+    // instruction picks one): [piece][wm][lo, hi][lane % 16]; B's by 128 columns.
+    const uint32_t *const wsa = (const uint32_t *)(lds + 2 * kBuffer) + wm * 32 + fr;
+    const uint8_t *const wsb = (const uint8_t *)lds + 2 * kBuffer + kScaleA + (wn >> 1);
+    int sa[2] = {0, 0}, sb = 0;
+
+    Frag fa[4], bl[2], bh[2], bn[2];
+    auto quarter = [&](int h, int k, const Frag (&b)[2]) {   // rows half h, columns half k
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            mma_big<TYPE, 0, 0>(acc[4 * h + 0][2 * k + j], fa[0], b[j], sa[h], sb);
+            mma_big<TYPE, 1, 0>(acc[4 * h + 1][2 * k + j], fa[1], b[j], sa[h], sb);
+            mma_big<TYPE, 2, 0>(acc[4 * h + 2][2 * k + j], fa[2], b[j], sa[h], sb);
+            mma_big<TYPE, 3, 0>(acc[4 * h + 3][2 * k + j], fa[3], b[j], sa[h], sb);
+        }
+        // (the sums are pinned here, or the compiler moves the products past the barriers)
+        asm volatile("" : "+v"(acc[4 * h][2 * k]), "+v"(acc[4 * h + 1][2 * k]), "+v"(acc[4 * h + 2][2 * k]),
+                     "+v"(acc[4 * h + 3][2 * k]), "+v"(acc[4 * h][2 * k + 1]), "+v"(acc[4 * h + 1][2 * k + 1]),
+                     "+v"(acc[4 * h + 2][2 * k + 1]), "+v"(acc[4 * h + 3][2 * k + 1]));
+        __builtin_amdgcn_s_setprio(0);
+    };
+    // waits until at most N loads are outstanding, N by the pieces left behind
+    // this one (two or more, one, none): the loads issued after the awaited ones
+    auto wait_for = [&](int left, auto n2, auto n1, auto n0) {
+        if (left >= 2) wait_copies<decltype(n2)::value>();
+        else if (left == 1) wait_copies<decltype(n1)::value>();
+        else wait_copies<decltype(n0)::value>();
+    };
+    using std::integral_constant;
+    auto piece = [&](int t) {
+        const int left = nt - 1 - t;
+        // quarter 0
+        read_a(fa, t, 0);
+        if constexpr (TYPE == TILE_FP8) {
+            sa[0] = (int)wsa[t * 64];
+            sa[1] = (int)wsa[t * 64 + 16];
+            sb = wsb[t * 2];
+        }
+        if (left >= 1) copy(1, t + 1);
+        wait_for(left, integral_constant<int, 10>{}, integral_constant<int, 10>{}, integral_constant<int, 2>{});
+        turn();
+        quarter(0, 0, bl);
+        turn();
+        // quarter 1
+        read_b(bh, t, 1);
+        if (left >= 2) copy(2, t + 2);
+        wait_for(left, integral_constant<int, 10>{}, integral_constant<int, 8>{}, integral_constant<int, 0>{});
+        turn();
+        quarter(0, 1, bh);
+        turn();
+        // quarter 2
+        read_a(fa, t, 1);
+        if (left >= 2) copy(0, t + 2);
+        wait_for(left, integral_constant<int, 10>{}, integral_constant<int, 6>{}, integral_constant<int, 0>{});
+        turn();
+        quarter(1, 1, bh);
+        turn();
+        // quarter 3 (behind the last piece the read is of a stale one, unused)
+        read_b(bn, t + 1, 0);
+        if (left >= 2) copy(3, t + 2);
+        wait_for(left, integral_constant<int, 10>{}, integral_constant<int, 4>{}, integral_constant<int, 0>{});
+        turn();
+        wait_reads();   // bn's: its region is refilled in quarter 1, before bn is used
+        quarter(1, 0, bl);
+        turn();
+        bl[0] = bn[0];
+        bl[1] = bn[1];
+    };
+    if (nt > 0) {
+        if constexpr (TYPE == TILE_FP8) {
+            // (before any copy is in flight: these loads are waited for)
+            uint8_t *s8 = (uint8_t *)lds + 2 * kBuffer;
+            for (int i = threadIdx.x; i < kBigT * nt; i += kBigThreads) {
+                const int r = i / nt, t = i - r * nt;   // row of the tile: wm 128 + lo/hi 64 + block 16 + lane
+                s8[(t * 64 + (r >> 7) * 32 + ((r >> 6) & 1) * 16 + (r & 15)) * 4 + ((r >> 4) & 3)] =
+                    p.sa[(int64_t)min(m0 + r, p.M - 1) * p.ldsa + kt0 + t];
+            }
+            for (int i = threadIdx.x; i < 2 * nt; i += kBigThreads)
+                s8[kScaleA + i] = p.sb[(int64_t)(min(n0 + (i & 1) * 128, p.N - 1) / kRows8Block) * p.sb_n +
+                                       (int64_t)(kt0 + (i >> 1)) * p.sb_k];
+            __syncthreads();
+        }
+        copy(2, 0);
+        copy(0, 0);
+        copy(3, 0);
+        copy(1, 0);
+        if (nt > 1) {
+            copy(2, 1);
+            copy(0, 1);
+            copy(3, 1);
+            wait_copies<10>();
+        } else {
+            wait_copies<4>();
+        }
+        turn();
+        read_b(bl, 0, 0);
+        wait_reads();
+        if (wm) turn();
+        for (int t = 0; t < nt; ++t) piece(t);
+        if (!wm) turn();
+    }
+    finish<EPI, kBigT, kBigT, 2, 4, 8, 4>(a, c, acc, lds);
+}
+
 __global__ __launch_bounds__(256) void reduce_kernel(int32_t splits, int64_t count, int32_t N, const float *acc,
                                                      void *out, int out_bf16, int64_t ldo) {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
@@ -393,24 +616,39 @@ __global__ __launch_bounds__(256) void reduce_kernel(int32_t splits, int64_t cou
 }
 
 template <int TYPE, int EPI>
-void launch_small(const Args &a, unsigned grid, hipStream_t s) {
+void launch(bool big, const Args &a, unsigned grid, hipStream_t s) {
+    if constexpr (TYPE != TILE_FP8_EXACT) {
+        if (big) {
+            hipLaunchKernelGGL((big_kernel<TYPE, EPI>), dim3(grid), dim3(kBigThreads), 0, s, a);
+            return;
+        }
+    }
     hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 128, 128, 2, 2>), dim3(grid), dim3(256), 0, s, a);
 }
 
+int64_t tiles_of(int64_t M, int64_t N, int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); }
+
 }  // namespace
 
-TileShape tile_shape(TileType, TileEpilogue, int32_t, int32_t, int32_t) { return TileShape{128, 128}; }
+TileShape tile_shape(TileType type, const TileProduct &p) {
+    const int32_t splits = std::max(1, p.splits), per = (p.kt + splits - 1) / splits;
+    const bool big = type != TILE_FP8_EXACT && tiles_of(p.M, p.N, kBigT) * splits >= 160 && per >= 4 &&
+                     (type == TILE_BF16 || per <= kBigPieces) && std::max(p.lda, p.ldb) < (1 << 24);
+    return big ? TileShape{kBigT, kBigT} : TileShape{128, 128};
+}
 
 int32_t tile_splits(TileType type, int32_t M, int32_t N, int32_t kt) {
-    const TileShape t = tile_shape(type, TILE_PARTIAL, M, N, kt);
-    const int64_t tiles = (int64_t)((M + t.m - 1) / t.m) * ((N + t.n - 1) / t.n);
-    const int64_t sp = std::min<int64_t>(512 / std::max<int64_t>(1, tiles), kt / 8);
+    (void)type;
+    const int64_t tiles = std::max<int64_t>(1, tiles_of(M, N, kBigT));
+    int64_t sp = std::max<int64_t>(1, 256 / tiles);
+    if (sp > kt / 8) sp = std::min<int64_t>(512 / std::max<int64_t>(1, tiles_of(M, N, 128)), kt / 8);
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>(sp, 64));
 }
 
 int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStream_t s) {
     if (p.M <= 0 || p.N <= 0) return GCN_OK;
-    const TileShape t = tile_shape(type, epi, p.M, p.N, p.kt);
+    const TileShape t = tile_shape(type, p);
+    const bool big = t.m == kBigT;
     Args a;
     a.p = p;
     a.tiles_m = (p.M + t.m - 1) / t.m;
@@ -426,16 +664,16 @@ int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStrea
     }
     const unsigned grid = (unsigned)(8 * a.per_xcd);
     if (type == TILE_BF16) {
-        if (epi == TILE_STORE) launch_small<TILE_BF16, TILE_STORE>(a, grid, s);
-        else if (epi == TILE_PARTIAL) launch_small<TILE_BF16, TILE_PARTIAL>(a, grid, s);
-        else if (epi == TILE_STATS) launch_small<TILE_BF16, TILE_STATS>(a, grid, s);
-        else launch_small<TILE_BF16, TILE_GRAD>(a, grid, s);
+        if (epi == TILE_STORE) launch<TILE_BF16, TILE_STORE>(big, a, grid, s);
+        else if (epi == TILE_PARTIAL) launch<TILE_BF16, TILE_PARTIAL>(big, a, grid, s);
+        else if (epi == TILE_STATS) launch<TILE_BF16, TILE_STATS>(big, a, grid, s);
+        else launch<TILE_BF16, TILE_GRAD>(big, a, grid, s);
     } else if (type == TILE_FP8) {
-        if (epi == TILE_STORE) launch_small<TILE_FP8, TILE_STORE>(a, grid, s);
-        else launch_small<TILE_FP8, TILE_PARTIAL>(a, grid, s);
+        if (epi == TILE_STORE) launch<TILE_FP8, TILE_STORE>(big, a, grid, s);
+        else launch<TILE_FP8, TILE_PARTIAL>(big, a, grid, s);
     } else {
-        if (epi == TILE_STORE) launch_small<TILE_FP8_EXACT, TILE_STORE>(a, grid, s);
-        else launch_small<TILE_FP8_EXACT, TILE_PARTIAL>(a, grid, s);
+        if (epi == TILE_STORE) launch<TILE_FP8_EXACT, TILE_STORE>(big, a, grid, s);
+        else launch<TILE_FP8_EXACT, TILE_PARTIAL>(big, a, grid, s);
     }
     GCN_LAUNCH_CHECK("tile_kernel");
     return GCN_OK;

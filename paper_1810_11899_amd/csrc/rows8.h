@@ -54,8 +54,11 @@ struct TileProduct {
     float *colpart;                 // [tiles_m x N]
 };
 // rows and columns of the tiles that this product runs on
-struct TileShape { int32_t m, n; };
-TileShape tile_shape(TileType type, TileEpilogue epi, int32_t M, int32_t N, int32_t kt);
+// the tiles that this product runs on: rows and columns of each
+struct TileShape {
+    int32_t m, n;
+};
+TileShape tile_shape(TileType type, const TileProduct &p);
 int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStream_t s);
 // out (float32, or bfloat16 rows of ldo) = the sum of `splits` partials M x N, in order
 int tile_reduce(int32_t splits, int32_t M, int32_t N, const float *acc, void *out, int out_bf16, int64_t ldo,

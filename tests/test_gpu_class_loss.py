@@ -83,7 +83,7 @@ def check(H, W, b, lab, out, dtype):
 
 
 SIZES = [(1, 1, 1), (1, 64, 3), (2, 3, 2), (17, 50, 41), (64, 64, 128), (65, 130, 129), (130, 96, 1000), (300, 257, 517),
-         (33, 512, 4099)]
+         (33, 512, 4099), (2100, 200, 5300), (2600, 1030, 4500)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

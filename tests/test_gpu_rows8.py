@@ -165,6 +165,35 @@ def test_product(n, K, N, transpose, pad, dtype):
             assert float(torch.as_strided(Y, (n, N + pad), (N + pad, 1))[:, N:].min()) == 7.0
 
 
+@pytest.mark.parametrize("n, K, N, transpose", [(3001, 1400, 3500, False), (4000, 1, 3003, True), (4100, 640, 2900, True),
+                                                (33, 4000, 20000, False), (2600, 16500, 4200, False)])
+def test_product_of_many_tiles(n, K, N, transpose):
+    """Sizes of the large tiles, against float64 on the GPU; the bound of product_bound."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n + K)
+    x = torch.randn(n, K, generator=g, device="cuda") * torch.exp(torch.randn(n, 1, generator=g, device="cuda"))
+    w = torch.randn(*((N, K) if transpose else (K, N)), generator=g, device="cuda") / 64
+    b = torch.randn(N, generator=g, device="cuda")
+    X8, W8 = B.gcn_rows8_pack(x, B.Rows8(n, K)), B.gcn_weights8_pack(w, B.Weights8(*w.shape))
+    xv = B.gcn_rows8_unpack(X8, torch.empty_like(x)).double()
+    e = W8.scale.double().repeat_interleave(128, 0)[:w.shape[0]].repeat_interleave(128, 1)[:, :w.shape[1]] - 127
+    wv = W8.values.double() * torch.ldexp(torch.ones((), dtype=torch.float64, device="cuda"), e)
+    wv = wv.T.contiguous() if transpose else wv
+    y, mag = xv @ wv + b, xv.abs() @ wv.abs() + b.abs()
+    ws = B.Workspace()
+    for t in (torch.float32, torch.bfloat16):
+        Y = torch.full((n, N), 7.0, dtype=t, device="cuda")
+        B.gcn_rows8_product(X8, W8, Y, ws, bias=b, relu=False, transpose=transpose)
+        tol = (K + 2) * 2.0 ** -23 * mag
+        if t == torch.bfloat16:   # (the largest of 8 products is at most their sum)
+            tol = tol + 7 * 2.0 ** -13 * mag
+            tol = tol + 2.0 ** -8 * (y.abs() + tol)
+        assert bool(((Y.double() - y).abs() <= tol).all()), float(((Y.double() - y).abs() / tol).max())
+        again = torch.empty_like(Y)
+        B.gcn_rows8_product(X8, W8, again, ws, bias=b, relu=False, transpose=transpose)
+        assert torch.equal(Y, again)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_product_at_the_ends_of_the_scale(dtype):
     """Scales whose product leaves float32, and blocks of very unlike scale in one sum."""
