@@ -6,10 +6,8 @@
 //     it, joined into the row's running maximum and sum
 //   loss: row_loss = max + log(sum) - label's logit
 //   pass 2, per piece: the logits again, G = (softmax - onehot) / n_l in the
-//     same registers, written as bfloat16 rows and transposed rows; then
-//     dHL += G W_piece^T and dW_piece = HL^T G.
-// Every product is C = A B^T of operands contiguous along the contraction, so
-// W's piece is transposed once a pass and HL once a call.
+//     same registers, written as bfloat16 rows; then dHL += G W_piece^T and
+//     dW_piece = HL^T G.
 #include <algorithm>
 
 #include "gcn_classes.h"
@@ -39,16 +37,17 @@ __global__ __launch_bounds__(1024) void count_kernel(int32_t n, int32_t C, const
     }
 }
 
-// dst [rows x ldd] = src [rows x cols] (lds), zero past cols and in rows
-// without a label
+// dst [drows x ldd] = src [rows x cols] (lds), zero past rows and cols and in
+// rows without a label
 template <class T>
-__global__ __launch_bounds__(kTB) void copy_rows_kernel(int32_t rows, int32_t cols, const T *src, int64_t lds, T *dst,
-                                                        int64_t ldd, const int32_t *labels, int32_t C) {
-    const int64_t total = (int64_t)rows * ldd;
+__global__ __launch_bounds__(kTB) void copy_rows_kernel(int32_t drows, int32_t rows, int32_t cols, const T *src,
+                                                        int64_t lds, T *dst, int64_t ldd, const int32_t *labels,
+                                                        int32_t C) {
+    const int64_t total = (int64_t)drows * ldd;
     for (int64_t i = (int64_t)blockIdx.x * kTB + threadIdx.x; i < total; i += (int64_t)gridDim.x * kTB) {
         const int64_t r = i / ldd;
         const int32_t c = (int32_t)(i - r * ldd);
-        dst[i] = c < cols && (!labels || has_label(labels[r], C)) ? src[r * lds + c] : (T)0;
+        dst[i] = r < rows && c < cols && (!labels || has_label(labels[r], C)) ? src[r * lds + c] : (T)0;
     }
 }
 
@@ -186,7 +185,7 @@ struct Plan {
 };
 struct Buffers {
     float *inv_count, *run_max, *run_sum, *label_logit, *lse, *tile_max, *tile_sum, *colpart, *acc, *part, *X, *tmp;
-    uint16_t *H, *HT, *WT, *W, *G, *GT;
+    uint16_t *H, *WT, *W, *G;
     float *Hz;
     void *gemm_ws, *col_ws;
     size_t gemm_bytes, col_bytes;
@@ -200,8 +199,7 @@ GemmProblem dw_f32(int32_t f, int32_t P, int32_t n) {
     return w;
 }
 
-// The elements of a piece: bfloat16 G and its transpose take 4 bytes each
-// together, float32 logits 4.
+// The elements of a piece: bfloat16 G takes 2 bytes each, float32 logits 4.
 constexpr int64_t kPieceElems = (int64_t)1 << 28, kPieceElemsF32 = (int64_t)1 << 26;
 
 Plan plan_of(int32_t n, int32_t f, int32_t C, bool bf, bool grad, void *ws, size_t ws_bytes, Buffers &b) {
@@ -225,17 +223,15 @@ Plan plan_of(int32_t n, int32_t f, int32_t C, bool bf, bool grad, void *ws, size
         const int64_t tn = (p.piece + kSmallTile - 1) / kSmallTile;
         b.tile_max = ar.take<float>(tn * rows);
         b.tile_sum = ar.take<float>(tn * rows);
-        b.H = ar.take<uint16_t>(rows * p.fp);
+        b.H = ar.take<uint16_t>(p.np * p.fp);
         b.WT = ar.take<uint16_t>((size_t)p.piece * p.fp);
         if (grad) {
             const int64_t pp = up(p.piece, 64);
-            b.HT = ar.take<uint16_t>(f * p.np);
             b.W = ar.take<uint16_t>(f * pp);
-            b.G = ar.take<uint16_t>(rows * pp);
-            b.GT = ar.take<uint16_t>((size_t)p.piece * p.np);
+            b.G = ar.take<uint16_t>(p.np * pp);
             b.colpart = ar.take<float>((rows + kSmallTile - 1) / kSmallTile * p.piece);
-            p.split_h = tile_splits(TILE_BF16, n, f, (int32_t)(pp / 64));
-            p.split_w = tile_splits(TILE_BF16, f, p.piece, (int32_t)(p.np / 64));
+            p.split_h = tile_splits(n, f, (int32_t)(pp / 64));
+            p.split_w = tile_splits(f, p.piece, (int32_t)(p.np / 64));
             b.acc = ar.take<float>((size_t)p.split_h * rows * f);
             if (p.split_w > 1) b.part = ar.take<float>((size_t)p.split_w * f * p.piece);
         }
@@ -264,11 +260,8 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
     {
         ProfScope prof(K_CLASS_PREP, s, 0.0, 4.0 * n * f);
         hipLaunchKernelGGL(count_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, b.inv_count);
-        hipLaunchKernelGGL(copy_rows_kernel<uint16_t>, dim3(grid_of(n * p.fp)), dim3(kTB), 0, s, n, f, HL, ldhl, b.H,
-                           p.fp, labels, C);
-        if (dHL)
-            hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)(p.np / 64), (unsigned)((f + 63) / 64)), dim3(kTB), 0, s,
-                               n, f, HL, ldhl, b.HT, p.np, labels, C);
+        hipLaunchKernelGGL(copy_rows_kernel<uint16_t>, dim3(grid_of(p.np * p.fp)), dim3(kTB), 0, s, (int32_t)p.np, n, f,
+                           HL, ldhl, b.H, p.fp, labels, C);
         GCN_LAUNCH_CHECK("class_prep");
     }
     auto logits = [&](int32_t c0, int32_t P) {
@@ -318,8 +311,7 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         t.inv_count = b.inv_count;
         t.G = b.G;
         t.ldg = pp;
-        t.GT = b.GT;
-        t.ldgt = p.np;
+        t.g_rows = p.np;
         t.colpart = b.colpart;
         {
             ProfScope prof(K_CLASS_GRAD, s, 2.0 * n * f * P, 2.0 * ((double)n + P) * f + 4.0 * n * P);
@@ -327,7 +319,7 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         }
         const TileShape sh = tile_shape(TILE_BF16, t);
         if ((rc = colsum_reduce_rows((n + sh.m - 1) / sh.m, P, b.colpart, db + c0, s))) return rc;
-        hipLaunchKernelGGL(copy_rows_kernel<uint16_t>, dim3(grid_of(f * pp)), dim3(kTB), 0, s, f, P, W + c0, (int64_t)C,
+        hipLaunchKernelGGL(copy_rows_kernel<uint16_t>, dim3(grid_of(f * pp)), dim3(kTB), 0, s, f, f, P, W + c0, (int64_t)C,
                            b.W, pp, (const int32_t *)nullptr, 0);
         GCN_LAUNCH_CHECK("copy_rows_kernel");
         ProfScope prof(K_CLASS_PRODUCT, s, 4.0 * n * f * P, 4.0 * n * P);
@@ -344,23 +336,23 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         h.accumulate = i > 0;
         if ((rc = tile_product(TILE_BF16, TILE_PARTIAL, h, s))) return rc;
         TileProduct w{};
-        w.A = (const uint8_t *)b.HT;
-        w.lda = 2 * p.np;
-        w.B = (const uint8_t *)b.GT;
-        w.ldb = 2 * p.np;
+        w.A = (const uint8_t *)b.H;
+        w.lda = 2 * p.fp;
+        w.B = (const uint8_t *)b.G;
+        w.ldb = 2 * pp;
         w.M = f;
         w.N = P;
         w.kt = (int32_t)(p.np / 64);
         w.splits = p.split_w;
         if (p.split_w > 1) {
             w.acc = b.part;
-            if ((rc = tile_product(TILE_BF16, TILE_PARTIAL, w, s))) return rc;
+            if ((rc = tile_product(TILE_BF16_KM, TILE_PARTIAL, w, s))) return rc;
             if ((rc = tile_reduce(p.split_w, f, P, b.part, dW + c0, 1, C, s))) return rc;
         } else {
             w.C = dW + c0;
             w.ldc = C;
             w.c_bf16 = 1;
-            if ((rc = tile_product(TILE_BF16, TILE_STORE, w, s))) return rc;
+            if ((rc = tile_product(TILE_BF16_KM, TILE_STORE, w, s))) return rc;
         }
     }
     return tile_reduce(p.split_h, n, f, b.acc, dHL, 1, lddhl, s);
@@ -371,7 +363,7 @@ int loss_f32(const Plan &p, const Buffers &b, const float *HL, int32_t n, int32_
              float *dW, float *db, hipStream_t s) {
     int rc;
     hipLaunchKernelGGL(count_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, b.inv_count);
-    hipLaunchKernelGGL(copy_rows_kernel<float>, dim3(grid_of((int64_t)n * f)), dim3(kTB), 0, s, n, f, HL, ldhl, b.Hz,
+    hipLaunchKernelGGL(copy_rows_kernel<float>, dim3(grid_of((int64_t)n * f)), dim3(kTB), 0, s, n, n, f, HL, ldhl, b.Hz,
                        (int64_t)f, labels, C);
     GCN_LAUNCH_CHECK("class_prep");
     auto logits = [&](int32_t c0, int32_t P) {

@@ -61,7 +61,7 @@ struct Frag {
 
 template <int TYPE>
 __device__ __forceinline__ void mma(f32x4 &acc, const Frag &a, const Frag &b, int sa, int sb) {
-    if constexpr (TYPE == TILE_BF16) {
+    if constexpr (TYPE == TILE_BF16 || TYPE == TILE_BF16_KM) {
         acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16v8, b.lo),
                                                       __builtin_bit_cast(bf16v8, a.lo), acc, 0, 0, 0);
         acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16v8, b.hi),
@@ -70,6 +70,27 @@ __device__ __forceinline__ void mma(f32x4 &acc, const Frag &a, const Frag &b, in
         acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i32x8, b),
                                                                __builtin_bit_cast(i32x8, a), acc, 0, 0, 0, sb, 0, sa);
     }
+}
+
+// Operands stored along the other way (KM: K x rows): a stage holds 64 k-rows
+// of 128 elements, 16 chunks of 16 bytes each, chunk c of k-row k at place
+// c ^ 4 (k % 4).  The gfx950 transposing LDS read gives a group of 16 lanes, whose
+// lane j addresses 4 elements of k-row kb + j / 4 at 4 (j % 4), the elements of
+// its own column at k-rows kb .. kb + 3; the swizzle keeps the four k-rows of a
+// group on different banks.  km_place: lane's byte offset for the 16 columns
+// from chunk c0 (c0 even) in group g's k-rows 8 g ..; a fragment is the four
+// pieces of k-rows 8 g, 8 g + 4 and 32 further on.
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ int km_place(int lane, int c0) {
+    const int j = lane & 15, k = 8 * (lane >> 4) + (j >> 2);
+    return k * 256 + (((c0 + ((j & 3) >> 1)) ^ (4 * (j >> 2))) * 16) + (j & 1) * 8;
+}
+__device__ __forceinline__ uint2 km_read(const char *p) {
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16 *)p));
+}
+__device__ __forceinline__ Frag km_frag(const char *p) {
+    const uint2 a = km_read(p), b = km_read(p + 4 * 256), c = km_read(p + 32 * 256), d = km_read(p + 36 * 256);
+    return Frag{make_uint4(a.x, a.y, b.x, b.y), make_uint4(c.x, c.y, d.x, d.y)};
 }
 
 // eight e4m3 values as bfloat16, exactly
@@ -243,13 +264,9 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
                         g[e] = has ? (prob(acc[i][j][e], lse) - (col + e == lab && lab < p.N ? 1.0f : 0.0f)) * inv : 0.0f;
                         cs[j][e] += g[e];
                     }
-                    if (in && col < p.ldg)
+                    if (row < p.g_rows && col < p.ldg)
                         *(uint2 *)(p.G + (int64_t)row * p.ldg + col) =
                             make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]));
-                    if (row < p.ldgt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (col + e < p.N) p.GT[(int64_t)(col + e) * p.ldgt + row] = to_bf16(g[e]);
                 }
             }
             // column sums: 16 lanes of a wavefront, then the WM wavefronts
@@ -298,20 +315,32 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
     // which holds the row's chunk (thread % 8) ^ (row % 8); rows past the
     // extent are clamped (their products are dropped)
     const int lr = threadIdx.x >> 3, chunk = ((threadIdx.x & 7) ^ (lr & 7)) * 16;
+    constexpr bool KM = TYPE == TILE_BF16_KM;
+    static_assert(!KM || (BM == 128 && BN == 128), "k-rows of 16 chunks");
+    const int64_t step_a = KM ? 64 * p.lda : kPiece, step_b = KM ? 64 * p.ldb : kPiece;
     const uint8_t *ga[LA], *gb[LB];
+    if constexpr (KM) {   // k-row (u T + thread) / 16, its chunks clamped to the last whole one
+#pragma unroll
+        for (int u = 0; u < LA; ++u) {
+            const int k = (u * T + threadIdx.x) >> 4, ch = 8 * ((threadIdx.x & 15) ^ (4 * (k & 3)));
+            ga[u] = p.A + k * p.lda + 2 * (int64_t)min(m0 + ch, ((p.M + 7) & ~7) - 8);
+            gb[u] = p.B + k * p.ldb + 2 * (int64_t)min(n0 + ch, ((p.N + 7) & ~7) - 8);
+        }
+    } else {
 #pragma unroll
     for (int u = 0; u < LA; ++u) ga[u] = p.A + (int64_t)min(m0 + u * (T / 8) + lr, p.M - 1) * p.lda + chunk;
 #pragma unroll
     for (int u = 0; u < LB; ++u) gb[u] = p.B + (int64_t)min(n0 + u * (T / 8) + lr, p.N - 1) * p.ldb + chunk;
+    }
     auto copy = [&](int kt, int stage) {
         char *d = lds + stage * kStage + wave * 1024;
 #pragma unroll
         for (int u = 0; u < LA; ++u)
-            __builtin_amdgcn_global_load_lds((const void *)(ga[u] + (int64_t)kt * kPiece),
+            __builtin_amdgcn_global_load_lds((const void *)(ga[u] + kt * step_a),
                                              (void __attribute__((address_space(3))) *)(d + u * T * 16), 16, 0, 0);
 #pragma unroll
         for (int u = 0; u < LB; ++u)
-            __builtin_amdgcn_global_load_lds((const void *)(gb[u] + (int64_t)kt * kPiece),
+            __builtin_amdgcn_global_load_lds((const void *)(gb[u] + kt * step_b),
                                              (void __attribute__((address_space(3))) *)(d + BM * kPiece + u * T * 16), 16,
                                              0, 0);
     };
@@ -323,6 +352,7 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
     const int fr = lane & 15, g = lane >> 4;
     const int o0 = (g ^ (fr & 7)) * 16, o1 = ((g + 4) ^ (fr & 7)) * 16;   // (a fragment's rows start at multiples of 16)
     auto frag = [&](const char *tile, int row) {
+        if constexpr (KM) return km_frag(tile + km_place(lane, row / 8));
         const char *q = tile + (row + fr) * kPiece;
         return Frag{*(const uint4 *)(q + o0), *(const uint4 *)(q + o1)};
     };
@@ -455,13 +485,28 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
 
     // Copies: region row (8 u + wave) 8 + lane / 8, stored chunk lane % 8 with
     // the row's chunk (lane % 8) ^ (row % 8); rows past the extent are clamped.
-    const uint8_t *const ba = p.A + (int64_t)m0 * p.lda + (int64_t)kt0 * kPiece;
-    const uint8_t *const bb = p.B + (int64_t)n0 * p.ldb + (int64_t)kt0 * kPiece;
+    // KM: k-row (8 u + wave) 4 + lane / 16, stored chunk lane % 16, which is one
+    // of the 8 of A's first or second half's columns in the region, or of the 4
+    // of B's four quarters'; chunks past the extent are clamped to the last.
+    constexpr bool KM = TYPE == TILE_BF16_KM;
+    const int64_t step_a = KM ? 64 * p.lda : kPiece, step_b = KM ? 64 * p.ldb : kPiece;
+    const uint8_t *const ba = p.A + (KM ? (int64_t)m0 * 2 : (int64_t)m0 * p.lda) + kt0 * step_a;
+    const uint8_t *const bb = p.B + (KM ? (int64_t)n0 * 2 : (int64_t)n0 * p.ldb) + kt0 * step_b;
     uint32_t oa[2][2], ob[2][2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const int rr = (8 * u + wave) * 8 + (lane >> 3);
         const uint32_t ch = (uint32_t)(((lane & 7) ^ (rr & 7)) * 16);
+        if constexpr (KM) {
+            const int k = (8 * u + wave) * 4 + (lane >> 4), gc = (lane & 15) ^ (4 * (k & 3));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                oa[h][u] = (uint32_t)k * (uint32_t)p.lda +
+                           2 * (uint32_t)min((gc >> 3) * 128 + 64 * h + (gc & 7) * 8, ((p.M + 7) & ~7) - 8 - m0);
+                ob[h][u] = (uint32_t)k * (uint32_t)p.ldb +
+                           2 * (uint32_t)min((gc >> 2) * 64 + 32 * h + (gc & 3) * 8, ((p.N + 7) & ~7) - 8 - n0);
+            }
+        } else
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             oa[h][u] = (uint32_t)min((rr >> 6) * 128 + (rr & 63) + 64 * h, p.M - 1 - m0) * (uint32_t)p.lda + ch;
@@ -471,7 +516,7 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
     // region 0, 1: A-lo, A-hi; 2, 3: B-lo, B-hi
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * 1024;
     auto copy = [&](int region, int t) {
-        const uint8_t *g = (region < 2 ? ba : bb) + (int64_t)t * kPiece;
+        const uint8_t *g = region < 2 ? ba + t * step_a : bb + t * step_b;
         const uint32_t d = lds0 + (t & 1) * kBuffer + region * kRegion;
 #pragma unroll
         for (int u = 0; u < 2; ++u) copy_to_lds(g, region < 2 ? oa[region & 1][u] : ob[region & 1][u], d + u * 8192);
@@ -485,9 +530,15 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
     const int fr = lane & 15, g = lane >> 4;
     const int o0 = (g ^ (fr & 7)) * 16, o1 = ((g + 4) ^ (fr & 7)) * 16;
     const char *const la = lds + (wm * 64 + fr) * kPiece, *const lb = lds + 2 * kRegion + (wn * 32 + fr) * kPiece;
+    const char *const ka[2] = {lds + km_place(lane, wm * 8), lds + km_place(lane, wm * 8 + 4)};
+    const char *const kb = lds + 2 * kRegion + km_place(lane, wn * 4);
     auto read_a = [&](Frag (&f)[4], int t, int h) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+            if constexpr (KM) {
+                f[i] = km_frag(ka[i >> 1] + (t & 1) * kBuffer + h * kRegion + (i & 1) * 32);
+                continue;
+            }
             const char *q = la + (t & 1) * kBuffer + h * kRegion + i * 16 * kPiece;
             f[i] = Frag{*(const uint4 *)(q + o0), *(const uint4 *)(q + o1)};
         }
@@ -495,6 +546,10 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
     auto read_b = [&](Frag (&f)[2], int t, int h) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
+            if constexpr (KM) {
+                f[j] = km_frag(kb + (t & 1) * kBuffer + h * kRegion + j * 32);
+                continue;
+            }
             const char *q = lb + (t & 1) * kBuffer + h * kRegion + j * 16 * kPiece;
             f[j] = Frag{*(const uint4 *)(q + o0), *(const uint4 *)(q + o1)};
         }
@@ -633,12 +688,11 @@ int64_t tiles_of(int64_t M, int64_t N, int64_t t) { return ((M + t - 1) / t) * (
 TileShape tile_shape(TileType type, const TileProduct &p) {
     const int32_t splits = std::max(1, p.splits), per = (p.kt + splits - 1) / splits;
     const bool big = type != TILE_FP8_EXACT && tiles_of(p.M, p.N, kBigT) * splits >= 160 && per >= 4 &&
-                     (type == TILE_BF16 || per <= kBigPieces) && std::max(p.lda, p.ldb) < (1 << 24);
+                     (type != TILE_FP8 || per <= kBigPieces) && std::max(p.lda, p.ldb) < (1 << 24);
     return big ? TileShape{kBigT, kBigT} : TileShape{128, 128};
 }
 
-int32_t tile_splits(TileType type, int32_t M, int32_t N, int32_t kt) {
-    (void)type;
+int32_t tile_splits(int32_t M, int32_t N, int32_t kt) {
     const int64_t tiles = std::max<int64_t>(1, tiles_of(M, N, kBigT));
     int64_t sp = std::max<int64_t>(1, 256 / tiles);
     if (sp > kt / 8) sp = std::min<int64_t>(512 / std::max<int64_t>(1, tiles_of(M, N, 128)), kt / 8);
@@ -668,6 +722,9 @@ int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStrea
         else if (epi == TILE_PARTIAL) launch<TILE_BF16, TILE_PARTIAL>(big, a, grid, s);
         else if (epi == TILE_STATS) launch<TILE_BF16, TILE_STATS>(big, a, grid, s);
         else launch<TILE_BF16, TILE_GRAD>(big, a, grid, s);
+    } else if (type == TILE_BF16_KM) {
+        if (epi == TILE_STORE) launch<TILE_BF16_KM, TILE_STORE>(big, a, grid, s);
+        else launch<TILE_BF16_KM, TILE_PARTIAL>(big, a, grid, s);
     } else if (type == TILE_FP8) {
         if (epi == TILE_STORE) launch<TILE_FP8, TILE_STORE>(big, a, grid, s);
         else launch<TILE_FP8, TILE_PARTIAL>(big, a, grid, s);

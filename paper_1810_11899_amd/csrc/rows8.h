@@ -14,16 +14,20 @@ inline int64_t blocks8(int64_t f) { return (f + kRows8Block - 1) / kRows8Block; 
 // C[M x N] = A B^T on the matrix cores, A [M x K] and B [N x K] in rows of kt
 // 128-byte pieces (64 bfloat16 or 128 e4m3 values), 16-byte aligned, the
 // columns past K zero in at least one of them and finite in the other.
+// TILE_BF16_KM: A [K x M] and B [K x N] with kt 64-row pieces, rows of whole
+// 16-byte chunks (M and N rounded up to 8 elements are readable), the rows past
+// K zero in one and finite in the other.
 enum TileType {
     TILE_BF16 = 0,       // bfloat16 operands
     TILE_FP8 = 1,        // e4m3 operands with scales, 8-bit matrix instructions
-    TILE_FP8_EXACT = 2   // the same, as bfloat16 products (exact), one float32 sum per 128 columns
+    TILE_FP8_EXACT = 2,  // the same, as bfloat16 products (exact), one float32 sum per 128 columns
+    TILE_BF16_KM = 3     // C = A^T B of bfloat16 operands stored K x M and K x N
 };
 enum TileEpilogue {
     TILE_STORE = 0,    // C (float32 or bfloat16), bias, ReLU
     TILE_PARTIAL = 1,  // split s's sums to acc + s M N (float32), or added to what is there
     TILE_STATS = 2,    // per row and column tile: maximum and sum of exponentials
-    TILE_GRAD = 3      // softmax gradient rows, transposed rows, column sums
+    TILE_GRAD = 3      // softmax gradient rows, column sums
 };
 struct TileProduct {
     const uint8_t *A, *B;
@@ -49,8 +53,8 @@ struct TileProduct {
     float *tile_max, *tile_sum;     // [tiles_n x M]
     float *label_logit;             // [M]
     const float *lse, *inv_count;   // [M], [1]
-    uint16_t *G, *GT;               // [M x ldg], [N x ldgt] bfloat16
-    int64_t ldg, ldgt;
+    uint16_t *G;                    // [g_rows x ldg] bfloat16, zeros past M and N
+    int64_t ldg, g_rows;
     float *colpart;                 // [tiles_m x N]
 };
 // rows and columns of the tiles that this product runs on
@@ -65,7 +69,7 @@ int tile_reduce(int32_t splits, int32_t M, int32_t N, const float *acc, void *ou
                 hipStream_t s);
 
 // how many parts to split `kt` pieces over, for a product with few tiles
-int32_t tile_splits(TileType type, int32_t M, int32_t N, int32_t kt);
+int32_t tile_splits(int32_t M, int32_t N, int32_t kt);
 
 // ------------------------------------------------------------ 8-bit rows
 int check_rows8(const gcn_rows8 *r, const char *who);
