@@ -51,35 +51,30 @@ __global__ __launch_bounds__(kTB) void copy_rows_kernel(int32_t drows, int32_t r
     }
 }
 
-// dst [cols x ldd] = src^T, src [rows x cols] (lds) bfloat16; columns rows ..
-// ldd - 1 of dst zero, and those of rows without a label
-__global__ __launch_bounds__(kTB) void transpose_kernel(int32_t rows, int32_t cols, const uint16_t *src, int64_t lds,
-                                                        uint16_t *dst, int64_t ldd, const int32_t *labels, int32_t C) {
-    __shared__ uint16_t t[64][66];
-    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
-    for (int i = threadIdx.x; i < 64 * 64; i += kTB) {
-        const int64_t r = r0 + i / 64, c = c0 + i % 64;
-        t[i / 64][i % 64] = r < rows && c < cols && (!labels || has_label(labels[r], C)) ? src[r * lds + c] : (uint16_t)0;
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 64 * 64; i += kTB) {
-        const int64_t c = c0 + i / 64, r = r0 + i % 64;
-        if (c < cols && r < ldd) dst[c * ldd + r] = t[i % 64][i / 64];
-    }
-}
-
-// the tiles' maxima and sums of one piece joined into the running ones
+// the tiles' maxima and sums of one piece joined into the running ones: 32 rows
+// to a workgroup, eight threads a row, so that many loads are in flight
 __global__ __launch_bounds__(kTB) void join_kernel(int32_t n, int32_t tiles, const float *tile_max,
                                                    const float *tile_sum, float *run_max, float *run_sum, int first) {
-    const int32_t i = blockIdx.x * kTB + threadIdx.x;
-    if (i >= n) return;
-    float m = first ? -INFINITY : run_max[i], s = first ? 0.0f : run_sum[i];
-    for (int32_t t = 0; t < tiles; ++t) {
-        const float q = tile_max[(int64_t)t * n + i], u = tile_sum[(int64_t)t * n + i];
+    __shared__ float sm[8][32], ss[8][32];
+    const int lr = threadIdx.x & 31, part = threadIdx.x >> 5;
+    const int32_t i = blockIdx.x * 32 + lr;
+    float m = -INFINITY, s = 0.0f;
+    auto join = [&](float q, float u) {
         const float b = fmaxf(m, q);
         s = (m == b ? s : s * __expf(m - b)) + (q == b ? u : u * __expf(q - b));
         m = b;
+    };
+    if (i < n) {
+#pragma unroll 4
+        for (int32_t t = part; t < tiles; t += 8) join(tile_max[(int64_t)t * n + i], tile_sum[(int64_t)t * n + i]);
     }
+    sm[part][lr] = m;
+    ss[part][lr] = s;
+    __syncthreads();
+    if (part != 0 || i >= n) return;
+#pragma unroll
+    for (int k = 1; k < 8; ++k) join(sm[k][lr], ss[k][lr]);
+    if (!first) join(run_max[i], run_sum[i]);
     run_max[i] = m;
     run_sum[i] = s;
 }
@@ -181,11 +176,12 @@ struct Plan {
     int64_t fp, np;            // f and n in whole 64-column pieces (bfloat16)
     int32_t piece, pieces;     // classes per piece
     int32_t split_h, split_w;  // parts of the two gradient products
+    bool in_place;             // W_pred's own rows serve as operands
     size_t total;
 };
 struct Buffers {
     float *inv_count, *run_max, *run_sum, *label_logit, *lse, *tile_max, *tile_sum, *colpart, *acc, *part, *X, *tmp;
-    uint16_t *H, *WT, *W, *G;
+    uint16_t *H, *W, *G;
     float *Hz;
     void *gemm_ws, *col_ws;
     size_t gemm_bytes, col_bytes;
@@ -202,12 +198,14 @@ GemmProblem dw_f32(int32_t f, int32_t P, int32_t n) {
 // The elements of a piece: bfloat16 G takes 2 bytes each, float32 logits 4.
 constexpr int64_t kPieceElems = (int64_t)1 << 28, kPieceElemsF32 = (int64_t)1 << 26;
 
-Plan plan_of(int32_t n, int32_t f, int32_t C, bool bf, bool grad, void *ws, size_t ws_bytes, Buffers &b) {
+// W: the weights, or null in the workspace query, which counts on copying them.
+Plan plan_of(int32_t n, int32_t f, int32_t C, bool bf, bool grad, const void *W, void *ws, size_t ws_bytes, Buffers &b) {
     Plan p{};
     Arena ar(ws, ws_bytes);
     const int64_t rows = std::max(n, 1);
     p.fp = up(f, 64);
     p.np = up(rows, 64);
+    p.in_place = W && (uintptr_t)W % 16 == 0 && C % 8 == 0 && f % 64 == 0;
     int64_t piece = std::max<int64_t>(256, (bf ? kPieceElems / p.np : kPieceElemsF32 / rows) / 256 * 256);
     piece = std::min<int64_t>(piece, up(C, 256));
     p.pieces = (int32_t)((C + piece - 1) / piece);
@@ -224,10 +222,13 @@ Plan plan_of(int32_t n, int32_t f, int32_t C, bool bf, bool grad, void *ws, size
         b.tile_max = ar.take<float>(tn * rows);
         b.tile_sum = ar.take<float>(tn * rows);
         b.H = ar.take<uint16_t>(p.np * p.fp);
-        b.WT = ar.take<uint16_t>((size_t)p.piece * p.fp);
+        // (a piece of whole 64-column parts is read in place where W_pred's rows
+        // are 16-byte aligned and f is whole: only a ragged last piece is copied)
+        const int32_t last = C - (p.pieces - 1) * p.piece;
+        const int64_t copied = std::max(p.in_place && p.piece % 64 == 0 ? 0 : p.piece, p.in_place && last % 64 == 0 ? 0 : last);
+        b.W = copied ? ar.take<uint16_t>(p.fp * up(copied, 64)) : nullptr;
         if (grad) {
             const int64_t pp = up(p.piece, 64);
-            b.W = ar.take<uint16_t>(f * pp);
             b.G = ar.take<uint16_t>(p.np * pp);
             b.colpart = ar.take<float>((rows + kSmallTile - 1) / kSmallTile * p.piece);
             p.split_h = tile_splits(n, f, (int32_t)(pp / 64));
@@ -264,15 +265,30 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
                            HL, ldhl, b.H, p.fp, labels, C);
         GCN_LAUNCH_CHECK("class_prep");
     }
-    auto logits = [&](int32_t c0, int32_t P) {
+    // the piece's columns of W_pred, rows of ldw elements: in place, or copied to
+    // whole 64 x 64 pieces
+    const uint16_t *Wp = nullptr;
+    int64_t ldw = 0;
+    auto weights = [&](int32_t c0, int32_t P) -> int {
+        if (p.in_place && P % 64 == 0) {
+            Wp = W + c0;
+            ldw = C;
+            return GCN_OK;
+        }
+        ldw = up(P, 64);
+        Wp = b.W;
         ProfScope prof(K_CLASS_PREP, s, 0.0, 4.0 * f * P);
-        hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)(p.fp / 64), (unsigned)((P + 63) / 64)), dim3(kTB), 0, s, f, P,
-                           W + c0, (int64_t)C, b.WT, p.fp, (const int32_t *)nullptr, 0);
+        hipLaunchKernelGGL(copy_rows_kernel<uint16_t>, dim3(grid_of(p.fp * ldw)), dim3(kTB), 0, s, (int32_t)p.fp, f, P,
+                           W + c0, (int64_t)C, b.W, ldw, (const int32_t *)nullptr, 0);
+        GCN_LAUNCH_CHECK("copy_rows_kernel");
+        return GCN_OK;
+    };
+    auto logits = [&](int32_t c0, int32_t P) {
         TileProduct t{};
         t.A = (const uint8_t *)b.H;
         t.lda = 2 * p.fp;
-        t.B = (const uint8_t *)b.WT;
-        t.ldb = 2 * p.fp;
+        t.B = (const uint8_t *)Wp;
+        t.ldb = 2 * ldw;
         t.M = n;
         t.N = P;
         t.kt = (int32_t)(p.fp / 64);
@@ -285,17 +301,18 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
     };
     for (int32_t i = 0; i < p.pieces; ++i) {
         const int32_t c0 = i * p.piece, P = std::min(p.piece, C - c0);
+        if ((rc = weights(c0, P))) return rc;
         TileProduct t = logits(c0, P);
         t.tile_max = b.tile_max;
         t.tile_sum = b.tile_sum;
         t.label_logit = b.label_logit;
         {
             ProfScope prof(K_CLASS_STATS, s, 2.0 * n * f * P, 2.0 * ((double)n + P) * f);
-            if ((rc = tile_product(TILE_BF16, TILE_STATS, t, s))) return rc;
+            if ((rc = tile_product(TILE_BF16_NN, TILE_STATS, t, s))) return rc;
         }
-        const TileShape sh = tile_shape(TILE_BF16, t);
+        const TileShape sh = tile_shape(TILE_BF16_NN, t);
         ProfScope prof(K_CLASS_PREP, s, 0.0, 8.0 * n * ((P + sh.n - 1) / sh.n));
-        hipLaunchKernelGGL(join_kernel, dim3((unsigned)((n + kTB - 1) / kTB)), dim3(kTB), 0, s, n, (P + sh.n - 1) / sh.n,
+        hipLaunchKernelGGL(join_kernel, dim3((unsigned)((n + 31) / 32)), dim3(kTB), 0, s, n, (P + sh.n - 1) / sh.n,
                            b.tile_max, b.tile_sum, b.run_max, b.run_sum, i == 0);
         GCN_LAUNCH_CHECK("join_kernel");
     }
@@ -306,6 +323,7 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
     for (int32_t i = 0; i < p.pieces; ++i) {
         const int32_t c0 = i * p.piece, P = std::min(p.piece, C - c0);
         const int64_t pp = up(P, 64);
+        if ((rc = weights(c0, P))) return rc;
         TileProduct t = logits(c0, P);
         t.lse = b.lse;
         t.inv_count = b.inv_count;
@@ -315,19 +333,16 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         t.colpart = b.colpart;
         {
             ProfScope prof(K_CLASS_GRAD, s, 2.0 * n * f * P, 2.0 * ((double)n + P) * f + 4.0 * n * P);
-            if ((rc = tile_product(TILE_BF16, TILE_GRAD, t, s))) return rc;
+            if ((rc = tile_product(TILE_BF16_NN, TILE_GRAD, t, s))) return rc;
         }
-        const TileShape sh = tile_shape(TILE_BF16, t);
+        const TileShape sh = tile_shape(TILE_BF16_NN, t);
         if ((rc = colsum_reduce_rows((n + sh.m - 1) / sh.m, P, b.colpart, db + c0, s))) return rc;
-        hipLaunchKernelGGL(copy_rows_kernel<uint16_t>, dim3(grid_of(f * pp)), dim3(kTB), 0, s, f, f, P, W + c0, (int64_t)C,
-                           b.W, pp, (const int32_t *)nullptr, 0);
-        GCN_LAUNCH_CHECK("copy_rows_kernel");
         ProfScope prof(K_CLASS_PRODUCT, s, 4.0 * n * f * P, 4.0 * n * P);
         TileProduct h{};
         h.A = (const uint8_t *)b.G;
         h.lda = 2 * pp;
-        h.B = (const uint8_t *)b.W;
-        h.ldb = 2 * pp;
+        h.B = (const uint8_t *)Wp;
+        h.ldb = 2 * ldw;
         h.M = n;
         h.N = f;
         h.kt = (int32_t)(pp / 64);
@@ -346,13 +361,13 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         w.splits = p.split_w;
         if (p.split_w > 1) {
             w.acc = b.part;
-            if ((rc = tile_product(TILE_BF16_KM, TILE_PARTIAL, w, s))) return rc;
+            if ((rc = tile_product(TILE_BF16_TN, TILE_PARTIAL, w, s))) return rc;
             if ((rc = tile_reduce(p.split_w, f, P, b.part, dW + c0, 1, C, s))) return rc;
         } else {
             w.C = dW + c0;
             w.ldc = C;
             w.c_bf16 = 1;
-            if ((rc = tile_product(TILE_BF16_KM, TILE_STORE, w, s))) return rc;
+            if ((rc = tile_product(TILE_BF16_TN, TILE_STORE, w, s))) return rc;
         }
     }
     return tile_reduce(p.split_h, n, f, b.acc, dHL, 1, lddhl, s);
@@ -430,7 +445,7 @@ extern "C" {
 size_t gcn_class_loss_workspace_bytes(int32_t n, int32_t f, int32_t C, gcn_rows_type type, int need_grad) {
     if (n < 0 || f <= 0 || C <= 0) return 0;
     Buffers b;
-    return plan_of(n, f, C, type == GCN_ROWS_BF16, need_grad != 0, nullptr, 0, b).total;
+    return plan_of(n, f, C, type == GCN_ROWS_BF16, need_grad != 0, nullptr, nullptr, 0, b).total;
 }
 
 int gcn_class_loss(const void *HL, int32_t n, int32_t f, int32_t ldhl, const void *W_pred, const float *b_pred,
@@ -449,7 +464,7 @@ int gcn_class_loss(const void *HL, int32_t n, int32_t f, int32_t ldhl, const voi
     GCN_REQUIRE((((uintptr_t)HL | (uintptr_t)W_pred | (uintptr_t)dHL | (uintptr_t)dW_pred) & el) == 0, GCN_EINVAL,
                 "gcn_class_loss: misaligned operand");
     Buffers b;
-    const Plan p = plan_of(n, f, C, bf, grad, ws, ws_bytes, b);
+    const Plan p = plan_of(n, f, C, bf, grad, W_pred, ws, ws_bytes, b);
     GCN_REQUIRE(ws && ((uintptr_t)ws & 255) == 0 && ws_bytes >= p.total, GCN_EWORKSPACE,
                 "gcn_class_loss: workspace %zu < %zu bytes, or not 256-byte aligned", ws_bytes, p.total);
     hipStream_t s = (hipStream_t)stream;

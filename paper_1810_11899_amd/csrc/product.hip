@@ -59,9 +59,14 @@ struct Frag {
     uint4 lo, hi;
 };
 
+constexpr bool is_bf16(int type) { return type != TILE_FP8 && type != TILE_FP8_EXACT; }
+// which operands are stored along the other way
+constexpr bool km_a(int type) { return type == TILE_BF16_TN; }
+constexpr bool km_b(int type) { return type == TILE_BF16_TN || type == TILE_BF16_NN; }
+
 template <int TYPE>
 __device__ __forceinline__ void mma(f32x4 &acc, const Frag &a, const Frag &b, int sa, int sb) {
-    if constexpr (TYPE == TILE_BF16 || TYPE == TILE_BF16_KM) {
+    if constexpr (is_bf16(TYPE)) {
         acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16v8, b.lo),
                                                       __builtin_bit_cast(bf16v8, a.lo), acc, 0, 0, 0);
         acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16v8, b.hi),
@@ -110,9 +115,6 @@ __device__ __forceinline__ int label_of(const TileProduct &p, int row) {
     const int l = row < p.M ? p.labels[row] : -1;
     return l >= 0 && l < p.classes ? l - p.class0 : kNoLabel;
 }
-
-// a softmax gradient's value; x - lse <= 0 up to rounding
-__device__ __forceinline__ float prob(float x, float lse) { return __expf(x - lse); }
 
 // ------------------------------------------------------------- epilogues
 // acc[i][j]: row m0 + 16 i + lane % 16 of C, columns n0 + 16 j + 4 (lane / 16)
@@ -184,7 +186,7 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
                 }
             }
     } else {
-        // bias, and columns past the last class to minus infinity
+        // the logits: bias, and columns past the last class at minus infinity
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
@@ -192,8 +194,10 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
                 const int col = c0 + 16 * j + e;
                 const float b = col < p.N ? (p.bias ? p.bias[col] : 0.0f) : -INFINITY;
 #pragma unroll
-                for (int i = 0; i < FM; ++i) acc[i][j][e] = col < p.N ? acc[i][j][e] + b : b;
+                for (int i = 0; i < FM; ++i) acc[i][j][e] += b;
             }
+        constexpr float kLog2e = 1.44269504088896340736f;
+        const int w0 = c.tn * BN + wn * (BN / WN);   // the wavefront's first column
         if constexpr (EPI == TILE_STATS) {
             // a row's columns lie in 4 lanes of WN wavefronts: maximum and sum
             // over the lane's own, two exchanges, then LDS across wavefronts
@@ -214,16 +218,18 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
 #pragma unroll
                 for (int j = 0; j < FN; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s += __expf(acc[i][j][e] - base);
+                    for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f((acc[i][j][e] - base) * kLog2e);
                 s += __shfl_xor(s, 16);
                 s += __shfl_xor(s, 32);
                 if (lane < 16) part[wn * BM + row - c.tm * BM] = make_float2(m, s);
                 const int lab = label_of(p, row);
+                if (__any(lab >= w0 && lab < w0 + BN / WN)) {   // (few wavefronts see one of their labels)
 #pragma unroll
-                for (int j = 0; j < FN; ++j)
+                    for (int j = 0; j < FN; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (c0 + 16 * j + e == lab && lab < p.N) p.label_logit[row] = acc[i][j][e];
+                        for (int e = 0; e < 4; ++e)
+                            if (c0 + 16 * j + e == lab && lab < p.N) p.label_logit[row] = acc[i][j][e];
+                }
             }
             __syncthreads();
             for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) {
@@ -247,23 +253,32 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
             for (int j = 0; j < FN; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) cs[j][e] = 0.0f;
-            const float inv = p.inv_count[0];
+            const float inv = p.inv_count[0], log_inv = __builtin_amdgcn_logf(inv);   // (base 2)
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
                 const int row = r0 + 16 * i;
-                const bool in = row < p.M;
-                const float lse = in ? p.lse[row] : 0.0f;
+                const float lse = row < p.M ? p.lse[row] : 0.0f;
                 const int lab = label_of(p, row);
-                const bool has = lab != kNoLabel;   // a row without a label has no gradient
+                // a row without a label has no gradient: 2^-infinity
+                const float shift = lab != kNoLabel ? log_inv : -INFINITY;
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        acc[i][j][e] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e] - lse, kLog2e, shift));
+                if (__any(lab >= w0 && lab < w0 + BN / WN)) {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (c0 + 16 * j + e == lab) acc[i][j][e] -= inv;
+                }
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
                     const int col = c0 + 16 * j;
-                    f32x4 g;
+                    const f32x4 g = acc[i][j];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        g[e] = has ? (prob(acc[i][j][e], lse) - (col + e == lab && lab < p.N ? 1.0f : 0.0f)) * inv : 0.0f;
-                        cs[j][e] += g[e];
-                    }
+                    for (int e = 0; e < 4; ++e) cs[j][e] += g[e];
                     if (row < p.g_rows && col < p.ldg)
                         *(uint2 *)(p.G + (int64_t)row * p.ldg + col) =
                             make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]));
@@ -315,23 +330,21 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
     // which holds the row's chunk (thread % 8) ^ (row % 8); rows past the
     // extent are clamped (their products are dropped)
     const int lr = threadIdx.x >> 3, chunk = ((threadIdx.x & 7) ^ (lr & 7)) * 16;
-    constexpr bool KM = TYPE == TILE_BF16_KM;
-    static_assert(!KM || (BM == 128 && BN == 128), "k-rows of 16 chunks");
-    const int64_t step_a = KM ? 64 * p.lda : kPiece, step_b = KM ? 64 * p.ldb : kPiece;
+    constexpr bool KA = km_a(TYPE), KB = km_b(TYPE);
+    static_assert((!KA || BM == 128) && (!KB || BN == 128), "k-rows of 16 chunks");
+    const int64_t step_a = KA ? 64 * p.lda : kPiece, step_b = KB ? 64 * p.ldb : kPiece;
+    // k-major: k-row (u T + thread) / 16, its chunks clamped to the last whole one
+    auto km_at = [&](const uint8_t *base, int64_t ld, int x0, int extent, int u) {
+        const int k = (u * T + threadIdx.x) >> 4, ch = 8 * ((threadIdx.x & 15) ^ (4 * (k & 3)));
+        return base + k * ld + 2 * (int64_t)min(x0 + ch, ((extent + 7) & ~7) - 8);
+    };
     const uint8_t *ga[LA], *gb[LB];
-    if constexpr (KM) {   // k-row (u T + thread) / 16, its chunks clamped to the last whole one
 #pragma unroll
-        for (int u = 0; u < LA; ++u) {
-            const int k = (u * T + threadIdx.x) >> 4, ch = 8 * ((threadIdx.x & 15) ^ (4 * (k & 3)));
-            ga[u] = p.A + k * p.lda + 2 * (int64_t)min(m0 + ch, ((p.M + 7) & ~7) - 8);
-            gb[u] = p.B + k * p.ldb + 2 * (int64_t)min(n0 + ch, ((p.N + 7) & ~7) - 8);
-        }
-    } else {
+    for (int u = 0; u < LA; ++u)
+        ga[u] = KA ? km_at(p.A, p.lda, m0, p.M, u) : p.A + (int64_t)min(m0 + u * (T / 8) + lr, p.M - 1) * p.lda + chunk;
 #pragma unroll
-    for (int u = 0; u < LA; ++u) ga[u] = p.A + (int64_t)min(m0 + u * (T / 8) + lr, p.M - 1) * p.lda + chunk;
-#pragma unroll
-    for (int u = 0; u < LB; ++u) gb[u] = p.B + (int64_t)min(n0 + u * (T / 8) + lr, p.N - 1) * p.ldb + chunk;
-    }
+    for (int u = 0; u < LB; ++u)
+        gb[u] = KB ? km_at(p.B, p.ldb, n0, p.N, u) : p.B + (int64_t)min(n0 + u * (T / 8) + lr, p.N - 1) * p.ldb + chunk;
     auto copy = [&](int kt, int stage) {
         char *d = lds + stage * kStage + wave * 1024;
 #pragma unroll
@@ -351,8 +364,8 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const int fr = lane & 15, g = lane >> 4;
     const int o0 = (g ^ (fr & 7)) * 16, o1 = ((g + 4) ^ (fr & 7)) * 16;   // (a fragment's rows start at multiples of 16)
-    auto frag = [&](const char *tile, int row) {
-        if constexpr (KM) return km_frag(tile + km_place(lane, row / 8));
+    auto frag = [&](const char *tile, int row, bool km) {
+        if (km) return km_frag(tile + km_place(lane, row / 8));
         const char *q = tile + (row + fr) * kPiece;
         return Frag{*(const uint4 *)(q + o0), *(const uint4 *)(q + o1)};
     };
@@ -363,7 +376,7 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
         if (kt + 1 < kt1) copy(kt + 1, st ^ 1);
         const char *ta = lds + st * kStage, *tb = ta + BM * kPiece;
         int sa[FM], sb[FN];
-        if constexpr (TYPE != TILE_BF16) {
+        if constexpr (!is_bf16(TYPE)) {
 #pragma unroll
             for (int i = 0; i < FM; ++i)
                 sa[i] = p.sa[(int64_t)min(m0 + wm * (BM / WM) + 16 * i + fr, p.M - 1) * p.ldsa + kt];
@@ -373,7 +386,7 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
         }
         Frag fb[FN];
 #pragma unroll
-        for (int j = 0; j < FN; ++j) fb[j] = frag(tb, wn * (BN / WN) + 16 * j);
+        for (int j = 0; j < FN; ++j) fb[j] = frag(tb, wn * (BN / WN) + 16 * j, KB);
         if constexpr (TYPE == TILE_FP8_EXACT) {
             bf16v8 wb[FN][4];
 #pragma unroll
@@ -385,7 +398,7 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
             }
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
-                const Frag fa = frag(ta, wm * (BM / WM) + 16 * i);
+                const Frag fa = frag(ta, wm * (BM / WM) + 16 * i, KA);
                 const bf16v8 wa[4] = {widen8(fa.lo.x, fa.lo.y), widen8(fa.lo.z, fa.lo.w), widen8(fa.hi.x, fa.hi.y),
                                       widen8(fa.hi.z, fa.hi.w)};
 #pragma unroll
@@ -402,7 +415,7 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
         } else {
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
-                const Frag fa = frag(ta, wm * (BM / WM) + 16 * i);
+                const Frag fa = frag(ta, wm * (BM / WM) + 16 * i, KA);
 #pragma unroll
                 for (int j = 0; j < FN; ++j) mma<TYPE>(acc[i][j], fa, fb[j], TYPE == TILE_FP8 ? sa[i] : 0, TYPE == TILE_FP8 ? sb[j] : 0);
             }
@@ -485,32 +498,31 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
 
     // Copies: region row (8 u + wave) 8 + lane / 8, stored chunk lane % 8 with
     // the row's chunk (lane % 8) ^ (row % 8); rows past the extent are clamped.
-    // KM: k-row (8 u + wave) 4 + lane / 16, stored chunk lane % 16, which is one
+    // k-major: k-row (8 u + wave) 4 + lane / 16, stored chunk lane % 16, which is one
     // of the 8 of A's first or second half's columns in the region, or of the 4
     // of B's four quarters'; chunks past the extent are clamped to the last.
-    constexpr bool KM = TYPE == TILE_BF16_KM;
-    const int64_t step_a = KM ? 64 * p.lda : kPiece, step_b = KM ? 64 * p.ldb : kPiece;
-    const uint8_t *const ba = p.A + (KM ? (int64_t)m0 * 2 : (int64_t)m0 * p.lda) + kt0 * step_a;
-    const uint8_t *const bb = p.B + (KM ? (int64_t)n0 * 2 : (int64_t)n0 * p.ldb) + kt0 * step_b;
+    constexpr bool KA = km_a(TYPE), KB = km_b(TYPE);
+    const int64_t step_a = KA ? 64 * p.lda : kPiece, step_b = KB ? 64 * p.ldb : kPiece;
+    const uint8_t *const ba = p.A + (KA ? (int64_t)m0 * 2 : (int64_t)m0 * p.lda) + kt0 * step_a;
+    const uint8_t *const bb = p.B + (KB ? (int64_t)n0 * 2 : (int64_t)n0 * p.ldb) + kt0 * step_b;
     uint32_t oa[2][2], ob[2][2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const int rr = (8 * u + wave) * 8 + (lane >> 3);
         const uint32_t ch = (uint32_t)(((lane & 7) ^ (rr & 7)) * 16);
-        if constexpr (KM) {
-            const int k = (8 * u + wave) * 4 + (lane >> 4), gc = (lane & 15) ^ (4 * (k & 3));
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                oa[h][u] = (uint32_t)k * (uint32_t)p.lda +
-                           2 * (uint32_t)min((gc >> 3) * 128 + 64 * h + (gc & 7) * 8, ((p.M + 7) & ~7) - 8 - m0);
-                ob[h][u] = (uint32_t)k * (uint32_t)p.ldb +
-                           2 * (uint32_t)min((gc >> 2) * 64 + 32 * h + (gc & 3) * 8, ((p.N + 7) & ~7) - 8 - n0);
-            }
-        } else
+        const int k = (8 * u + wave) * 4 + (lane >> 4), gc = (lane & 15) ^ (4 * (k & 3));
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            oa[h][u] = (uint32_t)min((rr >> 6) * 128 + (rr & 63) + 64 * h, p.M - 1 - m0) * (uint32_t)p.lda + ch;
-            ob[h][u] = (uint32_t)min((rr >> 5) * 64 + (rr & 31) + 32 * h, p.N - 1 - n0) * (uint32_t)p.ldb + ch;
+            if constexpr (KA)
+                oa[h][u] = (uint32_t)k * (uint32_t)p.lda +
+                           2 * (uint32_t)min((gc >> 3) * 128 + 64 * h + (gc & 7) * 8, ((p.M + 7) & ~7) - 8 - m0);
+            else
+                oa[h][u] = (uint32_t)min((rr >> 6) * 128 + (rr & 63) + 64 * h, p.M - 1 - m0) * (uint32_t)p.lda + ch;
+            if constexpr (KB)
+                ob[h][u] = (uint32_t)k * (uint32_t)p.ldb +
+                           2 * (uint32_t)min((gc >> 2) * 64 + 32 * h + (gc & 3) * 8, ((p.N + 7) & ~7) - 8 - n0);
+            else
+                ob[h][u] = (uint32_t)min((rr >> 5) * 64 + (rr & 31) + 32 * h, p.N - 1 - n0) * (uint32_t)p.ldb + ch;
         }
     }
     // region 0, 1: A-lo, A-hi; 2, 3: B-lo, B-hi
@@ -535,7 +547,7 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
     auto read_a = [&](Frag (&f)[4], int t, int h) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if constexpr (KM) {
+            if constexpr (KA) {
                 f[i] = km_frag(ka[i >> 1] + (t & 1) * kBuffer + h * kRegion + (i & 1) * 32);
                 continue;
             }
@@ -546,7 +558,7 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
     auto read_b = [&](Frag (&f)[2], int t, int h) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            if constexpr (KM) {
+            if constexpr (KB) {
                 f[j] = km_frag(kb + (t & 1) * kBuffer + h * kRegion + j * 32);
                 continue;
             }
@@ -717,20 +729,19 @@ int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStrea
         return GCN_EUNSUPPORTED;
     }
     const unsigned grid = (unsigned)(8 * a.per_xcd);
-    if (type == TILE_BF16) {
-        if (epi == TILE_STORE) launch<TILE_BF16, TILE_STORE>(big, a, grid, s);
-        else if (epi == TILE_PARTIAL) launch<TILE_BF16, TILE_PARTIAL>(big, a, grid, s);
-        else if (epi == TILE_STATS) launch<TILE_BF16, TILE_STATS>(big, a, grid, s);
-        else launch<TILE_BF16, TILE_GRAD>(big, a, grid, s);
-    } else if (type == TILE_BF16_KM) {
-        if (epi == TILE_STORE) launch<TILE_BF16_KM, TILE_STORE>(big, a, grid, s);
-        else launch<TILE_BF16_KM, TILE_PARTIAL>(big, a, grid, s);
-    } else if (type == TILE_FP8) {
-        if (epi == TILE_STORE) launch<TILE_FP8, TILE_STORE>(big, a, grid, s);
-        else launch<TILE_FP8, TILE_PARTIAL>(big, a, grid, s);
-    } else {
-        if (epi == TILE_STORE) launch<TILE_FP8_EXACT, TILE_STORE>(big, a, grid, s);
-        else launch<TILE_FP8_EXACT, TILE_PARTIAL>(big, a, grid, s);
+    // (the pairs that the entry points use)
+    if (type == TILE_BF16_NN && epi == TILE_STATS) launch<TILE_BF16_NN, TILE_STATS>(big, a, grid, s);
+    else if (type == TILE_BF16_NN && epi == TILE_GRAD) launch<TILE_BF16_NN, TILE_GRAD>(big, a, grid, s);
+    else if (type == TILE_BF16 && epi == TILE_PARTIAL) launch<TILE_BF16, TILE_PARTIAL>(big, a, grid, s);
+    else if (type == TILE_BF16_TN && epi == TILE_STORE) launch<TILE_BF16_TN, TILE_STORE>(big, a, grid, s);
+    else if (type == TILE_BF16_TN && epi == TILE_PARTIAL) launch<TILE_BF16_TN, TILE_PARTIAL>(big, a, grid, s);
+    else if (type == TILE_FP8 && epi == TILE_STORE) launch<TILE_FP8, TILE_STORE>(big, a, grid, s);
+    else if (type == TILE_FP8 && epi == TILE_PARTIAL) launch<TILE_FP8, TILE_PARTIAL>(big, a, grid, s);
+    else if (type == TILE_FP8_EXACT && epi == TILE_STORE) launch<TILE_FP8_EXACT, TILE_STORE>(big, a, grid, s);
+    else if (type == TILE_FP8_EXACT && epi == TILE_PARTIAL) launch<TILE_FP8_EXACT, TILE_PARTIAL>(big, a, grid, s);
+    else {
+        set_error("tile_product: type %d with epilogue %d", (int)type, (int)epi);
+        return GCN_EUNSUPPORTED;
     }
     GCN_LAUNCH_CHECK("tile_kernel");
     return GCN_OK;

@@ -14,14 +14,15 @@ inline int64_t blocks8(int64_t f) { return (f + kRows8Block - 1) / kRows8Block; 
 // C[M x N] = A B^T on the matrix cores, A [M x K] and B [N x K] in rows of kt
 // 128-byte pieces (64 bfloat16 or 128 e4m3 values), 16-byte aligned, the
 // columns past K zero in at least one of them and finite in the other.
-// TILE_BF16_KM: A [K x M] and B [K x N] with kt 64-row pieces, rows of whole
-// 16-byte chunks (M and N rounded up to 8 elements are readable), the rows past
-// K zero in one and finite in the other.
+// Operands stored along the other way (k-major; TN, NN) have kt 64-row pieces and
+// rows of whole 16-byte chunks (M and N rounded up to 8 elements are readable);
+// the rows past K are zero in one operand and finite in the other.
 enum TileType {
     TILE_BF16 = 0,       // bfloat16 operands
     TILE_FP8 = 1,        // e4m3 operands with scales, 8-bit matrix instructions
     TILE_FP8_EXACT = 2,  // the same, as bfloat16 products (exact), one float32 sum per 128 columns
-    TILE_BF16_KM = 3     // C = A^T B of bfloat16 operands stored K x M and K x N
+    TILE_BF16_TN = 3,    // C = A^T B of bfloat16 operands stored K x M and K x N
+    TILE_BF16_NN = 4     // C = A B, A bfloat16 rows and B stored K x N
 };
 enum TileEpilogue {
     TILE_STORE = 0,    // C (float32 or bfloat16), bias, ReLU
