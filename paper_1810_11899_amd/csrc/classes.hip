@@ -366,7 +366,6 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         } else {
             w.C = dW + c0;
             w.ldc = C;
-            w.c_bf16 = 1;
             if ((rc = tile_product(TILE_BF16_TN, TILE_STORE, w, s))) return rc;
         }
     }

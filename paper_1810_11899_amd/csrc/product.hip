@@ -116,9 +116,46 @@ __device__ __forceinline__ int label_of(const TileProduct &p, int row) {
     return l >= 0 && l < p.classes ? l - p.class0 : kNoLabel;
 }
 
+// bfloat16 rows out of a wavefront's 16 FM x 64 block, through its own part of
+// LDS so that each store fills whole 128-byte lines (8 rows of 16 bytes a lane;
+// straight from the registers a store is 16 pieces of 32 bytes, and 16,384 x
+// 16,384 results of K = 1024 take 695 us instead of 605).  Chunk c of 16 bytes of
+// row r lies at c ^ (r % 8).  `mine`: 16 FM rows of 128 bytes that no other
+// wavefront touches; row0, col0: the block's origin.
+template <int FM>
+__device__ __forceinline__ void store_rows(const f32x4 (&v)[FM][4], char *mine, uint16_t *dst, int64_t ld, int row0,
+                                           int col0, int64_t rows, int64_t cols) {
+    const int lane = threadIdx.x & 63, fr = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            *(uint2 *)(mine + (16 * i + fr) * 128 + (((2 * j + (g >> 1)) ^ (fr & 7)) * 16) + (g & 1) * 8) =
+                make_uint2(pack_bf16x2(v[i][j][0], v[i][j][1]), pack_bf16x2(v[i][j][2], v[i][j][3]));
+    asm volatile("" ::: "memory");   // (LDS accesses of one wavefront stay in order)
+    const int lr = lane >> 3, col = col0 + 8 * (lane & 7);
+    const bool vec = ld % 8 == 0 && ((uintptr_t)dst & 15) == 0 && col + 8 <= cols;
+#pragma unroll
+    for (int q = 0; q < 2 * FM; ++q) {
+        const int r = 8 * q + lr;
+        const uint4 x = *(const uint4 *)(mine + r * 128 + (((lane & 7) ^ (r & 7)) * 16));
+        if (row0 + r >= rows) continue;
+        uint16_t *d = dst + (int64_t)(row0 + r) * ld + col;
+        if (vec) {
+            *(uint4 *)d = x;
+        } else {
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e < cols) d[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+        }
+    }
+}
+
 // ------------------------------------------------------------- epilogues
 // acc[i][j]: row m0 + 16 i + lane % 16 of C, columns n0 + 16 j + 4 (lane / 16)
-// .. + 3; `scratch`: the idle operand LDS, at least 8 KB.
+// .. + 3; `scratch`: the idle
+// operand LDS.
 template <int EPI, int BM, int BN, int WM, int WN, int FM, int FN>
 __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&acc)[FM][FN], char *scratch) {
     const TileProduct &p = a.p;
@@ -126,42 +163,45 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
     const int wm = wave / WN, wn = wave % WN;
     const int r0 = c.tm * BM + wm * (BM / WM) + (lane & 15);
     const int c0 = c.tn * BN + wn * (BN / WN) + 4 * (lane >> 4);
-    if constexpr (EPI == TILE_STORE) {
+    static_assert(FN == 4, "a wavefront's block is 64 columns wide");
+    if constexpr (EPI == TILE_STORE || EPI == TILE_STORE_F32) {
+        f32x4 bias[FN];
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int col = c0 + 16 * j;
-            f32x4 bv = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (p.bias)
+        for (int j = 0; j < FN; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) bv[e] = col + e < p.N ? p.bias[col + e] : 0.0f;
-            const bool whole = col + 4 <= p.N && p.ldc % 4 == 0 && ((uintptr_t)p.C & (p.c_bf16 ? 7 : 15)) == 0;
+            for (int e = 0; e < 4; ++e)
+                bias[j][e] = p.bias && c0 + 16 * j + e < p.N ? p.bias[c0 + 16 * j + e] : 0.0f;
 #pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                const int row = r0 + 16 * i;
-                if (row >= p.M) continue;
-                f32x4 v = acc[i][j] + bv;
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                acc[i][j] += bias[j];
                 if (p.relu)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = v[e] < 0.0f ? 0.0f : v[e];   // (NaN stays)
-                const int64_t at = (int64_t)row * p.ldc + col;
-                if (p.c_bf16) {
-                    uint16_t *d = (uint16_t *)p.C + at;
-                    if (whole) {
-                        *(uint2 *)d = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-                    } else {
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = acc[i][j][e] < 0.0f ? 0.0f : acc[i][j][e];   // (NaN stays)
+            }
+        if constexpr (EPI == TILE_STORE) {
+            __syncthreads();   // the operands are read
+            store_rows<FM>(acc, scratch + wave * FM * 2048, (uint16_t *)p.C, p.ldc, c.tm * BM + wm * (BM / WM),
+                           c.tn * BN + wn * (BN / WN), p.M, p.N);
+            return;
+        }
+        const bool vec = p.ldc % 4 == 0 && ((uintptr_t)p.C & 15) == 0;
+        // (row by row: a wavefront's stores fill whole lines one after another)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (col + e < p.N) d[e] = to_bf16(v[e]);
-                    }
+        for (int i = 0; i < FM; ++i) {
+            const int row = r0 + 16 * i;
+            if (row >= p.M) continue;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int col = c0 + 16 * j;
+                float *d = (float *)p.C + (int64_t)row * p.ldc + col;
+                if (vec && col + 4 <= p.N) {
+                    *(f32x4 *)d = acc[i][j];
                 } else {
-                    float *d = (float *)p.C + at;
-                    if (whole) {
-                        *(f32x4 *)d = v;
-                    } else {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (col + e < p.N) d[e] = v[e];
-                    }
+                    for (int e = 0; e < 4; ++e)
+                        if (col + e < p.N) d[e] = acc[i][j][e];
                 }
             }
         }
@@ -169,9 +209,9 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
         float *base = p.acc + (int64_t)c.split * p.M * p.N;
         const bool vec = p.N % 4 == 0;
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+        for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int i = 0; i < FM; ++i) {
+            for (int j = 0; j < FN; ++j) {
                 const int row = r0 + 16 * i, col = c0 + 16 * j;
                 if (row >= p.M || col >= p.N) continue;
                 float *d = base + (int64_t)row * p.N + col;
@@ -274,16 +314,13 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
                             if (c0 + 16 * j + e == lab) acc[i][j][e] -= inv;
                 }
 #pragma unroll
-                for (int j = 0; j < FN; ++j) {
-                    const int col = c0 + 16 * j;
-                    const f32x4 g = acc[i][j];
+                for (int j = 0; j < FN; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) cs[j][e] += g[e];
-                    if (row < p.g_rows && col < p.ldg)
-                        *(uint2 *)(p.G + (int64_t)row * p.ldg + col) =
-                            make_uint2(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]));
-                }
+                    for (int e = 0; e < 4; ++e) cs[j][e] += acc[i][j][e];
             }
+            __syncthreads();   // the operands are read
+            // (G's columns past the last class: 2^-infinity)
+            store_rows<FM>(acc, scratch + wave * FM * 2048, p.G, p.ldg, c.tm * BM + wm * (BM / WM), w0, p.g_rows, p.ldg);
             // column sums: 16 lanes of a wavefront, then the WM wavefronts
             float *part = (float *)scratch;   // [WM][BN]
             __syncthreads();
@@ -737,7 +774,7 @@ int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStrea
     else if (type == TILE_BF16_TN && epi == TILE_PARTIAL) launch<TILE_BF16_TN, TILE_PARTIAL>(big, a, grid, s);
     else if (type == TILE_FP8 && epi == TILE_STORE) launch<TILE_FP8, TILE_STORE>(big, a, grid, s);
     else if (type == TILE_FP8 && epi == TILE_PARTIAL) launch<TILE_FP8, TILE_PARTIAL>(big, a, grid, s);
-    else if (type == TILE_FP8_EXACT && epi == TILE_STORE) launch<TILE_FP8_EXACT, TILE_STORE>(big, a, grid, s);
+    else if (type == TILE_FP8_EXACT && epi == TILE_STORE_F32) launch<TILE_FP8_EXACT, TILE_STORE_F32>(big, a, grid, s);
     else if (type == TILE_FP8_EXACT && epi == TILE_PARTIAL) launch<TILE_FP8_EXACT, TILE_PARTIAL>(big, a, grid, s);
     else {
         set_error("tile_product: type %d with epilogue %d", (int)type, (int)epi);
@@ -808,13 +845,13 @@ int gcn_rows8_product(const gcn_rows8 *X8, const gcn_weights8 *W8, int transpose
     p.sb_k = transpose ? 1 : W8->ldscale;
     p.C = Y;
     p.ldc = ldy;
-    p.c_bf16 = type == GCN_ROWS_BF16;
+    const bool bf = type == GCN_ROWS_BF16;
     p.relu = relu;
     p.bias = bias;
     hipStream_t s = (hipStream_t)stream;
     ProfScope prof(K_ROWS8_PRODUCT, s, 2.0 * p.M * N * K,
-                   (double)p.M * K + (double)N * K + (double)p.M * N * (p.c_bf16 ? 2.0 : 4.0));
-    return tile_product(p.c_bf16 ? TILE_FP8 : TILE_FP8_EXACT, TILE_STORE, p, s);
+                   (double)p.M * K + (double)N * K + (double)p.M * N * (bf ? 2.0 : 4.0));
+    return bf ? tile_product(TILE_FP8, TILE_STORE, p, s) : tile_product(TILE_FP8_EXACT, TILE_STORE_F32, p, s);
 }
 
 }  // extern "C"

@@ -25,10 +25,11 @@ enum TileType {
     TILE_BF16_NN = 4     // C = A B, A bfloat16 rows and B stored K x N
 };
 enum TileEpilogue {
-    TILE_STORE = 0,    // C (float32 or bfloat16), bias, ReLU
+    TILE_STORE = 0,    // C as bfloat16, bias, ReLU
     TILE_PARTIAL = 1,  // split s's sums to acc + s M N (float32), or added to what is there
     TILE_STATS = 2,    // per row and column tile: maximum and sum of exponentials
-    TILE_GRAD = 3      // softmax gradient rows, column sums
+    TILE_GRAD = 3,     // softmax gradient rows, column sums
+    TILE_STORE_F32 = 4 // C as float32, bias, ReLU
 };
 struct TileProduct {
     const uint8_t *A, *B;
@@ -39,10 +40,10 @@ struct TileProduct {
     // of row j, piece k at sb[(j / 128) * sb_n + k * sb_k]
     const uint8_t *sa, *sb;
     int64_t ldsa, sb_n, sb_k;
-    // TILE_STORE
+    // TILE_STORE, TILE_STORE_F32
     void *C;
     int64_t ldc;             // elements
-    int c_bf16, relu;
+    int relu;
     const float *bias;       // [N] or null (also TILE_STATS and TILE_GRAD)
     // TILE_PARTIAL
     float *acc;
