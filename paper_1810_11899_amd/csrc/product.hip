@@ -30,7 +30,7 @@ constexpr int kPiece = 128;   // bytes of a row in one stage
 struct Args {
     TileProduct p;
     int32_t tiles_m, tiles_n, kt_per_split, band;
-    int64_t total, per_xcd;
+    uint32_t total, per_xcd;
 };
 
 // Workgroups go round-robin over the 8 XCDs (workgroup b runs on XCD b % 8);
@@ -41,17 +41,16 @@ struct Coord {
     int split, tm, tn;
 };
 __device__ __forceinline__ bool coord_of(const Args &a, Coord &c) {
-    const int64_t L = (int64_t)(blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
+    const uint32_t L = (blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
     if (L >= a.total) return false;
-    const int64_t per_split = (int64_t)a.tiles_m * a.tiles_n;
+    const uint32_t per_split = (uint32_t)a.tiles_m * a.tiles_n;
     c.split = (int)(L / per_split);
-    const int64_t r = L % per_split;
-    const int64_t in_band = (int64_t)a.band * a.tiles_n;
-    const int b = (int)(r / in_band);
-    const int64_t q = r % in_band;
-    const int h = min(a.band, a.tiles_m - b * a.band);
-    c.tm = b * a.band + (int)(q % h);
+    const uint32_t r = L - c.split * per_split;
+    const uint32_t in_band = (uint32_t)a.band * a.tiles_n;
+    const uint32_t b = r / in_band, q = r - b * in_band;
+    const uint32_t h = (uint32_t)min(a.band, a.tiles_m - (int)b * a.band);
     c.tn = (int)(q / h);
+    c.tm = (int)b * a.band + (int)(q - c.tn * h);
     return true;
 }
 
@@ -708,14 +707,42 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
     finish<EPI, kBigT, kBigT, 2, 4, 8, 4>(a, c, acc, lds);
 }
 
-__global__ __launch_bounds__(256) void reduce_kernel(int32_t splits, int64_t count, int32_t N, const float *acc,
-                                                     void *out, int out_bf16, int64_t ldo) {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
-        float v = acc[i];
-        for (int s = 1; s < splits; ++s) v += acc[(int64_t)s * count + i];
+// out = the sum of the partials in split order; the blocks past `main` sum the
+// rows of a second small matrix (column sums) the same way.  V elements a
+// thread, the partials' loads eight at a time.
+template <int V, bool BF>
+__global__ __launch_bounds__(256) void reduce_kernel(int32_t splits, int64_t count, int32_t N, const float *acc, void *out,
+                                                     int64_t ldo, uint32_t main, int32_t rows2, int32_t N2,
+                                                     const float *acc2, float *out2) {
+    typedef float vec __attribute__((ext_vector_type(V)));
+    if (blockIdx.x >= main) {
+        const int32_t k = (int32_t)(blockIdx.x - main) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+        if (k >= N2) return;
+        float v = 0.0f;
+        for (int32_t r = lane; r < rows2; r += 64) v += acc2[(int64_t)r * N2 + k];
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+        if (lane == 0) out2[k] = v;
+        return;
+    }
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V; i < count; i += (int64_t)main * 256 * V) {
+        vec v = *(const vec *)(acc + i);
+        int32_t s = 1;
+        for (; s + 8 <= splits; s += 8) {
+            vec x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = *(const vec *)(acc + (int64_t)(s + u) * count + i);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v += x[u];
+        }
+        for (; s < splits; ++s) v += *(const vec *)(acc + (int64_t)s * count + i);
         const int64_t at = i / N * ldo + i % N;
-        if (out_bf16) ((uint16_t *)out)[at] = to_bf16(v);
-        else ((float *)out)[at] = v;
+        if constexpr (BF) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) ((uint16_t *)out)[at + e] = to_bf16(v[e]);
+        } else {
+            *(vec *)((float *)out + at) = v;
+        }
     }
 }
 
@@ -742,9 +769,11 @@ TileShape tile_shape(TileType type, const TileProduct &p) {
 }
 
 int32_t tile_splits(int32_t M, int32_t N, int32_t kt) {
+    // large tiles: one round of the 256 CUs; small ones: two blocks a CU, as
+    // long as a part has two pieces
     const int64_t tiles = std::max<int64_t>(1, tiles_of(M, N, kBigT));
     int64_t sp = std::max<int64_t>(1, 256 / tiles);
-    if (sp > kt / 8) sp = std::min<int64_t>(512 / std::max<int64_t>(1, tiles_of(M, N, 128)), kt / 8);
+    if (sp > kt / 8) sp = std::min<int64_t>(512 / std::max<int64_t>(1, tiles_of(M, N, 128)), kt / 2);
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>(sp, 64));
 }
 
@@ -759,13 +788,14 @@ int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStrea
     const int32_t splits = std::max(1, p.splits);
     a.kt_per_split = (p.kt + splits - 1) / splits;
     a.band = 8;
-    a.total = (int64_t)splits * a.tiles_m * a.tiles_n;
-    a.per_xcd = (a.total + 7) / 8;
-    if (8 * a.per_xcd > 0x7FFFFFFF) {
+    const int64_t total = (int64_t)splits * a.tiles_m * a.tiles_n;
+    if (total > 0x7FFFFFF0) {
         set_error("tile_product: %d x %d is too large", p.M, p.N);
         return GCN_EUNSUPPORTED;
     }
-    const unsigned grid = (unsigned)(8 * a.per_xcd);
+    a.total = (uint32_t)total;
+    a.per_xcd = (a.total + 7) / 8;
+    const unsigned grid = 8 * a.per_xcd;
     // (the pairs that the entry points use)
     if (type == TILE_BF16_NN && epi == TILE_STATS) launch<TILE_BF16_NN, TILE_STATS>(big, a, grid, s);
     else if (type == TILE_BF16_NN && epi == TILE_GRAD) launch<TILE_BF16_NN, TILE_GRAD>(big, a, grid, s);
@@ -784,12 +814,23 @@ int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStrea
     return GCN_OK;
 }
 
-int tile_reduce(int32_t splits, int32_t M, int32_t N, const float *acc, void *out, int out_bf16, int64_t ldo,
-                hipStream_t s) {
+int tile_reduce(int32_t splits, int32_t M, int32_t N, const float *acc, void *out, int out_bf16, int64_t ldo, hipStream_t s,
+                int32_t rows2, int32_t N2, const float *acc2, float *out2) {
     const int64_t count = (int64_t)M * N;
     if (count == 0) return GCN_OK;
-    const unsigned g = (unsigned)std::min<int64_t>((count + 255) / 256, 8192);
-    hipLaunchKernelGGL(reduce_kernel, dim3(g), dim3(256), 0, s, splits, count, N, acc, out, out_bf16, ldo);
+    const bool vec = N % 4 == 0 && ldo % 4 == 0 && (uintptr_t)out % 16 == 0;
+    const uint32_t main = (uint32_t)std::min<int64_t>((count / (vec ? 4 : 1) + 255) / 256, 8192);
+    const dim3 g(main + (uint32_t)((N2 + 3) / 4));
+#define GCN_REDUCE(V, BF) \
+    hipLaunchKernelGGL((reduce_kernel<V, BF>), g, dim3(256), 0, s, splits, count, N, acc, out, ldo, main, rows2, N2, acc2, out2)
+    if (vec) {
+        if (out_bf16) GCN_REDUCE(4, true);
+        else GCN_REDUCE(4, false);
+    } else {
+        if (out_bf16) GCN_REDUCE(1, true);
+        else GCN_REDUCE(1, false);
+    }
+#undef GCN_REDUCE
     GCN_LAUNCH_CHECK("reduce_kernel");
     return GCN_OK;
 }

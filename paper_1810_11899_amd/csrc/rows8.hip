@@ -100,21 +100,61 @@ __global__ __launch_bounds__(kTB) void pack_kernel(int64_t blocks, int32_t per_r
     }
 }
 
-__device__ __forceinline__ float e4m3_value(uint32_t b) {
-    return __builtin_amdgcn_cvt_f32_fp8((int)b, 0);
+// eight 8-bit values under one scale
+__device__ __forceinline__ void values8(uint2 q, int e, float (&x)[8]) {
+    const uint32_t w[2] = {q.x, q.y};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[h], true);
+        x[4 * h] = __builtin_amdgcn_ldexpf(lo[0], e);
+        x[4 * h + 1] = __builtin_amdgcn_ldexpf(lo[1], e);
+        x[4 * h + 2] = __builtin_amdgcn_ldexpf(hi[0], e);
+        x[4 * h + 3] = __builtin_amdgcn_ldexpf(hi[1], e);
+    }
 }
 
-template <bool BF>
+// eight columns to a thread; rows n .. drows - 1 and columns past f (to the last
+// whole eight, where ldx holds them) are written as zeros when PAD
+template <bool BF, bool VEC, bool PAD>
+__device__ __forceinline__ void unpack_rows(int64_t first, int64_t step, int32_t drows, int32_t n, int32_t f,
+                                            const uint8_t *q, int64_t ldq, const uint8_t *scale, int64_t lds, void *X,
+                                            int64_t ldx) {
+    const uint32_t per_row = (uint32_t)(f + 7) / 8;
+    const int64_t total = (int64_t)drows * per_row;
+    for (int64_t i = first; i < total; i += step) {
+        const int64_t row = i / per_row;
+        const int32_t c = (int32_t)(i - row * per_row) * 8;
+        float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        if (!PAD || row < n)   // (q's columns past f hold zeros)
+            values8(*(const uint2 *)(q + row * ldq + c), (int)scale[row * lds + c / kBlk] - 127, x);
+        if (BF) {
+            uint16_t *d = (uint16_t *)X + row * ldx + c;
+            if (VEC && (PAD || c + 8 <= f)) {
+                *(uint4 *)d = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                                         pack_bf16x2(x[6], x[7]));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c + e < f) d[e] = to_bf16(x[e]);
+            }
+        } else {
+            float *d = (float *)X + row * ldx + c;
+            if (VEC && c + 8 <= f) {
+                *(float4 *)d = make_float4(x[0], x[1], x[2], x[3]);
+                *(float4 *)(d + 4) = make_float4(x[4], x[5], x[6], x[7]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c + e < f) d[e] = x[e];
+            }
+        }
+    }
+}
+template <bool BF, bool VEC>
 __global__ __launch_bounds__(kTB) void unpack_kernel(int32_t n, int32_t f, const uint8_t *q, int64_t ldq,
                                                      const uint8_t *scale, int64_t lds, void *X, int64_t ldx) {
-    const int64_t total = (int64_t)n * f;
-    for (int64_t i = (int64_t)blockIdx.x * kTB + threadIdx.x; i < total; i += (int64_t)gridDim.x * kTB) {
-        const int64_t row = i / f;
-        const int32_t c = (int32_t)(i - row * f);
-        const float v = ldexpf(e4m3_value(q[row * ldq + c]), (int)scale[row * lds + c / kBlk] - 127);
-        if (BF) ((uint16_t *)X)[row * ldx + c] = to_bf16(v);
-        else ((float *)X)[row * ldx + c] = v;
-    }
+    unpack_rows<BF, VEC, false>((int64_t)blockIdx.x * kTB + threadIdx.x, (int64_t)gridDim.x * kTB, n, n, f, q, ldq, scale,
+                                lds, X, ldx);
 }
 
 // One 128 x 128 block of the weights to a workgroup: the largest magnitude in
@@ -164,22 +204,56 @@ __global__ __launch_bounds__(kTB) void pack_weights_kernel(int32_t K, int32_t N,
 // is a positive e4m3 value (1 .. 0x7E), zero elsewhere, as bfloat16 rows; the
 // column sums of a strip of rows; and, when wanted, dZ's 8-bit rows.  One
 // block of 128 columns and a strip of rows to a workgroup, 16 lanes a row, so
-// that one pass over dY and the mask serves all three.
+// that one pass over dY and the mask serves all three.  The rows from n to nz
+// are zeros.  The workgroups past the strips widen X8 to bfloat16 rows.
+struct MaskArgs {
+    int32_t n, nz, N, rows_per_strip, strips, blocks;   // blocks: of 128 columns
+    const void *dY;
+    int64_t lddy;
+    const uint8_t *mask;
+    int64_t ldm;
+    uint16_t *dZ;
+    int64_t lddz;
+    float *part;
+    uint8_t *q;
+    int64_t ldq;
+    uint8_t *scale;
+    int64_t lds;
+    // X8 [n x f] to X [nz x ldx]
+    int32_t f;
+    const uint8_t *xq;
+    int64_t ldxq;
+    const uint8_t *xscale;
+    int64_t ldxs;
+    uint16_t *X;
+    int64_t ldx;
+};
 template <bool BF, bool VEC>
-__global__ __launch_bounds__(kTB) void mask_kernel(int32_t n, int32_t N, int32_t rows_per_strip, const void *dY,
-                                                   int64_t lddy, const uint8_t *mask, int64_t ldm, uint16_t *dZ,
-                                                   int64_t lddz, float *part, uint8_t *q, int64_t ldq, uint8_t *scale,
-                                                   int64_t lds) {
+__global__ __launch_bounds__(kTB) void mask_kernel(MaskArgs a) {
     __shared__ float red[kTB / 16][kBlk];
-    const int c = blockIdx.x * kBlk + 8 * (int)(threadIdx.x & 15);
-    const int64_t r0 = (int64_t)blockIdx.y * rows_per_strip;
-    const int64_t r1 = min(r0 + rows_per_strip, (int64_t)n);
+    const int strip = (int)(blockIdx.x / a.blocks), cb = (int)(blockIdx.x % a.blocks);
+    if (strip >= a.strips) {
+        const int64_t b = (int64_t)blockIdx.x - (int64_t)a.strips * a.blocks;
+        unpack_rows<true, true, true>(b * kTB + threadIdx.x, ((int64_t)gridDim.x - (int64_t)a.strips * a.blocks) * kTB, a.nz,
+                                      a.n, a.f, a.xq, a.ldxq, a.xscale, a.ldxs, a.X, a.ldx);
+        return;
+    }
+    const int32_t n = a.n, N = a.N;
+    const void *const dY = a.dY;
+    const int64_t lddy = a.lddy, ldm = a.ldm, lddz = a.lddz, ldq = a.ldq, lds = a.lds;
+    const uint8_t *const mask = a.mask;
+    uint16_t *const dZ = a.dZ;
+    float *const part = a.part;
+    uint8_t *const q = a.q, *const scale = a.scale;
+    const int c = cb * kBlk + 8 * (int)(threadIdx.x & 15);
+    const int64_t r0 = (int64_t)strip * a.rows_per_strip;
+    const int64_t r1 = min(r0 + a.rows_per_strip, (int64_t)a.nz);
     float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     // (the strip's rows in steps of 16; the lanes past its end stay for the
     // exchanges of pack_block)
     for (int64_t b = r0; b < r1; b += kTB / 16) {
         const int64_t r = b + threadIdx.x / 16;
-        const bool in = r < r1;
+        const bool in = r < r1 && r < n;
         float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
         if (in) {
             load8<BF, VEC>((const char *)dY + r * lddy * (BF ? 2 : 4), c, N, x);
@@ -203,22 +277,24 @@ __global__ __launch_bounds__(kTB) void mask_kernel(int32_t n, int32_t N, int32_t
                 x[i] = byte - 1u < 0x7Eu ? v : 0.0f;
                 sum[i] += x[i];
             }
+        }
+        if (r < r1) {
             if (c < lddz)
                 *(uint4 *)(dZ + r * lddz + c) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
                                                            pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
         }
-        if (q) pack_block(x, q + (in ? r : r0) * ldq + blockIdx.x * kBlk, scale + (in ? r : r0) * lds + blockIdx.x, in);
+        if (q) pack_block(x, q + (in ? r : 0) * ldq + cb * kBlk, scale + (in ? r : 0) * lds + cb, in);
     }
     if (!part) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) red[threadIdx.x / 16][8 * (threadIdx.x & 15) + i] = sum[i];
     __syncthreads();
-    const int k = blockIdx.x * kBlk + threadIdx.x;
+    const int k = cb * kBlk + threadIdx.x;
     if (threadIdx.x < kBlk && k < N) {
         float t = 0.0f;
 #pragma unroll
         for (int g = 0; g < kTB / 16; ++g) t += red[g][threadIdx.x];
-        part[(int64_t)blockIdx.y * N + k] = t;
+        part[(int64_t)strip * N + k] = t;
     }
 }
 
@@ -293,15 +369,21 @@ int gcn_rows8_unpack(const gcn_rows8 *r, void *X, gcn_rows_type type, int32_t ld
     GCN_REQUIRE(r->n == 0 || X, GCN_EINVAL, "gcn_rows8_unpack: null pointer");
     if (r->n == 0) return GCN_OK;
     hipStream_t s = (hipStream_t)stream;
-    const int64_t total = (int64_t)r->n * r->f;
-    ProfScope prof(K_ROWS8_PACK, s, 0.0, (double)total * (type == GCN_ROWS_BF16 ? 3.0 : 5.0));
-    const unsigned g = grid_of(total, kTB, 16384);
-    if (type == GCN_ROWS_BF16)
-        hipLaunchKernelGGL(unpack_kernel<true>, dim3(g), dim3(kTB), 0, s, r->n, r->f, r->q, (int64_t)r->ldq, r->scale,
-                           (int64_t)r->ldscale, X, (int64_t)ldx);
-    else
-        hipLaunchKernelGGL(unpack_kernel<false>, dim3(g), dim3(kTB), 0, s, r->n, r->f, r->q, (int64_t)r->ldq, r->scale,
-                           (int64_t)r->ldscale, X, (int64_t)ldx);
+    const bool bf = type == GCN_ROWS_BF16;
+    ProfScope prof(K_ROWS8_PACK, s, 0.0, (double)r->n * r->f * (bf ? 3.0 : 5.0));
+    const bool vec = aligned(X, 16) && ldx % (bf ? 8 : 4) == 0;
+    const unsigned g = grid_of((int64_t)r->n * ((r->f + 7) / 8), kTB, 16384);
+#define GCN_UNPACK(BF, VEC)                                                                                       \
+    hipLaunchKernelGGL((unpack_kernel<BF, VEC>), dim3(g), dim3(kTB), 0, s, r->n, r->f, r->q, (int64_t)r->ldq, r->scale, \
+                       (int64_t)r->ldscale, X, (int64_t)ldx)
+    if (bf) {
+        if (vec) GCN_UNPACK(true, true);
+        else GCN_UNPACK(true, false);
+    } else {
+        if (vec) GCN_UNPACK(false, true);
+        else GCN_UNPACK(false, false);
+    }
+#undef GCN_UNPACK
     GCN_LAUNCH_CHECK("unpack_kernel");
     return GCN_OK;
 }
@@ -338,33 +420,30 @@ int gcn_weights8_pack(const void *W, gcn_rows_type type, int32_t ldw, const gcn_
 }
 
 namespace {
+// Rows and columns of the operands in whole 64-row pieces and 16-byte chunks.
 struct GradPlan {
-    int32_t Np, fp, split, strip, strips;
-    size_t gemm, total;
+    int32_t nz, Np, fp, splits, strip, strips;
+    size_t total;
 };
-GemmProblem grad_problem(int32_t f, int32_t N, int32_t n) {
-    GemmProblem w{};
-    w.M = f;
-    w.N = N;
-    w.seg[0].K = n;
-    return w;
-}
-GradPlan plan_grad(int32_t n, int32_t f, int32_t N) {
+struct GradBuffers {
+    uint16_t *dZ, *X;
+    float *part, *acc;
+};
+GradPlan plan_grad(int32_t n, int32_t f, int32_t N, void *ws, size_t ws_bytes, GradBuffers &b) {
     GradPlan p{};
+    p.nz = (int32_t)std::min<int64_t>(((int64_t)n + 63) / 64 * 64, 0x7FFFFFC0);
     p.Np = (N + 7) / 8 * 8;
     p.fp = (f + 7) / 8 * 8;
-    const GemmProblem w = grad_problem(f, N, n);
-    p.split = gemm_pick_split(1, &w, true);
-    p.gemm = gemm_workspace_bytes(1, &w, p.split);
+    p.splits = tile_splits(f, N, p.nz / 64);
     // strips: about 2048 workgroups, at least 16 rows each
     const int64_t most = std::max<int64_t>(1, 2048 / blocks8(N));
-    p.strip = (int32_t)std::max<int64_t>(16, ((n + most - 1) / most + 15) / 16 * 16);
-    p.strips = std::max(1, (n + p.strip - 1) / p.strip);
-    Arena ar(nullptr, 0);
-    ar.take<uint16_t>((size_t)n * p.Np);
-    ar.take<uint16_t>((size_t)n * p.fp);
-    ar.take<float>((size_t)p.strips * N);
-    ar.take<char>(p.gemm);
+    p.strip = (int32_t)std::max<int64_t>(16, ((p.nz + most - 1) / most + 15) / 16 * 16);
+    p.strips = std::max(1, (int32_t)(((int64_t)p.nz + p.strip - 1) / p.strip));
+    Arena ar(ws, ws_bytes);
+    b.dZ = ar.take<uint16_t>((size_t)p.nz * p.Np);
+    b.X = ar.take<uint16_t>((size_t)p.nz * p.fp);
+    b.part = ar.take<float>((size_t)p.strips * N);
+    b.acc = ar.take<float>((size_t)p.splits * f * N);
     p.total = ar.used + 256;
     return p;
 }
@@ -372,7 +451,8 @@ GradPlan plan_grad(int32_t n, int32_t f, int32_t N) {
 
 size_t gcn_rows8_weight_grad_workspace_bytes(int32_t n, int32_t f, int32_t N) {
     if (n < 0 || f <= 0 || N <= 0) return 0;
-    return plan_grad(n, f, N).total;
+    GradBuffers b;
+    return plan_grad(n, f, N, nullptr, 0, b).total;
 }
 
 int gcn_rows8_weight_grad(const gcn_rows8 *X8, const uint8_t *mask, int32_t ldmask, const void *dY, gcn_rows_type type,
@@ -391,7 +471,9 @@ int gcn_rows8_weight_grad(const gcn_rows8 *X8, const uint8_t *mask, int32_t ldma
         GCN_REQUIRE(dZ8->n == n && dZ8->f == N, GCN_ESHAPE, "gcn_rows8_weight_grad: dZ8 is %d x %d, not %d x %d", dZ8->n,
                     dZ8->f, n, N);
     }
-    const GradPlan p = plan_grad(n, f, N);
+    GradBuffers b;
+    const GradPlan p = plan_grad(n, f, N, ws, ws_bytes, b);
+    GCN_REQUIRE(n <= 0x7FFFFFC0, GCN_EUNSUPPORTED, "gcn_rows8_weight_grad: n=%d", n);
     GCN_REQUIRE(ws && aligned(ws, 256) && ws_bytes >= p.total, GCN_EWORKSPACE,
                 "gcn_rows8_weight_grad: workspace %zu < %zu bytes, or not 256-byte aligned", ws_bytes, p.total);
     hipStream_t s = (hipStream_t)stream;
@@ -400,39 +482,38 @@ int gcn_rows8_weight_grad(const gcn_rows8 *X8, const uint8_t *mask, int32_t ldma
             if ((rc = fill_zero(dW + (int64_t)i * lddw, N, s))) return rc;
         return db ? fill_zero(db, N, s) : GCN_OK;
     }
-    Arena ar(ws, ws_bytes);
-    uint16_t *dZ = ar.take<uint16_t>((size_t)n * p.Np), *X = ar.take<uint16_t>((size_t)n * p.fp);
-    float *part = ar.take<float>((size_t)p.strips * N);
-    void *gw = p.gemm ? ar.take<char>(p.gemm) : nullptr;
     {
         const bool bf = type == GCN_ROWS_BF16;
-        ProfScope prof(K_ROWS8_MASK, s, 0.0, (double)n * N * ((bf ? 4.0 : 6.0) + (mask ? 1.0 : 0.0) + (dZ8 ? 1.0 : 0.0)));
+        ProfScope prof(K_ROWS8_MASK, s, 0.0,
+                       (double)n * N * ((bf ? 4.0 : 6.0) + (mask ? 1.0 : 0.0) + (dZ8 ? 1.0 : 0.0)) + 3.0 * n * f);
         const bool vec = aligned(dY, 16) && lddy % (bf ? 8 : 4) == 0 && (!mask || (aligned(mask, 8) && ldmask % 8 == 0));
-        const dim3 g((unsigned)blocks8(N), (unsigned)p.strips);
-#define GCN_MASK(BF, VEC)                                                                                              \
-    hipLaunchKernelGGL((mask_kernel<BF, VEC>), g, dim3(kTB), 0, s, n, N, p.strip, dY, (int64_t)lddy, mask,             \
-                       (int64_t)ldmask, dZ, (int64_t)p.Np, db ? part : nullptr, dZ8 ? dZ8->q : nullptr,                \
-                       dZ8 ? (int64_t)dZ8->ldq : 0, dZ8 ? dZ8->scale : nullptr, dZ8 ? (int64_t)dZ8->ldscale : 0)
+        const int32_t blocks = (int32_t)blocks8(N);
+        const MaskArgs m{n, p.nz, N, p.strip, p.strips, blocks, dY, lddy, mask, ldmask, b.dZ, p.Np, db ? b.part : nullptr,
+                         dZ8 ? dZ8->q : nullptr, dZ8 ? dZ8->ldq : 0, dZ8 ? dZ8->scale : nullptr, dZ8 ? dZ8->ldscale : 0,
+                         f, X8->q, X8->ldq, X8->scale, X8->ldscale, b.X, p.fp};
+        const dim3 g((unsigned)(p.strips * blocks) + grid_of((int64_t)p.nz * (p.fp / 8), kTB, 4096));
         if (bf) {
-            if (vec) GCN_MASK(true, true);
-            else GCN_MASK(true, false);
+            if (vec) hipLaunchKernelGGL((mask_kernel<true, true>), g, dim3(kTB), 0, s, m);
+            else hipLaunchKernelGGL((mask_kernel<true, false>), g, dim3(kTB), 0, s, m);
         } else {
-            if (vec) GCN_MASK(false, true);
-            else GCN_MASK(false, false);
+            if (vec) hipLaunchKernelGGL((mask_kernel<false, true>), g, dim3(kTB), 0, s, m);
+            else hipLaunchKernelGGL((mask_kernel<false, false>), g, dim3(kTB), 0, s, m);
         }
-#undef GCN_MASK
         GCN_LAUNCH_CHECK("mask_kernel");
     }
-    if (db && (rc = colsum_reduce_rows(p.strips, N, part, db, s))) return rc;
-    ProfScope prof(K_ROWS8_WEIGHT_GRAD, s, 2.0 * n * f * N, (double)n * f + 2.0 * n * N + 4.0 * f * N);
-    hipLaunchKernelGGL(unpack_kernel<true>, dim3(grid_of((int64_t)n * f, kTB, 16384)), dim3(kTB), 0, s, n, f, X8->q,
-                       (int64_t)X8->ldq, X8->scale, (int64_t)X8->ldscale, (void *)X, (int64_t)p.fp);
-    GCN_LAUNCH_CHECK("unpack_kernel");
-    GemmProblem w = grad_problem(f, N, n);
-    w.C = dW;
-    w.ldc = lddw;
-    w.seg[0] = GemmSeg{X, p.fp, dZ, p.Np, n};
-    return gemm(L_TN, 1, &w, 1, p.split, gw, p.gemm, s);
+    ProfScope prof(K_ROWS8_WEIGHT_GRAD, s, 2.0 * n * f * N, 2.0 * n * f + 2.0 * n * N + 4.0 * f * N);
+    TileProduct w{};
+    w.A = (const uint8_t *)b.X;
+    w.lda = 2 * (int64_t)p.fp;
+    w.B = (const uint8_t *)b.dZ;
+    w.ldb = 2 * (int64_t)p.Np;
+    w.M = f;
+    w.N = N;
+    w.kt = p.nz / 64;
+    w.splits = p.splits;
+    w.acc = b.acc;
+    if ((rc = tile_product(TILE_BF16_TN, TILE_PARTIAL, w, s))) return rc;
+    return tile_reduce(p.splits, f, N, b.acc, dW, 0, lddw, s, p.strips, db ? N : 0, b.part, db);
 }
 
 }  // extern "C"
