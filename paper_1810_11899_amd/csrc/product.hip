@@ -345,53 +345,84 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
     }
 }
 
+// ---------------------------------------------------------------- copies
+// 16 bytes a lane from base + off straight to LDS at dst + 16 lane (base, dst
+// uniform).  In assembly because the compiler, which sees only that both touch
+// LDS, puts a wait for every outstanding copy before each LDS read, and these
+// kernels keep copies in flight over many of them.  The instruction has no
+// register result that could be taken for written, its operands are read as it
+// is issued, and the kernel waits by wait_copies and a barrier.
+__device__ __forceinline__ void copy_to_lds(const uint8_t *base, uint32_t off, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void copy_to_lds(const uint8_t *from, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(from) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// a barrier alone: the fence of __syncthreads would wait for every copy
+__device__ __forceinline__ void turn() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // ------------------------------------------------------------ small tiles
-// WM x WN wavefronts, two LDS stages: the next piece is copied while one is
-// multiplied, and several blocks a CU cover each other's waits.
-template <int TYPE, int EPI, int BM, int BN, int WM, int WN>
+// WM x WN wavefronts and a ring of S stages: while piece t is multiplied, the
+// copies of the next S - 1 are in flight (with two stages a piece took 1.4 us
+// whatever its size, the latency of one copy), and one barrier a piece both
+// publishes it and frees the stage of the piece before.  Scales are staged for
+// kScalePieces pieces at a time.
+constexpr int kScalePieces = 64;
+template <int TYPE, int EPI, int BM, int BN, int WM, int WN, int S>
 __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16, T = 64 * WM * WN;
     constexpr int kStage = (BM + BN) * kPiece;
-    constexpr int LA = BM * kPiece / 16 / T, LB = BN * kPiece / 16 / T;
+    constexpr int LA = BM * kPiece / 16 / T, LB = BN * kPiece / 16 / T, L = LA + LB;
     static_assert(LA * T * 16 == BM * kPiece && LB * T * 16 == BN * kPiece, "whole chunks per lane");
-    __shared__ __attribute__((aligned(16))) char lds[2 * kStage];
+    static_assert(S >= 2 && S <= 4 && kRows8Block % BN == 0, "a tile's columns share a scale");
+    constexpr bool SCALED = !is_bf16(TYPE);
+    __shared__ __attribute__((aligned(16))) char lds[S * kStage + (SCALED ? kScalePieces * (BM + 1) : 0)];
     Coord c;
     if (!coord_of(a, c)) return;
     const TileProduct &p = a.p;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const int m0 = c.tm * BM, n0 = c.tn * BN;
-    const int kt0 = c.split * a.kt_per_split, kt1 = min(kt0 + a.kt_per_split, p.kt);
-    // lane of copy u: tile row (u T + thread) / 8, stored chunk thread % 8,
-    // which holds the row's chunk (thread % 8) ^ (row % 8); rows past the
-    // extent are clamped (their products are dropped)
-    const int lr = threadIdx.x >> 3, chunk = ((threadIdx.x & 7) ^ (lr & 7)) * 16;
+    const int kt0 = c.split * a.kt_per_split, nt = min(a.kt_per_split, p.kt - kt0);
     constexpr bool KA = km_a(TYPE), KB = km_b(TYPE);
     static_assert((!KA || BM == 128) && (!KB || BN == 128), "k-rows of 16 chunks");
     const int64_t step_a = KA ? 64 * p.lda : kPiece, step_b = KB ? 64 * p.ldb : kPiece;
-    // k-major: k-row (u T + thread) / 16, its chunks clamped to the last whole one
-    auto km_at = [&](const uint8_t *base, int64_t ld, int x0, int extent, int u) {
+    // Copy u of a thread: tile row (u T + thread) / 8, stored chunk thread % 8,
+    // which holds the row's chunk (thread % 8) ^ (row % 8); rows past the extent
+    // are clamped (their products are dropped).  k-major: k-row (u T + thread) /
+    // 16, its chunks clamped to the last whole one.
+    const int lr = threadIdx.x >> 3, chunk = ((threadIdx.x & 7) ^ (lr & 7)) * 16;
+    auto km_at = [&](int64_t ld, int x0, int extent, int u) {
         const int k = (u * T + threadIdx.x) >> 4, ch = 8 * ((threadIdx.x & 15) ^ (4 * (k & 3)));
-        return base + k * ld + 2 * (int64_t)min(x0 + ch, ((extent + 7) & ~7) - 8);
+        return k * ld + 2 * (int64_t)min(x0 + ch, ((extent + 7) & ~7) - 8);
     };
     const uint8_t *ga[LA], *gb[LB];
 #pragma unroll
     for (int u = 0; u < LA; ++u)
-        ga[u] = KA ? km_at(p.A, p.lda, m0, p.M, u) : p.A + (int64_t)min(m0 + u * (T / 8) + lr, p.M - 1) * p.lda + chunk;
+        ga[u] = p.A + kt0 * step_a +
+                (KA ? km_at(p.lda, m0, p.M, u) : (int64_t)min(m0 + u * (T / 8) + lr, p.M - 1) * p.lda + chunk);
 #pragma unroll
     for (int u = 0; u < LB; ++u)
-        gb[u] = KB ? km_at(p.B, p.ldb, n0, p.N, u) : p.B + (int64_t)min(n0 + u * (T / 8) + lr, p.N - 1) * p.ldb + chunk;
-    auto copy = [&](int kt, int stage) {
-        char *d = lds + stage * kStage + wave * 1024;
+        gb[u] = p.B + kt0 * step_b +
+                (KB ? km_at(p.ldb, n0, p.N, u) : (int64_t)min(n0 + u * (T / 8) + lr, p.N - 1) * p.ldb + chunk);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * 1024;
+    auto copy = [&](int t, int stage) {
+        const uint32_t d = lds0 + stage * kStage;
 #pragma unroll
-        for (int u = 0; u < LA; ++u)
-            __builtin_amdgcn_global_load_lds((const void *)(ga[u] + kt * step_a),
-                                             (void __attribute__((address_space(3))) *)(d + u * T * 16), 16, 0, 0);
+        for (int u = 0; u < LA; ++u) copy_to_lds(ga[u] + t * step_a, d + u * T * 16);
 #pragma unroll
-        for (int u = 0; u < LB; ++u)
-            __builtin_amdgcn_global_load_lds((const void *)(gb[u] + kt * step_b),
-                                             (void __attribute__((address_space(3))) *)(d + BM * kPiece + u * T * 16), 16,
-                                             0, 0);
+        for (int u = 0; u < LB; ++u) copy_to_lds(gb[u] + t * step_b, d + BM * kPiece + u * T * 16);
     };
     f32x4 acc[FM][FN];
 #pragma unroll
@@ -405,20 +436,47 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
         const char *q = tile + (row + fr) * kPiece;
         return Frag{*(const uint4 *)(q + o0), *(const uint4 *)(q + o1)};
     };
-    if (kt0 < kt1) copy(kt0, 0);
-    __syncthreads();
-    for (int kt = kt0; kt < kt1; ++kt) {
-        const int st = (kt - kt0) & 1;
-        if (kt + 1 < kt1) copy(kt + 1, st ^ 1);
-        const char *ta = lds + st * kStage, *tb = ta + BM * kPiece;
-        int sa[FM], sb[FN];
-        if constexpr (!is_bf16(TYPE)) {
+    uint8_t *const s8 = (uint8_t *)lds + S * kStage;   // [piece][BM rows], then [piece]
+    auto scales = [&](int t) {
+        const int w = min(kScalePieces, nt - t);
+        for (int i = threadIdx.x; i < BM * w; i += T) {
+            const int r = i / w, k = i - r * w;
+            s8[k * BM + r] = p.sa[(int64_t)min(m0 + r, p.M - 1) * p.ldsa + kt0 + t + k];
+        }
+        for (int k = threadIdx.x; k < w; k += T)
+            s8[kScalePieces * BM + k] = p.sb[(int64_t)(n0 / kRows8Block) * p.sb_n + (int64_t)(kt0 + t + k) * p.sb_k];
+    };
+    if constexpr (SCALED) {
+        if (nt > 0) scales(0);
+        wait_copies<0>();   // (the loads above, ahead of the counted copies)
+    }
 #pragma unroll
-            for (int i = 0; i < FM; ++i)
-                sa[i] = p.sa[(int64_t)min(m0 + wm * (BM / WM) + 16 * i + fr, p.M - 1) * p.ldsa + kt];
+    for (int t = 0; t < S - 1; ++t)
+        if (t < nt) copy(t, t);
+    int stage = 0;
+    for (int t = 0; t < nt; ++t) {
+        if constexpr (SCALED) {
+            if (t % kScalePieces == 0 && t) {
+                turn();   // every wavefront has read the old ones
+                scales(t);
+            }
+            wait_reads();   // the scales' LDS writes, ahead of the barrier
+        }
+        // piece t has landed when only the later ones' copies are outstanding
+        const int later = min(nt - 1 - t, S - 2);
+        if (S >= 4 && later >= 2) wait_copies<2 * L>();
+        else if (S >= 3 && later >= 1) wait_copies<L>();
+        else wait_copies<0>();
+        turn();
+        // (every wavefront has used what it read of piece t - 1: its stage is free)
+        if (t + S - 1 < nt) copy(t + S - 1, stage ? stage - 1 : S - 1);
+        const char *ta = lds + stage * kStage, *tb = ta + BM * kPiece;
+        int sa[FM], sb = 0;
+        if constexpr (SCALED) {
+            const int k = t % kScalePieces;
 #pragma unroll
-            for (int j = 0; j < FN; ++j)
-                sb[j] = p.sb[(int64_t)(min(n0 + wn * (BN / WN) + 16 * j, p.N - 1) / kRows8Block) * p.sb_n + kt * p.sb_k];
+            for (int i = 0; i < FM; ++i) sa[i] = s8[k * BM + wm * (BM / WM) + 16 * i + fr];
+            sb = s8[kScalePieces * BM + k];
         }
         Frag fb[FN];
 #pragma unroll
@@ -437,13 +495,13 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
                 const Frag fa = frag(ta, wm * (BM / WM) + 16 * i, KA);
                 const bf16v8 wa[4] = {widen8(fa.lo.x, fa.lo.y), widen8(fa.lo.z, fa.lo.w), widen8(fa.hi.x, fa.hi.y),
                                       widen8(fa.hi.z, fa.hi.w)};
+                const int e = sa[i] + sb - 254;
 #pragma unroll
                 for (int j = 0; j < FN; ++j) {
                     f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][k], wa[k], z, 0, 0, 0);
-                    const int e = sa[i] + sb[j] - 254;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) acc[i][j][q] += __builtin_amdgcn_ldexpf(z[q], e);
                 }
@@ -453,11 +511,17 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
             for (int i = 0; i < FM; ++i) {
                 const Frag fa = frag(ta, wm * (BM / WM) + 16 * i, KA);
 #pragma unroll
-                for (int j = 0; j < FN; ++j) mma<TYPE>(acc[i][j], fa, fb[j], TYPE == TILE_FP8 ? sa[i] : 0, TYPE == TILE_FP8 ? sb[j] : 0);
+                for (int j = 0; j < FN; ++j) mma<TYPE>(acc[i][j], fa, fb[j], TYPE == TILE_FP8 ? sa[i] : 0, sb);
             }
         }
-        __syncthreads();   // (also waits for the copies of the next piece)
+        // what was read is used before the next barrier: the products stay above it
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) asm volatile("" : "+v"(acc[i][j]));
+        stage = stage + 1 == S ? 0 : stage + 1;
     }
+    __syncthreads();
     finish<EPI, BM, BN, WM, WN, FM, FN>(a, c, acc, lds);
 }
 
@@ -488,28 +552,6 @@ constexpr int kBigT = 256, kBigThreads = 512;
 constexpr int kRegion = 128 * kPiece, kBuffer = 4 * kRegion;
 constexpr int kBigPieces = 120;                          // pieces whose scales fit in LDS
 constexpr int kScaleA = kBigPieces * 64 * 4, kScaleB = kBigPieces * 2;
-
-// 16 bytes a lane from base + off straight to LDS at dst + 16 lane (base, dst
-// uniform).  In assembly because the compiler, which sees only that both touch
-// LDS, puts a wait for every outstanding copy before each LDS read, and this
-// kernel keeps five quarters of copies in flight.  The instruction has no
-// register result that could be taken for written, its operands are read as it
-// is issued, and the kernel waits by wait_copies and a barrier.
-__device__ __forceinline__ void copy_to_lds(const uint8_t *base, uint32_t off, uint32_t dst) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory");
-}
-template <int N>
-__device__ __forceinline__ void wait_copies() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-__device__ __forceinline__ void turn() {
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
 
 template <int TYPE, int I, int J>
 __device__ __forceinline__ void mma_big(f32x4 &acc, const Frag &a, const Frag &b, int sa, int sb) {
@@ -707,6 +749,78 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
     finish<EPI, kBigT, kBigT, 2, 4, 8, 4>(a, c, acc, lds);
 }
 
+// --------------------------------------------------------------- few rows
+// Up to 16 FM rows: the weights are read once and there is little to multiply, so
+// nothing goes through LDS on the way in.  A workgroup has 16 columns of C and
+// all rows; its eight wavefronts take every eighth piece of K, fragments straight
+// from memory to registers, and add their sums in wavefront order.
+constexpr int kThinWaves = 8, kThin = 64;   // wavefronts; the most rows
+template <int TYPE, int EPI, int FM>
+__global__ __launch_bounds__(64 * kThinWaves) void thin_kernel(TileProduct p) {
+    __shared__ f32x4 part[kThinWaves][FM][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * 16;
+    const uint8_t *const b = p.B + (int64_t)min(n0 + fr, p.N - 1) * p.ldb + g * 16;
+    const uint8_t *const sbp = p.sb + (int64_t)(n0 / kRows8Block) * p.sb_n;
+    const uint8_t *a[FM], *sap[FM];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int64_t r = min(16 * i + fr, p.M - 1);
+        a[i] = p.A + r * p.lda + g * 16;
+        sap[i] = p.sa + r * p.ldsa;
+    }
+    f32x4 acc[FM];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int t = wave; t < p.kt; t += kThinWaves) {   // (a second piece's loads in flight: no faster)
+        const int64_t o = (int64_t)t * kPiece;
+        const Frag fb = {*(const uint4 *)(b + o), *(const uint4 *)(b + o + 64)};
+        const int sb = sbp[t * p.sb_k];
+        bf16v8 wb[4];
+        if constexpr (TYPE == TILE_FP8_EXACT) {
+            wb[0] = widen8(fb.lo.x, fb.lo.y);
+            wb[1] = widen8(fb.lo.z, fb.lo.w);
+            wb[2] = widen8(fb.hi.x, fb.hi.y);
+            wb[3] = widen8(fb.hi.z, fb.hi.w);
+        }
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const Frag fa = {*(const uint4 *)(a[i] + o), *(const uint4 *)(a[i] + o + 64)};
+            const int sa = sap[i][t];
+            if constexpr (TYPE == TILE_FP8_EXACT) {
+                const bf16v8 wa[4] = {widen8(fa.lo.x, fa.lo.y), widen8(fa.lo.z, fa.lo.w), widen8(fa.hi.x, fa.hi.y),
+                                      widen8(fa.hi.z, fa.hi.w)};
+                f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[k], wa[k], z, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][e] += __builtin_amdgcn_ldexpf(z[e], sa + sb - 254);
+            } else {
+                mma<TYPE>(acc[i], fa, fb, sa, sb);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i) part[wave][i][lane] = acc[i];
+    __syncthreads();
+    if (wave >= FM) return;
+    f32x4 v = part[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < kThinWaves; ++w) v += part[w][wave][lane];
+    const int row = 16 * wave + fr;
+    if (row >= p.M) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int col = n0 + 4 * g + e;
+        if (col >= p.N) break;
+        float x = v[e] + (p.bias ? p.bias[col] : 0.0f);
+        if (p.relu) x = x < 0.0f ? 0.0f : x;
+        const int64_t at = (int64_t)row * p.ldc + col;
+        if constexpr (EPI == TILE_STORE) ((uint16_t *)p.C)[at] = to_bf16(x);
+        else ((float *)p.C)[at] = x;
+    }
+}
+
 // out = the sum of the partials in split order; the blocks past `main` sum the
 // rows of a second small matrix (column sums) the same way.  V elements a
 // thread, the partials' loads eight at a time.
@@ -747,14 +861,27 @@ __global__ __launch_bounds__(256) void reduce_kernel(int32_t splits, int64_t cou
 }
 
 template <int TYPE, int EPI>
-void launch(bool big, const Args &a, unsigned grid, hipStream_t s) {
+void launch(TileShape t, const Args &a, unsigned grid, hipStream_t s) {
+    if constexpr (TYPE == TILE_FP8 || TYPE == TILE_FP8_EXACT) {
+        if (t.n == 16) {
+            const dim3 g((unsigned)((a.p.N + 15) / 16)), b(64 * kThinWaves);
+            if (a.p.M <= 16) hipLaunchKernelGGL((thin_kernel<TYPE, EPI, 1>), g, b, 0, s, a.p);
+            else if (a.p.M <= 32) hipLaunchKernelGGL((thin_kernel<TYPE, EPI, 2>), g, b, 0, s, a.p);
+            else hipLaunchKernelGGL((thin_kernel<TYPE, EPI, 4>), g, b, 0, s, a.p);
+            return;
+        }
+        if (t.m == 64) {
+            hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 64, 64, 4, 1, 2>), dim3(grid), dim3(256), 0, s, a);
+            return;
+        }
+    }
     if constexpr (TYPE != TILE_FP8_EXACT) {
-        if (big) {
+        if (t.m == kBigT) {
             hipLaunchKernelGGL((big_kernel<TYPE, EPI>), dim3(grid), dim3(kBigThreads), 0, s, a);
             return;
         }
     }
-    hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 128, 128, 2, 2>), dim3(grid), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 128, 128, 2, 2, 2>), dim3(grid), dim3(256), 0, s, a);
 }
 
 int64_t tiles_of(int64_t M, int64_t N, int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); }
@@ -765,7 +892,20 @@ TileShape tile_shape(TileType type, const TileProduct &p) {
     const int32_t splits = std::max(1, p.splits), per = (p.kt + splits - 1) / splits;
     const bool big = type != TILE_FP8_EXACT && tiles_of(p.M, p.N, kBigT) * splits >= 160 && per >= 4 &&
                      (type != TILE_FP8 || per <= kBigPieces) && std::max(p.lda, p.ldb) < (1 << 24);
-    return big ? TileShape{kBigT, kBigT} : TileShape{128, 128};
+    if (big) return TileShape{kBigT, kBigT};
+    if (type == TILE_FP8 || type == TILE_FP8_EXACT) {
+        // Few rows (us, few rows / 64 x 64, 4096 x 4096): 1 row 5.0 / 14.7, 16 7.4 /
+        // 14.8, 32 10.3 / 14.8, 64 15.8 / 14.9, 128 27 / 15; float32 results 1 5.1 /
+        // 20.9, 64 16.1 / 21.4, 128 28 / 22; 64 rows, 1024 x 512 4.3 / 5.0.
+        if (p.M <= kThin) return TileShape{kThin, 16};
+        // 64 x 64 tiles where 128 x 128 ones leave CUs without a block (us, 128 /
+        // 64, 8-bit): 500 x 4096 x 4096 33 / 20, 2000 x 512 x 1024 11.2 / 6.8,
+        // 8000 x 512 x 640 10.3 / 9.4, but 8000 x 1024 x 512 (504 blocks) 12.1 /
+        // 13.8; float32 results 50 / 35, 16.4 / 9.0, 14.3 / 14.9 (6205 x 512 x
+        // 640), 8000 x 2048 x 2048 88 / 118.
+        if (tiles_of(p.M, p.N, 128) < 256) return TileShape{64, 64};
+    }
+    return TileShape{128, 128};
 }
 
 int32_t tile_splits(int32_t M, int32_t N, int32_t kt) {
@@ -780,7 +920,6 @@ int32_t tile_splits(int32_t M, int32_t N, int32_t kt) {
 int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStream_t s) {
     if (p.M <= 0 || p.N <= 0) return GCN_OK;
     const TileShape t = tile_shape(type, p);
-    const bool big = t.m == kBigT;
     Args a;
     a.p = p;
     a.tiles_m = (p.M + t.m - 1) / t.m;
@@ -797,15 +936,13 @@ int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStrea
     a.per_xcd = (a.total + 7) / 8;
     const unsigned grid = 8 * a.per_xcd;
     // (the pairs that the entry points use)
-    if (type == TILE_BF16_NN && epi == TILE_STATS) launch<TILE_BF16_NN, TILE_STATS>(big, a, grid, s);
-    else if (type == TILE_BF16_NN && epi == TILE_GRAD) launch<TILE_BF16_NN, TILE_GRAD>(big, a, grid, s);
-    else if (type == TILE_BF16 && epi == TILE_PARTIAL) launch<TILE_BF16, TILE_PARTIAL>(big, a, grid, s);
-    else if (type == TILE_BF16_TN && epi == TILE_STORE) launch<TILE_BF16_TN, TILE_STORE>(big, a, grid, s);
-    else if (type == TILE_BF16_TN && epi == TILE_PARTIAL) launch<TILE_BF16_TN, TILE_PARTIAL>(big, a, grid, s);
-    else if (type == TILE_FP8 && epi == TILE_STORE) launch<TILE_FP8, TILE_STORE>(big, a, grid, s);
-    else if (type == TILE_FP8 && epi == TILE_PARTIAL) launch<TILE_FP8, TILE_PARTIAL>(big, a, grid, s);
-    else if (type == TILE_FP8_EXACT && epi == TILE_STORE_F32) launch<TILE_FP8_EXACT, TILE_STORE_F32>(big, a, grid, s);
-    else if (type == TILE_FP8_EXACT && epi == TILE_PARTIAL) launch<TILE_FP8_EXACT, TILE_PARTIAL>(big, a, grid, s);
+    if (type == TILE_BF16_NN && epi == TILE_STATS) launch<TILE_BF16_NN, TILE_STATS>(t, a, grid, s);
+    else if (type == TILE_BF16_NN && epi == TILE_GRAD) launch<TILE_BF16_NN, TILE_GRAD>(t, a, grid, s);
+    else if (type == TILE_BF16 && epi == TILE_PARTIAL) launch<TILE_BF16, TILE_PARTIAL>(t, a, grid, s);
+    else if (type == TILE_BF16_TN && epi == TILE_STORE) launch<TILE_BF16_TN, TILE_STORE>(t, a, grid, s);
+    else if (type == TILE_BF16_TN && epi == TILE_PARTIAL) launch<TILE_BF16_TN, TILE_PARTIAL>(t, a, grid, s);
+    else if (type == TILE_FP8 && epi == TILE_STORE) launch<TILE_FP8, TILE_STORE>(t, a, grid, s);
+    else if (type == TILE_FP8_EXACT && epi == TILE_STORE_F32) launch<TILE_FP8_EXACT, TILE_STORE_F32>(t, a, grid, s);
     else {
         set_error("tile_product: type %d with epilogue %d", (int)type, (int)epi);
         return GCN_EUNSUPPORTED;

@@ -143,7 +143,8 @@ def product_bound(x, w, y, dtype, bias):
 @pytest.mark.parametrize("n, K, N, transpose, pad", [
     (1, 1, 1, False, 0), (1, 512, 300, False, 0), (2, 129, 5, True, 1), (16, 128, 128, False, 0),
     (33, 602, 128, False, 4), (130, 50, 257, True, 0), (300, 256, 64, False, 0), (129, 1030, 131, False, 3),
-    (257, 384, 260, True, 0)])
+    (257, 384, 260, True, 0), (40, 700, 515, False, 1), (64, 130, 77, True, 0), (70, 8320, 66, False, 0),
+    (7, 8320, 20, False, 0)])
 def test_product(n, K, N, transpose, pad, dtype):
     t = DT[dtype]
     g = gen(n + 7 * K + 11 * N)
