@@ -79,8 +79,8 @@ __global__ __launch_bounds__(kTB) void join_kernel(int32_t n, int32_t tiles, con
     run_sum[i] = s;
 }
 
-// logits of one piece (float32 rows) joined into the running maximum and sum,
-// a workgroup a row
+// logits of one piece (float32 rows of ldx, a multiple of 4) joined into the
+// running maximum and sum, a workgroup a row
 __global__ __launch_bounds__(kTB) void stats_rows_kernel(int32_t P, const float *X, int64_t ldx, const int32_t *labels,
                                                          int32_t class0, int32_t C, float *run_max, float *run_sum,
                                                          float *label_logit, int first) {
@@ -88,20 +88,26 @@ __global__ __launch_bounds__(kTB) void stats_rows_kernel(int32_t P, const float 
     const int32_t row = blockIdx.x;
     const float *x = X + row * ldx;
     float m = -INFINITY, s = 0.0f;
-    for (int32_t c = threadIdx.x; c < P; c += kTB) {
-        const float v = x[c], b = fmaxf(m, v);
-        if (!(v <= m)) {   // a new maximum (or NaN, which the sum keeps)
-            s = (m == -INFINITY ? 0.0f : s * expf(m - b)) + expf(v - (b == -INFINITY ? 0.0f : b));
-            m = b;
-        } else {
-            s += m == -INFINITY ? 0.0f : expf(v - m);
-        }
-    }
     auto join = [](float &m, float &s, float q, float u) {
         const float b = fmaxf(m, q);
         s = (m == b ? s : s * expf(m - b)) + (q == b ? u : u * expf(q - b));
         m = b;
     };
+    for (int32_t c = 4 * (int32_t)threadIdx.x; c < P; c += 4 * kTB) {
+        const float4 v = *(const float4 *)(x + c);
+        float y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 1; e < 4; ++e)
+            if (c + e >= P) y[e] = -INFINITY;
+        const float b = fmaxf(m, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
+        if (b > m) {
+            s *= expf(m - b);   // (0 of the empty sum: exp(-infinity))
+            m = b;
+        }
+        const float base = m == -INFINITY ? 0.0f : m;   // no finite logit yet: the sum stays 0
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += expf(y[e] - base);
+    }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
         const float q = __shfl_xor(m, d), u = __shfl_xor(s, d);
@@ -118,16 +124,35 @@ __global__ __launch_bounds__(kTB) void stats_rows_kernel(int32_t P, const float 
     if (has_label(l, C) && l >= class0 && l - class0 < P) label_logit[row] = x[l - class0];
 }
 
-__global__ __launch_bounds__(kTB) void grad_rows_kernel(int32_t P, float *X, int64_t ldx, const int32_t *labels,
-                                                        int32_t class0, int32_t C, const float *lse,
-                                                        const float *inv_count) {
-    const int32_t row = blockIdx.x;
-    float *x = X + row * ldx;
-    const int32_t l = labels[row];
-    const bool has = has_label(l, C);
-    const float z = lse[row], inv = inv_count[0];
-    for (int32_t c = threadIdx.x; c < P; c += kTB)
-        x[c] = has ? (expf(x[c] - z) - (class0 + c == l ? 1.0f : 0.0f)) * inv : 0.0f;
+// X <- G, and the column sums of strips of kStrip rows: a thread has a column
+constexpr int kStrip = 32;
+__global__ __launch_bounds__(kTB) void grad_rows_kernel(int32_t n, int32_t P, float *X, int64_t ldx,
+                                                        const int32_t *labels, int32_t class0, int32_t C,
+                                                        const float *lse, const float *inv_count, float *part) {
+    __shared__ float z[kStrip];
+    __shared__ int32_t lab[kStrip];
+    const int32_t c = blockIdx.x * kTB + threadIdx.x, strips = (n + kStrip - 1) / kStrip;
+    const float inv = inv_count[0];
+    for (int32_t strip = blockIdx.y; strip < strips; strip += gridDim.y) {
+        const int32_t r0 = strip * kStrip, rows = min(kStrip, n - r0);
+        __syncthreads();
+        if ((int32_t)threadIdx.x < rows) {
+            const int32_t l = labels[r0 + threadIdx.x];
+            z[threadIdx.x] = lse[r0 + threadIdx.x];
+            lab[threadIdx.x] = has_label(l, C) ? l : -1;
+        }
+        __syncthreads();
+        if (c >= P) continue;
+        float sum = 0.0f;
+        float *x = X + r0 * ldx + c;
+#pragma unroll 8
+        for (int32_t r = 0; r < rows; ++r, x += ldx) {
+            const float g = lab[r] >= 0 ? (expf(*x - z[r]) - (class0 + c == lab[r] ? 1.0f : 0.0f)) * inv : 0.0f;
+            *x = g;
+            sum += g;
+        }
+        part[(int64_t)strip * P + c] = sum;
+    }
 }
 
 // lse, the rows' losses and their mean, by one workgroup in a fixed order
@@ -175,7 +200,7 @@ int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 struct Plan {
     int64_t fp, np;            // f and n in whole 64-column pieces (bfloat16)
     int32_t piece, pieces;     // classes per piece
-    int32_t split_h, split_w;  // parts of the two gradient products
+    int32_t split_h, split_w;  // parts of the two gradient products (bfloat16)
     bool in_place;             // W_pred's own rows serve as operands
     size_t total;
 };
@@ -183,8 +208,8 @@ struct Buffers {
     float *inv_count, *run_max, *run_sum, *label_logit, *lse, *tile_max, *tile_sum, *colpart, *acc, *part, *X, *tmp;
     uint16_t *H, *W, *G;
     float *Hz;
-    void *gemm_ws, *col_ws;
-    size_t gemm_bytes, col_bytes;
+    void *gemm_ws;
+    size_t gemm_bytes;
 };
 
 GemmProblem dw_f32(int32_t f, int32_t P, int32_t n) {
@@ -193,6 +218,14 @@ GemmProblem dw_f32(int32_t f, int32_t P, int32_t n) {
     w.N = P;
     w.seg[0].K = n;
     return w;
+}
+
+GemmProblem dh_f32(int32_t n, int32_t f, int32_t P) {
+    GemmProblem d{};
+    d.M = n;
+    d.N = f;
+    d.seg[0].K = P;
+    return d;
 }
 
 // The elements of a piece: bfloat16 G takes 2 bytes each, float32 logits 4.
@@ -238,15 +271,17 @@ Plan plan_of(int32_t n, int32_t f, int32_t C, bool bf, bool grad, const void *W,
         }
     } else {
         b.Hz = ar.take<float>(rows * f);
-        b.X = ar.take<float>(rows * p.piece);
+        b.X = ar.take<float>(rows * up(p.piece, 4));
         if (grad) {
-            const GemmProblem w = dw_f32(f, p.piece, n);
-            p.split_w = gemm_pick_split(1, &w, true);
-            b.gemm_bytes = gemm_workspace_bytes(1, &w, p.split_w);
+            // (a last, smaller piece may be split more than the others)
+            const int32_t last = C - (p.pieces - 1) * p.piece;
+            for (int32_t P : {p.piece, last}) {
+                const GemmProblem w = dw_f32(f, P, n), h = dh_f32(n, f, P);
+                b.gemm_bytes = std::max(b.gemm_bytes, gemm_workspace_bytes(1, &w, gemm_pick_split(1, &w, true)));
+                b.gemm_bytes = std::max(b.gemm_bytes, gemm_workspace_bytes(1, &h, gemm_pick_split(1, &h, false)));
+            }
             b.gemm_ws = b.gemm_bytes ? ar.take<char>(b.gemm_bytes) : nullptr;
-            b.col_bytes = std::max(colsum_workspace_bytes(n, p.piece),
-                                   colsum_workspace_bytes(n, C - (p.pieces - 1) * p.piece));
-            b.col_ws = ar.take<char>(b.col_bytes);
+            b.colpart = ar.take<float>((rows + kStrip - 1) / kStrip * p.piece);
             if (p.pieces > 1) b.tmp = ar.take<float>(rows * f);
         }
     }
@@ -385,7 +420,7 @@ int loss_f32(const Plan &p, const Buffers &b, const float *HL, int32_t n, int32_
         g.M = n;
         g.N = P;
         g.C = b.X;
-        g.ldc = P;
+        g.ldc = up(P, 4);
         g.bias = bias ? bias + c0 : nullptr;
         g.seg[0] = GemmSeg{b.Hz, f, W + c0, C, f};
         return gemm(L_NN, 1, &g, 0, 1, nullptr, 0, s);
@@ -394,7 +429,7 @@ int loss_f32(const Plan &p, const Buffers &b, const float *HL, int32_t n, int32_
         const int32_t c0 = i * p.piece, P = std::min(p.piece, C - c0);
         if ((rc = logits(c0, P))) return rc;
         ProfScope prof(K_CLASS_STATS, s, 0.0, 4.0 * n * P);
-        hipLaunchKernelGGL(stats_rows_kernel, dim3((unsigned)n), dim3(kTB), 0, s, P, b.X, (int64_t)P, labels, c0, C,
+        hipLaunchKernelGGL(stats_rows_kernel, dim3((unsigned)n), dim3(kTB), 0, s, P, b.X, up(P, 4), labels, c0, C,
                            b.run_max, b.run_sum, b.label_logit, i == 0);
         GCN_LAUNCH_CHECK("stats_rows_kernel");
     }
@@ -404,28 +439,27 @@ int loss_f32(const Plan &p, const Buffers &b, const float *HL, int32_t n, int32_
     if (!dHL) return GCN_OK;
     for (int32_t i = 0; i < p.pieces; ++i) {
         const int32_t c0 = i * p.piece, P = std::min(p.piece, C - c0);
+        const int64_t ldx = up(P, 4);
         // (a single piece's logits are still in place)
         if (p.pieces > 1 && (rc = logits(c0, P))) return rc;
         {
             ProfScope prof(K_CLASS_GRAD, s, 0.0, 8.0 * n * P);
-            hipLaunchKernelGGL(grad_rows_kernel, dim3((unsigned)n), dim3(kTB), 0, s, P, b.X, (int64_t)P, labels, c0, C,
-                               b.lse, b.inv_count);
+            const dim3 g((unsigned)((P + kTB - 1) / kTB), (unsigned)std::min(65535, (n + kStrip - 1) / kStrip));
+            hipLaunchKernelGGL(grad_rows_kernel, g, dim3(kTB), 0, s, n, P, b.X, ldx, labels, c0, C, b.lse, b.inv_count,
+                               b.colpart);
             GCN_LAUNCH_CHECK("grad_rows_kernel");
         }
-        if ((rc = colsum(n, P, b.X, P, db + c0, b.col_ws, b.col_bytes, s))) return rc;
+        if ((rc = colsum_reduce_rows((n + kStrip - 1) / kStrip, P, b.colpart, db + c0, s))) return rc;
         GemmProblem w = dw_f32(f, P, n);
         w.C = dW + c0;
         w.ldc = C;
-        w.seg[0] = GemmSeg{b.Hz, f, b.X, P, n};
-        const int split = std::min(p.split_w, gemm_pick_split(1, &w, true));
-        if ((rc = gemm(L_TN, 1, &w, 0, split, b.gemm_ws, b.gemm_bytes, s))) return rc;
-        GemmProblem d{};
-        d.M = n;
-        d.N = f;
+        w.seg[0] = GemmSeg{b.Hz, f, b.X, ldx, n};
+        if ((rc = gemm(L_TN, 1, &w, 0, gemm_pick_split(1, &w, true), b.gemm_ws, b.gemm_bytes, s))) return rc;
+        GemmProblem d = dh_f32(n, f, P);
         d.C = i ? b.tmp : dHL;
         d.ldc = i ? f : lddhl;
-        d.seg[0] = GemmSeg{b.X, P, W + c0, C, P};
-        if ((rc = gemm(L_NT, 1, &d, 0, 1, nullptr, 0, s))) return rc;
+        d.seg[0] = GemmSeg{b.X, ldx, W + c0, C, P};
+        if ((rc = gemm(L_NT, 1, &d, 0, gemm_pick_split(1, &d, false), b.gemm_ws, b.gemm_bytes, s))) return rc;
         if (i) {
             hipLaunchKernelGGL(add_kernel, dim3(grid_of((int64_t)n * f)), dim3(kTB), 0, s, n, f, b.tmp, dHL, lddhl);
             GCN_LAUNCH_CHECK("add_kernel");
