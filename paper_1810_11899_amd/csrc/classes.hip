@@ -17,38 +17,83 @@ namespace gcn {
 namespace {
 
 constexpr int kTB = 256;
-constexpr int kSmallTile = 128;   // rows and columns of the smallest tiles
+constexpr int kSmallRows = 32, kSmallTile = 128;   // rows and columns of the smallest tiles
 
 __device__ __forceinline__ bool has_label(int32_t l, int32_t C) { return l >= 0 && l < C; }
 
-// inv_count = 1 / max(1, rows with a label), by one workgroup
-__global__ __launch_bounds__(1024) void count_kernel(int32_t n, int32_t C, const int32_t *labels, float *inv_count) {
-    __shared__ int32_t part[16];
-    int32_t k = 0;
-    for (int32_t i = threadIdx.x; i < n; i += 1024) k += has_label(labels[i], C);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) k += __shfl_xor(k, d);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = k;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        int32_t t = 0;
-        for (int w = 0; w < 16; ++w) t += part[w];
-        inv_count[0] = (float)(1.0 / (double)max(t, 1));
-    }
+// (m, s): a maximum and the sum of exponentials relative to it, joined with (q, u)
+__device__ __forceinline__ void join(float &m, float &s, float q, float u) {
+    const float b = fmaxf(m, q);
+    s = (m == b ? s : s * __expf(m - b)) + (q == b ? u : u * __expf(q - b));
+    m = b;
 }
 
 // dst [drows x ldd] = src [rows x cols] (lds), zero past rows and cols and in
 // rows without a label
 template <class T>
-__global__ __launch_bounds__(kTB) void copy_rows_kernel(int32_t drows, int32_t rows, int32_t cols, const T *src,
-                                                        int64_t lds, T *dst, int64_t ldd, const int32_t *labels,
-                                                        int32_t C) {
-    const int64_t total = (int64_t)drows * ldd;
-    for (int64_t i = (int64_t)blockIdx.x * kTB + threadIdx.x; i < total; i += (int64_t)gridDim.x * kTB) {
-        const int64_t r = i / ldd;
-        const int32_t c = (int32_t)(i - r * ldd);
-        dst[i] = r < rows && c < cols && (!labels || has_label(labels[r], C)) ? src[r * lds + c] : (T)0;
+struct CopyRows {
+    int32_t drows, rows, cols;
+    const T *src;
+    int64_t lds;
+    T *dst;
+    int64_t ldd;
+    const int32_t *labels;   // null: every row counts
+    int32_t C;
+};
+template <class T>
+__device__ __forceinline__ void copy_rows(const CopyRows<T> &a, int64_t first, int64_t step) {
+    constexpr int V = 16 / sizeof(T);   // elements of a vector; ldd is a multiple of it where rows are padded
+    if (a.ldd % V == 0 && (uintptr_t)a.dst % 16 == 0 && a.lds % V == 0 && (uintptr_t)a.src % 16 == 0) {
+        const int64_t per = a.ldd / V, total = a.drows * per;
+        for (int64_t i = first; i < total; i += step) {
+            const int64_t r = i / per;
+            const int32_t c = (int32_t)(i - r * per) * V;
+            const bool in = r < a.rows && (!a.labels || has_label(a.labels[r], a.C));
+            T v[V];
+            if (in && c + V <= a.cols) {
+                *(uint4 *)v = *(const uint4 *)(a.src + r * a.lds + c);
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = in && c + e < a.cols ? a.src[r * a.lds + c + e] : (T)0;
+            }
+            *(uint4 *)(a.dst + r * a.ldd + c) = *(uint4 *)v;
+        }
+        return;
     }
+    const int64_t total = a.drows * a.ldd;
+    for (int64_t i = first; i < total; i += step) {
+        const int64_t r = i / a.ldd;
+        const int32_t c = (int32_t)(i - r * a.ldd);
+        a.dst[i] = r < a.rows && c < a.cols && (!a.labels || has_label(a.labels[r], a.C)) ? a.src[r * a.lds + c] : (T)0;
+    }
+}
+// Block 0: inv_count = 1 / max(1, rows with a label); the next `split` blocks the
+// first copy, the others the second (which may be empty).
+template <class T>
+__global__ __launch_bounds__(kTB) void prep_kernel(int32_t n, float *inv_count, CopyRows<T> a, uint32_t split, CopyRows<T> b) {
+    if (blockIdx.x == 0) {
+        __shared__ int32_t part[kTB / 64];
+        int32_t k = 0;
+#pragma unroll 8
+        for (int32_t i = threadIdx.x; i < n; i += kTB) k += has_label(a.labels[i], a.C);
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) k += __shfl_xor(k, d);
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = k;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            int32_t t = 0;
+            for (int w = 0; w < kTB / 64; ++w) t += part[w];
+            inv_count[0] = (float)(1.0 / (double)max(t, 1));
+        }
+        return;
+    }
+    const uint32_t k = blockIdx.x - 1;
+    if (k < split) copy_rows(a, (int64_t)k * kTB + threadIdx.x, (int64_t)split * kTB);
+    else copy_rows(b, (int64_t)(k - split) * kTB + threadIdx.x, (int64_t)(gridDim.x - 1 - split) * kTB);
+}
+template <class T>
+__global__ __launch_bounds__(kTB) void copy_rows_kernel(CopyRows<T> a) {
+    copy_rows(a, (int64_t)blockIdx.x * kTB + threadIdx.x, (int64_t)gridDim.x * kTB);
 }
 
 // the tiles' maxima and sums of one piece joined into the running ones: 32 rows
@@ -59,22 +104,17 @@ __global__ __launch_bounds__(kTB) void join_kernel(int32_t n, int32_t tiles, con
     const int lr = threadIdx.x & 31, part = threadIdx.x >> 5;
     const int32_t i = blockIdx.x * 32 + lr;
     float m = -INFINITY, s = 0.0f;
-    auto join = [&](float q, float u) {
-        const float b = fmaxf(m, q);
-        s = (m == b ? s : s * __expf(m - b)) + (q == b ? u : u * __expf(q - b));
-        m = b;
-    };
     if (i < n) {
 #pragma unroll 4
-        for (int32_t t = part; t < tiles; t += 8) join(tile_max[(int64_t)t * n + i], tile_sum[(int64_t)t * n + i]);
+        for (int32_t t = part; t < tiles; t += 8) join(m, s, tile_max[(int64_t)t * n + i], tile_sum[(int64_t)t * n + i]);
     }
     sm[part][lr] = m;
     ss[part][lr] = s;
     __syncthreads();
     if (part != 0 || i >= n) return;
 #pragma unroll
-    for (int k = 1; k < 8; ++k) join(sm[k][lr], ss[k][lr]);
-    if (!first) join(run_max[i], run_sum[i]);
+    for (int k = 1; k < 8; ++k) join(m, s, sm[k][lr], ss[k][lr]);
+    if (!first) join(m, s, run_max[i], run_sum[i]);
     run_max[i] = m;
     run_sum[i] = s;
 }
@@ -88,11 +128,6 @@ __global__ __launch_bounds__(kTB) void stats_rows_kernel(int32_t P, const float 
     const int32_t row = blockIdx.x;
     const float *x = X + row * ldx;
     float m = -INFINITY, s = 0.0f;
-    auto join = [](float &m, float &s, float q, float u) {
-        const float b = fmaxf(m, q);
-        s = (m == b ? s : s * expf(m - b)) + (q == b ? u : u * expf(q - b));
-        m = b;
-    };
     for (int32_t c = 4 * (int32_t)threadIdx.x; c < P; c += 4 * kTB) {
         const float4 v = *(const float4 *)(x + c);
         float y[4] = {v.x, v.y, v.z, v.w};
@@ -155,14 +190,23 @@ __global__ __launch_bounds__(kTB) void grad_rows_kernel(int32_t n, int32_t P, fl
     }
 }
 
-// lse, the rows' losses and their mean, by one workgroup in a fixed order
-__global__ __launch_bounds__(1024) void loss_kernel(int32_t n, int32_t C, const int32_t *labels, const float *run_max,
+// lse, the rows' losses and their mean, by one workgroup in a fixed order.
+// tiles > 0: the only piece's tiles are joined here (few rows and tiles).
+__global__ __launch_bounds__(1024) void loss_kernel(int32_t n, int32_t C, const int32_t *labels, int32_t tiles,
+                                                    const float *tile_max, const float *tile_sum, const float *run_max,
                                                     const float *run_sum, const float *label_logit, float *lse,
                                                     float *row_loss, const float *inv_count, float *loss) {
     __shared__ double part[16];
     double t = 0.0;
     for (int32_t i = threadIdx.x; i < n; i += 1024) {
-        const float z = run_max[i] + logf(run_sum[i]);
+        float m, s;
+        if (tiles > 0) {
+            m = -INFINITY, s = 0.0f;
+            for (int32_t k = 0; k < tiles; ++k) join(m, s, tile_max[(int64_t)k * n + i], tile_sum[(int64_t)k * n + i]);
+        } else {
+            m = run_max[i], s = run_sum[i];
+        }
+        const float z = m + logf(s);
         lse[i] = z;
         const bool has = has_label(labels[i], C);
         const float v = has ? z - label_logit[i] : 0.0f;
@@ -263,7 +307,7 @@ Plan plan_of(int32_t n, int32_t f, int32_t C, bool bf, bool grad, const void *W,
         if (grad) {
             const int64_t pp = up(p.piece, 64);
             b.G = ar.take<uint16_t>(p.np * pp);
-            b.colpart = ar.take<float>((rows + kSmallTile - 1) / kSmallTile * p.piece);
+            b.colpart = ar.take<float>((p.np + kSmallRows - 1) / kSmallRows * p.piece);
             p.split_h = tile_splits(n, f, (int32_t)(pp / 64));
             p.split_w = tile_splits(f, p.piece, (int32_t)(p.np / 64));
             b.acc = ar.take<float>((size_t)p.split_h * rows * f);
@@ -293,12 +337,17 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
               const float *bias, int32_t C, const int32_t *labels, float *loss, float *row_loss, uint16_t *dHL,
               int64_t lddhl, uint16_t *dW, float *db, hipStream_t s) {
     int rc;
+    // (a single copied piece of W_pred goes along)
+    auto w_copy = [&](int32_t c0, int32_t P) {
+        return CopyRows<uint16_t>{(int32_t)p.fp, f, P, W + c0, C, b.W, up(P, 64), nullptr, 0};
+    };
+    const bool copied = p.pieces == 1 && !(p.in_place && C % 64 == 0);
     {
         ProfScope prof(K_CLASS_PREP, s, 0.0, 4.0 * n * f);
-        hipLaunchKernelGGL(count_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, b.inv_count);
-        hipLaunchKernelGGL(copy_rows_kernel<uint16_t>, dim3(grid_of(p.np * p.fp)), dim3(kTB), 0, s, (int32_t)p.np, n, f,
-                           HL, ldhl, b.H, p.fp, labels, C);
-        GCN_LAUNCH_CHECK("class_prep");
+        const CopyRows<uint16_t> h{(int32_t)p.np, n, f, HL, ldhl, b.H, p.fp, labels, C};
+        const unsigned gh = grid_of(p.np * p.fp / 8, 4096), gw = copied ? grid_of(p.fp * up(C, 64) / 8, 4096) : 0;
+        hipLaunchKernelGGL(prep_kernel<uint16_t>, dim3(1 + gh + gw), dim3(kTB), 0, s, n, b.inv_count, h, gh, w_copy(0, C));
+        GCN_LAUNCH_CHECK("prep_kernel");
     }
     // the piece's columns of W_pred, rows of ldw elements: in place, or copied to
     // whole 64 x 64 pieces
@@ -312,9 +361,9 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         }
         ldw = up(P, 64);
         Wp = b.W;
+        if (copied) return GCN_OK;
         ProfScope prof(K_CLASS_PREP, s, 0.0, 4.0 * f * P);
-        hipLaunchKernelGGL(copy_rows_kernel<uint16_t>, dim3(grid_of(p.fp * ldw)), dim3(kTB), 0, s, (int32_t)p.fp, f, P,
-                           W + c0, (int64_t)C, b.W, ldw, (const int32_t *)nullptr, 0);
+        hipLaunchKernelGGL(copy_rows_kernel<uint16_t>, dim3(grid_of(p.fp * ldw / 8)), dim3(kTB), 0, s, w_copy(c0, P));
         GCN_LAUNCH_CHECK("copy_rows_kernel");
         return GCN_OK;
     };
@@ -334,6 +383,7 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         t.classes = C;
         return t;
     };
+    int32_t tiles = 0;   // left to the loss's workgroup
     for (int32_t i = 0; i < p.pieces; ++i) {
         const int32_t c0 = i * p.piece, P = std::min(p.piece, C - c0);
         if ((rc = weights(c0, P))) return rc;
@@ -346,12 +396,17 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
             if ((rc = tile_product(TILE_BF16_NN, TILE_STATS, t, s))) return rc;
         }
         const TileShape sh = tile_shape(TILE_BF16_NN, t);
-        ProfScope prof(K_CLASS_PREP, s, 0.0, 8.0 * n * ((P + sh.n - 1) / sh.n));
-        hipLaunchKernelGGL(join_kernel, dim3((unsigned)((n + 31) / 32)), dim3(kTB), 0, s, n, (P + sh.n - 1) / sh.n,
+        tiles = (P + sh.n - 1) / sh.n;
+        // (up to 16 tiles of 1024 rows the loss's workgroup joins in no more time)
+        if (p.pieces == 1 && n <= 1024 && tiles <= 16) break;
+        ProfScope prof(K_CLASS_PREP, s, 0.0, 8.0 * n * tiles);
+        hipLaunchKernelGGL(join_kernel, dim3((unsigned)((n + 31) / 32)), dim3(kTB), 0, s, n, tiles,
                            b.tile_max, b.tile_sum, b.run_max, b.run_sum, i == 0);
+        tiles = 0;
         GCN_LAUNCH_CHECK("join_kernel");
     }
-    hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, b.run_max, b.run_sum, b.label_logit, b.lse,
+    hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, tiles, b.tile_max, b.tile_sum, b.run_max,
+                       b.run_sum, b.label_logit, b.lse,
                        row_loss, b.inv_count, loss);
     GCN_LAUNCH_CHECK("loss_kernel");
     if (!dHL) return GCN_OK;
@@ -365,13 +420,13 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         t.G = b.G;
         t.ldg = pp;
         t.g_rows = p.np;
-        t.colpart = b.colpart;
+        const int32_t row_tiles = tile_rows(tile_shape(TILE_BF16_NN, t), TILE_GRAD, t);
+        t.colpart = row_tiles == 1 ? db + c0 : b.colpart;   // (one row of tiles: the sums themselves)
         {
             ProfScope prof(K_CLASS_GRAD, s, 2.0 * n * f * P, 2.0 * ((double)n + P) * f + 4.0 * n * P);
             if ((rc = tile_product(TILE_BF16_NN, TILE_GRAD, t, s))) return rc;
         }
-        const TileShape sh = tile_shape(TILE_BF16_NN, t);
-        if ((rc = colsum_reduce_rows((n + sh.m - 1) / sh.m, P, b.colpart, db + c0, s))) return rc;
+        if (row_tiles > 1 && (rc = colsum_reduce_rows(row_tiles, P, b.colpart, db + c0, s))) return rc;
         ProfScope prof(K_CLASS_PRODUCT, s, 4.0 * n * f * P, 4.0 * n * P);
         TileProduct h{};
         h.A = (const uint8_t *)b.G;
@@ -411,9 +466,9 @@ int loss_f32(const Plan &p, const Buffers &b, const float *HL, int32_t n, int32_
              const float *bias, int32_t C, const int32_t *labels, float *loss, float *row_loss, float *dHL, int64_t lddhl,
              float *dW, float *db, hipStream_t s) {
     int rc;
-    hipLaunchKernelGGL(count_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, b.inv_count);
-    hipLaunchKernelGGL(copy_rows_kernel<float>, dim3(grid_of((int64_t)n * f)), dim3(kTB), 0, s, n, n, f, HL, ldhl, b.Hz,
-                       (int64_t)f, labels, C);
+    const CopyRows<float> h{n, n, f, HL, ldhl, b.Hz, f, labels, C};
+    const unsigned gh = grid_of((int64_t)n * f / 4, 4096);
+    hipLaunchKernelGGL(prep_kernel<float>, dim3(1 + gh), dim3(kTB), 0, s, n, b.inv_count, h, gh, h);
     GCN_LAUNCH_CHECK("class_prep");
     auto logits = [&](int32_t c0, int32_t P) {
         GemmProblem g{};
@@ -433,7 +488,8 @@ int loss_f32(const Plan &p, const Buffers &b, const float *HL, int32_t n, int32_
                            b.run_max, b.run_sum, b.label_logit, i == 0);
         GCN_LAUNCH_CHECK("stats_rows_kernel");
     }
-    hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, b.run_max, b.run_sum, b.label_logit, b.lse,
+    hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, 0, b.tile_max, b.tile_sum, b.run_max,
+                       b.run_sum, b.label_logit, b.lse,
                        row_loss, b.inv_count, loss);
     GCN_LAUNCH_CHECK("loss_kernel");
     if (!dHL) return GCN_OK;

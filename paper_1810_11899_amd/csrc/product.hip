@@ -875,6 +875,12 @@ void launch(TileShape t, const Args &a, unsigned grid, hipStream_t s) {
             return;
         }
     }
+    if constexpr (TYPE == TILE_BF16_NN) {
+        if (t.m == 32) {
+            hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 32, 128, 2, 2, 2>), dim3(grid), dim3(256), 0, s, a);
+            return;
+        }
+    }
     if constexpr (TYPE != TILE_FP8_EXACT) {
         if (t.m == kBigT) {
             hipLaunchKernelGGL((big_kernel<TYPE, EPI>), dim3(grid), dim3(kBigThreads), 0, s, a);
@@ -905,6 +911,7 @@ TileShape tile_shape(TileType type, const TileProduct &p) {
         // 640), 8000 x 2048 x 2048 88 / 118.
         if (tiles_of(p.M, p.N, 128) < 256) return TileShape{64, 64};
     }
+    if (type == TILE_BF16_NN && tiles_of(p.M, p.N, 128) < 256) return TileShape{32, 128};
     return TileShape{128, 128};
 }
 
@@ -917,12 +924,16 @@ int32_t tile_splits(int32_t M, int32_t N, int32_t kt) {
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>(sp, 64));
 }
 
+int32_t tile_rows(TileShape t, TileEpilogue epi, const TileProduct &p) {
+    return (int32_t)(((epi == TILE_GRAD ? std::max<int64_t>(p.M, p.g_rows) : p.M) + t.m - 1) / t.m);
+}
+
 int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStream_t s) {
     if (p.M <= 0 || p.N <= 0) return GCN_OK;
     const TileShape t = tile_shape(type, p);
     Args a;
     a.p = p;
-    a.tiles_m = (p.M + t.m - 1) / t.m;
+    a.tiles_m = tile_rows(t, epi, p);
     a.tiles_n = (p.N + t.n - 1) / t.n;
     const int32_t splits = std::max(1, p.splits);
     a.kt_per_split = (p.kt + splits - 1) / splits;

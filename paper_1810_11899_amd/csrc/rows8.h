@@ -65,6 +65,8 @@ struct TileShape {
     int32_t m, n;
 };
 TileShape tile_shape(TileType type, const TileProduct &p);
+// rows of tiles (with TILE_GRAD they cover the rows of zeros behind the last one)
+int32_t tile_rows(TileShape t, TileEpilogue epi, const TileProduct &p);
 int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStream_t s);
 // out (float32, or bfloat16 rows of ldo) = the sum of `splits` partials M x N, in
 // order; out2 [N2] = the column sums of acc2 [rows2 x N2] in the same launch
