@@ -420,7 +420,7 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         t.G = b.G;
         t.ldg = pp;
         t.g_rows = p.np;
-        const int32_t row_tiles = tile_rows(tile_shape(TILE_BF16_NN, t), TILE_GRAD, t);
+        const int32_t row_tiles = tile_rows(tile_shape(TILE_BF16_NN, t), TILE_STATS, t);   // (those with real rows)
         t.colpart = row_tiles == 1 ? db + c0 : b.colpart;   // (one row of tiles: the sums themselves)
         {
             ProfScope prof(K_CLASS_GRAD, s, 2.0 * n * f * P, 2.0 * ((double)n + P) * f + 4.0 * n * P);

@@ -236,6 +236,9 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
                 for (int i = 0; i < FM; ++i) acc[i][j][e] += b;
             }
         constexpr float kLog2e = 1.44269504088896340736f;
+        int labs[FM];   // (all loads before the first use: behind a store each would wait for the one before)
+#pragma unroll
+        for (int i = 0; i < FM; ++i) labs[i] = label_of(p, r0 + 16 * i);
         const int w0 = c.tn * BN + wn * (BN / WN);   // the wavefront's first column
         if constexpr (EPI == TILE_STATS) {
             // a row's columns lie in 4 lanes of WN wavefronts: maximum and sum
@@ -261,7 +264,7 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
                 s += __shfl_xor(s, 16);
                 s += __shfl_xor(s, 32);
                 if (lane < 16) part[wn * BM + row - c.tm * BM] = make_float2(m, s);
-                const int lab = label_of(p, row);
+                const int lab = labs[i];
                 if (__any(lab >= w0 && lab < w0 + BN / WN)) {   // (few wavefronts see one of their labels)
 #pragma unroll
                     for (int j = 0; j < FN; ++j)
@@ -293,11 +296,13 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
 #pragma unroll
                 for (int e = 0; e < 4; ++e) cs[j][e] = 0.0f;
             const float inv = p.inv_count[0], log_inv = __builtin_amdgcn_logf(inv);   // (base 2)
+            float lses[FM];
+#pragma unroll
+            for (int i = 0; i < FM; ++i) lses[i] = r0 + 16 * i < p.M ? p.lse[r0 + 16 * i] : 0.0f;
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
-                const int row = r0 + 16 * i;
-                const float lse = row < p.M ? p.lse[row] : 0.0f;
-                const int lab = label_of(p, row);
+                const float lse = lses[i];
+                const int lab = labs[i];
                 // a row without a label has no gradient: 2^-infinity
                 const float shift = lab != kNoLabel ? log_inv : -INFINITY;
 #pragma unroll
@@ -335,7 +340,7 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
             __syncthreads();
             for (int k = threadIdx.x; k < BN; k += 64 * WM * WN) {
                 const int col = c.tn * BN + k;
-                if (col >= p.N) continue;
+                if (col >= p.N || c.tm * BM >= p.M) continue;   // (a tile of the rows behind the last has no sums)
                 float v = 0.0f;
 #pragma unroll
                 for (int w = 0; w < WM; ++w) v += part[w * BN + k];
