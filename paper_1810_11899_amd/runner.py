@@ -230,6 +230,121 @@ class StepRunner:
                          self.spec.classes if self.head is not None else 0)
 
 
+class StepRunner8:
+    """The fwd+bwd step of an L-layer GCN with a softmax cross entropy head that
+    keeps its activations as 8-bit rows and no logits (gcn_rows8.h,
+    gcn_classes.h).
+
+    Per layer the 8-bit rows of its input H and of A H are all that stays for
+    the backward pass, a quarter of their float32 size; the layer's float32
+    output lives in one of two buffers that the layers share.  With X8, G8 the
+    8-bit rows and Ws8, Wn8 the 8-bit weights:
+
+        Y  = max([X8 Ws8 || G8 Wn8] + b, 0),  G8 = rows8(A H)
+        dW_self = X8^T dZs,  dW_neigh = G8^T dZn,  dZ = dY [Y8 > 0]
+        dH = Z8 [Ws8 || Wn8]^T,  Z8 = rows8([dZs || A^T dZn])
+
+    the last line by linearity, so that the input gradient is one product.  The
+    head reads the last layer's output and W_pred as bfloat16."""
+
+    def __init__(self, wl, device: str = "cuda"):
+        if wl.spec.head != "ce":
+            raise ValueError("the 8-bit step has a softmax cross entropy head")
+        d = self.dev = torch.device(device)
+        self.n, self.L = wl.n, len(wl.layers)
+        self.dims = [(l.f_in, l.h) for l in wl.layers]
+        self.ws = B.Workspace(d)
+        n, g = self.n, wl.graph
+        f = lambda a: torch.as_tensor(a, dtype=torch.float32).to(d)
+        empty = lambda *s, dtype=torch.float32: torch.empty(s, dtype=dtype, device=d)
+        self.A = B.DeviceCSR.from_host(n, n, g.indptr, g.indices, g.vals, device=d)
+        self.symmetric = B.gcn_csr_pattern_symmetric_host(g.indptr, g.indices)
+        if self.symmetric:
+            self.AT = B.DeviceCSR(n, n, self.A.indptr, self.A.indices, empty(max(g.nnz, 1))[:g.nnz])
+        else:
+            self.AT = B.DeviceCSR(n, n, empty(n + 1, dtype=torch.int32), empty(max(g.nnz, 1), dtype=torch.int32)[:g.nnz],
+                                  empty(max(g.nnz, 1))[:g.nnz])
+        self.H0 = f(wl.H)
+        self.labels = torch.as_tensor(wl.labels, dtype=torch.int32).to(d)
+        self.W = [(f(l.W_self), f(l.W_neigh), f(l.bias)) for l in wl.layers]
+        # [W_self || W_neigh] side by side for the input gradient (its columns
+        # are the masters of the two)
+        self.Wb = [torch.cat(w[:2], dim=1) for w in self.W]
+        self.W8 = [(B.Weights8(fi, h, d), B.Weights8(fi, h, d), B.Weights8(fi, 2 * h, d) if li else None)
+                   for li, (fi, h) in enumerate(self.dims)]
+        self.X8 = [B.Rows8(n, fi, d) for fi, _ in self.dims]
+        self.G8 = [B.Rows8(n, fi, d) for fi, _ in self.dims]
+        hl = 2 * self.dims[-1][1]
+        self.Y8 = B.Rows8(n, hl, d)           # the last layer's output, for its ReLU derivative
+        self.Z8 = [None] + [B.Rows8(n, 2 * h, d) for _, h in self.dims[1:]]
+        self.dZs8 = [B.Rows8(n, h, d) for _, h in self.dims]
+        self.dZn8 = [B.Rows8(n, h, d) for _, h in self.dims]
+        width = max(max(fi, 2 * h) for fi, h in self.dims)
+        self._rows = [empty(n, width), empty(n, width)]
+        self._agg = empty(n, width)
+        self.HL, self.dHL = empty(n, hl, dtype=torch.bfloat16), empty(n, hl, dtype=torch.bfloat16)
+        self.W_pred, self.b_pred = f(wl.W_pred).to(torch.bfloat16), f(wl.b_pred)
+        self.loss, self.row_loss = empty(1), empty(n)
+        self.dW_pred, self.db_pred = torch.empty_like(self.W_pred), torch.empty_like(self.b_pred)
+        self.dWs = [empty(fi, h) for fi, h in self.dims]
+        self.dWn = [empty(fi, h) for fi, h in self.dims]
+        self.db = [empty(2 * h) for _, h in self.dims]
+        self.dH = [None] + [empty(n, fi) for fi, _ in self.dims[1:]]
+
+    def kept_bytes(self) -> int:
+        """Bytes that stay from the forward to the backward pass."""
+        return sum(t.values.shape[0] * t.struct.ldq + t.scale.numel() for t in self.X8 + self.G8 + [self.Y8])
+
+    def forward(self, stream=None):
+        H = self.H0
+        for li, (fi, h) in enumerate(self.dims):
+            Ws, Wn, b = self.W[li]
+            Ws8, Wn8, Wb8 = self.W8[li]
+            B.gcn_weights8_pack(Ws, Ws8, stream)
+            B.gcn_weights8_pack(Wn, Wn8, stream)
+            if Wb8 is not None:
+                B.gcn_weights8_pack(self.Wb[li], Wb8, stream)
+            B.gcn_rows8_pack(H, self.X8[li], stream)
+            agg = B.gcn_aggregate(self.A, H, self._agg[:, :fi], self.ws, B.GCN_BF16, stream)
+            B.gcn_rows8_pack(agg, self.G8[li], stream)
+            Y = self.HL if li == self.L - 1 else self._rows[li % 2][:, :2 * h]
+            B.gcn_rows8_product(self.X8[li], Ws8, Y[:, :h], self.ws, bias=b[:h], relu=True, stream=stream)
+            B.gcn_rows8_product(self.G8[li], Wn8, Y[:, h:], self.ws, bias=b[h:], relu=True, stream=stream)
+            H = Y
+        B.gcn_rows8_pack(self.HL, self.Y8, stream)
+
+    def head(self, stream=None):
+        B.gcn_class_loss(self.HL, self.W_pred, self.b_pred, self.labels, self.loss, self.ws, row_loss=self.row_loss,
+                         dHL=self.dHL, dW_pred=self.dW_pred, db_pred=self.db_pred, stream=stream)
+
+    def backward(self, stream=None):
+        if self.symmetric:
+            B.gcn_csr_transpose_symmetric(self.A, self.ws, self.AT.vals, stream)
+        else:
+            B.gcn_csr_transpose_into(self.A, self.AT.indptr, self.AT.indices, self.AT.vals, self.ws, stream)
+        dY = self.dHL
+        for li in range(self.L - 1, -1, -1):
+            h = self.dims[li][1]
+            mask = (self.Y8 if li == self.L - 1 else self.X8[li + 1]).values
+            for k, X8, dW, dZ8 in ((0, self.X8, self.dWs, self.dZs8), (1, self.G8, self.dWn, self.dZn8)):
+                c = slice(k * h, (k + 1) * h)
+                B.gcn_rows8_weight_grad(X8[li], dY[:, c], dW[li], self.ws, db=self.db[li][c], mask=mask[:, c],
+                                        dZ8=dZ8[li] if li else None, stream=stream)
+            if li == 0:
+                break
+            Z = self._rows[0][:, :2 * h]
+            B.gcn_rows8_unpack(self.dZs8[li], Z[:, :h], stream)
+            dZn = B.gcn_rows8_unpack(self.dZn8[li], self._agg[:, :h], stream)
+            B.gcn_aggregate(self.AT, dZn, Z[:, h:], self.ws, B.GCN_BF16, stream)
+            B.gcn_rows8_pack(Z, self.Z8[li], stream)
+            dY = B.gcn_rows8_product(self.Z8[li], self.W8[li][2], self.dH[li], self.ws, transpose=True, stream=stream)
+
+    def step(self, stream=None):
+        self.forward(stream)
+        self.head(stream)
+        self.backward(stream)
+
+
 def tune_orders(wl, prec: int = B.GCN_F32, device: str = "cuda", first_layer_dH: Optional[bool] = None,
                 index_bits: int = 32, warmup: int = 2, reps: int = 5, float_outputs: bool = True):
     """Measure the whole model step for every combination of the layers'
