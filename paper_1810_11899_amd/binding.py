@@ -180,8 +180,8 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _stream(stream=None):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    # (the current stream's handle without its Python object: a call's largest cost on the host)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
 
 
 def _ld(t: torch.Tensor) -> int:
@@ -558,6 +558,26 @@ def _rows_type(t: torch.Tensor, name: str) -> int:
     return GCN_ROWS_F32 if t.dtype == torch.float32 else GCN_ROWS_BF16
 
 
+def _launch(where: str, device: int, stream, *args):
+    """The library call `where` on `stream`, or on the current one of `device`, the operands'."""
+    fn = getattr(lib(), where)
+    if device == torch.cuda.current_device():
+        _check(fn(*args, _stream(stream)), where)
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream(stream)), where)
+
+
+def _one_device(first: torch.Tensor, *others) -> int:
+    d = first.get_device()
+    if d < 0:
+        raise TypeError("CUDA/HIP tensors are needed")
+    for t in others:
+        if t is not None and t.get_device() != d:
+            raise ValueError("all tensors of a call must be on one device")
+    return d
+
+
 def _want(t: torch.Tensor, name: str, dtype, shape):
     if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape):
         raise TypeError(f"{name} must be a {dtype} CUDA/HIP tensor of shape {tuple(shape)}")
@@ -605,6 +625,7 @@ class Rows8:
             raise TypeError("scale must be a contiguous uint8 CUDA/HIP tensor, n x ceil(f / 128)")
         self.struct = gcn_rows8(self.n, self.f, _ld8(values, "values"), _blocks8(self.f), values.data_ptr(),
                                 scale.data_ptr())
+        self.ref = ctypes.byref(self.struct)
 
 
 class Weights8:
@@ -633,29 +654,28 @@ class Weights8:
             raise ValueError("scale must be contiguous")
         self.struct = gcn_weights8(self.K, self.N, _ld8(values, "values"), _ld8(values_t, "values_t"),
                                    _blocks8(self.N), values.data_ptr(), values_t.data_ptr(), scale.data_ptr())
+        self.ref = ctypes.byref(self.struct)
 
 
 def gcn_rows8_pack(X: torch.Tensor, out: Rows8, stream=None) -> Rows8:
     if tuple(X.shape) != (out.n, out.f):
         raise ValueError("X and the 8-bit rows differ in shape")
-    _check(lib().gcn_rows8_pack(_ptr(X), _rows_type(X, "X"), _ld(X), ctypes.byref(out.struct), _stream(stream)),
-           "gcn_rows8_pack")
+    _launch("gcn_rows8_pack", _one_device(X, out.values), stream, X.data_ptr(), _rows_type(X, "X"), _ld(X), out.ref)
     return out
 
 
 def gcn_rows8_unpack(rows: Rows8, out: torch.Tensor, stream=None) -> torch.Tensor:
     if tuple(out.shape) != (rows.n, rows.f):
         raise ValueError("out and the 8-bit rows differ in shape")
-    _check(lib().gcn_rows8_unpack(ctypes.byref(rows.struct), _ptr(out), _rows_type(out, "out"), _ld(out),
-                                  _stream(stream)), "gcn_rows8_unpack")
+    _launch("gcn_rows8_unpack", _one_device(out, rows.values), stream, rows.ref, out.data_ptr(), _rows_type(out, "out"),
+            _ld(out))
     return out
 
 
 def gcn_weights8_pack(W: torch.Tensor, out: Weights8, stream=None) -> Weights8:
     if tuple(W.shape) != (out.K, out.N):
         raise ValueError("W and the 8-bit weights differ in shape")
-    _check(lib().gcn_weights8_pack(_ptr(W), _rows_type(W, "W"), _ld(W), ctypes.byref(out.struct), _stream(stream)),
-           "gcn_weights8_pack")
+    _launch("gcn_weights8_pack", _one_device(W, out.scale), stream, W.data_ptr(), _rows_type(W, "W"), _ld(W), out.ref)
     return out
 
 
@@ -671,9 +691,8 @@ def gcn_rows8_product(X8: Rows8, W8: Weights8, Y: torch.Tensor, ws: Workspace, b
         if bias.numel() != cols or not bias.is_contiguous():
             raise ValueError("bias needs one contiguous element per column of Y")
     w, wb = ws.args(L.gcn_rows8_product_workspace_bytes(X8.n, W8.K, W8.N))
-    _check(L.gcn_rows8_product(ctypes.byref(X8.struct), ctypes.byref(W8.struct), int(bool(transpose)), _ptr(bias),
-                               int(bool(relu)), _ptr(Y), _rows_type(Y, "Y"), _ld(Y), w, wb, _stream(stream)),
-           "gcn_rows8_product")
+    _launch("gcn_rows8_product", _one_device(Y, X8.values, W8.scale, bias, ws.buf), stream, X8.ref, W8.ref,
+            int(bool(transpose)), _ptr(bias), int(bool(relu)), Y.data_ptr(), _rows_type(Y, "Y"), _ld(Y), w, wb)
     return Y
 
 
@@ -698,9 +717,10 @@ def gcn_rows8_weight_grad(X8: Rows8, dY: torch.Tensor, dW: torch.Tensor, ws: Wor
             raise ValueError("mask and dY differ in shape")
         ldm = max(_ld8(mask, "mask"), N)
     w, wb = ws.args(L.gcn_rows8_weight_grad_workspace_bytes(X8.n, X8.f, N))
-    _check(L.gcn_rows8_weight_grad(ctypes.byref(X8.struct), _ptr(mask), ldm, _ptr(dY), _rows_type(dY, "dY"), _ld(dY), N,
-                                   _ptr(dW), _ld(dW), _ptr(db), None if dZ8 is None else ctypes.byref(dZ8.struct), w,
-                                   wb, _stream(stream)), "gcn_rows8_weight_grad")
+    _launch("gcn_rows8_weight_grad",
+            _one_device(dW, X8.values, dY, db, mask, None if dZ8 is None else dZ8.values, ws.buf), stream, X8.ref,
+            _ptr(mask), ldm, dY.data_ptr(), _rows_type(dY, "dY"), _ld(dY), N, dW.data_ptr(), _ld(dW), _ptr(db),
+            None if dZ8 is None else dZ8.ref, w, wb)
 
 
 # ------------------------------------------------------------- many classes
@@ -726,9 +746,9 @@ def gcn_class_loss(HL: torch.Tensor, W_pred: torch.Tensor, b_pred: Optional[torc
         if x is not None and not x.is_contiguous():
             raise ValueError(f"{nm} must be contiguous")
     w, wb = ws.args(L.gcn_class_loss_workspace_bytes(n, f, C, t, int(dW_pred is not None)))
-    _check(L.gcn_class_loss(_ptr(HL), n, f, _ld(HL), _ptr(W_pred), _ptr(b_pred), C, _ptr(labels), t, _ptr(loss),
-                            _ptr(row_loss), _ptr(dHL), 0 if dHL is None else _ld(dHL), _ptr(dW_pred), _ptr(db_pred), w,
-                            wb, _stream(stream)), "gcn_class_loss")
+    _launch("gcn_class_loss", _one_device(HL, W_pred, b_pred, labels, loss, row_loss, dHL, dW_pred, db_pred, ws.buf), stream,
+            HL.data_ptr(), n, f, _ld(HL), W_pred.data_ptr(), _ptr(b_pred), C, _ptr(labels), t, loss.data_ptr(),
+            _ptr(row_loss), _ptr(dHL), 0 if dHL is None else _ld(dHL), _ptr(dW_pred), _ptr(db_pred), w, wb)
 
 
 # ---------------------------------------------------------------- optimiser
