@@ -38,7 +38,8 @@ extern "C" {
  * not written) and db_pred are float32.  dHL, dW_pred and db_pred all NULL: the
  * loss alone, for evaluation.  GCN_ROWS_F32: float32 products.
  * GCN_ROWS_BF16: bfloat16 products with float32 sums; logits, softmax and
- * db_pred stay float32, G is rounded to bfloat16 as an operand.
+ * db_pred stay float32, n_l G is rounded to bfloat16 as an operand (1 / n_l is
+ * applied to the float32 sums).
  * A class whose b_pred is minus infinity has probability 0.  Logits that are NaN
  * or plus infinity, or a row whose logits are all minus infinity, give NaN. */
 size_t gcn_class_loss_workspace_bytes(int32_t n, int32_t f, int32_t C, gcn_rows_type type, int need_grad);

@@ -5,9 +5,11 @@
 //     and column tile their maximum and the sum of exponentials relative to
 //     it, joined into the row's running maximum and sum
 //   loss: row_loss = max + log(sum) - label's logit
-//   pass 2, per piece: the logits again, G = (softmax - onehot) / n_l in the
-//     same registers, written as bfloat16 rows; then dHL += G W_piece^T and
-//     dW_piece = HL^T G.
+//   pass 2, per piece: the logits again, n_l G = softmax - onehot in the same
+//     registers, written as bfloat16 rows; then n_l dHL += n_l G W_piece^T and
+//     n_l dW_piece = HL^T n_l G.  1 / n_l is a factor of the float32 sums: in G it
+//     would be rounded, and the same way in every row (17 rows: the gradients
+//     0.0036 off in the 2-norm instead of 0.0018).
 #include <algorithm>
 
 #include "gcn_classes.h"
@@ -181,11 +183,19 @@ __global__ __launch_bounds__(kTB) void grad_rows_kernel(int32_t n, int32_t P, fl
         if (c >= P) continue;
         float sum = 0.0f;
         float *x = X + r0 * ldx + c;
-#pragma unroll 8
-        for (int32_t r = 0; r < rows; ++r, x += ldx) {
-            const float g = lab[r] >= 0 ? (expf(*x - z[r]) - (class0 + c == lab[r] ? 1.0f : 0.0f)) * inv : 0.0f;
-            *x = g;
-            sum += g;
+        // (eight loads before the first store, behind which the next one would wait)
+        for (int32_t r = 0; r < rows; r += 8, x += 8 * ldx) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = r + e < rows ? x[e * ldx] : 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (r + e >= rows) break;
+                const int32_t l = lab[r + e];
+                const float g = l >= 0 ? (expf(v[e] - z[r + e]) - (class0 + c == l ? 1.0f : 0.0f)) * inv : 0.0f;
+                x[e * ldx] = g;
+                sum += g;
+            }
         }
         part[(int64_t)strip * P + c] = sum;
     }
@@ -424,7 +434,7 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         if ((rc = weights(c0, P))) return rc;
         TileProduct t = logits(c0, P);
         t.lse = b.lse;
-        t.inv_count = b.inv_count;
+        t.scale = b.inv_count;
         t.G = b.G;
         t.ldg = pp;
         t.g_rows = p.np;
@@ -460,14 +470,15 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         if (p.split_w > 1) {
             w.acc = b.part;
             if ((rc = tile_product(TILE_BF16_TN, TILE_PARTIAL, w, s))) return rc;
-            if ((rc = tile_reduce(p.split_w, f, P, b.part, dW + c0, 1, C, s))) return rc;
+            if ((rc = tile_reduce(p.split_w, f, P, b.part, dW + c0, 1, C, s, 0, 0, nullptr, nullptr, b.inv_count))) return rc;
         } else {
             w.C = dW + c0;
             w.ldc = C;
+            w.scale = b.inv_count;
             if ((rc = tile_product(TILE_BF16_TN, TILE_STORE, w, s))) return rc;
         }
     }
-    return tile_reduce(p.split_h, n, f, b.acc, dHL, 1, lddhl, s);
+    return tile_reduce(p.split_h, n, f, b.acc, dHL, 1, lddhl, s, 0, 0, nullptr, nullptr, b.inv_count);
 }
 
 int loss_f32(const Plan &p, const Buffers &b, const float *HL, int32_t n, int32_t f, int64_t ldhl, const float *W,

@@ -165,6 +165,7 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
     static_assert(FN == 4, "a wavefront's block is 64 columns wide");
     if constexpr (EPI == TILE_STORE || EPI == TILE_STORE_F32) {
         f32x4 bias[FN];
+        const float scale = p.scale ? p.scale[0] : 1.0f;
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
@@ -174,7 +175,7 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
         for (int i = 0; i < FM; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                acc[i][j] += bias[j];
+                acc[i][j] = acc[i][j] * scale + bias[j];
                 if (p.relu)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[i][j][e] = acc[i][j][e] < 0.0f ? 0.0f : acc[i][j][e];   // (NaN stays)
@@ -295,7 +296,6 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
             for (int j = 0; j < FN; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) cs[j][e] = 0.0f;
-            const float inv = p.inv_count[0], log_inv = __builtin_amdgcn_logf(inv);   // (base 2)
             float lses[FM];
 #pragma unroll
             for (int i = 0; i < FM; ++i) lses[i] = r0 + 16 * i < p.M ? p.lse[r0 + 16 * i] : 0.0f;
@@ -304,7 +304,7 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
                 const float lse = lses[i];
                 const int lab = labs[i];
                 // a row without a label has no gradient: 2^-infinity
-                const float shift = lab != kNoLabel ? log_inv : -INFINITY;
+                const float shift = lab != kNoLabel ? 0.0f : -INFINITY;
 #pragma unroll
                 for (int j = 0; j < FN; ++j)
 #pragma unroll
@@ -315,7 +315,7 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
                     for (int j = 0; j < FN; ++j)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (c0 + 16 * j + e == lab) acc[i][j][e] -= inv;
+                            if (c0 + 16 * j + e == lab) acc[i][j][e] -= 1.0f;
                 }
 #pragma unroll
                 for (int j = 0; j < FN; ++j)
@@ -344,6 +344,7 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
                 float v = 0.0f;
 #pragma unroll
                 for (int w = 0; w < WM; ++w) v += part[w * BN + k];
+                v *= p.scale[0];
                 p.colpart[(int64_t)c.tm * p.N + col] = v;
             }
         }
@@ -832,7 +833,7 @@ __global__ __launch_bounds__(64 * kThinWaves) void thin_kernel(TileProduct p) {
 template <int V, bool BF>
 __global__ __launch_bounds__(256) void reduce_kernel(int32_t splits, int64_t count, int32_t N, const float *acc, void *out,
                                                      int64_t ldo, uint32_t main, int32_t rows2, int32_t N2,
-                                                     const float *acc2, float *out2) {
+                                                     const float *acc2, float *out2, const float *scale) {
     typedef float vec __attribute__((ext_vector_type(V)));
     if (blockIdx.x >= main) {
         const int32_t k = (int32_t)(blockIdx.x - main) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -855,6 +856,7 @@ __global__ __launch_bounds__(256) void reduce_kernel(int32_t splits, int64_t cou
             for (int u = 0; u < 8; ++u) v += x[u];
         }
         for (; s < splits; ++s) v += *(const vec *)(acc + (int64_t)s * count + i);
+        if (scale) v *= scale[0];
         const int64_t at = i / N * ldo + i % N;
         if constexpr (BF) {
 #pragma unroll
@@ -968,14 +970,14 @@ int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStrea
 }
 
 int tile_reduce(int32_t splits, int32_t M, int32_t N, const float *acc, void *out, int out_bf16, int64_t ldo, hipStream_t s,
-                int32_t rows2, int32_t N2, const float *acc2, float *out2) {
+                int32_t rows2, int32_t N2, const float *acc2, float *out2, const float *scale) {
     const int64_t count = (int64_t)M * N;
     if (count == 0) return GCN_OK;
     const bool vec = N % 4 == 0 && ldo % 4 == 0 && (uintptr_t)out % 16 == 0;
     const uint32_t main = (uint32_t)std::min<int64_t>((count / (vec ? 4 : 1) + 255) / 256, 8192);
     const dim3 g(main + (uint32_t)((N2 + 3) / 4));
 #define GCN_REDUCE(V, BF) \
-    hipLaunchKernelGGL((reduce_kernel<V, BF>), g, dim3(256), 0, s, splits, count, N, acc, out, ldo, main, rows2, N2, acc2, out2)
+    hipLaunchKernelGGL((reduce_kernel<V, BF>), g, dim3(256), 0, s, splits, count, N, acc, out, ldo, main, rows2, N2, acc2, out2, scale)
     if (vec) {
         if (out_bf16) GCN_REDUCE(4, true);
         else GCN_REDUCE(4, false);

@@ -45,6 +45,7 @@ struct TileProduct {
     int64_t ldc;             // elements
     int relu;
     const float *bias;       // [N] or null (also TILE_STATS and TILE_GRAD)
+    const float *scale;      // [1] or null: a factor of the sums (TILE_GRAD: of the column sums)
     // TILE_PARTIAL
     float *acc;
     int accumulate;
@@ -54,7 +55,7 @@ struct TileProduct {
     int32_t class0, classes;
     float *tile_max, *tile_sum;     // [tiles_n x M]
     float *label_logit;             // [M]
-    const float *lse, *inv_count;   // [M], [1]
+    const float *lse;               // [M]
     uint16_t *G;                    // [g_rows x ldg] bfloat16, zeros past M and N
     int64_t ldg, g_rows;
     float *colpart;                 // [tiles_m x N]
@@ -69,9 +70,10 @@ TileShape tile_shape(TileType type, const TileProduct &p);
 int32_t tile_rows(TileShape t, TileEpilogue epi, const TileProduct &p);
 int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStream_t s);
 // out (float32, or bfloat16 rows of ldo) = the sum of `splits` partials M x N, in
-// order; out2 [N2] = the column sums of acc2 [rows2 x N2] in the same launch
+// order, times *scale when given; out2 [N2] = the column sums of acc2 [rows2 x N2] in the same launch
 int tile_reduce(int32_t splits, int32_t M, int32_t N, const float *acc, void *out, int out_bf16, int64_t ldo,
-                hipStream_t s, int32_t rows2 = 0, int32_t N2 = 0, const float *acc2 = nullptr, float *out2 = nullptr);
+                hipStream_t s, int32_t rows2 = 0, int32_t N2 = 0, const float *acc2 = nullptr, float *out2 = nullptr,
+                const float *scale = nullptr);
 // how many parts to split `kt` pieces over, for a product with few tiles
 int32_t tile_splits(int32_t M, int32_t N, int32_t kt);
 
