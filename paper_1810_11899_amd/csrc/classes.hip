@@ -203,12 +203,16 @@ __global__ __launch_bounds__(kTB) void grad_rows_kernel(int32_t n, int32_t P, fl
 
 // lse, the rows' losses and their mean, by one workgroup in a fixed order.
 // tiles > 0: the only piece's tiles are joined here (few rows and tiles).
-__global__ __launch_bounds__(1024) void loss_kernel(int32_t n, int32_t C, const int32_t *labels, int32_t tiles,
-                                                    const float *tile_max, const float *tile_sum, const float *run_max,
-                                                    const float *run_sum, const float *label_logit, float *lse,
-                                                    float *row_loss, const float *inv_count, float *loss) {
+__global__ __launch_bounds__(1024) void loss_kernel(int32_t n, int32_t C, const int32_t *__restrict__ labels,
+                                                    int32_t tiles, const float *__restrict__ tile_max,
+                                                    const float *__restrict__ tile_sum, const float *__restrict__ run_max,
+                                                    const float *__restrict__ run_sum,
+                                                    const float *__restrict__ label_logit, float *__restrict__ lse,
+                                                    float *__restrict__ row_loss, const float *__restrict__ inv_count,
+                                                    float *__restrict__ loss) {
     __shared__ double part[16];
     double t = 0.0;
+#pragma unroll 4
     for (int32_t i = threadIdx.x; i < n; i += 1024) {
         float m, s;
         if (tiles > 0) {
@@ -551,7 +555,7 @@ using namespace gcn;
 extern "C" {
 
 size_t gcn_class_loss_workspace_bytes(int32_t n, int32_t f, int32_t C, gcn_rows_type type, int need_grad) {
-    if (n < 0 || f <= 0 || C <= 0) return 0;
+    if (n < 0 || f <= 0 || C <= 0 || std::max({n, f, C}) > kMostRows) return 0;
     Buffers b;
     return plan_of(n, f, C, type == GCN_ROWS_BF16, need_grad != 0, nullptr, nullptr, 0, b).total;
 }
@@ -562,6 +566,7 @@ int gcn_class_loss(const void *HL, int32_t n, int32_t f, int32_t ldhl, const voi
     GCN_REQUIRE(n >= 0 && f > 0 && C > 0, GCN_ESHAPE, "gcn_class_loss: n=%d f=%d C=%d", n, f, C);
     GCN_REQUIRE(type == GCN_ROWS_F32 || type == GCN_ROWS_BF16, GCN_EINVAL, "gcn_class_loss: bad element type %d",
                 (int)type);
+    GCN_REQUIRE(n <= kMostRows && f <= kMostRows && C <= kMostRows, GCN_EUNSUPPORTED, "gcn_class_loss: n=%d f=%d C=%d", n, f, C);
     const bool grad = dW_pred != nullptr, bf = type == GCN_ROWS_BF16;
     GCN_REQUIRE((db_pred != nullptr) == grad && (dHL != nullptr || (grad && n == 0) || !grad) && (grad || !dHL), GCN_EINVAL,
                 "gcn_class_loss: dHL, dW_pred and db_pred are given together or not at all");

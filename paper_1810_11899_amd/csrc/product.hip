@@ -827,13 +827,22 @@ __global__ __launch_bounds__(64 * kThinWaves) void thin_kernel(TileProduct p) {
     }
 }
 
+template <int V>
+__device__ __forceinline__ auto load_bias(const float *b) {
+    typedef float vec __attribute__((ext_vector_type(V)));
+    vec v;
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = b[e];
+    return v;
+}
 // out = the sum of the partials in split order; the blocks past `main` sum the
 // rows of a second small matrix (column sums) the same way.  V elements a
 // thread, the partials' loads eight at a time.
 template <int V, bool BF>
 __global__ __launch_bounds__(256) void reduce_kernel(int32_t splits, int64_t count, int32_t N, const float *acc, void *out,
                                                      int64_t ldo, uint32_t main, int32_t rows2, int32_t N2,
-                                                     const float *acc2, float *out2, const float *scale) {
+                                                     const float *acc2, float *out2, const float *scale,
+                                                     const float *bias, int relu) {
     typedef float vec __attribute__((ext_vector_type(V)));
     if (blockIdx.x >= main) {
         const int32_t k = (int32_t)(blockIdx.x - main) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -858,6 +867,10 @@ __global__ __launch_bounds__(256) void reduce_kernel(int32_t splits, int64_t cou
         for (; s < splits; ++s) v += *(const vec *)(acc + (int64_t)s * count + i);
         if (scale) v *= scale[0];
         const int64_t at = i / N * ldo + i % N;
+        if (bias) v += load_bias<V>(bias + i % N);
+        if (relu)
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = v[e] < 0.0f ? 0.0f : v[e];   // (NaN stays)
         if constexpr (BF) {
 #pragma unroll
             for (int e = 0; e < V; ++e) ((uint16_t *)out)[at + e] = to_bf16(v[e]);
@@ -870,7 +883,7 @@ __global__ __launch_bounds__(256) void reduce_kernel(int32_t splits, int64_t cou
 template <int TYPE, int EPI>
 void launch(TileShape t, const Args &a, unsigned grid, hipStream_t s) {
     if constexpr (TYPE == TILE_FP8 || TYPE == TILE_FP8_EXACT) {
-        if (t.n == 16) {
+        if constexpr (EPI != TILE_PARTIAL) if (t.n == 16) {
             const dim3 g((unsigned)((a.p.N + 15) / 16)), b(64 * kThinWaves);
             if (a.p.M <= 16) hipLaunchKernelGGL((thin_kernel<TYPE, EPI, 1>), g, b, 0, s, a.p);
             else if (a.p.M <= 32) hipLaunchKernelGGL((thin_kernel<TYPE, EPI, 2>), g, b, 0, s, a.p);
@@ -888,13 +901,14 @@ void launch(TileShape t, const Args &a, unsigned grid, hipStream_t s) {
             return;
         }
     }
-    if constexpr (TYPE != TILE_FP8_EXACT) {
+    if constexpr (TYPE != TILE_FP8_EXACT && !(TYPE == TILE_FP8 && EPI == TILE_PARTIAL)) {
         if (t.m == kBigT) {
             hipLaunchKernelGGL((big_kernel<TYPE, EPI>), dim3(grid), dim3(kBigThreads), 0, s, a);
             return;
         }
     }
-    hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 128, 128, 2, 2, 2>), dim3(grid), dim3(256), 0, s, a);
+    if constexpr (!((TYPE == TILE_FP8 || TYPE == TILE_FP8_EXACT) && EPI == TILE_PARTIAL))
+        hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 128, 128, 2, 2, 2>), dim3(grid), dim3(256), 0, s, a);
 }
 
 int64_t tiles_of(int64_t M, int64_t N, int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); }
@@ -903,6 +917,7 @@ int64_t tiles_of(int64_t M, int64_t N, int64_t t) { return ((M + t - 1) / t) * (
 
 TileShape tile_shape(TileType type, const TileProduct &p) {
     const int32_t splits = std::max(1, p.splits), per = (p.kt + splits - 1) / splits;
+    if (splits > 1 && (type == TILE_FP8 || type == TILE_FP8_EXACT)) return TileShape{64, 64};   // (split8)
     const bool big = type != TILE_FP8_EXACT && tiles_of(p.M, p.N, kBigT) * splits >= 160 && per >= 4 &&
                      (type != TILE_FP8 || per <= kBigPieces) && std::max(p.lda, p.ldb) < (1 << 24);
     if (big) return TileShape{kBigT, kBigT};
@@ -937,11 +952,15 @@ int32_t tile_rows(TileShape t, TileEpilogue epi, const TileProduct &p) {
 
 int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStream_t s) {
     if (p.M <= 0 || p.N <= 0) return GCN_OK;
+    if (std::max(p.M, p.N) > kMostRows) {   // (row numbers past the last tile's end stay within 32 bits)
+        set_error("tile_product: %d x %d is too large", p.M, p.N);
+        return GCN_EUNSUPPORTED;
+    }
     const TileShape t = tile_shape(type, p);
     Args a;
     a.p = p;
     a.tiles_m = tile_rows(t, epi, p);
-    a.tiles_n = (p.N + t.n - 1) / t.n;
+    a.tiles_n = (int32_t)(((int64_t)p.N + t.n - 1) / t.n);
     const int32_t splits = std::max(1, p.splits);
     a.kt_per_split = (p.kt + splits - 1) / splits;
     a.band = 8;
@@ -960,6 +979,8 @@ int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStrea
     else if (type == TILE_BF16_TN && epi == TILE_STORE) launch<TILE_BF16_TN, TILE_STORE>(t, a, grid, s);
     else if (type == TILE_BF16_TN && epi == TILE_PARTIAL) launch<TILE_BF16_TN, TILE_PARTIAL>(t, a, grid, s);
     else if (type == TILE_FP8 && epi == TILE_STORE) launch<TILE_FP8, TILE_STORE>(t, a, grid, s);
+    else if (type == TILE_FP8 && epi == TILE_PARTIAL) launch<TILE_FP8, TILE_PARTIAL>(t, a, grid, s);
+    else if (type == TILE_FP8_EXACT && epi == TILE_PARTIAL) launch<TILE_FP8_EXACT, TILE_PARTIAL>(t, a, grid, s);
     else if (type == TILE_FP8_EXACT && epi == TILE_STORE_F32) launch<TILE_FP8_EXACT, TILE_STORE_F32>(t, a, grid, s);
     else {
         set_error("tile_product: type %d with epilogue %d", (int)type, (int)epi);
@@ -970,14 +991,15 @@ int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStrea
 }
 
 int tile_reduce(int32_t splits, int32_t M, int32_t N, const float *acc, void *out, int out_bf16, int64_t ldo, hipStream_t s,
-                int32_t rows2, int32_t N2, const float *acc2, float *out2, const float *scale) {
+                int32_t rows2, int32_t N2, const float *acc2, float *out2, const float *scale,
+                const float *bias, int relu) {
     const int64_t count = (int64_t)M * N;
     if (count == 0) return GCN_OK;
     const bool vec = N % 4 == 0 && ldo % 4 == 0 && (uintptr_t)out % 16 == 0;
     const uint32_t main = (uint32_t)std::min<int64_t>((count / (vec ? 4 : 1) + 255) / 256, 8192);
     const dim3 g(main + (uint32_t)((N2 + 3) / 4));
 #define GCN_REDUCE(V, BF) \
-    hipLaunchKernelGGL((reduce_kernel<V, BF>), g, dim3(256), 0, s, splits, count, N, acc, out, ldo, main, rows2, N2, acc2, out2, scale)
+    hipLaunchKernelGGL((reduce_kernel<V, BF>), g, dim3(256), 0, s, splits, count, N, acc, out, ldo, main, rows2, N2, acc2, out2, scale, bias, relu)
     if (vec) {
         if (out_bf16) GCN_REDUCE(4, true);
         else GCN_REDUCE(4, false);
@@ -994,11 +1016,29 @@ int tile_reduce(int32_t splits, int32_t M, int32_t N, const float *acc, void *ou
 
 using namespace gcn;
 
+// Parts of a product's contraction: where 64 x 64 tiles leave half of the CUs
+// without a block and there are pieces enough to pay for a second launch (us,
+// unsplit / split: 500 x 4096 x 512 15.3 / 10.9, 500 x 2048 x 512 9.4 / 10.5, 1000 x
+// 1024 x 512 7.9 / 10.6; float32 results 500 x 4096 x 512 21.6 / 12.9, 300 x 2048 x
+// 256 12.5 / 10.2, 100 x 1024 x 256 8.4 / 10.4).
+static int32_t split8(int32_t M, int32_t N, int32_t kt, bool bf) {
+    const int64_t tiles = ((int64_t)M + 63) / 64 * (((int64_t)N + 63) / 64);
+    if (M <= 64 || tiles > 128 || kt < (bf ? 24 : 16)) return 1;
+    const int32_t sp = (int32_t)std::min<int64_t>(256 / tiles, kt / 4), per = (kt + sp - 1) / sp;
+    return (kt + per - 1) / per;
+}
+
 extern "C" {
 
 size_t gcn_rows8_product_workspace_bytes(int32_t n, int32_t K, int32_t N) {
-    (void)n, (void)K, (void)N;
-    return 256;
+    if (n < 0 || K <= 0 || N <= 0) return 0;
+    // (either direction; float32 results are split earlier)
+    size_t most = 0;
+    for (int t = 0; t < 2; ++t) {
+        const int32_t cols = t ? K : N, sp = split8(n, cols, (int32_t)blocks8(t ? N : K), false);
+        if (sp > 1) most = std::max(most, (size_t)sp * n * cols);
+    }
+    return 256 + sizeof(float) * most;
 }
 
 int gcn_rows8_product(const gcn_rows8 *X8, const gcn_weights8 *W8, int transpose, const float *bias, int relu, void *Y,
@@ -1022,8 +1062,12 @@ int gcn_rows8_product(const gcn_rows8 *X8, const gcn_weights8 *W8, int transpose
                 (long long)blocks8(W8->N));
     GCN_REQUIRE(ldy >= N, GCN_ESHAPE, "gcn_rows8_product: ldy=%d < %d", ldy, N);
     GCN_REQUIRE(X8->n == 0 || Y, GCN_EINVAL, "gcn_rows8_product: null Y");
-    GCN_REQUIRE(ws && ws_bytes >= gcn_rows8_product_workspace_bytes(X8->n, W8->K, W8->N), GCN_EWORKSPACE,
-                "gcn_rows8_product: workspace %zu bytes too small", ws_bytes);
+    GCN_REQUIRE(X8->n == 0 || (uintptr_t)Y % (type == GCN_ROWS_BF16 ? 2 : 4) == 0, GCN_EINVAL,
+                "gcn_rows8_product: misaligned Y");
+    GCN_REQUIRE(ws && (uintptr_t)ws % 256 == 0 &&
+                    ws_bytes >= gcn_rows8_product_workspace_bytes(X8->n, W8->K, W8->N), GCN_EWORKSPACE,
+                "gcn_rows8_product: workspace %zu < %zu bytes, or not 256-byte aligned", ws_bytes,
+                gcn_rows8_product_workspace_bytes(X8->n, W8->K, W8->N));
     if (X8->n == 0) return GCN_OK;
     TileProduct p{};
     p.A = X8->q;
@@ -1047,6 +1091,12 @@ int gcn_rows8_product(const gcn_rows8 *X8, const gcn_weights8 *W8, int transpose
     hipStream_t s = (hipStream_t)stream;
     ProfScope prof(K_ROWS8_PRODUCT, s, 2.0 * p.M * N * K,
                    (double)p.M * K + (double)N * K + (double)p.M * N * (bf ? 2.0 : 4.0));
+    p.splits = split8(p.M, p.N, p.kt, bf);
+    if (p.splits > 1) {
+        p.acc = (float *)ws;
+        if ((rc = tile_product(bf ? TILE_FP8 : TILE_FP8_EXACT, TILE_PARTIAL, p, s))) return rc;
+        return tile_reduce(p.splits, p.M, p.N, p.acc, Y, bf, ldy, s, 0, 0, nullptr, nullptr, nullptr, bias, relu);
+    }
     return bf ? tile_product(TILE_FP8, TILE_STORE, p, s) : tile_product(TILE_FP8_EXACT, TILE_STORE_F32, p, s);
 }
 

@@ -7,6 +7,7 @@
 
 namespace gcn {
 
+constexpr int32_t kMostRows = 0x7FFFFE00;   // of an operand
 constexpr int kRows8Block = 128;   // columns (and, for weights, rows) under one scale
 inline int64_t blocks8(int64_t f) { return (f + kRows8Block - 1) / kRows8Block; }
 
@@ -70,10 +71,10 @@ TileShape tile_shape(TileType type, const TileProduct &p);
 int32_t tile_rows(TileShape t, TileEpilogue epi, const TileProduct &p);
 int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStream_t s);
 // out (float32, or bfloat16 rows of ldo) = the sum of `splits` partials M x N, in
-// order, times *scale when given; out2 [N2] = the column sums of acc2 [rows2 x N2] in the same launch
+// order, times *scale, plus bias [N], through the ReLU, where given; out2 [N2] = the column sums of acc2 [rows2 x N2] in the same launch
 int tile_reduce(int32_t splits, int32_t M, int32_t N, const float *acc, void *out, int out_bf16, int64_t ldo,
                 hipStream_t s, int32_t rows2 = 0, int32_t N2 = 0, const float *acc2 = nullptr, float *out2 = nullptr,
-                const float *scale = nullptr);
+                const float *scale = nullptr, const float *bias = nullptr, int relu = 0);
 // how many parts to split `kt` pieces over, for a product with few tiles
 int32_t tile_splits(int32_t M, int32_t N, int32_t kt);
 

@@ -304,6 +304,7 @@ int check_type(gcn_rows_type t, const char *who) {
 }
 
 bool aligned(const void *p, uintptr_t b) { return (uintptr_t)p % b == 0; }
+uintptr_t el(gcn_rows_type t) { return t == GCN_ROWS_BF16 ? 2 : 4; }
 
 unsigned grid_of(int64_t work, int64_t per_block, int64_t most) {
     return (unsigned)std::max<int64_t>(1, std::min(most, (work + per_block - 1) / per_block));
@@ -356,7 +357,7 @@ int gcn_rows8_pack(const void *X, gcn_rows_type type, int32_t ldx, const gcn_row
     if (rc) return rc;
     if ((rc = check_type(type, "gcn_rows8_pack"))) return rc;
     GCN_REQUIRE(ldx >= out->f, GCN_ESHAPE, "gcn_rows8_pack: ldx=%d < f=%d", ldx, out->f);
-    GCN_REQUIRE(out->n == 0 || X, GCN_EINVAL, "gcn_rows8_pack: null pointer");
+    GCN_REQUIRE(out->n == 0 || (X && aligned(X, el(type))), GCN_EINVAL, "gcn_rows8_pack: null or misaligned pointer");
     return rows8_pack(out->n, out->f, X, type == GCN_ROWS_BF16, ldx, out->q, out->ldq, out->scale, out->ldscale,
                       (hipStream_t)stream);
 }
@@ -366,7 +367,7 @@ int gcn_rows8_unpack(const gcn_rows8 *r, void *X, gcn_rows_type type, int32_t ld
     if (rc) return rc;
     if ((rc = check_type(type, "gcn_rows8_unpack"))) return rc;
     GCN_REQUIRE(ldx >= r->f, GCN_ESHAPE, "gcn_rows8_unpack: ldx=%d < f=%d", ldx, r->f);
-    GCN_REQUIRE(r->n == 0 || X, GCN_EINVAL, "gcn_rows8_unpack: null pointer");
+    GCN_REQUIRE(r->n == 0 || (X && aligned(X, el(type))), GCN_EINVAL, "gcn_rows8_unpack: null or misaligned pointer");
     if (r->n == 0) return GCN_OK;
     hipStream_t s = (hipStream_t)stream;
     const bool bf = type == GCN_ROWS_BF16;
@@ -394,6 +395,7 @@ int gcn_weights8_pack(const void *W, gcn_rows_type type, int32_t ldw, const gcn_
     GCN_REQUIRE(K > 0 && N > 0, GCN_ESHAPE, "gcn_weights8_pack: K=%d N=%d", K, N);
     int rc = check_type(type, "gcn_weights8_pack");
     if (rc) return rc;
+    GCN_REQUIRE(aligned(W, el(type)), GCN_EINVAL, "gcn_weights8_pack: misaligned pointer");
     GCN_REQUIRE(ldw >= N, GCN_ESHAPE, "gcn_weights8_pack: ldw=%d < N=%d", ldw, N);
     GCN_REQUIRE((out->q || out->qT) && out->scale, GCN_EINVAL, "gcn_weights8_pack: null 8-bit weights");
     GCN_REQUIRE(!out->q || (out->ldq % 16 == 0 && out->ldq >= kBlk * blocks8(N) && aligned(out->q, 16)), GCN_ESHAPE,
@@ -431,7 +433,7 @@ struct GradBuffers {
 };
 GradPlan plan_grad(int32_t n, int32_t f, int32_t N, void *ws, size_t ws_bytes, GradBuffers &b) {
     GradPlan p{};
-    p.nz = (int32_t)std::min<int64_t>(((int64_t)n + 63) / 64 * 64, 0x7FFFFFC0);
+    p.nz = (n + 63) / 64 * 64;
     p.Np = (N + 7) / 8 * 8;
     p.fp = (f + 7) / 8 * 8;
     p.splits = tile_splits(f, N, p.nz / 64);
@@ -450,7 +452,7 @@ GradPlan plan_grad(int32_t n, int32_t f, int32_t N, void *ws, size_t ws_bytes, G
 }  // namespace
 
 size_t gcn_rows8_weight_grad_workspace_bytes(int32_t n, int32_t f, int32_t N) {
-    if (n < 0 || f <= 0 || N <= 0) return 0;
+    if (n < 0 || f <= 0 || N <= 0 || n > kMostRows) return 0;
     GradBuffers b;
     return plan_grad(n, f, N, nullptr, 0, b).total;
 }
@@ -465,7 +467,10 @@ int gcn_rows8_weight_grad(const gcn_rows8 *X8, const uint8_t *mask, int32_t ldma
     GCN_REQUIRE(N > 0, GCN_ESHAPE, "gcn_rows8_weight_grad: N=%d", N);
     GCN_REQUIRE(lddy >= N && lddw >= N && (!mask || ldmask >= N), GCN_ESHAPE,
                 "gcn_rows8_weight_grad: lddy=%d lddw=%d ldmask=%d < N=%d", lddy, lddw, ldmask, N);
-    GCN_REQUIRE(dW && (n == 0 || dY), GCN_EINVAL, "gcn_rows8_weight_grad: null pointer");
+    GCN_REQUIRE(dW && (n == 0 || (dY && aligned(dY, el(type)))) && aligned(dW, 4) && aligned(db, 4), GCN_EINVAL,
+                "gcn_rows8_weight_grad: null or misaligned pointer");
+    GCN_REQUIRE(n <= kMostRows && N <= kMostRows && f <= kMostRows, GCN_EUNSUPPORTED,
+                "gcn_rows8_weight_grad: n=%d f=%d N=%d", n, f, N);
     if (dZ8) {
         if ((rc = check_rows8(dZ8, "gcn_rows8_weight_grad"))) return rc;
         GCN_REQUIRE(dZ8->n == n && dZ8->f == N, GCN_ESHAPE, "gcn_rows8_weight_grad: dZ8 is %d x %d, not %d x %d", dZ8->n,
@@ -473,12 +478,13 @@ int gcn_rows8_weight_grad(const gcn_rows8 *X8, const uint8_t *mask, int32_t ldma
     }
     GradBuffers b;
     const GradPlan p = plan_grad(n, f, N, ws, ws_bytes, b);
-    GCN_REQUIRE(n <= 0x7FFFFFC0, GCN_EUNSUPPORTED, "gcn_rows8_weight_grad: n=%d", n);
     GCN_REQUIRE(ws && aligned(ws, 256) && ws_bytes >= p.total, GCN_EWORKSPACE,
                 "gcn_rows8_weight_grad: workspace %zu < %zu bytes, or not 256-byte aligned", ws_bytes, p.total);
     hipStream_t s = (hipStream_t)stream;
     if (n == 0) {
-        for (int32_t i = 0; i < f; ++i)
+        if (lddw == N) rc = fill_zero(dW, (int64_t)f * N, s);
+        if (rc) return rc;
+        for (int32_t i = 0; lddw != N && i < f; ++i)
             if ((rc = fill_zero(dW + (int64_t)i * lddw, N, s))) return rc;
         return db ? fill_zero(db, N, s) : GCN_OK;
     }

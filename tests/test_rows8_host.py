@@ -102,6 +102,8 @@ def test_pack_argument_errors(L):
     assert L.gcn_rows8_pack(FAKE, 2, 200, ctypes.byref(r), None) == B.GCN_EINVAL
     assert L.gcn_rows8_pack(FAKE, 0, 199, ctypes.byref(r), None) == B.GCN_ESHAPE
     assert L.gcn_rows8_pack(None, 0, 200, ctypes.byref(r), None) == B.GCN_EINVAL
+    assert L.gcn_rows8_pack(P(0x10002), 0, 200, ctypes.byref(r), None) == B.GCN_EINVAL
+    assert L.gcn_rows8_pack(P(0x10001), 1, 200, ctypes.byref(r), None) == B.GCN_EINVAL
     assert L.gcn_rows8_pack(FAKE, 0, 200, None, None) == B.GCN_EINVAL
     assert L.gcn_rows8_unpack(ctypes.byref(r), None, 1, 200, None) == B.GCN_EINVAL
     assert L.gcn_rows8_unpack(ctypes.byref(r), FAKE, 1, 100, None) == B.GCN_ESHAPE
@@ -133,6 +135,13 @@ def test_product_argument_errors(L):
     assert product(r=rows8(f=300, ldq=384, lds=3), w=weights8(q=None), t=1) == B.GCN_EINVAL
     assert product(w=weights8(ldqT=240)) == B.GCN_ESHAPE
     assert product(r=rows8(n=0, q=None, scale=None), Y=None) == B.GCN_OK
+    assert product(Y=P(0x10002)) == B.GCN_EINVAL                 # float32 at a 2-byte address
+    assert product(ws=P(0x10010)) == B.GCN_EWORKSPACE
+    need = L.gcn_rows8_product_workspace_bytes(500, 4096, 512)   # few tiles, long sums: partials
+    assert need > 4 * 500 * 512
+    r, w = rows8(n=500, f=4096, ldq=4096, lds=32), weights8(K=4096, N=512, ldq=512, ldqT=4096, lds=4)
+    assert L.gcn_rows8_product(ctypes.byref(r), ctypes.byref(w), 0, None, 0, FAKE, 0, 512, FAKE, need - 1,
+                               None) == B.GCN_EWORKSPACE
 
 
 def test_weight_grad_argument_errors(L):
@@ -148,6 +157,8 @@ def test_weight_grad_argument_errors(L):
     assert wg(ty=-1) == B.GCN_EINVAL
     assert wg(dW=None) == B.GCN_EINVAL
     assert wg(dY=None) == B.GCN_EINVAL
+    assert wg(dY=P(0x10002)) == B.GCN_EINVAL
+    assert wg(dW=P(0x10002)) == B.GCN_EINVAL
     assert wg(dz=rows8(f=63)) == B.GCN_ESHAPE
     assert wg(dz=rows8(n=9, f=64)) == B.GCN_ESHAPE
     assert wg(wb=L.gcn_rows8_weight_grad_workspace_bytes(10, 200, 64) - 1) == B.GCN_EWORKSPACE
@@ -172,6 +183,7 @@ def test_class_loss_argument_errors(L):
     assert loss(ws=P(0x10010)) == B.GCN_EWORKSPACE
     need = L.gcn_class_loss_workspace_bytes(10, 8, 5, 0, 1)
     assert need > 0 and loss(wb=need - 1) == B.GCN_EWORKSPACE
+    assert loss(C=2 ** 31 - 1) == B.GCN_EUNSUPPORTED
 
 
 @pytest.mark.parametrize("n, f, C", [(1, 1, 1), (16384, 1024, 131072), (1 << 20, 512, 200000), (0, 64, 10)])
