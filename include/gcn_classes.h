@@ -30,8 +30,8 @@ extern "C" {
  *     loss        = (1 / n_l) sum_i row_loss[i]
  *     G_i         = (softmax(X_i) - onehot(labels[i])) / n_l
  * A row without a label has row_loss 0 and G_i = 0, and what HL holds there
- * reaches no output unless it is not finite (0 times infinity is NaN in
- * dW_pred); with no label at all the loss and the gradients are 0.
+ * reaches no output; with no label at all the loss and the gradients are 0
+ * (dHL where W_pred is finite).
  *     dHL [n x f] (lddhl) = G W_pred^T,  dW_pred [f x C] = HL^T G,
  *     db_pred [C] = sum_i G_i
  * `type` is that of HL, W_pred, dHL and dW_pred; loss [1], row_loss [n] (NULL:
@@ -41,7 +41,8 @@ extern "C" {
  * db_pred stay float32, n_l G is rounded to bfloat16 as an operand (1 / n_l is
  * applied to the float32 sums).
  * A class whose b_pred is minus infinity has probability 0.  Logits that are NaN
- * or plus infinity, or a row whose logits are all minus infinity, give NaN. */
+ * or plus infinity, or a row whose logits are all minus infinity, give NaN where
+ * the row has a label.  The outputs must not overlap the inputs or each other. */
 size_t gcn_class_loss_workspace_bytes(int32_t n, int32_t f, int32_t C, gcn_rows_type type, int need_grad);
 int gcn_class_loss(const void *HL, int32_t n, int32_t f, int32_t ldhl, const void *W_pred, const float *b_pred,
                    int32_t C, const int32_t *labels, gcn_rows_type type, float *loss, float *row_loss, void *dHL,

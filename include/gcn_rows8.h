@@ -85,9 +85,10 @@ int gcn_weights8_pack(const void *W, gcn_rows_type type, int32_t ldw, const gcn_
  * Y has ldy elements a row and `type`; bias (one float32 per column of Y) may
  * be NULL; act is max(., 0) with relu != 0, else nothing.  Sums are float32,
  * rounded once to `type`.  For bfloat16 results the 8-bit matrix instruction
- * is used, whose sum of products is good to about 2^-16 of its largest terms;
- * for float32 results the same products run as bfloat16 ones, which hold every
- * 8-bit value exactly.  Y must not overlap the operands. */
+ * is used, which adds groups of 8 products with their bits below 2^-13 of the
+ * group's largest cut off (1.5e-5 in the 2-norm on normal data, a hundredth of
+ * the result's rounding); for float32 results the same products run as bfloat16
+ * ones, which hold every 8-bit value exactly.  Y must not overlap the operands. */
 size_t gcn_rows8_product_workspace_bytes(int32_t n, int32_t K, int32_t N);
 int gcn_rows8_product(const gcn_rows8 *X8, const gcn_weights8 *W8, int transpose, const float *bias, int relu,
                       void *Y, gcn_rows_type type, int32_t ldy, void *ws, size_t ws_bytes, void *stream);
@@ -99,7 +100,8 @@ int gcn_rows8_product(const gcn_rows8 *X8, const gcn_weights8 *W8, int transpose
  *     dZ8 = the 8-bit rows of dZ (NULL: not formed), for the input gradient
  * dY is n x N (lddy elements) of `type`; its elements are rounded to bfloat16,
  * X8's 8-bit values are bfloat16 exactly, and sums are float32.  A position
- * whose mask is not positive gives exactly zero whatever dY holds there. */
+ * whose mask is not positive gives exactly zero whatever dY holds there.  The
+ * outputs must not overlap the operands or each other. */
 size_t gcn_rows8_weight_grad_workspace_bytes(int32_t n, int32_t f, int32_t N);
 int gcn_rows8_weight_grad(const gcn_rows8 *X8, const uint8_t *mask, int32_t ldmask, const void *dY,
                           gcn_rows_type type, int32_t lddy, int32_t N, float *dW, int32_t lddw, float *db,

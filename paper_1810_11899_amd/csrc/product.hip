@@ -153,8 +153,7 @@ __device__ __forceinline__ void store_rows(const f32x4 (&v)[FM][4], char *mine, 
 
 // ------------------------------------------------------------- epilogues
 // acc[i][j]: row m0 + 16 i + lane % 16 of C, columns n0 + 16 j + 4 (lane / 16)
-// .. + 3; `scratch`: the idle
-// operand LDS.
+// .. + 3 of the wavefront's block; `scratch`: the idle operand LDS.
 template <int EPI, int BM, int BN, int WM, int WN, int FM, int FN>
 __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&acc)[FM][FN], char *scratch) {
     const TileProduct &p = a.p;
@@ -303,19 +302,23 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
             for (int i = 0; i < FM; ++i) {
                 const float lse = lses[i];
                 const int lab = labs[i];
-                // a row without a label has no gradient: 2^-infinity
-                const float shift = lab != kNoLabel ? 0.0f : -INFINITY;
 #pragma unroll
                 for (int j = 0; j < FN; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        acc[i][j][e] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e] - lse, kLog2e, shift));
+                        acc[i][j][e] = __builtin_amdgcn_exp2f((acc[i][j][e] - lse) * kLog2e);
                 if (__any(lab >= w0 && lab < w0 + BN / WN)) {
 #pragma unroll
                     for (int j = 0; j < FN; ++j)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             if (c0 + 16 * j + e == lab) acc[i][j][e] -= 1.0f;
+                }
+                if (__any(lab == kNoLabel)) {   // no gradient, whatever its logits are
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j][e] = lab == kNoLabel ? 0.0f : acc[i][j][e];
                 }
 #pragma unroll
                 for (int j = 0; j < FN; ++j)
@@ -379,21 +382,22 @@ __device__ __forceinline__ void turn() {
 }
 
 // ------------------------------------------------------------ small tiles
-// WM x WN wavefronts and a ring of S stages: while piece t is multiplied, the
-// copies of the next S - 1 are in flight (with two stages a piece took 1.4 us
-// whatever its size, the latency of one copy), and one barrier a piece both
-// publishes it and frees the stage of the piece before.  Scales are staged for
+// WM x WN wavefronts and two stages: while piece t is multiplied, the copies of
+// the next are in flight, and one barrier a piece both publishes it and frees
+// the stage of the piece before.  Two or more workgroups a CU hide what a copy
+// takes beyond that (three and four stages, which leave room for fewer of
+// them, were no faster at any of the sizes below).  Scales are staged for
 // kScalePieces pieces at a time.
 constexpr int kScalePieces = 64;
-template <int TYPE, int EPI, int BM, int BN, int WM, int WN, int S>
+template <int TYPE, int EPI, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16, T = 64 * WM * WN;
     constexpr int kStage = (BM + BN) * kPiece;
-    constexpr int LA = BM * kPiece / 16 / T, LB = BN * kPiece / 16 / T, L = LA + LB;
+    constexpr int LA = BM * kPiece / 16 / T, LB = BN * kPiece / 16 / T;
     static_assert(LA * T * 16 == BM * kPiece && LB * T * 16 == BN * kPiece, "whole chunks per lane");
-    static_assert(S >= 2 && S <= 4 && kRows8Block % BN == 0, "a tile's columns share a scale");
+    static_assert(kRows8Block % BN == 0, "a tile's columns share a scale");
     constexpr bool SCALED = !is_bf16(TYPE);
-    __shared__ __attribute__((aligned(16))) char lds[S * kStage + (SCALED ? kScalePieces * (BM + 1) : 0)];
+    __shared__ __attribute__((aligned(16))) char lds[2 * kStage + (SCALED ? kScalePieces * (BM + 1) : 0)];
     Coord c;
     if (!coord_of(a, c)) return;
     const TileProduct &p = a.p;
@@ -442,7 +446,7 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
         const char *q = tile + (row + fr) * kPiece;
         return Frag{*(const uint4 *)(q + o0), *(const uint4 *)(q + o1)};
     };
-    uint8_t *const s8 = (uint8_t *)lds + S * kStage;   // [piece][BM rows], then [piece]
+    uint8_t *const s8 = (uint8_t *)lds + 2 * kStage;   // [piece][BM rows], then [piece]
     auto scales = [&](int t) {
         const int w = min(kScalePieces, nt - t);
         for (int i = threadIdx.x; i < BM * w; i += T) {
@@ -454,12 +458,8 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
     };
     if constexpr (SCALED) {
         if (nt > 0) scales(0);
-        wait_copies<0>();   // (the loads above, ahead of the counted copies)
     }
-#pragma unroll
-    for (int t = 0; t < S - 1; ++t)
-        if (t < nt) copy(t, t);
-    int stage = 0;
+    if (nt > 0) copy(0, 0);
     for (int t = 0; t < nt; ++t) {
         if constexpr (SCALED) {
             if (t % kScalePieces == 0 && t) {
@@ -468,15 +468,11 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
             }
             wait_reads();   // the scales' LDS writes, ahead of the barrier
         }
-        // piece t has landed when only the later ones' copies are outstanding
-        const int later = min(nt - 1 - t, S - 2);
-        if (S >= 4 && later >= 2) wait_copies<2 * L>();
-        else if (S >= 3 && later >= 1) wait_copies<L>();
-        else wait_copies<0>();
+        wait_copies<0>();   // piece t has landed
         turn();
         // (every wavefront has used what it read of piece t - 1: its stage is free)
-        if (t + S - 1 < nt) copy(t + S - 1, stage ? stage - 1 : S - 1);
-        const char *ta = lds + stage * kStage, *tb = ta + BM * kPiece;
+        if (t + 1 < nt) copy(t + 1, (t + 1) & 1);
+        const char *ta = lds + (t & 1) * kStage, *tb = ta + BM * kPiece;
         int sa[FM], sb = 0;
         if constexpr (SCALED) {
             const int k = t % kScalePieces;
@@ -525,7 +521,6 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
         for (int i = 0; i < FM; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) asm volatile("" : "+v"(acc[i][j]));
-        stage = stage + 1 == S ? 0 : stage + 1;
     }
     __syncthreads();
     finish<EPI, BM, BN, WM, WN, FM, FN>(a, c, acc, lds);
@@ -559,7 +554,7 @@ constexpr int kRegion = 128 * kPiece, kBuffer = 4 * kRegion;
 constexpr int kBigPieces = 120;                          // pieces whose scales fit in LDS
 constexpr int kScaleA = kBigPieces * 64 * 4, kScaleB = kBigPieces * 2;
 
-template <int TYPE, int I, int J>
+template <int TYPE, int I>
 __device__ __forceinline__ void mma_big(f32x4 &acc, const Frag &a, const Frag &b, int sa, int sb) {
     if constexpr (TYPE == TILE_FP8)
         acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i32x8, b),
@@ -661,10 +656,10 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            mma_big<TYPE, 0, 0>(acc[4 * h + 0][2 * k + j], fa[0], b[j], sa[h], sb);
-            mma_big<TYPE, 1, 0>(acc[4 * h + 1][2 * k + j], fa[1], b[j], sa[h], sb);
-            mma_big<TYPE, 2, 0>(acc[4 * h + 2][2 * k + j], fa[2], b[j], sa[h], sb);
-            mma_big<TYPE, 3, 0>(acc[4 * h + 3][2 * k + j], fa[3], b[j], sa[h], sb);
+            mma_big<TYPE, 0>(acc[4 * h + 0][2 * k + j], fa[0], b[j], sa[h], sb);
+            mma_big<TYPE, 1>(acc[4 * h + 1][2 * k + j], fa[1], b[j], sa[h], sb);
+            mma_big<TYPE, 2>(acc[4 * h + 2][2 * k + j], fa[2], b[j], sa[h], sb);
+            mma_big<TYPE, 3>(acc[4 * h + 3][2 * k + j], fa[3], b[j], sa[h], sb);
         }
         // (the sums are pinned here, or the compiler moves the products past the barriers)
         asm volatile("" : "+v"(acc[4 * h][2 * k]), "+v"(acc[4 * h + 1][2 * k]), "+v"(acc[4 * h + 2][2 * k]),
@@ -891,13 +886,13 @@ void launch(TileShape t, const Args &a, unsigned grid, hipStream_t s) {
             return;
         }
         if (t.m == 64) {
-            hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 64, 64, 4, 1, 2>), dim3(grid), dim3(256), 0, s, a);
+            hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 64, 64, 4, 1>), dim3(grid), dim3(256), 0, s, a);
             return;
         }
     }
     if constexpr (TYPE == TILE_BF16_NN) {
         if (t.m == 32) {
-            hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 32, 128, 2, 2, 2>), dim3(grid), dim3(256), 0, s, a);
+            hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 32, 128, 2, 2>), dim3(grid), dim3(256), 0, s, a);
             return;
         }
     }
@@ -908,7 +903,7 @@ void launch(TileShape t, const Args &a, unsigned grid, hipStream_t s) {
         }
     }
     if constexpr (!((TYPE == TILE_FP8 || TYPE == TILE_FP8_EXACT) && EPI == TILE_PARTIAL))
-        hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 128, 128, 2, 2, 2>), dim3(grid), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 128, 128, 2, 2>), dim3(grid), dim3(256), 0, s, a);
 }
 
 int64_t tiles_of(int64_t M, int64_t N, int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); }

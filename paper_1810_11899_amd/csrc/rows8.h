@@ -62,7 +62,6 @@ struct TileProduct {
     float *colpart;                 // [tiles_m x N]
 };
 // rows and columns of the tiles that this product runs on
-// the tiles that this product runs on: rows and columns of each
 struct TileShape {
     int32_t m, n;
 };
@@ -71,7 +70,8 @@ TileShape tile_shape(TileType type, const TileProduct &p);
 int32_t tile_rows(TileShape t, TileEpilogue epi, const TileProduct &p);
 int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStream_t s);
 // out (float32, or bfloat16 rows of ldo) = the sum of `splits` partials M x N, in
-// order, times *scale, plus bias [N], through the ReLU, where given; out2 [N2] = the column sums of acc2 [rows2 x N2] in the same launch
+// order, times *scale, plus bias [N], through the ReLU, where given; out2 [N2] =
+// the column sums of acc2 [rows2 x N2] in the same launch
 int tile_reduce(int32_t splits, int32_t M, int32_t N, const float *acc, void *out, int out_bf16, int64_t ldo,
                 hipStream_t s, int32_t rows2 = 0, int32_t N2 = 0, const float *acc2 = nullptr, float *out2 = nullptr,
                 const float *scale = nullptr, const float *bias = nullptr, int relu = 0);

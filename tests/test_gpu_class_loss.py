@@ -131,6 +131,19 @@ def test_rows_without_a_label_reach_nothing(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [float("-inf"), float("inf"), float("nan")])
+def test_rows_without_a_label_and_no_logit_left(dtype, value):
+    """Without a label every result is 0 whatever the logits are: all minus infinity, plus infinity, NaN."""
+    n, f, C = 150, 40, 270
+    H, W, b, lab = inputs(n, f, C, dtype)
+    b[:] = value
+    lab[:] = -1
+    out = Out(n, f, C, DT[dtype])
+    call(H.cuda(), W.cuda(), b.cuda(), torch.from_numpy(lab).cuda(), out)
+    assert all(float(x.abs().max()) == 0.0 for x in out.all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_classes_switched_off(dtype):
     """A bias of minus infinity or of the type's lowest value; whole column tiles of them, the first and the last."""
     n, f, C = 40, 32, 700
