@@ -45,8 +45,7 @@ struct CopyRows {
 template <class T>
 __device__ __forceinline__ void copy_rows(const CopyRows<T> &a, int64_t first, int64_t step) {
     constexpr int V = 16 / sizeof(T);   // elements of a store
-    const bool wide = a.ldd % V == 0 && (uintptr_t)a.dst % 16 == 0;
-    const bool vec = a.lds % V == 0 && (uintptr_t)a.src % 16 == 0;
+    const bool wide = a.ldd % V == 0;
     const int64_t per = (a.ldd + V - 1) / V, total = a.drows * per;
     for (int64_t i = first; i < total; i += step) {
         const int64_t r = i / per;
@@ -54,8 +53,8 @@ __device__ __forceinline__ void copy_rows(const CopyRows<T> &a, int64_t first, i
         const bool in = r < a.rows && (!a.labels || has_label(a.labels[r], a.C));
         const T *x = a.src + r * a.lds + c;
         T v[V];
-        if (vec && in && c + V <= a.cols) {
-            *(uint4 *)v = *(const uint4 *)x;
+        if (in && c + V <= a.cols) {
+            *(uint4 *)v = load16(x);
         } else {
 #pragma unroll
             for (int e = 0; e < V; ++e) v[e] = in && c + e < a.cols ? x[e] : (T)0;

@@ -133,7 +133,7 @@ __device__ __forceinline__ void store_rows(const f32x4 (&v)[FM][4], char *mine, 
                 make_uint2(pack_bf16x2(v[i][j][0], v[i][j][1]), pack_bf16x2(v[i][j][2], v[i][j][3]));
     asm volatile("" ::: "memory");   // (LDS accesses of one wavefront stay in order)
     const int lr = lane >> 3, col = col0 + 8 * (lane & 7);
-    const bool vec = ld % 8 == 0 && ((uintptr_t)dst & 15) == 0 && col + 8 <= cols;
+    const bool vec = col + 8 <= cols;
 #pragma unroll
     for (int q = 0; q < 2 * FM; ++q) {
         const int r = 8 * q + lr;
@@ -141,7 +141,7 @@ __device__ __forceinline__ void store_rows(const f32x4 (&v)[FM][4], char *mine, 
         if (row0 + r >= rows) continue;
         uint16_t *d = dst + (int64_t)(row0 + r) * ld + col;
         if (vec) {
-            *(uint4 *)d = x;
+            store16(d, x);
         } else {
             const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
@@ -185,7 +185,6 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
                            c.tn * BN + wn * (BN / WN), p.M, p.N);
             return;
         }
-        const bool vec = p.ldc % 4 == 0 && ((uintptr_t)p.C & 15) == 0;
         // (row by row: a wavefront's stores fill whole lines one after another)
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
@@ -195,8 +194,8 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
             for (int j = 0; j < FN; ++j) {
                 const int col = c0 + 16 * j;
                 float *d = (float *)p.C + (int64_t)row * p.ldc + col;
-                if (vec && col + 4 <= p.N) {
-                    *(f32x4 *)d = acc[i][j];
+                if (col + 4 <= p.N) {
+                    store16(d, __builtin_bit_cast(uint4, acc[i][j]));
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
@@ -206,7 +205,6 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
         }
     } else if constexpr (EPI == TILE_PARTIAL) {
         float *base = p.acc + (int64_t)c.split * p.M * p.N;
-        const bool vec = p.N % 4 == 0;
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -214,10 +212,10 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
                 const int row = r0 + 16 * i, col = c0 + 16 * j;
                 if (row >= p.M || col >= p.N) continue;
                 float *d = base + (int64_t)row * p.N + col;
-                if (vec) {
+                if (col + 4 <= p.N) {
                     f32x4 v = acc[i][j];
-                    if (p.accumulate) v += *(const f32x4 *)d;
-                    *(f32x4 *)d = v;
+                    if (p.accumulate) v += __builtin_bit_cast(f32x4, load16(d));
+                    store16(d, __builtin_bit_cast(uint4, v));
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)

@@ -11,6 +11,15 @@ constexpr int32_t kMostRows = 0x7FFFFE00;   // of an operand
 constexpr int kRows8Block = 128;   // columns (and, for weights, rows) under one scale
 inline int64_t blocks8(int64_t f) { return (f + kRows8Block - 1) / kRows8Block; }
 
+// 16 bytes at any element's address: global memory needs no more alignment, and
+// rows of an odd length would take eight loads or stores otherwise
+__device__ __forceinline__ uint4 load16(const void *p) {
+    uint4 v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+__device__ __forceinline__ void store16(void *p, uint4 v) { __builtin_memcpy(p, &v, 16); }
+
 // ---------------------------------------------------------------- products
 // C[M x N] = A B^T on the matrix cores, A [M x K] and B [N x K] in rows of kt
 // 128-byte pieces (64 bfloat16 or 128 e4m3 values), 16-byte aligned, the

@@ -42,11 +42,11 @@ __device__ __forceinline__ uint32_t held4(const float (&x)[4], float inv) {
 }
 
 // eight consecutive elements from column c of a row (zeros past f)
-template <bool BF, bool VEC>
+template <bool BF>
 __device__ __forceinline__ void load8(const void *row, int c, int f, float (&x)[8]) {
-    if (VEC && c + 8 <= f) {
+    if (c + 8 <= f) {
         if (BF) {
-            const uint4 v = *(const uint4 *)((const uint16_t *)row + c);
+            const uint4 v = load16((const uint16_t *)row + c);
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -54,8 +54,10 @@ __device__ __forceinline__ void load8(const void *row, int c, int f, float (&x)[
                 x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
             }
         } else {
-            const float4 a = *(const float4 *)((const float *)row + c), b = *(const float4 *)((const float *)row + c + 4);
-            x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+            const uint4 a = load16((const float *)row + c), b = load16((const float *)row + c + 4);
+            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
         }
     } else {
 #pragma unroll
@@ -85,7 +87,7 @@ __device__ __forceinline__ void pack_block(const float (&x)[8], uint8_t *q, uint
 
 // One block of 128 columns to 16 lanes, the lanes of a wavefront along the row
 // (whole lines both ways).
-template <bool BF, bool VEC>
+template <bool BF>
 __global__ __launch_bounds__(kTB) void pack_kernel(int64_t blocks, int32_t per_row, int32_t f, const void *X,
                                                    int64_t ldx, uint8_t *q, int64_t ldq, uint8_t *scale,
                                                    int64_t lds) {
@@ -95,7 +97,7 @@ __global__ __launch_bounds__(kTB) void pack_kernel(int64_t blocks, int32_t per_r
         const int64_t row = in ? b / per_row : 0;
         const int32_t bc = in ? (int32_t)(b - row * per_row) : 0;
         float x[8];
-        load8<BF, VEC>((const char *)X + row * ldx * (BF ? 2 : 4), bc * kBlk + 8 * (int)(threadIdx.x & 15), f, x);
+        load8<BF>((const char *)X + row * ldx * (BF ? 2 : 4), bc * kBlk + 8 * (int)(threadIdx.x & 15), f, x);
         pack_block(x, q + row * ldq + bc * kBlk, scale + row * lds + bc, in);
     }
 }
@@ -115,7 +117,7 @@ __device__ __forceinline__ void values8(uint2 q, int e, float (&x)[8]) {
 
 // eight columns to a thread; rows n .. drows - 1 and columns past f (to the last
 // whole eight, where ldx holds them) are written as zeros when PAD
-template <bool BF, bool VEC, bool PAD>
+template <bool BF, bool PAD>
 __device__ __forceinline__ void unpack_rows(int64_t first, int64_t step, int32_t drows, int32_t n, int32_t f,
                                             const uint8_t *q, int64_t ldq, const uint8_t *scale, int64_t lds, void *X,
                                             int64_t ldx) {
@@ -129,9 +131,9 @@ __device__ __forceinline__ void unpack_rows(int64_t first, int64_t step, int32_t
             values8(*(const uint2 *)(q + row * ldq + c), (int)scale[row * lds + c / kBlk] - 127, x);
         if (BF) {
             uint16_t *d = (uint16_t *)X + row * ldx + c;
-            if (VEC && (PAD || c + 8 <= f)) {
-                *(uint4 *)d = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                                         pack_bf16x2(x[6], x[7]));
+            if (PAD || c + 8 <= f) {
+                store16(d, make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                                      pack_bf16x2(x[6], x[7])));
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -139,9 +141,11 @@ __device__ __forceinline__ void unpack_rows(int64_t first, int64_t step, int32_t
             }
         } else {
             float *d = (float *)X + row * ldx + c;
-            if (VEC && c + 8 <= f) {
-                *(float4 *)d = make_float4(x[0], x[1], x[2], x[3]);
-                *(float4 *)(d + 4) = make_float4(x[4], x[5], x[6], x[7]);
+            if (c + 8 <= f) {
+#pragma unroll
+                for (int h = 0; h < 8; h += 4)
+                    store16(d + h, make_uint4(__float_as_uint(x[h]), __float_as_uint(x[h + 1]), __float_as_uint(x[h + 2]),
+                                              __float_as_uint(x[h + 3])));
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -150,10 +154,10 @@ __device__ __forceinline__ void unpack_rows(int64_t first, int64_t step, int32_t
         }
     }
 }
-template <bool BF, bool VEC>
+template <bool BF>
 __global__ __launch_bounds__(kTB) void unpack_kernel(int32_t n, int32_t f, const uint8_t *q, int64_t ldq,
                                                      const uint8_t *scale, int64_t lds, void *X, int64_t ldx) {
-    unpack_rows<BF, VEC, false>((int64_t)blockIdx.x * kTB + threadIdx.x, (int64_t)gridDim.x * kTB, n, n, f, q, ldq, scale,
+    unpack_rows<BF, false>((int64_t)blockIdx.x * kTB + threadIdx.x, (int64_t)gridDim.x * kTB, n, n, f, q, ldq, scale,
                                 lds, X, ldx);
 }
 
@@ -228,13 +232,13 @@ struct MaskArgs {
     uint16_t *X;
     int64_t ldx;
 };
-template <bool BF, bool VEC>
+template <bool BF>
 __global__ __launch_bounds__(kTB) void mask_kernel(MaskArgs a) {
     __shared__ float red[kTB / 16][kBlk];
     const int strip = (int)(blockIdx.x / a.blocks), cb = (int)(blockIdx.x % a.blocks);
     if (strip >= a.strips) {
         const int64_t b = (int64_t)blockIdx.x - (int64_t)a.strips * a.blocks;
-        unpack_rows<true, true, true>(b * kTB + threadIdx.x, ((int64_t)gridDim.x - (int64_t)a.strips * a.blocks) * kTB, a.nz,
+        unpack_rows<true, true>(b * kTB + threadIdx.x, ((int64_t)gridDim.x - (int64_t)a.strips * a.blocks) * kTB, a.nz,
                                       a.n, a.f, a.xq, a.ldxq, a.xscale, a.ldxs, a.X, a.ldx);
         return;
     }
@@ -256,13 +260,12 @@ __global__ __launch_bounds__(kTB) void mask_kernel(MaskArgs a) {
         const bool in = r < r1 && r < n;
         float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
         if (in) {
-            load8<BF, VEC>((const char *)dY + r * lddy * (BF ? 2 : 4), c, N, x);
+            load8<BF>((const char *)dY + r * lddy * (BF ? 2 : 4), c, N, x);
             uint32_t m[2] = {0x01010101u, 0x01010101u};
             if (mask) {
                 const uint8_t *mp = mask + r * ldm + c;
-                if (VEC && c + 8 <= N) {
-                    const uint2 v = *(const uint2 *)mp;
-                    m[0] = v.x, m[1] = v.y;
+                if (c + 8 <= N) {
+                    __builtin_memcpy(m, mp, 8);
                 } else {
                     m[0] = m[1] = 0u;
 #pragma unroll
@@ -331,17 +334,10 @@ int rows8_pack(int32_t n, int32_t f, const void *X, int x_bf16, int64_t ldx, uin
     const int64_t blocks = (int64_t)n * per_row;
     ProfScope prof(K_ROWS8_PACK, s, 0.0, (double)n * f * (x_bf16 ? 3.0 : 5.0) + (double)blocks);
     const unsigned g = grid_of(blocks, kTB / 16, 16384);
-    const bool vec = aligned(X, 16) && ldx % (x_bf16 ? 8 : 4) == 0;
-#define GCN_PACK(BF, VEC) \
-    hipLaunchKernelGGL((pack_kernel<BF, VEC>), dim3(g), dim3(kTB), 0, s, blocks, per_row, f, X, ldx, q, ldq, scale, lds)
-    if (x_bf16) {
-        if (vec) GCN_PACK(true, true);
-        else GCN_PACK(true, false);
-    } else {
-        if (vec) GCN_PACK(false, true);
-        else GCN_PACK(false, false);
-    }
-#undef GCN_PACK
+    if (x_bf16)
+        hipLaunchKernelGGL(pack_kernel<true>, dim3(g), dim3(kTB), 0, s, blocks, per_row, f, X, ldx, q, ldq, scale, lds);
+    else
+        hipLaunchKernelGGL(pack_kernel<false>, dim3(g), dim3(kTB), 0, s, blocks, per_row, f, X, ldx, q, ldq, scale, lds);
     GCN_LAUNCH_CHECK("pack_kernel");
     return GCN_OK;
 }
@@ -372,19 +368,13 @@ int gcn_rows8_unpack(const gcn_rows8 *r, void *X, gcn_rows_type type, int32_t ld
     hipStream_t s = (hipStream_t)stream;
     const bool bf = type == GCN_ROWS_BF16;
     ProfScope prof(K_ROWS8_PACK, s, 0.0, (double)r->n * r->f * (bf ? 3.0 : 5.0));
-    const bool vec = aligned(X, 16) && ldx % (bf ? 8 : 4) == 0;
     const unsigned g = grid_of((int64_t)r->n * ((r->f + 7) / 8), kTB, 16384);
-#define GCN_UNPACK(BF, VEC)                                                                                       \
-    hipLaunchKernelGGL((unpack_kernel<BF, VEC>), dim3(g), dim3(kTB), 0, s, r->n, r->f, r->q, (int64_t)r->ldq, r->scale, \
-                       (int64_t)r->ldscale, X, (int64_t)ldx)
-    if (bf) {
-        if (vec) GCN_UNPACK(true, true);
-        else GCN_UNPACK(true, false);
-    } else {
-        if (vec) GCN_UNPACK(false, true);
-        else GCN_UNPACK(false, false);
-    }
-#undef GCN_UNPACK
+    if (bf)
+        hipLaunchKernelGGL(unpack_kernel<true>, dim3(g), dim3(kTB), 0, s, r->n, r->f, r->q, (int64_t)r->ldq, r->scale,
+                           (int64_t)r->ldscale, X, (int64_t)ldx);
+    else
+        hipLaunchKernelGGL(unpack_kernel<false>, dim3(g), dim3(kTB), 0, s, r->n, r->f, r->q, (int64_t)r->ldq, r->scale,
+                           (int64_t)r->ldscale, X, (int64_t)ldx);
     GCN_LAUNCH_CHECK("unpack_kernel");
     return GCN_OK;
 }
@@ -492,19 +482,13 @@ int gcn_rows8_weight_grad(const gcn_rows8 *X8, const uint8_t *mask, int32_t ldma
         const bool bf = type == GCN_ROWS_BF16;
         ProfScope prof(K_ROWS8_MASK, s, 0.0,
                        (double)n * N * ((bf ? 4.0 : 6.0) + (mask ? 1.0 : 0.0) + (dZ8 ? 1.0 : 0.0)) + 3.0 * n * f);
-        const bool vec = aligned(dY, 16) && lddy % (bf ? 8 : 4) == 0 && (!mask || (aligned(mask, 8) && ldmask % 8 == 0));
         const int32_t blocks = (int32_t)blocks8(N);
         const MaskArgs m{n, p.nz, N, p.strip, p.strips, blocks, dY, lddy, mask, ldmask, b.dZ, p.Np, db ? b.part : nullptr,
                          dZ8 ? dZ8->q : nullptr, dZ8 ? dZ8->ldq : 0, dZ8 ? dZ8->scale : nullptr, dZ8 ? dZ8->ldscale : 0,
                          f, X8->q, X8->ldq, X8->scale, X8->ldscale, b.X, p.fp};
         const dim3 g((unsigned)(p.strips * blocks) + grid_of((int64_t)p.nz * (p.fp / 8), kTB, 4096));
-        if (bf) {
-            if (vec) hipLaunchKernelGGL((mask_kernel<true, true>), g, dim3(kTB), 0, s, m);
-            else hipLaunchKernelGGL((mask_kernel<true, false>), g, dim3(kTB), 0, s, m);
-        } else {
-            if (vec) hipLaunchKernelGGL((mask_kernel<false, true>), g, dim3(kTB), 0, s, m);
-            else hipLaunchKernelGGL((mask_kernel<false, false>), g, dim3(kTB), 0, s, m);
-        }
+        if (bf) hipLaunchKernelGGL(mask_kernel<true>, g, dim3(kTB), 0, s, m);
+        else hipLaunchKernelGGL(mask_kernel<false>, g, dim3(kTB), 0, s, m);
         GCN_LAUNCH_CHECK("mask_kernel");
     }
     ProfScope prof(K_ROWS8_WEIGHT_GRAD, s, 2.0 * n * f * N, 2.0 * n * f + 2.0 * n * N + 4.0 * f * N);
