@@ -122,43 +122,45 @@ __global__ __launch_bounds__(kTB) void join_kernel(int32_t n, int32_t tiles, con
 }
 
 // logits of one piece (float32 rows of ldx, a multiple of 4) joined into the
-// running maximum and sum, a workgroup a row
-__global__ __launch_bounds__(kTB) void stats_rows_kernel(int32_t P, const float *X, int64_t ldx, const int32_t *labels,
+// running maximum and sum, a workgroup a row (and grid rows on, beyond 2^20)
+__global__ __launch_bounds__(kTB) void stats_rows_kernel(int32_t n, int32_t P, const float *X, int64_t ldx, const int32_t *labels,
                                                          int32_t class0, int32_t C, float *run_max, float *run_sum,
                                                          float *label_logit, int first) {
     __shared__ float sm[kTB / 64], ss[kTB / 64];
-    const int32_t row = blockIdx.x;
-    const float *x = X + row * ldx;
-    float m = -INFINITY, s = 0.0f;
-    for (int32_t c = 4 * (int32_t)threadIdx.x; c < P; c += 4 * kTB) {
-        const float4 v = *(const float4 *)(x + c);
-        float y[4] = {v.x, v.y, v.z, v.w};
+    for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
+        __syncthreads();   // (the row before has been read)
+        const float *x = X + row * ldx;
+        float m = -INFINITY, s = 0.0f;
+        for (int32_t c = 4 * (int32_t)threadIdx.x; c < P; c += 4 * kTB) {
+            const float4 v = *(const float4 *)(x + c);
+            float y[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int e = 1; e < 4; ++e)
-            if (c + e >= P) y[e] = -INFINITY;
-        const float b = fmaxf(m, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
-        if (b > m) {
-            s *= expf(m - b);   // (0 of the empty sum: exp(-infinity))
-            m = b;
+            for (int e = 1; e < 4; ++e)
+                if (c + e >= P) y[e] = -INFINITY;
+            const float b = fmaxf(m, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
+            if (b > m) {
+                s *= expf(m - b);   // (0 of the empty sum: exp(-infinity))
+                m = b;
+            }
+            const float base = m == -INFINITY ? 0.0f : m;   // no finite logit yet: the sum stays 0
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s += expf(y[e] - base);
         }
-        const float base = m == -INFINITY ? 0.0f : m;   // no finite logit yet: the sum stays 0
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s += expf(y[e] - base);
+        for (int d = 1; d < 64; d *= 2) {
+            const float q = __shfl_xor(m, d), u = __shfl_xor(s, d);
+            join(m, s, q, u);
+        }
+        if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m, ss[threadIdx.x >> 6] = s;
+        __syncthreads();
+        if (threadIdx.x != 0) continue;
+        for (int w = 1; w < kTB / 64; ++w) join(m, s, sm[w], ss[w]);
+        if (!first) join(m, s, run_max[row], run_sum[row]);
+        run_max[row] = m;
+        run_sum[row] = s;
+        const int32_t l = labels[row];
+        if (has_label(l, C) && l >= class0 && l - class0 < P) label_logit[row] = x[l - class0];
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const float q = __shfl_xor(m, d), u = __shfl_xor(s, d);
-        join(m, s, q, u);
-    }
-    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m, ss[threadIdx.x >> 6] = s;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    for (int w = 1; w < kTB / 64; ++w) join(m, s, sm[w], ss[w]);
-    if (!first) join(m, s, run_max[row], run_sum[row]);
-    run_max[row] = m;
-    run_sum[row] = s;
-    const int32_t l = labels[row];
-    if (has_label(l, C) && l >= class0 && l - class0 < P) label_logit[row] = x[l - class0];
 }
 
 // X <- G, and the column sums of strips of kStrip rows: a thread has a column
@@ -460,7 +462,6 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         h.splits = p.split_h;
         h.acc = b.acc;
         h.accumulate = i > 0;
-        if ((rc = tile_product(TILE_BF16, TILE_PARTIAL, h, s))) return rc;
         TileProduct w{};
         w.A = (const uint8_t *)b.H;
         w.lda = 2 * p.fp;
@@ -472,14 +473,15 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         w.splits = p.split_w;
         if (p.split_w > 1) {
             w.acc = b.part;
-            if ((rc = tile_product(TILE_BF16_TN, TILE_PARTIAL, w, s))) return rc;
-            if ((rc = tile_reduce(p.split_w, f, P, b.part, dW + c0, 1, C, s, 0, 0, nullptr, nullptr, b.inv_count))) return rc;
         } else {
             w.C = dW + c0;
             w.ldc = C;
             w.scale = b.inv_count;
-            if ((rc = tile_product(TILE_BF16_TN, TILE_STORE, w, s))) return rc;
         }
+        if ((rc = tile_products(h, w, p.split_w > 1 ? TILE_PARTIAL : TILE_STORE, s))) return rc;
+        if (p.split_w > 1 &&
+            (rc = tile_reduce(p.split_w, f, P, b.part, dW + c0, 1, C, s, 0, 0, nullptr, nullptr, b.inv_count)))
+            return rc;
     }
     return tile_reduce(p.split_h, n, f, b.acc, dHL, 1, lddhl, s, 0, 0, nullptr, nullptr, b.inv_count);
 }
@@ -506,7 +508,7 @@ int loss_f32(const Plan &p, const Buffers &b, const float *HL, int32_t n, int32_
         const int32_t c0 = i * p.piece, P = std::min(p.piece, C - c0);
         if ((rc = logits(c0, P))) return rc;
         ProfScope prof(K_CLASS_STATS, s, 0.0, 4.0 * n * P);
-        hipLaunchKernelGGL(stats_rows_kernel, dim3((unsigned)n), dim3(kTB), 0, s, P, b.X, up(P, 4), labels, c0, C,
+        hipLaunchKernelGGL(stats_rows_kernel, dim3((unsigned)std::min(n, 1 << 20)), dim3(kTB), 0, s, n, P, b.X, up(P, 4), labels, c0, C,
                            b.run_max, b.run_sum, b.label_logit, i == 0);
         GCN_LAUNCH_CHECK("stats_rows_kernel");
     }

@@ -40,8 +40,8 @@ struct Args {
 struct Coord {
     int split, tm, tn;
 };
-__device__ __forceinline__ bool coord_of(const Args &a, Coord &c) {
-    const uint32_t L = (blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
+__device__ __forceinline__ bool coord_of(const Args &a, uint32_t block, Coord &c) {
+    const uint32_t L = (block & 7) * a.per_xcd + (block >> 3);
     if (L >= a.total) return false;
     const uint32_t per_split = (uint32_t)a.tiles_m * a.tiles_n;
     c.split = (int)(L / per_split);
@@ -152,10 +152,49 @@ __device__ __forceinline__ void store_rows(const f32x4 (&v)[FM][4], char *mine, 
 }
 
 // ------------------------------------------------------------- epilogues
+// What an epilogue reads besides the sums.  The small tiles of the loss load it
+// ahead of their products (17 rows of 128 columns, 1009 classes: the call 33.8 ->
+// 32.5 us); the others, whose registers it would take meanwhile, behind them (8000 x 512
+// x 1024 11.9 instead of 12.2).
+template <int FM, int FN>
+struct Extras {
+    float bias[FN][4];
+    float scale;
+    int lab[FM];
+    float lse[FM];
+};
+template <int EPI, int BM, int BN, int WM, int WN, int FM, int FN>
+__device__ __forceinline__ void load_extras(const TileProduct &p, const Coord &c, Extras<FM, FN> &x) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int r0 = c.tm * BM + wave / WN * (BM / WM) + (lane & 15);
+    const int c0 = c.tn * BN + wave % WN * (BN / WN) + 4 * (lane >> 4);
+    if constexpr (EPI != TILE_PARTIAL) {
+        // (the logits' columns past the last class: minus infinity)
+        const float past = EPI == TILE_STATS || EPI == TILE_GRAD ? -INFINITY : 0.0f;
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int col = c0 + 16 * j + e;
+                x.bias[j][e] = col < p.N ? (p.bias ? p.bias[col] : 0.0f) : past;
+            }
+    }
+    if constexpr (EPI != TILE_PARTIAL && EPI != TILE_STATS) x.scale = p.scale ? p.scale[0] : 1.0f;
+    if constexpr (EPI == TILE_STATS || EPI == TILE_GRAD) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i) x.lab[i] = label_of(p, r0 + 16 * i);
+    }
+    if constexpr (EPI == TILE_GRAD) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i) x.lse[i] = r0 + 16 * i < p.M ? p.lse[r0 + 16 * i] : 0.0f;
+    }
+}
+
 // acc[i][j]: row m0 + 16 i + lane % 16 of C, columns n0 + 16 j + 4 (lane / 16)
 // .. + 3 of the wavefront's block; `scratch`: the idle operand LDS.
 template <int EPI, int BM, int BN, int WM, int WN, int FM, int FN>
-__device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&acc)[FM][FN], char *scratch) {
+__device__ __forceinline__ void finish(const Args &a, const Coord &c, const Extras<FM, FN> &x,
+                                       f32x4 (&acc)[FM][FN], char *scratch) {
     const TileProduct &p = a.p;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int wm = wave / WN, wn = wave % WN;
@@ -163,18 +202,12 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
     const int c0 = c.tn * BN + wn * (BN / WN) + 4 * (lane >> 4);
     static_assert(FN == 4, "a wavefront's block is 64 columns wide");
     if constexpr (EPI == TILE_STORE || EPI == TILE_STORE_F32) {
-        f32x4 bias[FN];
-        const float scale = p.scale ? p.scale[0] : 1.0f;
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                bias[j][e] = p.bias && c0 + 16 * j + e < p.N ? p.bias[c0 + 16 * j + e] : 0.0f;
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                acc[i][j] = acc[i][j] * scale + bias[j];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = acc[i][j][e] * x.scale + x.bias[j][e];
                 if (p.relu)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[i][j][e] = acc[i][j][e] < 0.0f ? 0.0f : acc[i][j][e];   // (NaN stays)
@@ -223,20 +256,14 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
                 }
             }
     } else {
-        // the logits: bias, and columns past the last class at minus infinity
+        // the logits
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+        for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int col = c0 + 16 * j + e;
-                const float b = col < p.N ? (p.bias ? p.bias[col] : 0.0f) : -INFINITY;
+            for (int j = 0; j < FN; ++j)
 #pragma unroll
-                for (int i = 0; i < FM; ++i) acc[i][j][e] += b;
-            }
+                for (int e = 0; e < 4; ++e) acc[i][j][e] += x.bias[j][e];
         constexpr float kLog2e = 1.44269504088896340736f;
-        int labs[FM];   // (all loads before the first use: behind a store each would wait for the one before)
-#pragma unroll
-        for (int i = 0; i < FM; ++i) labs[i] = label_of(p, r0 + 16 * i);
         const int w0 = c.tn * BN + wn * (BN / WN);   // the wavefront's first column
         if constexpr (EPI == TILE_STATS) {
             // a row's columns lie in 4 lanes of WN wavefronts: maximum and sum
@@ -262,7 +289,7 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
                 s += __shfl_xor(s, 16);
                 s += __shfl_xor(s, 32);
                 if (lane < 16) part[wn * BM + row - c.tm * BM] = make_float2(m, s);
-                const int lab = labs[i];
+                const int lab = x.lab[i];
                 if (__any(lab >= w0 && lab < w0 + BN / WN)) {   // (few wavefronts see one of their labels)
 #pragma unroll
                     for (int j = 0; j < FN; ++j)
@@ -293,13 +320,10 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
             for (int j = 0; j < FN; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) cs[j][e] = 0.0f;
-            float lses[FM];
-#pragma unroll
-            for (int i = 0; i < FM; ++i) lses[i] = r0 + 16 * i < p.M ? p.lse[r0 + 16 * i] : 0.0f;
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
-                const float lse = lses[i];
-                const int lab = labs[i];
+                const float lse = x.lse[i];
+                const int lab = x.lab[i];
 #pragma unroll
                 for (int j = 0; j < FN; ++j)
 #pragma unroll
@@ -345,7 +369,7 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, f32x4 (&ac
                 float v = 0.0f;
 #pragma unroll
                 for (int w = 0; w < WM; ++w) v += part[w * BN + k];
-                v *= p.scale[0];
+                v *= x.scale;
                 p.colpart[(int64_t)c.tm * p.N + col] = v;
             }
         }
@@ -387,17 +411,19 @@ __device__ __forceinline__ void turn() {
 // them, were no faster at any of the sizes below).  Scales are staged for
 // kScalePieces pieces at a time.
 constexpr int kScalePieces = 64;
+constexpr int small_lds(int type, int BM, int BN) {
+    return 2 * (BM + BN) * kPiece + (is_bf16(type) ? 0 : kScalePieces * (BM + 1));
+}
 template <int TYPE, int EPI, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
+__device__ __forceinline__ void small_tile(const Args &a, uint32_t block, char *lds) {
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16, T = 64 * WM * WN;
     constexpr int kStage = (BM + BN) * kPiece;
     constexpr int LA = BM * kPiece / 16 / T, LB = BN * kPiece / 16 / T;
     static_assert(LA * T * 16 == BM * kPiece && LB * T * 16 == BN * kPiece, "whole chunks per lane");
     static_assert(kRows8Block % BN == 0, "a tile's columns share a scale");
     constexpr bool SCALED = !is_bf16(TYPE);
-    __shared__ __attribute__((aligned(16))) char lds[2 * kStage + (SCALED ? kScalePieces * (BM + 1) : 0)];
     Coord c;
-    if (!coord_of(a, c)) return;
+    if (!coord_of(a, block, c)) return;
     const TileProduct &p = a.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -437,6 +463,9 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    Extras<FM, FN> extras;
+    constexpr bool kEarly = FM == 1 && (EPI == TILE_STATS || EPI == TILE_GRAD);
+    if constexpr (kEarly) load_extras<EPI, BM, BN, WM, WN>(p, c, extras);
     const int fr = lane & 15, g = lane >> 4;
     const int o0 = (g ^ (fr & 7)) * 16, o1 = ((g + 4) ^ (fr & 7)) * 16;   // (a fragment's rows start at multiples of 16)
     auto frag = [&](const char *tile, int row, bool km) {
@@ -521,7 +550,24 @@ __global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
             for (int j = 0; j < FN; ++j) asm volatile("" : "+v"(acc[i][j]));
     }
     __syncthreads();
-    finish<EPI, BM, BN, WM, WN, FM, FN>(a, c, acc, lds);
+    if constexpr (!kEarly) load_extras<EPI, BM, BN, WM, WN>(p, c, extras);
+    finish<EPI, BM, BN, WM, WN, FM, FN>(a, c, extras, acc, lds);
+}
+template <int TYPE, int EPI, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM *WN) void tile_kernel(Args a) {
+    __shared__ __attribute__((aligned(16))) char lds[small_lds(TYPE, BM, BN)];
+    small_tile<TYPE, EPI, BM, BN, WM, WN>(a, blockIdx.x, lds);
+}
+// two products in one launch, `first` workgroups (a multiple of 8) for the first:
+// few tiles leave CUs idle, and a launch costs about 4 us (the whole loss, in two
+// launches / one: 17 x 128, 1009 classes 32.5 / 28.6 us; 2000 x 256, 1009 classes 58 /
+// 51)
+template <int TYPE, int EPI, int TYPE2, int EPI2>
+__global__ __launch_bounds__(256) void pair_kernel(Args a, Args b, uint32_t first) {
+    constexpr int la = small_lds(TYPE, 128, 128), lb = small_lds(TYPE2, 128, 128);
+    __shared__ __attribute__((aligned(16))) char lds[la > lb ? la : lb];
+    if (blockIdx.x < first) small_tile<TYPE, EPI, 128, 128, 2, 2>(a, blockIdx.x, lds);
+    else small_tile<TYPE2, EPI2, 128, 128, 2, 2>(b, blockIdx.x - first, lds);
 }
 
 // ------------------------------------------------------------ large tiles
@@ -565,7 +611,7 @@ template <int TYPE, int EPI>
 __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void big_kernel(Args a) {
     __shared__ __attribute__((aligned(16))) char lds[2 * kBuffer + (TYPE == TILE_FP8 ? kScaleA + kScaleB : 0)];
     Coord c;
-    if (!coord_of(a, c)) return;
+    if (!coord_of(a, blockIdx.x, c)) return;
     const TileProduct &p = a.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 2, wn = wave & 3;
@@ -745,7 +791,9 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
         for (int t = 0; t < nt; ++t) piece(t);
         if (!wm) turn();
     }
-    finish<EPI, kBigT, kBigT, 2, 4, 8, 4>(a, c, acc, lds);
+    Extras<8, 4> extras;
+    load_extras<EPI, kBigT, kBigT, 2, 4>(p, c, extras);
+    finish<EPI, kBigT, kBigT, 2, 4, 8, 4>(a, c, extras, acc, lds);
 }
 
 // --------------------------------------------------------------- few rows
@@ -943,14 +991,12 @@ int32_t tile_rows(TileShape t, TileEpilogue epi, const TileProduct &p) {
     return (int32_t)(((epi == TILE_GRAD ? std::max<int64_t>(p.M, p.g_rows) : p.M) + t.m - 1) / t.m);
 }
 
-int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStream_t s) {
-    if (p.M <= 0 || p.N <= 0) return GCN_OK;
+// a product's tiles and grid
+static int tile_args(const TileShape &t, TileEpilogue epi, const TileProduct &p, Args &a, unsigned &grid) {
     if (std::max(p.M, p.N) > kMostRows) {   // (row numbers past the last tile's end stay within 32 bits)
         set_error("tile_product: %d x %d is too large", p.M, p.N);
         return GCN_EUNSUPPORTED;
     }
-    const TileShape t = tile_shape(type, p);
-    Args a;
     a.p = p;
     a.tiles_m = tile_rows(t, epi, p);
     a.tiles_n = (int32_t)(((int64_t)p.N + t.n - 1) / t.n);
@@ -958,13 +1004,42 @@ int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStrea
     a.kt_per_split = (p.kt + splits - 1) / splits;
     a.band = 8;
     const int64_t total = (int64_t)splits * a.tiles_m * a.tiles_n;
-    if (total > 0x7FFFFFF0) {
+    if (total > 0x7FFFF0) {   // (threads of a launch: 32 bits)
         set_error("tile_product: %d x %d is too large", p.M, p.N);
         return GCN_EUNSUPPORTED;
     }
     a.total = (uint32_t)total;
     a.per_xcd = (a.total + 7) / 8;
-    const unsigned grid = 8 * a.per_xcd;
+    grid = 8 * a.per_xcd;
+    return GCN_OK;
+}
+
+int tile_products(const TileProduct &nt, const TileProduct &tn, TileEpilogue epi, hipStream_t s) {
+    const TileShape t = tile_shape(TILE_BF16, nt), u = tile_shape(TILE_BF16_TN, tn);
+    int rc;
+    if (t.m != 128 || u.m != 128) {
+        if ((rc = tile_product(TILE_BF16, TILE_PARTIAL, nt, s))) return rc;
+        return tile_product(TILE_BF16_TN, epi, tn, s);
+    }
+    Args a, b;
+    unsigned ga, gb;
+    if ((rc = tile_args(t, TILE_PARTIAL, nt, a, ga)) || (rc = tile_args(u, epi, tn, b, gb))) return rc;
+    if (epi == TILE_STORE)
+        hipLaunchKernelGGL((pair_kernel<TILE_BF16, TILE_PARTIAL, TILE_BF16_TN, TILE_STORE>), dim3(ga + gb), dim3(256), 0,
+                           s, a, b, ga);
+    else
+        hipLaunchKernelGGL((pair_kernel<TILE_BF16, TILE_PARTIAL, TILE_BF16_TN, TILE_PARTIAL>), dim3(ga + gb), dim3(256), 0,
+                           s, a, b, ga);
+    GCN_LAUNCH_CHECK("pair_kernel");
+    return GCN_OK;
+}
+
+int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStream_t s) {
+    if (p.M <= 0 || p.N <= 0) return GCN_OK;
+    const TileShape t = tile_shape(type, p);
+    Args a;
+    unsigned grid;
+    if (const int rc = tile_args(t, epi, p, a, grid)) return rc;
     // (the pairs that the entry points use)
     if (type == TILE_BF16_NN && epi == TILE_STATS) launch<TILE_BF16_NN, TILE_STATS>(t, a, grid, s);
     else if (type == TILE_BF16_NN && epi == TILE_GRAD) launch<TILE_BF16_NN, TILE_GRAD>(t, a, grid, s);

@@ -78,6 +78,10 @@ TileShape tile_shape(TileType type, const TileProduct &p);
 // rows of tiles (with TILE_GRAD they cover the rows of zeros behind the last one)
 int32_t tile_rows(TileShape t, TileEpilogue epi, const TileProduct &p);
 int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStream_t s);
+// TILE_BF16 with TILE_PARTIAL, and TILE_BF16_TN with `epi` (TILE_STORE or
+// TILE_PARTIAL); neither is empty, and neither reads what the other writes.  In
+// one launch where both run on small tiles
+int tile_products(const TileProduct &nt, const TileProduct &tn, TileEpilogue epi, hipStream_t s);
 // out (float32, or bfloat16 rows of ldo) = the sum of `splits` partials M x N, in
 // order, times *scale, plus bias [N], through the ReLU, where given; out2 [N2] =
 // the column sums of acc2 [rows2 x N2] in the same launch
