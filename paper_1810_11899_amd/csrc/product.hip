@@ -931,6 +931,10 @@ void launch(TileShape t, const Args &a, unsigned grid, hipStream_t s) {
             else hipLaunchKernelGGL((thin_kernel<TYPE, EPI, 4>), g, b, 0, s, a.p);
             return;
         }
+        if constexpr (EPI == TILE_STORE_F32) if (t.m == 64 && t.n == 128) {
+            hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 64, 128, 2, 2>), dim3(grid), dim3(256), 0, s, a);
+            return;
+        }
         if (t.m == 64) {
             hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 64, 64, 4, 1>), dim3(grid), dim3(256), 0, s, a);
             return;
@@ -972,6 +976,13 @@ TileShape tile_shape(TileType type, const TileProduct &p) {
         // 8000 x 512 x 640 10.3 / 9.4, but 8000 x 1024 x 512 (504 blocks) 12.1 /
         // 13.8; float32 results 50 / 35, 16.4 / 9.0, 14.3 / 14.9 (6205 x 512 x
         // 640), 8000 x 2048 x 2048 88 / 118.
+        // 64 x 128 tiles for float32 results widen fewer operands a product; where two
+        // of them a CU replace four 64 x 64 ones (us, 64 / 64 x 128): 6205 x 602 x 512
+        // 15.1 / 12.8, 8000 x 2048 x 512 30.0 / 26.3, 7000 x 512 x 512 12.3 / 10.8; but
+        // 1500 x 4096 x 2048 (three and one and a half) 40 / 45, 8000 x 1024 x 1024 (128 x
+        // 128 ones) 27 / 29, and bfloat16 results 1000 x 4096 x 2048 18.7 / 21.8.
+        const int64_t wide = ((int64_t)p.M + 63) / 64 * (((int64_t)p.N + 127) / 128);
+        if (type == TILE_FP8_EXACT && splits == 1 && wide > 384 && wide <= 512) return TileShape{64, 128};
         if (tiles_of(p.M, p.N, 128) < 256) return TileShape{64, 64};
     }
     if (type == TILE_BF16_NN && tiles_of(p.M, p.N, 128) < 256) return TileShape{32, 128};

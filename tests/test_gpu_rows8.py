@@ -167,7 +167,8 @@ def test_product(n, K, N, transpose, pad, dtype):
 
 
 @pytest.mark.parametrize("n, K, N, transpose", [(3001, 1400, 3500, False), (4000, 1, 3003, True), (4100, 640, 2900, True),
-                                                (33, 4000, 20000, False), (2600, 16500, 4200, False)])
+                                                (33, 4000, 20000, False), (2600, 16500, 4200, False),
+                                                (3333, 300, 970, False), (5000, 515, 601, True)])
 def test_product_of_many_tiles(n, K, N, transpose):
     """Sizes of the large tiles, against float64 on the GPU; the bound of product_bound."""
     g = torch.Generator(device="cuda")
