@@ -121,84 +121,44 @@ __global__ __launch_bounds__(kTB) void join_kernel(int32_t n, int32_t tiles, con
     run_sum[i] = s;
 }
 
-// logits of one piece (float32 rows of ldx, a multiple of 4) joined into the
-// running maximum and sum, a workgroup a row (and grid rows on, beyond 2^20)
-__global__ __launch_bounds__(kTB) void stats_rows_kernel(int32_t n, int32_t P, const float *X, int64_t ldx, const int32_t *labels,
-                                                         int32_t class0, int32_t C, float *run_max, float *run_sum,
-                                                         float *label_logit, int first) {
-    __shared__ float sm[kTB / 64], ss[kTB / 64];
-    for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
-        __syncthreads();   // (the row before has been read)
-        const float *x = X + row * ldx;
-        float m = -INFINITY, s = 0.0f;
-        for (int32_t c = 4 * (int32_t)threadIdx.x; c < P; c += 4 * kTB) {
-            const float4 v = *(const float4 *)(x + c);
-            float y[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int e = 1; e < 4; ++e)
-                if (c + e >= P) y[e] = -INFINITY;
-            const float b = fmaxf(m, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
-            if (b > m) {
-                s *= expf(m - b);   // (0 of the empty sum: exp(-infinity))
-                m = b;
-            }
-            const float base = m == -INFINITY ? 0.0f : m;   // no finite logit yet: the sum stays 0
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s += expf(y[e] - base);
-        }
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const float q = __shfl_xor(m, d), u = __shfl_xor(s, d);
-            join(m, s, q, u);
-        }
-        if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m, ss[threadIdx.x >> 6] = s;
-        __syncthreads();
-        if (threadIdx.x != 0) continue;
-        for (int w = 1; w < kTB / 64; ++w) join(m, s, sm[w], ss[w]);
-        if (!first) join(m, s, run_max[row], run_sum[row]);
-        run_max[row] = m;
-        run_sum[row] = s;
-        const int32_t l = labels[row];
-        if (has_label(l, C) && l >= class0 && l - class0 < P) label_logit[row] = x[l - class0];
-    }
-}
-
-// X <- G, and the column sums of strips of kStrip rows: a thread has a column
+// X <- G (float32), and the column sums of strips of kStrip rows: a thread has a
+// column.  Zeros in the columns past P and the rows past n, which the products read.
 constexpr int kStrip = 32;
 __global__ __launch_bounds__(kTB) void grad_rows_kernel(int32_t n, int32_t P, float *X, int64_t ldx,
                                                         const int32_t *labels, int32_t class0, int32_t C,
                                                         const float *lse, const float *inv_count, float *part) {
     __shared__ float z[kStrip];
     __shared__ int32_t lab[kStrip];
-    const int32_t c = blockIdx.x * kTB + threadIdx.x, strips = (n + kStrip - 1) / kStrip;
+    const int64_t c = (int64_t)blockIdx.x * kTB + threadIdx.x;
+    const int32_t strips = (n + kStrip - 1) / kStrip;
     const float inv = inv_count[0];
     for (int32_t strip = blockIdx.y; strip < strips; strip += gridDim.y) {
-        const int32_t r0 = strip * kStrip, rows = min(kStrip, n - r0);
+        const int64_t r0 = (int64_t)strip * kStrip;
         __syncthreads();
-        if ((int32_t)threadIdx.x < rows) {
-            const int32_t l = labels[r0 + threadIdx.x];
-            z[threadIdx.x] = lse[r0 + threadIdx.x];
+        if (threadIdx.x < kStrip) {
+            const int64_t row = r0 + threadIdx.x;
+            const int32_t l = row < n ? labels[row] : -1;
+            z[threadIdx.x] = row < n ? lse[row] : 0.0f;
             lab[threadIdx.x] = has_label(l, C) ? l : -1;
         }
         __syncthreads();
-        if (c >= P) continue;
+        if (c >= ldx) continue;
         float sum = 0.0f;
         float *x = X + r0 * ldx + c;
         // (eight loads before the first store, behind which the next one would wait)
-        for (int32_t r = 0; r < rows; r += 8, x += 8 * ldx) {
+        for (int32_t r = 0; r < kStrip; r += 8, x += 8 * ldx) {
             float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = r + e < rows ? x[e * ldx] : 0.0f;
+            for (int e = 0; e < 8; ++e) v[e] = lab[r + e] >= 0 && c < P ? x[e * ldx] : 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (r + e >= rows) break;
                 const int32_t l = lab[r + e];
-                const float g = l >= 0 ? (expf(v[e] - z[r + e]) - (class0 + c == l ? 1.0f : 0.0f)) * inv : 0.0f;
+                const float g = l >= 0 && c < P ? (expf(v[e] - z[r + e]) - (class0 + c == l ? 1.0f : 0.0f)) * inv : 0.0f;
                 x[e * ldx] = g;
                 sum += g;
             }
         }
-        part[(int64_t)strip * P + c] = sum;
+        if (c < P) part[(int64_t)strip * P + c] = sum;
     }
 }
 
@@ -240,12 +200,6 @@ __global__ __launch_bounds__(1024) void loss_kernel(int32_t n, int32_t C, const 
     }
 }
 
-__global__ __launch_bounds__(kTB) void add_kernel(int32_t rows, int32_t cols, const float *x, float *y, int64_t ldy) {
-    const int64_t total = (int64_t)rows * cols;
-    for (int64_t i = (int64_t)blockIdx.x * kTB + threadIdx.x; i < total; i += (int64_t)gridDim.x * kTB)
-        y[i / cols * ldy + i % cols] += x[i];
-}
-
 __global__ __launch_bounds__(kTB) void zero_kernel(uint16_t *x, int64_t rows, int64_t cols, int64_t ld) {
     for (int64_t i = (int64_t)blockIdx.x * kTB + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * kTB)
         x[i / cols * ld + i % cols] = 0;
@@ -256,149 +210,115 @@ unsigned grid_of(int64_t work, int64_t most = 8192) {
 }
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
-// How a call is cut and what of the workspace it uses.
+// How a call is cut and what of the workspace it uses.  T: the elements' type.
 struct Plan {
-    int64_t fp, np;            // f and n in whole 64-column pieces (bfloat16)
+    int32_t unit;              // elements of a 128-byte piece
+    int64_t fp, np;            // f and n in whole units
     int32_t piece, pieces;     // classes per piece
-    int32_t split_h, split_w;  // parts of the two gradient products (bfloat16)
+    int32_t split_h, split_w;  // parts of the two gradient products
     bool in_place;             // W_pred's own rows serve as operands
     size_t total;
 };
+template <class T>
 struct Buffers {
-    float *inv_count, *run_max, *run_sum, *label_logit, *lse, *tile_max, *tile_sum, *colpart, *acc, *part, *X, *tmp;
-    uint16_t *H, *W, *G;
-    float *Hz;
-    void *gemm_ws;
-    size_t gemm_bytes;
+    float *inv_count, *run_max, *run_sum, *label_logit, *lse, *tile_max, *tile_sum, *colpart, *acc, *part;
+    T *H, *W, *G;              // (float32: G holds the logits first)
 };
 
-GemmProblem dw_f32(int32_t f, int32_t P, int32_t n) {
-    GemmProblem w{};
-    w.M = f;
-    w.N = P;
-    w.seg[0].K = n;
-    return w;
-}
-
-// About 640 blocks: the library's rule for weight gradients fills four blocks a
-// CU, whose partials here are as wide as the classes (2000 x 256, 10,007 classes,
-// the call: 1 part 445 us, 2 384, 4 359, 6 407, 8 398, 16 461).
-int32_t dw_split_f32(const GemmProblem &w) {
-    const int64_t tiles = ((int64_t)w.M + 127) / 128 * (((int64_t)w.N + 127) / 128);
-    return (int32_t)std::min<int64_t>(gemm_pick_split(1, &w, true), std::max<int64_t>(1, 640 / tiles));
-}
-GemmProblem dh_f32(int32_t n, int32_t f, int32_t P) {
-    GemmProblem d{};
-    d.M = n;
-    d.N = f;
-    d.seg[0].K = P;
-    return d;
-}
-
-// The elements of a piece: bfloat16 G takes 2 bytes each, float32 logits 4.
-constexpr int64_t kPieceElems = (int64_t)1 << 28, kPieceElemsF32 = (int64_t)1 << 26;
+// The elements of a piece: 512 MB of bfloat16 gradient rows, or of float32 logits.
+constexpr int64_t kPieceElems = (int64_t)1 << 28, kPieceElemsF32 = (int64_t)1 << 27;
 
 // W: the weights, or null in the workspace query, which counts on copying them.
-Plan plan_of(int32_t n, int32_t f, int32_t C, bool bf, bool grad, const void *W, void *ws, size_t ws_bytes, Buffers &b) {
+template <class T>
+Plan plan_of(int32_t n, int32_t f, int32_t C, bool grad, const void *W, void *ws, size_t ws_bytes, Buffers<T> &b) {
+    constexpr bool bf = sizeof(T) == 2;
     Plan p{};
     Arena ar(ws, ws_bytes);
-    const int64_t rows = std::max(n, 1);
-    p.fp = up(f, 64);
-    p.np = up(rows, 64);
-    p.in_place = W && (uintptr_t)W % 16 == 0 && C % 8 == 0 && f % 64 == 0;
-    int64_t piece = std::max<int64_t>(256, (bf ? kPieceElems / p.np : kPieceElemsF32 / rows) / 256 * 256);
+    const int64_t rows = std::max(n, 1), u = 128 / sizeof(T);
+    p.unit = (int32_t)u;
+    p.fp = up(f, u);
+    p.np = up(rows, u);
+    p.in_place = W && (uintptr_t)W % 16 == 0 && C % (16 / sizeof(T)) == 0 && f % u == 0;
+    int64_t piece = std::max<int64_t>(256, (bf ? kPieceElems : kPieceElemsF32) / p.np / 256 * 256);
     piece = std::min<int64_t>(piece, up(C, 256));
     p.pieces = (int32_t)((C + piece - 1) / piece);
     p.piece = (int32_t)std::min<int64_t>(piece, C);
-    b = Buffers{};
+    b = Buffers<T>{};
     b.inv_count = ar.take<float>(1);
     b.run_max = ar.take<float>(rows);
     b.run_sum = ar.take<float>(rows);
     b.label_logit = ar.take<float>(rows);
     b.lse = ar.take<float>(rows);
-    if (bf) {
-        // (sized for the smallest tiles: a last, smaller piece may run on them)
-        const int64_t tn = (p.piece + kSmallTile - 1) / kSmallTile;
-        b.tile_max = ar.take<float>(tn * rows);
-        b.tile_sum = ar.take<float>(tn * rows);
-        b.H = ar.take<uint16_t>(p.np * p.fp);
-        // (a piece of whole 64-column parts is read in place where W_pred's rows
-        // are 16-byte aligned and f is whole: only a ragged last piece is copied)
-        const int32_t last = C - (p.pieces - 1) * p.piece;
-        const int64_t copied = std::max(p.in_place && p.piece % 64 == 0 ? 0 : p.piece, p.in_place && last % 64 == 0 ? 0 : last);
-        b.W = copied ? ar.take<uint16_t>(p.fp * up(copied, 64)) : nullptr;
-        if (grad) {
-            const int64_t pp = up(p.piece, 64);
-            b.G = ar.take<uint16_t>(p.np * pp);
-            b.colpart = ar.take<float>((p.np + kSmallRows - 1) / kSmallRows * p.piece);
-            p.split_h = tile_splits(n, f, (int32_t)(pp / 64));
-            p.split_w = tile_splits(f, p.piece, (int32_t)(p.np / 64));
-            b.acc = ar.take<float>((size_t)p.split_h * rows * f);
-            if (p.split_w > 1) b.part = ar.take<float>((size_t)p.split_w * f * p.piece);
-        }
-    } else {
-        b.Hz = ar.take<float>(rows * f);
-        b.X = ar.take<float>(rows * up(p.piece, 4));
-        if (grad) {
-            // (a last, smaller piece may be split more than the others)
-            const int32_t last = C - (p.pieces - 1) * p.piece;
-            for (int32_t P : {p.piece, last}) {
-                const GemmProblem w = dw_f32(f, P, n), h = dh_f32(n, f, P);
-                b.gemm_bytes = std::max(b.gemm_bytes, gemm_workspace_bytes(1, &w, dw_split_f32(w)));
-                b.gemm_bytes = std::max(b.gemm_bytes, gemm_workspace_bytes(1, &h, gemm_pick_split(1, &h, false)));
-            }
-            b.gemm_ws = b.gemm_bytes ? ar.take<char>(b.gemm_bytes) : nullptr;
-            b.colpart = ar.take<float>((rows + kStrip - 1) / kStrip * p.piece);
-            if (p.pieces > 1) b.tmp = ar.take<float>(rows * f);
-        }
+    // (sized for the smallest tiles: a last, smaller piece may run on them)
+    const int64_t tn = (p.piece + kSmallTile - 1) / kSmallTile;
+    b.tile_max = ar.take<float>(tn * rows);
+    b.tile_sum = ar.take<float>(tn * rows);
+    b.H = ar.take<T>(p.np * p.fp);
+    // (a piece of whole units is read in place where W_pred's rows are 16-byte
+    // aligned and f is whole: only a ragged last piece is copied)
+    const int32_t last = C - (p.pieces - 1) * p.piece;
+    const int64_t copied = std::max(p.in_place && p.piece % u == 0 ? 0 : p.piece, p.in_place && last % u == 0 ? 0 : last);
+    b.W = copied ? ar.take<T>(p.fp * up(copied, u)) : nullptr;
+    if (grad) {
+        const int64_t pp = up(p.piece, u);
+        b.G = ar.take<T>(p.np * pp);
+        b.colpart = ar.take<float>((p.np + kSmallRows - 1) / kSmallRows * p.piece);
+        p.split_h = tile_splits(n, f, (int32_t)(pp / u), !bf);
+        p.split_w = tile_splits(f, p.piece, (int32_t)(p.np / u), !bf);
+        b.acc = ar.take<float>((size_t)p.split_h * rows * f);
+        if (p.split_w > 1) b.part = ar.take<float>((size_t)p.split_w * f * p.piece);
     }
     p.total = ar.used + 256;
     return p;
 }
 
-int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, int32_t f, int64_t ldhl, const uint16_t *W,
-              const float *bias, int32_t C, const int32_t *labels, float *loss, float *row_loss, uint16_t *dHL,
-              int64_t lddhl, uint16_t *dW, float *db, hipStream_t s) {
+template <class T>
+int class_loss(const Plan &p, const Buffers<T> &b, const T *HL, int32_t n, int32_t f, int64_t ldhl, const T *W,
+               const float *bias, int32_t C, const int32_t *labels, float *loss, float *row_loss, T *dHL, int64_t lddhl,
+               T *dW, float *db, hipStream_t s) {
+    constexpr bool bf = sizeof(T) == 2;
+    constexpr TileType kNN = bf ? TILE_BF16_NN : TILE_F32_NN;
+    constexpr int64_t E = sizeof(T), U = 128 / E, V = 16 / E;
     int rc;
     // (a single copied piece of W_pred goes along)
     auto w_copy = [&](int32_t c0, int32_t P) {
-        return CopyRows<uint16_t>{(int32_t)p.fp, f, P, W + c0, C, b.W, up(P, 64), nullptr, 0};
+        return CopyRows<T>{(int32_t)p.fp, f, P, W + c0, C, b.W, up(P, U), nullptr, 0};
     };
-    const bool copied = p.pieces == 1 && !(p.in_place && C % 64 == 0);
+    const bool copied = p.pieces == 1 && !(p.in_place && C % U == 0);
     {
-        ProfScope prof(K_CLASS_PREP, s, 0.0, 4.0 * n * f);
-        const CopyRows<uint16_t> h{(int32_t)p.np, n, f, HL, ldhl, b.H, p.fp, labels, C};
-        const unsigned gh = grid_of(p.np * p.fp / 8, 4096), gw = copied ? grid_of(p.fp * up(C, 64) / 8, 4096) : 0;
-        hipLaunchKernelGGL(prep_kernel<uint16_t>, dim3(1 + gh + gw), dim3(kTB), 0, s, n, b.inv_count, h, gh, w_copy(0, C));
+        ProfScope prof(K_CLASS_PREP, s, 0.0, 2.0 * E * n * f);
+        const CopyRows<T> h{(int32_t)p.np, n, f, HL, ldhl, b.H, p.fp, labels, C};
+        const unsigned gh = grid_of(p.np * p.fp / V, 4096), gw = copied ? grid_of(p.fp * up(C, U) / V, 4096) : 0;
+        hipLaunchKernelGGL(prep_kernel<T>, dim3(1 + gh + gw), dim3(kTB), 0, s, n, b.inv_count, h, gh, w_copy(0, C));
         GCN_LAUNCH_CHECK("prep_kernel");
     }
     // the piece's columns of W_pred, rows of ldw elements: in place, or copied to
-    // whole 64 x 64 pieces
-    const uint16_t *Wp = nullptr;
+    // whole pieces
+    const T *Wp = nullptr;
     int64_t ldw = 0;
     auto weights = [&](int32_t c0, int32_t P) -> int {
-        if (p.in_place && P % 64 == 0) {
+        if (p.in_place && P % U == 0) {
             Wp = W + c0;
             ldw = C;
             return GCN_OK;
         }
-        ldw = up(P, 64);
+        ldw = up(P, U);
         Wp = b.W;
         if (copied) return GCN_OK;
-        ProfScope prof(K_CLASS_PREP, s, 0.0, 4.0 * f * P);
-        hipLaunchKernelGGL(copy_rows_kernel<uint16_t>, dim3(grid_of(p.fp * ldw / 8)), dim3(kTB), 0, s, w_copy(c0, P));
+        ProfScope prof(K_CLASS_PREP, s, 0.0, 2.0 * E * f * P);
+        hipLaunchKernelGGL(copy_rows_kernel<T>, dim3(grid_of(p.fp * ldw / V)), dim3(kTB), 0, s, w_copy(c0, P));
         GCN_LAUNCH_CHECK("copy_rows_kernel");
         return GCN_OK;
     };
     auto logits = [&](int32_t c0, int32_t P) {
         TileProduct t{};
         t.A = (const uint8_t *)b.H;
-        t.lda = 2 * p.fp;
+        t.lda = E * p.fp;
         t.B = (const uint8_t *)Wp;
-        t.ldb = 2 * ldw;
+        t.ldb = E * ldw;
         t.M = n;
         t.N = P;
-        t.kt = (int32_t)(p.fp / 64);
+        t.kt = (int32_t)(p.fp / U);
         t.splits = 1;
         t.bias = bias ? bias + c0 : nullptr;
         t.labels = labels;
@@ -414,11 +334,16 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         t.tile_max = b.tile_max;
         t.tile_sum = b.tile_sum;
         t.label_logit = b.label_logit;
+        const bool keep = !bf && p.pieces == 1 && dHL;   // (float32 logits of a single piece stay where G will be)
+        t.C = b.G;
+        t.ldc = up(P, U);
         {
-            ProfScope prof(K_CLASS_STATS, s, 2.0 * n * f * P, 2.0 * ((double)n + P) * f);
-            if ((rc = tile_product(TILE_BF16_NN, TILE_STATS, t, s))) return rc;
+            ProfScope prof(K_CLASS_STATS, s, 2.0 * n * f * P, E * ((double)n + P) * f + (keep ? 4.0 * n * P : 0.0));
+            if constexpr (bf) rc = tile_product(kNN, TILE_STATS, t, s);
+            else rc = tile_product(kNN, keep ? TILE_STATS_STORE : TILE_STATS, t, s);
+            if (rc) return rc;
         }
-        const TileShape sh = tile_shape(TILE_BF16_NN, t);
+        const TileShape sh = tile_shape(kNN, t);
         tiles = (P + sh.n - 1) / sh.n;
         // (up to 16 tiles of 1024 rows the loss's workgroup joins in no more time)
         if (p.pieces == 1 && n <= 1024 && tiles <= 16) break;
@@ -429,123 +354,76 @@ int loss_bf16(const Plan &p, const Buffers &b, const uint16_t *HL, int32_t n, in
         GCN_LAUNCH_CHECK("join_kernel");
     }
     hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, tiles, b.tile_max, b.tile_sum, b.run_max,
-                       b.run_sum, b.label_logit, b.lse,
-                       row_loss, b.inv_count, loss);
+                       b.run_sum, b.label_logit, b.lse, row_loss, b.inv_count, loss);
     GCN_LAUNCH_CHECK("loss_kernel");
     if (!dHL) return GCN_OK;
+    const float *const factor = bf ? b.inv_count : nullptr;   // (float32 G has it already)
     for (int32_t i = 0; i < p.pieces; ++i) {
         const int32_t c0 = i * p.piece, P = std::min(p.piece, C - c0);
-        const int64_t pp = up(P, 64);
+        const int64_t pp = up(P, U);
         if ((rc = weights(c0, P))) return rc;
         TileProduct t = logits(c0, P);
-        t.lse = b.lse;
-        t.scale = b.inv_count;
-        t.G = b.G;
-        t.ldg = pp;
-        t.g_rows = p.np;
-        const int32_t row_tiles = tile_rows(tile_shape(TILE_BF16_NN, t), TILE_STATS, t);   // (those with real rows)
-        t.colpart = row_tiles == 1 ? db + c0 : b.colpart;   // (one row of tiles: the sums themselves)
-        {
-            ProfScope prof(K_CLASS_GRAD, s, 2.0 * n * f * P, 2.0 * ((double)n + P) * f + 4.0 * n * P);
-            if ((rc = tile_product(TILE_BF16_NN, TILE_GRAD, t, s))) return rc;
+        if constexpr (bf) {
+            t.lse = b.lse;
+            t.scale = b.inv_count;
+            t.G = b.G;
+            t.ldg = pp;
+            t.g_rows = p.np;
+            const int32_t row_tiles = tile_rows(tile_shape(kNN, t), TILE_STATS, t);   // (those with real rows)
+            t.colpart = row_tiles == 1 ? db + c0 : b.colpart;   // (one row of tiles: the sums themselves)
+            {
+                ProfScope prof(K_CLASS_GRAD, s, 2.0 * n * f * P, E * ((double)n + P) * f + 4.0 * n * P);
+                if ((rc = tile_product(kNN, TILE_GRAD, t, s))) return rc;
+            }
+            if (row_tiles > 1 && (rc = colsum_reduce_rows(row_tiles, P, b.colpart, db + c0, s))) return rc;
+        } else {
+            const int32_t strips = (n + kStrip - 1) / kStrip;
+            {
+                ProfScope prof(K_CLASS_GRAD, s, p.pieces > 1 ? 2.0 * n * f * P : 0.0, 8.0 * n * P);
+                t.C = b.G;
+                t.ldc = pp;
+                if (p.pieces > 1 && (rc = tile_product(kNN, TILE_STORE_F32, t, s))) return rc;
+                const dim3 g((unsigned)((pp + kTB - 1) / kTB), (unsigned)std::min(65535, strips));
+                hipLaunchKernelGGL(grad_rows_kernel, g, dim3(kTB), 0, s, n, P, b.G, pp, labels, c0, C, b.lse,
+                                   b.inv_count, strips == 1 ? db + c0 : b.colpart);
+                GCN_LAUNCH_CHECK("grad_rows_kernel");
+            }
+            if (strips > 1 && (rc = colsum_reduce_rows(strips, P, b.colpart, db + c0, s))) return rc;
         }
-        if (row_tiles > 1 && (rc = colsum_reduce_rows(row_tiles, P, b.colpart, db + c0, s))) return rc;
         ProfScope prof(K_CLASS_PRODUCT, s, 4.0 * n * f * P, 4.0 * n * P);
         TileProduct h{};
         h.A = (const uint8_t *)b.G;
-        h.lda = 2 * pp;
+        h.lda = E * pp;
         h.B = (const uint8_t *)Wp;
-        h.ldb = 2 * ldw;
+        h.ldb = E * ldw;
         h.M = n;
         h.N = f;
-        h.kt = (int32_t)(pp / 64);
+        h.kt = (int32_t)(pp / U);
         h.splits = p.split_h;
         h.acc = b.acc;
         h.accumulate = i > 0;
         TileProduct w{};
         w.A = (const uint8_t *)b.H;
-        w.lda = 2 * p.fp;
+        w.lda = E * p.fp;
         w.B = (const uint8_t *)b.G;
-        w.ldb = 2 * pp;
+        w.ldb = E * pp;
         w.M = f;
         w.N = P;
-        w.kt = (int32_t)(p.np / 64);
+        w.kt = (int32_t)(p.np / U);
         w.splits = p.split_w;
         if (p.split_w > 1) {
             w.acc = b.part;
         } else {
             w.C = dW + c0;
             w.ldc = C;
-            w.scale = b.inv_count;
+            w.scale = factor;
         }
-        if ((rc = tile_products(h, w, p.split_w > 1 ? TILE_PARTIAL : TILE_STORE, s))) return rc;
+        if ((rc = tile_products(!bf, h, w, p.split_w > 1 ? TILE_PARTIAL : bf ? TILE_STORE : TILE_STORE_F32, s))) return rc;
         if (p.split_w > 1 &&
-            (rc = tile_reduce(p.split_w, f, P, b.part, dW + c0, 1, C, s, 0, 0, nullptr, nullptr, b.inv_count)))
+            (rc = tile_reduce(p.split_w, f, P, b.part, dW + c0, bf, C, s, 0, 0, nullptr, nullptr, factor)))
             return rc;
     }
-    return tile_reduce(p.split_h, n, f, b.acc, dHL, 1, lddhl, s, 0, 0, nullptr, nullptr, b.inv_count);
-}
-
-int loss_f32(const Plan &p, const Buffers &b, const float *HL, int32_t n, int32_t f, int64_t ldhl, const float *W,
-             const float *bias, int32_t C, const int32_t *labels, float *loss, float *row_loss, float *dHL, int64_t lddhl,
-             float *dW, float *db, hipStream_t s) {
-    int rc;
-    const CopyRows<float> h{n, n, f, HL, ldhl, b.Hz, f, labels, C};
-    const unsigned gh = grid_of((int64_t)n * f / 4, 4096);
-    hipLaunchKernelGGL(prep_kernel<float>, dim3(1 + gh), dim3(kTB), 0, s, n, b.inv_count, h, gh, h);
-    GCN_LAUNCH_CHECK("class_prep");
-    auto logits = [&](int32_t c0, int32_t P) {
-        GemmProblem g{};
-        g.M = n;
-        g.N = P;
-        g.C = b.X;
-        g.ldc = up(P, 4);
-        g.bias = bias ? bias + c0 : nullptr;
-        g.seg[0] = GemmSeg{b.Hz, f, W + c0, C, f};
-        return gemm(L_NN, 1, &g, 0, 1, nullptr, 0, s);
-    };
-    for (int32_t i = 0; i < p.pieces; ++i) {
-        const int32_t c0 = i * p.piece, P = std::min(p.piece, C - c0);
-        if ((rc = logits(c0, P))) return rc;
-        ProfScope prof(K_CLASS_STATS, s, 0.0, 4.0 * n * P);
-        hipLaunchKernelGGL(stats_rows_kernel, dim3((unsigned)std::min(n, 1 << 20)), dim3(kTB), 0, s, n, P, b.X, up(P, 4), labels, c0, C,
-                           b.run_max, b.run_sum, b.label_logit, i == 0);
-        GCN_LAUNCH_CHECK("stats_rows_kernel");
-    }
-    hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, 0, b.tile_max, b.tile_sum, b.run_max,
-                       b.run_sum, b.label_logit, b.lse,
-                       row_loss, b.inv_count, loss);
-    GCN_LAUNCH_CHECK("loss_kernel");
-    if (!dHL) return GCN_OK;
-    for (int32_t i = 0; i < p.pieces; ++i) {
-        const int32_t c0 = i * p.piece, P = std::min(p.piece, C - c0);
-        const int64_t ldx = up(P, 4);
-        // (a single piece's logits are still in place)
-        if (p.pieces > 1 && (rc = logits(c0, P))) return rc;
-        {
-            ProfScope prof(K_CLASS_GRAD, s, 0.0, 8.0 * n * P);
-            const dim3 g((unsigned)((P + kTB - 1) / kTB), (unsigned)std::min(65535, (n + kStrip - 1) / kStrip));
-            hipLaunchKernelGGL(grad_rows_kernel, g, dim3(kTB), 0, s, n, P, b.X, ldx, labels, c0, C, b.lse, b.inv_count,
-                               b.colpart);
-            GCN_LAUNCH_CHECK("grad_rows_kernel");
-        }
-        if ((rc = colsum_reduce_rows((n + kStrip - 1) / kStrip, P, b.colpart, db + c0, s))) return rc;
-        GemmProblem w = dw_f32(f, P, n);
-        w.C = dW + c0;
-        w.ldc = C;
-        w.seg[0] = GemmSeg{b.Hz, f, b.X, ldx, n};
-        if ((rc = gemm(L_TN, 1, &w, 0, dw_split_f32(w), b.gemm_ws, b.gemm_bytes, s))) return rc;
-        GemmProblem d = dh_f32(n, f, P);
-        d.C = i ? b.tmp : dHL;
-        d.ldc = i ? f : lddhl;
-        d.seg[0] = GemmSeg{b.X, ldx, W + c0, C, P};
-        if ((rc = gemm(L_NT, 1, &d, 0, gemm_pick_split(1, &d, false), b.gemm_ws, b.gemm_bytes, s))) return rc;
-        if (i) {
-            hipLaunchKernelGGL(add_kernel, dim3(grid_of((int64_t)n * f)), dim3(kTB), 0, s, n, f, b.tmp, dHL, lddhl);
-            GCN_LAUNCH_CHECK("add_kernel");
-        }
-    }
-    return GCN_OK;
+    return tile_reduce(p.split_h, n, f, b.acc, dHL, bf, lddhl, s, 0, 0, nullptr, nullptr, factor);
 }
 
 }  // namespace
@@ -557,8 +435,10 @@ extern "C" {
 
 size_t gcn_class_loss_workspace_bytes(int32_t n, int32_t f, int32_t C, gcn_rows_type type, int need_grad) {
     if (n < 0 || f <= 0 || C <= 0 || std::max({n, f, C}) > kMostRows) return 0;
-    Buffers b;
-    return plan_of(n, f, C, type == GCN_ROWS_BF16, need_grad != 0, nullptr, nullptr, 0, b).total;
+    Buffers<uint16_t> b;
+    Buffers<float> c;
+    return type == GCN_ROWS_BF16 ? plan_of(n, f, C, need_grad != 0, nullptr, nullptr, 0, b).total
+                                 : plan_of(n, f, C, need_grad != 0, nullptr, nullptr, 0, c).total;
 }
 
 int gcn_class_loss(const void *HL, int32_t n, int32_t f, int32_t ldhl, const void *W_pred, const float *b_pred,
@@ -577,8 +457,9 @@ int gcn_class_loss(const void *HL, int32_t n, int32_t f, int32_t ldhl, const voi
     const uintptr_t el = bf ? 1 : 3;
     GCN_REQUIRE((((uintptr_t)HL | (uintptr_t)W_pred | (uintptr_t)dHL | (uintptr_t)dW_pred) & el) == 0, GCN_EINVAL,
                 "gcn_class_loss: misaligned operand");
-    Buffers b;
-    const Plan p = plan_of(n, f, C, bf, grad, W_pred, ws, ws_bytes, b);
+    Buffers<uint16_t> b;
+    Buffers<float> c;
+    const Plan p = bf ? plan_of(n, f, C, grad, W_pred, ws, ws_bytes, b) : plan_of(n, f, C, grad, W_pred, ws, ws_bytes, c);
     GCN_REQUIRE(ws && ((uintptr_t)ws & 255) == 0 && ws_bytes >= p.total, GCN_EWORKSPACE,
                 "gcn_class_loss: workspace %zu < %zu bytes, or not 256-byte aligned", ws_bytes, p.total);
     hipStream_t s = (hipStream_t)stream;
@@ -597,10 +478,10 @@ int gcn_class_loss(const void *HL, int32_t n, int32_t f, int32_t ldhl, const voi
         return rc;
     }
     if (bf)
-        return loss_bf16(p, b, (const uint16_t *)HL, n, f, ldhl, (const uint16_t *)W_pred, b_pred, C, labels, loss,
-                         row_loss, (uint16_t *)dHL, lddhl, (uint16_t *)dW_pred, db_pred, s);
-    return loss_f32(p, b, (const float *)HL, n, f, ldhl, (const float *)W_pred, b_pred, C, labels, loss, row_loss,
-                    (float *)dHL, lddhl, (float *)dW_pred, db_pred, s);
+        return class_loss(p, b, (const uint16_t *)HL, n, f, ldhl, (const uint16_t *)W_pred, b_pred, C, labels, loss, row_loss,
+                          (uint16_t *)dHL, lddhl, (uint16_t *)dW_pred, db_pred, s);
+    return class_loss(p, c, (const float *)HL, n, f, ldhl, (const float *)W_pred, b_pred, C, labels, loss, row_loss,
+                      (float *)dHL, lddhl, (float *)dW_pred, db_pred, s);
 }
 
 }  // extern "C"

@@ -58,14 +58,16 @@ struct Frag {
     uint4 lo, hi;
 };
 
-constexpr bool is_bf16(int type) { return type != TILE_FP8 && type != TILE_FP8_EXACT; }
+constexpr bool is_fp8(int type) { return type == TILE_FP8 || type == TILE_FP8_EXACT; }
+constexpr bool is_f32(int type) { return type == TILE_F32 || type == TILE_F32_TN || type == TILE_F32_NN; }
 // which operands are stored along the other way
-constexpr bool km_a(int type) { return type == TILE_BF16_TN; }
-constexpr bool km_b(int type) { return type == TILE_BF16_TN || type == TILE_BF16_NN; }
+constexpr bool km_a(int type) { return type == TILE_BF16_TN || type == TILE_F32_TN; }
+constexpr bool km_b(int type) { return km_a(type) || type == TILE_BF16_NN || type == TILE_F32_NN; }
+constexpr bool is_stats(int epi) { return epi == TILE_STATS || epi == TILE_STATS_STORE; }
 
 template <int TYPE>
 __device__ __forceinline__ void mma(f32x4 &acc, const Frag &a, const Frag &b, int sa, int sb) {
-    if constexpr (is_bf16(TYPE)) {
+    if constexpr (!is_fp8(TYPE)) {
         acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16v8, b.lo),
                                                       __builtin_bit_cast(bf16v8, a.lo), acc, 0, 0, 0);
         acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16v8, b.hi),
@@ -95,6 +97,22 @@ __device__ __forceinline__ uint2 km_read(const char *p) {
 __device__ __forceinline__ Frag km_frag(const char *p) {
     const uint2 a = km_read(p), b = km_read(p + 4 * 256), c = km_read(p + 32 * 256), d = km_read(p + 36 * 256);
     return Frag{make_uint4(a.x, a.y, b.x, b.y), make_uint4(c.x, c.y, d.x, d.y)};
+}
+
+// The same of float32: a stage holds 32 k-rows of 128 elements, 32 chunks each,
+// chunk c of k-row k at place c ^ 4 (k / 4 % 4), which keeps the k-rows 4 g + q that
+// one read takes on different banks; an element at a time.
+__device__ __forceinline__ Frag km_frag_f32(const char *tile, int lane, int col) {
+    const int fr = lane & 15, g = lane >> 4;
+    const char *p = tile + 4 * g * 512 + (((col + fr) / 4) ^ (4 * g)) * 16 + (fr & 3) * 4;
+    Frag f;
+    uint32_t *l = (uint32_t *)&f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        l[q] = *(const uint32_t *)(p + q * 512);
+        l[q + 4] = *(const uint32_t *)(p + (q + 16) * 512);
+    }
+    return f;
 }
 
 // eight e4m3 values as bfloat16, exactly
@@ -170,7 +188,7 @@ __device__ __forceinline__ void load_extras(const TileProduct &p, const Coord &c
     const int c0 = c.tn * BN + wave % WN * (BN / WN) + 4 * (lane >> 4);
     if constexpr (EPI != TILE_PARTIAL) {
         // (the logits' columns past the last class: minus infinity)
-        const float past = EPI == TILE_STATS || EPI == TILE_GRAD ? -INFINITY : 0.0f;
+        const float past = is_stats(EPI) || EPI == TILE_GRAD ? -INFINITY : 0.0f;
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
@@ -179,8 +197,8 @@ __device__ __forceinline__ void load_extras(const TileProduct &p, const Coord &c
                 x.bias[j][e] = col < p.N ? (p.bias ? p.bias[col] : 0.0f) : past;
             }
     }
-    if constexpr (EPI != TILE_PARTIAL && EPI != TILE_STATS) x.scale = p.scale ? p.scale[0] : 1.0f;
-    if constexpr (EPI == TILE_STATS || EPI == TILE_GRAD) {
+    if constexpr (EPI != TILE_PARTIAL && !is_stats(EPI)) x.scale = p.scale ? p.scale[0] : 1.0f;
+    if constexpr (is_stats(EPI) || EPI == TILE_GRAD) {
 #pragma unroll
         for (int i = 0; i < FM; ++i) x.lab[i] = label_of(p, r0 + 16 * i);
     }
@@ -192,6 +210,28 @@ __device__ __forceinline__ void load_extras(const TileProduct &p, const Coord &c
 
 // acc[i][j]: row m0 + 16 i + lane % 16 of C, columns n0 + 16 j + 4 (lane / 16)
 // .. + 3 of the wavefront's block; `scratch`: the idle operand LDS.
+// float32 results, row by row: a wavefront's stores fill whole lines one after another
+template <int FM, int FN>
+__device__ __forceinline__ void store_f32(const f32x4 (&acc)[FM][FN], const TileProduct &p, int r0, int c0) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int row = r0 + 16 * i;
+        if (row >= p.M) continue;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int col = c0 + 16 * j;
+            float *d = (float *)p.C + (int64_t)row * p.ldc + col;
+            if (col + 4 <= p.N) {
+                store16(d, __builtin_bit_cast(uint4, acc[i][j]));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col + e < p.N) d[e] = acc[i][j][e];
+            }
+        }
+    }
+}
+
 template <int EPI, int BM, int BN, int WM, int WN, int FM, int FN>
 __device__ __forceinline__ void finish(const Args &a, const Coord &c, const Extras<FM, FN> &x,
                                        f32x4 (&acc)[FM][FN], char *scratch) {
@@ -218,24 +258,7 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, const Extr
                            c.tn * BN + wn * (BN / WN), p.M, p.N);
             return;
         }
-        // (row by row: a wavefront's stores fill whole lines one after another)
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const int row = r0 + 16 * i;
-            if (row >= p.M) continue;
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int col = c0 + 16 * j;
-                float *d = (float *)p.C + (int64_t)row * p.ldc + col;
-                if (col + 4 <= p.N) {
-                    store16(d, __builtin_bit_cast(uint4, acc[i][j]));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (col + e < p.N) d[e] = acc[i][j][e];
-                }
-            }
-        }
+        store_f32<FM, FN>(acc, p, r0, c0);
     } else if constexpr (EPI == TILE_PARTIAL) {
         float *base = p.acc + (int64_t)c.split * p.M * p.N;
 #pragma unroll
@@ -263,9 +286,10 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, const Extr
             for (int j = 0; j < FN; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[i][j][e] += x.bias[j][e];
+        if constexpr (EPI == TILE_STATS_STORE) store_f32<FM, FN>(acc, p, r0, c0);
         constexpr float kLog2e = 1.44269504088896340736f;
         const int w0 = c.tn * BN + wn * (BN / WN);   // the wavefront's first column
-        if constexpr (EPI == TILE_STATS) {
+        if constexpr (is_stats(EPI)) {
             // a row's columns lie in 4 lanes of WN wavefronts: maximum and sum
             // over the lane's own, two exchanges, then LDS across wavefronts
             float2 *part = (float2 *)scratch;   // [WN][BM]
@@ -412,7 +436,7 @@ __device__ __forceinline__ void turn() {
 // kScalePieces pieces at a time.
 constexpr int kScalePieces = 64;
 constexpr int small_lds(int type, int BM, int BN) {
-    return 2 * (BM + BN) * kPiece + (is_bf16(type) ? 0 : kScalePieces * (BM + 1));
+    return 2 * (BM + BN) * kPiece + (is_fp8(type) ? kScalePieces * (BM + 1) : 0);
 }
 template <int TYPE, int EPI, int BM, int BN, int WM, int WN>
 __device__ __forceinline__ void small_tile(const Args &a, uint32_t block, char *lds) {
@@ -421,7 +445,7 @@ __device__ __forceinline__ void small_tile(const Args &a, uint32_t block, char *
     constexpr int LA = BM * kPiece / 16 / T, LB = BN * kPiece / 16 / T;
     static_assert(LA * T * 16 == BM * kPiece && LB * T * 16 == BN * kPiece, "whole chunks per lane");
     static_assert(kRows8Block % BN == 0, "a tile's columns share a scale");
-    constexpr bool SCALED = !is_bf16(TYPE);
+    constexpr bool SCALED = is_fp8(TYPE);
     Coord c;
     if (!coord_of(a, block, c)) return;
     const TileProduct &p = a.p;
@@ -430,16 +454,17 @@ __device__ __forceinline__ void small_tile(const Args &a, uint32_t block, char *
     const int m0 = c.tm * BM, n0 = c.tn * BN;
     const int kt0 = c.split * a.kt_per_split, nt = min(a.kt_per_split, p.kt - kt0);
     constexpr bool KA = km_a(TYPE), KB = km_b(TYPE);
-    static_assert((!KA || BM == 128) && (!KB || BN == 128), "k-rows of 16 chunks");
-    const int64_t step_a = KA ? 64 * p.lda : kPiece, step_b = KB ? 64 * p.ldb : kPiece;
+    static_assert((!KA || BM == 128) && (!KB || BN == 128), "k-rows of 128 elements");
+    constexpr int E = is_f32(TYPE) ? 4 : 2, V = 16 / E, CH = 128 / V;   // of k-major operands: bytes, elements a chunk, chunks a row
+    const int64_t step_a = KA ? kPiece / E * p.lda : kPiece, step_b = KB ? kPiece / E * p.ldb : kPiece;
     // Copy u of a thread: tile row (u T + thread) / 8, stored chunk thread % 8,
     // which holds the row's chunk (thread % 8) ^ (row % 8); rows past the extent
     // are clamped (their products are dropped).  k-major: k-row (u T + thread) /
-    // 16, its chunks clamped to the last whole one.
+    // CH, its chunks clamped to the last whole one.
     const int lr = threadIdx.x >> 3, chunk = ((threadIdx.x & 7) ^ (lr & 7)) * 16;
     auto km_at = [&](int64_t ld, int x0, int extent, int u) {
-        const int k = (u * T + threadIdx.x) >> 4, ch = 8 * ((threadIdx.x & 15) ^ (4 * (k & 3)));
-        return k * ld + 2 * (int64_t)min(x0 + ch, ((extent + 7) & ~7) - 8);
+        const int k = (u * T + threadIdx.x) / CH, ch = V * ((threadIdx.x % CH) ^ (4 * ((is_f32(TYPE) ? k >> 2 : k) & 3)));
+        return k * ld + E * (int64_t)min(x0 + ch, ((extent + V - 1) & -V) - V);
     };
     const uint8_t *ga[LA], *gb[LB];
 #pragma unroll
@@ -464,12 +489,12 @@ __device__ __forceinline__ void small_tile(const Args &a, uint32_t block, char *
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     Extras<FM, FN> extras;
-    constexpr bool kEarly = FM == 1 && (EPI == TILE_STATS || EPI == TILE_GRAD);
+    constexpr bool kEarly = FM == 1 && (is_stats(EPI) || EPI == TILE_GRAD);
     if constexpr (kEarly) load_extras<EPI, BM, BN, WM, WN>(p, c, extras);
     const int fr = lane & 15, g = lane >> 4;
     const int o0 = (g ^ (fr & 7)) * 16, o1 = ((g + 4) ^ (fr & 7)) * 16;   // (a fragment's rows start at multiples of 16)
     auto frag = [&](const char *tile, int row, bool km) {
-        if (km) return km_frag(tile + km_place(lane, row / 8));
+        if (km) return is_f32(TYPE) ? km_frag_f32(tile, lane, row) : km_frag(tile + km_place(lane, row / 8));
         const char *q = tile + (row + fr) * kPiece;
         return Frag{*(const uint4 *)(q + o0), *(const uint4 *)(q + o1)};
     };
@@ -535,6 +560,20 @@ __device__ __forceinline__ void small_tile(const Args &a, uint32_t block, char *
                     for (int q = 0; q < 4; ++q) acc[i][j][q] += __builtin_amdgcn_ldexpf(z[q], e);
                 }
             }
+        } else if constexpr (is_f32(TYPE)) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const Frag fa = frag(ta, wm * (BM / WM) + 16 * i, KA);
+                // element q of the lo and hi chunks: k = 4 g + q, 16 + 4 g + q; the columns
+                // innermost, so that a product does not wait for the sum before it
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                            __builtin_bit_cast(f32x4, q < 4 ? fb[j].lo : fb[j].hi)[q & 3],
+                            __builtin_bit_cast(f32x4, q < 4 ? fa.lo : fa.hi)[q & 3], acc[i][j], 0, 0, 0);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
@@ -547,7 +586,10 @@ __device__ __forceinline__ void small_tile(const Args &a, uint32_t block, char *
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) asm volatile("" : "+v"(acc[i][j]));
+            for (int j = 0; j < FN; ++j) {
+                if constexpr (TYPE == TILE_FP8_EXACT) asm volatile("" : "+v"(acc[i][j]));
+                else asm volatile("" : "+a"(acc[i][j]));   // (where the products leave them: pinned elsewhere they are moved there and back)
+            }
     }
     __syncthreads();
     if constexpr (!kEarly) load_extras<EPI, BM, BN, WM, WN>(p, c, extras);
@@ -940,13 +982,13 @@ void launch(TileShape t, const Args &a, unsigned grid, hipStream_t s) {
             return;
         }
     }
-    if constexpr (TYPE == TILE_BF16_NN) {
+    if constexpr (TYPE == TILE_BF16_NN || TYPE == TILE_F32_NN) {
         if (t.m == 32) {
             hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 32, 128, 2, 2>), dim3(grid), dim3(256), 0, s, a);
             return;
         }
     }
-    if constexpr (TYPE != TILE_FP8_EXACT && !(TYPE == TILE_FP8 && EPI == TILE_PARTIAL)) {
+    if constexpr (TYPE != TILE_FP8_EXACT && !is_f32(TYPE) && !(TYPE == TILE_FP8 && EPI == TILE_PARTIAL)) {
         if (t.m == kBigT) {
             hipLaunchKernelGGL((big_kernel<TYPE, EPI>), dim3(grid), dim3(kBigThreads), 0, s, a);
             return;
@@ -963,7 +1005,7 @@ int64_t tiles_of(int64_t M, int64_t N, int64_t t) { return ((M + t - 1) / t) * (
 TileShape tile_shape(TileType type, const TileProduct &p) {
     const int32_t splits = std::max(1, p.splits), per = (p.kt + splits - 1) / splits;
     if (splits > 1 && (type == TILE_FP8 || type == TILE_FP8_EXACT)) return TileShape{64, 64};   // (split8)
-    const bool big = type != TILE_FP8_EXACT && tiles_of(p.M, p.N, kBigT) * splits >= 160 && per >= 4 &&
+    const bool big = type != TILE_FP8_EXACT && !is_f32(type) && tiles_of(p.M, p.N, kBigT) * splits >= 160 && per >= 4 &&
                      (type != TILE_FP8 || per <= kBigPieces) && std::max(p.lda, p.ldb) < (1 << 24);
     if (big) return TileShape{kBigT, kBigT};
     if (type == TILE_FP8 || type == TILE_FP8_EXACT) {
@@ -985,11 +1027,13 @@ TileShape tile_shape(TileType type, const TileProduct &p) {
         if (type == TILE_FP8_EXACT && splits == 1 && wide > 384 && wide <= 512) return TileShape{64, 128};
         if (tiles_of(p.M, p.N, 128) < 256) return TileShape{64, 64};
     }
-    if (type == TILE_BF16_NN && tiles_of(p.M, p.N, 128) < 256) return TileShape{32, 128};
+    if ((type == TILE_BF16_NN || type == TILE_F32_NN) && tiles_of(p.M, p.N, 128) < 256) return TileShape{32, 128};
     return TileShape{128, 128};
 }
 
-int32_t tile_splits(int32_t M, int32_t N, int32_t kt) {
+int32_t tile_splits(int32_t M, int32_t N, int32_t kt, bool f32) {
+    if (f32)   // one round of two blocks a CU, four pieces or more each
+        return (int32_t)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(1, tiles_of(M, N, 128)), kt / 4, 64}));
     // large tiles: one round of the 256 CUs; small ones: two blocks a CU, as
     // long as a part has two pieces
     const int64_t tiles = std::max<int64_t>(1, tiles_of(M, N, kBigT));
@@ -1025,22 +1069,24 @@ static int tile_args(const TileShape &t, TileEpilogue epi, const TileProduct &p,
     return GCN_OK;
 }
 
-int tile_products(const TileProduct &nt, const TileProduct &tn, TileEpilogue epi, hipStream_t s) {
-    const TileShape t = tile_shape(TILE_BF16, nt), u = tile_shape(TILE_BF16_TN, tn);
+int tile_products(bool f32, const TileProduct &nt, const TileProduct &tn, TileEpilogue epi, hipStream_t s) {
+    const TileType tt = f32 ? TILE_F32 : TILE_BF16, ut = f32 ? TILE_F32_TN : TILE_BF16_TN;
+    const TileShape t = tile_shape(tt, nt), u = tile_shape(ut, tn);
     int rc;
     if (t.m != 128 || u.m != 128) {
-        if ((rc = tile_product(TILE_BF16, TILE_PARTIAL, nt, s))) return rc;
-        return tile_product(TILE_BF16_TN, epi, tn, s);
+        if ((rc = tile_product(tt, TILE_PARTIAL, nt, s))) return rc;
+        return tile_product(ut, epi, tn, s);
     }
     Args a, b;
     unsigned ga, gb;
     if ((rc = tile_args(t, TILE_PARTIAL, nt, a, ga)) || (rc = tile_args(u, epi, tn, b, gb))) return rc;
-    if (epi == TILE_STORE)
-        hipLaunchKernelGGL((pair_kernel<TILE_BF16, TILE_PARTIAL, TILE_BF16_TN, TILE_STORE>), dim3(ga + gb), dim3(256), 0,
-                           s, a, b, ga);
-    else
-        hipLaunchKernelGGL((pair_kernel<TILE_BF16, TILE_PARTIAL, TILE_BF16_TN, TILE_PARTIAL>), dim3(ga + gb), dim3(256), 0,
-                           s, a, b, ga);
+#define GCN_PAIR(NT, TN, EPI) \
+    hipLaunchKernelGGL((pair_kernel<NT, TILE_PARTIAL, TN, EPI>), dim3(ga + gb), dim3(256), 0, s, a, b, ga)
+    if (f32 && epi == TILE_STORE_F32) GCN_PAIR(TILE_F32, TILE_F32_TN, TILE_STORE_F32);
+    else if (f32) GCN_PAIR(TILE_F32, TILE_F32_TN, TILE_PARTIAL);
+    else if (epi == TILE_STORE) GCN_PAIR(TILE_BF16, TILE_BF16_TN, TILE_STORE);
+    else GCN_PAIR(TILE_BF16, TILE_BF16_TN, TILE_PARTIAL);
+#undef GCN_PAIR
     GCN_LAUNCH_CHECK("pair_kernel");
     return GCN_OK;
 }
@@ -1054,6 +1100,9 @@ int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStrea
     // (the pairs that the entry points use)
     if (type == TILE_BF16_NN && epi == TILE_STATS) launch<TILE_BF16_NN, TILE_STATS>(t, a, grid, s);
     else if (type == TILE_BF16_NN && epi == TILE_GRAD) launch<TILE_BF16_NN, TILE_GRAD>(t, a, grid, s);
+    else if (type == TILE_F32_NN && epi == TILE_STATS) launch<TILE_F32_NN, TILE_STATS>(t, a, grid, s);
+    else if (type == TILE_F32_NN && epi == TILE_STATS_STORE) launch<TILE_F32_NN, TILE_STATS_STORE>(t, a, grid, s);
+    else if (type == TILE_F32_NN && epi == TILE_STORE_F32) launch<TILE_F32_NN, TILE_STORE_F32>(t, a, grid, s);
     else if (type == TILE_BF16 && epi == TILE_PARTIAL) launch<TILE_BF16, TILE_PARTIAL>(t, a, grid, s);
     else if (type == TILE_BF16_TN && epi == TILE_STORE) launch<TILE_BF16_TN, TILE_STORE>(t, a, grid, s);
     else if (type == TILE_BF16_TN && epi == TILE_PARTIAL) launch<TILE_BF16_TN, TILE_PARTIAL>(t, a, grid, s);

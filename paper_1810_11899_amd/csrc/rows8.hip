@@ -426,7 +426,7 @@ GradPlan plan_grad(int32_t n, int32_t f, int32_t N, void *ws, size_t ws_bytes, G
     p.nz = (n + 63) / 64 * 64;
     p.Np = (N + 7) / 8 * 8;
     p.fp = (f + 7) / 8 * 8;
-    p.splits = tile_splits(f, N, p.nz / 64);
+    p.splits = tile_splits(f, N, p.nz / 64, false);
     // strips: about 2048 workgroups, at least 16 rows each
     const int64_t most = std::max<int64_t>(1, 2048 / blocks8(N));
     p.strip = (int32_t)std::max<int64_t>(16, ((p.nz + most - 1) / most + 15) / 16 * 16);
