@@ -1,11 +1,12 @@
-// Products C = A B^T of bfloat16 or 8-bit rows on the matrix cores, with the
-// epilogues of the 8-bit layer products and of the many-class loss.
+// Products C = A B^T of bfloat16, 8-bit or float32 rows on the matrix cores, with
+// the epilogues of the 8-bit layer products and of the many-class loss.
 //
-// Both operands come in rows of 128-byte pieces (64 bfloat16 or 128 e4m3
-// values), so one tile loop serves both types: a piece of each tile row is
+// Both operands come in rows of 128-byte pieces (32 float32, 64 bfloat16 or 128
+// e4m3 values), so one tile loop serves all types: a piece of each tile row is
 // copied from global memory straight into LDS (16 bytes a lane), and a lane's
 // share of a fragment is the two 16-byte chunks g and g + 4 of a row (g = lane
-// / 16): two k-steps of v_mfma_f32_16x16x32_bf16, or the one of
+// / 16): eight k-steps of v_mfma_f32_16x16x4_f32, two of
+// v_mfma_f32_16x16x32_bf16, or the one of
 // v_mfma_scale_f32_16x16x128_f8f6f4.  Which 16 of the 128 columns a chunk holds
 // does not matter as long as both operands agree.  LDS rows are 128 bytes with
 // their chunks XOR-swizzled by row, so that the 16 lanes of a fragment read
