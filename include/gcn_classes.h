@@ -6,7 +6,8 @@
  * and 16,384 vertices they are 8.6 GB.  gcn_class_loss works through the
  * classes in pieces: the logits of a piece exist only inside the product's
  * registers, where they join the running maximum and sum of each row; the
- * gradient computes them again, piece by piece.
+ * gradient computes them again, piece by piece.  (With float32 rows the gradient
+ * has one piece of logits in the workspace: 512 MB, or 256 classes.)
  *
  * Conventions are those of gcn_layer.h, with the element types of gcn_rows8.h.
  * The call may be captured into a HIP graph.

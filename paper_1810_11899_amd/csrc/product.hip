@@ -636,6 +636,10 @@ __global__ __launch_bounds__(256) void pair_kernel(Args a, Args b, uint32_t firs
 // copies over them go out in quarter q + 2, turn 2q + 4 at the earliest.  A
 // wavefront waits for its own copies of what quarter q + 1 reads in quarter q,
 // turn 2q + 1 at the latest; quarter q + 1 reads at turn 2q + 2 at the earliest.
+//
+// 16,384 x 4096 x 8192 of 8-bit operands: 450 us, 2.4 PFLOP/s; 16,384 x 1024 x
+// 16,384 of bfloat16 ones: 410-425 us, 1300 TFLOP/s.  The chip's power bounds both
+// (zeros instead of random operands: 505 -> 385 us).
 constexpr int kBigT = 256, kBigThreads = 512;
 constexpr int kRegion = 128 * kPiece, kBuffer = 4 * kRegion;
 constexpr int kBigPieces = 120;                          // pieces whose scales fit in LDS
@@ -843,7 +847,8 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
 // Up to 16 FM rows: the weights are read once and there is little to multiply, so
 // nothing goes through LDS on the way in.  A workgroup has 16 columns of C and
 // all rows; its eight wavefronts take every eighth piece of K, fragments straight
-// from memory to registers, and add their sums in wavefront order.
+// from memory to registers, and add their sums in wavefront order.  1 x 4096 x 4096:
+// 7.2 us, 2.3 TB/s; the launch and a chain of four loads are most of it.
 constexpr int kThinWaves = 8, kThin = 64;   // wavefronts; the most rows
 template <int TYPE, int EPI, int FM>
 __global__ __launch_bounds__(64 * kThinWaves) void thin_kernel(TileProduct p) {

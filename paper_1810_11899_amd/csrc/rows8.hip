@@ -86,7 +86,7 @@ __device__ __forceinline__ void pack_block(const float (&x)[8], uint8_t *q, uint
 }
 
 // One block of 128 columns to 16 lanes, the lanes of a wavefront along the row
-// (whole lines both ways).
+// (whole lines both ways).  Bound by memory: 65,536 x 1024 bfloat16 48 us, 4.2 TB/s.
 template <bool BF>
 __global__ __launch_bounds__(kTB) void pack_kernel(int64_t blocks, int32_t per_row, int32_t f, const void *X,
                                                    int64_t ldx, uint8_t *q, int64_t ldq, uint8_t *scale,
@@ -209,7 +209,9 @@ __global__ __launch_bounds__(kTB) void pack_weights_kernel(int32_t K, int32_t N,
 // column sums of a strip of rows; and, when wanted, dZ's 8-bit rows.  One
 // block of 128 columns and a strip of rows to a workgroup, 16 lanes a row, so
 // that one pass over dY and the mask serves all three.  The rows from n to nz
-// are zeros.  The workgroups past the strips widen X8 to bfloat16 rows.
+// are zeros.  The workgroups past the strips widen X8 to bfloat16 rows.  Bound by
+// memory: 65,536 x 512 bfloat16 dY beside 65,536 x 1024 X8 67 us for 400 MB (part of
+// it in the last-level cache), as long as the product behind it.
 struct MaskArgs {
     int32_t n, nz, N, rows_per_strip, strips, blocks;   // blocks: of 128 columns
     const void *dY;

@@ -187,7 +187,8 @@ def test_far_logits():
         assert np.array_equal(np64(out.rows), np.array([0, 2000, 1000, 0, 2000, 1000, 0, 0.0]))
 
 
-@pytest.mark.parametrize("dtype, n, f, C", [("bf16", 300000, 16, 1500), ("f32", 60000, 8, 2500)])
+@pytest.mark.parametrize("dtype, n, f, C", [("bf16", 300000, 16, 1500), ("f32", 60000, 8, 2500),
+                                            ("f32", 140000, 32, 1100), ("bf16", 600000, 64, 712)])
 def test_several_pieces(dtype, n, f, C):
     """Sizes that are cut into pieces of the classes, the last one ragged, against torch in float64 on the GPU."""
     t = DT[dtype]
