@@ -271,6 +271,9 @@ Plan plan_of(int32_t n, int32_t f, int32_t C, bool grad, const void *W, void *ws
         b.G = ar.take<T>(p.np * pp);
         b.colpart = ar.take<float>((p.np + kSmallRows - 1) / kSmallRows * p.piece);
         p.split_h = tile_splits(n, f, (int32_t)(pp / u), !bf);
+        // (float32: parts of about 64 pieces fill the last round of the other product, in
+        // the same launch)
+        if (!bf) p.split_h = (int32_t)std::max<int64_t>(p.split_h, std::min<int64_t>(64, pp / u / 64));
         p.split_w = tile_splits(f, p.piece, (int32_t)(p.np / u), !bf);
         b.acc = ar.take<float>((size_t)p.split_h * rows * f);
         if (p.split_w > 1) b.part = ar.take<float>((size_t)p.split_w * f * p.piece);

@@ -1086,8 +1086,9 @@ int tile_products(bool f32, const TileProduct &nt, const TileProduct &tn, TileEp
     Args a, b;
     unsigned ga, gb;
     if ((rc = tile_args(t, TILE_PARTIAL, nt, a, ga)) || (rc = tile_args(u, epi, tn, b, gb))) return rc;
+    // (the long sums first: the other's many short parts fill what their last round leaves)
 #define GCN_PAIR(NT, TN, EPI) \
-    hipLaunchKernelGGL((pair_kernel<NT, TILE_PARTIAL, TN, EPI>), dim3(ga + gb), dim3(256), 0, s, a, b, ga)
+    hipLaunchKernelGGL((pair_kernel<TN, EPI, NT, TILE_PARTIAL>), dim3(ga + gb), dim3(256), 0, s, b, a, gb)
     if (f32 && epi == TILE_STORE_F32) GCN_PAIR(TILE_F32, TILE_F32_TN, TILE_STORE_F32);
     else if (f32) GCN_PAIR(TILE_F32, TILE_F32_TN, TILE_PARTIAL);
     else if (epi == TILE_STORE) GCN_PAIR(TILE_BF16, TILE_BF16_TN, TILE_STORE);
