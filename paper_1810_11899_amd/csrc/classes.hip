@@ -15,7 +15,7 @@
 // and pass 2 turns them into G (1 / n_l included, no rounding to fewer bits) by an
 // elementwise pass; with several pieces it computes them again.  The products
 // run at 100-110 TFLOP/s (peak 157) and are nine tenths of the time at 2000 x 256,
-// 10,007 classes (359 us; 17 x 128, 1009 classes: 36 us of launches).  bfloat16:
+// 10,007 classes (349 us; 17 x 128, 1009 classes: 36 us of launches).  bfloat16:
 // 16,384 x 1024, 131,072 classes 15.6 ms, four products of 1080-1330 TFLOP/s.
 #include <algorithm>
 
