@@ -715,7 +715,10 @@ def gcn_rows8_weight_grad(X8: Rows8, dY: torch.Tensor, dW: torch.Tensor, ws: Wor
     if mask is not None:
         if tuple(mask.shape) != (X8.n, N):
             raise ValueError("mask and dY differ in shape")
-        ldm = max(_ld8(mask, "mask"), N)
+        # (a single row's stride says nothing; others below N, of rows that share memory, the library refuses)
+        ldm = _ld8(mask, "mask")
+        if X8.n <= 1:
+            ldm = max(ldm, N)
     w, wb = ws.args(L.gcn_rows8_weight_grad_workspace_bytes(X8.n, X8.f, N))
     _launch("gcn_rows8_weight_grad",
             _one_device(dW, X8.values, dY, db, mask, None if dZ8 is None else dZ8.values, ws.buf), stream, X8.ref,

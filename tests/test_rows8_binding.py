@@ -1,0 +1,61 @@
+"""What the Python binding makes of the tensors of the 8-bit rows, on the CPU:
+tensors that say they are on a device, and the library's call recorded."""
+import pytest
+import torch
+
+from paper_1810_11899_amd import binding as B
+
+
+class OnDevice(torch.Tensor):
+    """A CPU tensor that the binding takes for one on device 0, or on the device of its `where`."""
+    where = 0
+    is_cuda = property(lambda self: True)
+
+    def get_device(self):
+        return self.where
+
+
+def dev(t, where=0):
+    t = t.as_subclass(OnDevice)
+    t.where = where
+    return t
+
+
+def rows8(n, f):
+    nb = -(-f // 128)
+    values = torch.zeros((max(n, 1), nb * 128), dtype=torch.uint8).view(torch.float8_e4m3fn)[:n, :f]
+    return B.Rows8.of(dev(values), dev(torch.zeros((n, nb), dtype=torch.uint8)))
+
+
+class Space:
+    """Stands for a Workspace."""
+    buf = dev(torch.zeros(8, dtype=torch.uint8))
+
+    def args(self, nbytes):
+        return 0x10000, nbytes
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The library's calls, (name, arguments), which are not made."""
+    made = []
+    monkeypatch.setattr(B, "_launch", lambda where, device, stream, *args: made.append((where, args)))
+    return made
+
+
+# ---------------------------------------------------------------- the mask's rows
+def mask_stride(calls, mask, n, N):
+    B.gcn_rows8_weight_grad(rows8(n, 64), dev(torch.zeros(n, N)), dev(torch.zeros(64, N)), Space(), mask=dev(mask))
+    return calls[-1][1][2]
+
+
+def test_mask_rows_that_share_memory_keep_their_stride(calls):
+    """The library refuses a row stride below the columns: the binding passes it on as it is."""
+    e4m3 = lambda *s: torch.zeros(*s, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    n, N = 50, 32
+    assert mask_stride(calls, e4m3(1, N).expand(n, N), n, N) == 0
+    assert mask_stride(calls, torch.as_strided(e4m3(n + N), (n, N), (1, 1)), n, N) == 1
+    assert mask_stride(calls, e4m3(n, N), n, N) == N
+    assert mask_stride(calls, e4m3(n, 128)[:, 64:64 + N], n, N) == 128
+    assert mask_stride(calls, e4m3(1, N).expand(1, N), 1, N) >= N          # one row: any stride
+    assert mask_stride(calls, torch.as_strided(e4m3(N), (1, N), (0, 1)), 1, N) >= N
