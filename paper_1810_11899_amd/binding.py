@@ -600,6 +600,17 @@ def _ld8(t: torch.Tensor, name: str) -> int:
     return int(t.stride(0))
 
 
+def _whole_blocks(t: torch.Tensor, name: str) -> int:
+    """The stride of 8-bit rows, which the calls read and write in whole blocks of 128, behind the last column too:
+    the blocks of every row must lie in the tensor's memory."""
+    ld = _ld8(t, name)
+    end = t.storage_offset() + (t.shape[0] - 1) * ld + _blocks8(int(t.shape[1])) * ROWS8_BLOCK
+    if t.shape[0] and end > t.untyped_storage().nbytes():
+        raise ValueError(f"{name} must be a view of rows of whole {ROWS8_BLOCK}-column blocks: its last row's end "
+                         "lies behind the memory")
+    return ld
+
+
 class Rows8:
     """n x f activations in 8 bits: `values` (float8_e4m3fn, n x f, in rows of
     whole 128-column blocks) and `scale` (uint8, n x ceil(f / 128)); an element
@@ -623,7 +634,8 @@ class Rows8:
         if scale.dtype != torch.uint8 or tuple(scale.shape) != (self.n, _blocks8(self.f)) or not scale.is_cuda \
                 or (self.n and not scale.is_contiguous()):
             raise TypeError("scale must be a contiguous uint8 CUDA/HIP tensor, n x ceil(f / 128)")
-        self.struct = gcn_rows8(self.n, self.f, _ld8(values, "values"), _blocks8(self.f), values.data_ptr(),
+        _one_device(values, scale)
+        self.struct = gcn_rows8(self.n, self.f, _whole_blocks(values, "values"), _blocks8(self.f), values.data_ptr(),
                                 scale.data_ptr())
         self.ref = ctypes.byref(self.struct)
 
@@ -652,7 +664,8 @@ class Weights8:
         _want(scale, "scale", torch.uint8, (_blocks8(self.K), _blocks8(self.N)))
         if not scale.is_contiguous():
             raise ValueError("scale must be contiguous")
-        self.struct = gcn_weights8(self.K, self.N, _ld8(values, "values"), _ld8(values_t, "values_t"),
+        _one_device(values, values_t, scale)
+        self.struct = gcn_weights8(self.K, self.N, _whole_blocks(values, "values"), _whole_blocks(values_t, "values_t"),
                                    _blocks8(self.N), values.data_ptr(), values_t.data_ptr(), scale.data_ptr())
         self.ref = ctypes.byref(self.struct)
 

@@ -34,3 +34,13 @@ def test_weight_grad_refuses_a_mask_whose_rows_share_memory():
     one = B.gcn_rows8_pack(torch.ones((1, f), device="cuda"), B.Rows8(1, f))
     B.gcn_rows8_weight_grad(one, dY[:1], dW, ws, mask=e4m3(1, N).expand(1, N))
     assert np.all(dW.cpu().numpy() == 1.0)
+
+
+def test_rows_of_whole_blocks_only():
+    buf = torch.zeros((8, 304), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    scale = torch.zeros((8, 1), dtype=torch.uint8, device="cuda")
+    with pytest.raises(ValueError):
+        B.Rows8.of(buf[:, 192:292], scale)
+    r = B.Rows8.of(buf[:, 176:276], scale)     # the last row's block ends with the buffer
+    B.gcn_rows8_pack(torch.ones((8, 100), device="cuda"), r)
+    assert np.all(B.gcn_rows8_unpack(r, torch.empty((8, 100), device="cuda")).cpu().numpy() == 1.0)

@@ -59,3 +59,40 @@ def test_mask_rows_that_share_memory_keep_their_stride(calls):
     assert mask_stride(calls, e4m3(n, 128)[:, 64:64 + N], n, N) == 128
     assert mask_stride(calls, e4m3(1, N).expand(1, N), 1, N) >= N          # one row: any stride
     assert mask_stride(calls, torch.as_strided(e4m3(N), (1, N), (0, 1)), 1, N) >= N
+
+
+# ---------------------------------------------------- 8-bit rows kept elsewhere
+def kept(rows, cols, where=0):
+    return dev(torch.zeros((rows, cols), dtype=torch.uint8).view(torch.float8_e4m3fn), where)
+
+
+def scale(rows, blocks, where=0):
+    return dev(torch.zeros((rows, blocks), dtype=torch.uint8), where)
+
+
+def test_rows_whose_blocks_end_behind_the_memory_are_refused():
+    """100 columns from column 192 on of rows of 304: the last row's block of 128 ends 16 bytes behind the buffer."""
+    buf = kept(8, 304)
+    with pytest.raises(ValueError, match="whole"):
+        B.Rows8.of(buf[:, 192:292], scale(8, 1))
+    with pytest.raises(ValueError, match="whole"):
+        B.Rows8.of(kept(1, 112)[:, :100], scale(1, 1))
+    assert B.Rows8.of(buf[:, 176:276], scale(8, 1)).struct.ldq == 304      # up to the very end
+    assert B.Rows8.of(buf[:7, 192:292], scale(7, 1)).struct.ldq == 304     # (the row behind the last holds it)
+    assert B.Rows8.of(kept(8, 256)[:0, :200], scale(0, 2)).n == 0
+
+
+def test_weights_whose_blocks_end_behind_the_memory_are_refused():
+    whole, cut = kept(100, 128), kept(100, 112)
+    assert B.Weights8.of(whole[:, :100], whole[:, :100], scale(1, 1)).K == 100
+    for v, vt in ((cut[:, :100], whole[:, :100]), (whole[:, :100], cut[:, :100])):
+        with pytest.raises(ValueError, match="whole"):
+            B.Weights8.of(v, vt, scale(1, 1))
+
+
+def test_parts_on_different_devices_are_refused():
+    with pytest.raises(ValueError, match="one device"):
+        B.Rows8.of(kept(8, 128), scale(8, 1, where=1))
+    for at in ((1, 0, 0), (0, 1, 0), (0, 0, 1)):
+        with pytest.raises(ValueError, match="one device"):
+            B.Weights8.of(kept(128, 128, at[0]), kept(128, 128, at[1]), scale(1, 1, at[2]))
