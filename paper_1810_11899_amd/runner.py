@@ -266,10 +266,10 @@ class StepRunner8:
                                   empty(max(g.nnz, 1))[:g.nnz])
         self.H0 = f(wl.H)
         self.labels = torch.as_tensor(wl.labels, dtype=torch.int32).to(d)
-        self.W = [(f(l.W_self), f(l.W_neigh), f(l.bias)) for l in wl.layers]
-        # [W_self || W_neigh] side by side for the input gradient (its columns
-        # are the masters of the two)
-        self.Wb = [torch.cat(w[:2], dim=1) for w in self.W]
+        # [W_self || W_neigh] side by side, as the input gradient reads them; W's
+        # two are its column ranges, so that both directions see an update
+        self.Wb = [torch.cat((f(l.W_self), f(l.W_neigh)), dim=1) for l in wl.layers]
+        self.W = [(wb[:, :l.h], wb[:, l.h:], f(l.bias)) for wb, l in zip(self.Wb, wl.layers)]
         self.W8 = [(B.Weights8(fi, h, d), B.Weights8(fi, h, d), B.Weights8(fi, 2 * h, d) if li else None)
                    for li, (fi, h) in enumerate(self.dims)]
         self.X8 = [B.Rows8(n, fi, d) for fi, _ in self.dims]
