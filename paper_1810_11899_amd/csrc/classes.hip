@@ -4,8 +4,10 @@
 //   pass 1, per piece: logits of the piece in the product's registers; per row
 //     and column tile their maximum and the sum of exponentials relative to
 //     it, joined into the row's running maximum and sum
-//   loss: row_loss = max + log(sum) - label's logit
-//   pass 2, per piece: the logits again, n_l G = softmax - onehot in the same
+//   loss: row_loss = (max - label's logit) + log(sum).  max and log(sum) stay two
+//     numbers, here and in G: where a row is sure of its label log(sum) is all of
+//     its loss, and added to a max of 1000 it would be rounded to steps of 2^-14
+//   pass 2, per piece: the logits again, n_l G = exp((x - max) - log(sum)) - onehot in the same
 //     registers, written as bfloat16 rows; then n_l dHL += n_l G W_piece^T and
 //     n_l dW_piece = HL^T n_l G.  1 / n_l is a factor of the float32 sums: in G it
 //     would be rounded, and the same way in every row (17 rows: the gradients
@@ -133,8 +135,9 @@ __global__ __launch_bounds__(kTB) void join_kernel(int32_t n, int32_t tiles, con
 constexpr int kStrip = 32;
 __global__ __launch_bounds__(kTB) void grad_rows_kernel(int32_t n, int32_t P, float *X, int64_t ldx,
                                                         const int32_t *labels, int32_t class0, int32_t C,
-                                                        const float *lse, const float *inv_count, float *part) {
-    __shared__ float z[kStrip];
+                                                        const float *row_max, const float *log_sum,
+                                                        const float *inv_count, float *part) {
+    __shared__ float top[kStrip], ls[kStrip];
     __shared__ int32_t lab[kStrip];
     const int64_t c = (int64_t)blockIdx.x * kTB + threadIdx.x;
     const int32_t strips = (n + kStrip - 1) / kStrip;
@@ -145,7 +148,8 @@ __global__ __launch_bounds__(kTB) void grad_rows_kernel(int32_t n, int32_t P, fl
         if (threadIdx.x < kStrip) {
             const int64_t row = r0 + threadIdx.x;
             const int32_t l = row < n ? labels[row] : -1;
-            z[threadIdx.x] = row < n ? lse[row] : 0.0f;
+            top[threadIdx.x] = row < n ? row_max[row] : 0.0f;
+            ls[threadIdx.x] = row < n ? log_sum[row] : 0.0f;
             lab[threadIdx.x] = has_label(l, C) ? l : -1;
         }
         __syncthreads();
@@ -160,7 +164,7 @@ __global__ __launch_bounds__(kTB) void grad_rows_kernel(int32_t n, int32_t P, fl
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int32_t l = lab[r + e];
-                const float g = l >= 0 && c < P ? (expf(v[e] - z[r + e]) - (class0 + c == l ? 1.0f : 0.0f)) * inv : 0.0f;
+                const float g = l >= 0 && c < P ? (expf((v[e] - top[r + e]) - ls[r + e]) - (class0 + c == l ? 1.0f : 0.0f)) * inv : 0.0f;
                 x[e * ldx] = g;
                 sum += g;
             }
@@ -169,13 +173,13 @@ __global__ __launch_bounds__(kTB) void grad_rows_kernel(int32_t n, int32_t P, fl
     }
 }
 
-// lse, the rows' losses and their mean, by one workgroup in a fixed order.
-// tiles > 0: the only piece's tiles are joined here (few rows and tiles).
+// The sums' logarithms, the rows' losses and their mean, by one workgroup in a fixed
+// order.  tiles > 0: the only piece's tiles are joined here (few rows and tiles).
 __global__ __launch_bounds__(1024) void loss_kernel(int32_t n, int32_t C, const int32_t *__restrict__ labels,
                                                     int32_t tiles, const float *__restrict__ tile_max,
-                                                    const float *__restrict__ tile_sum, const float *__restrict__ run_max,
+                                                    const float *__restrict__ tile_sum, float *__restrict__ run_max,
                                                     const float *__restrict__ run_sum,
-                                                    const float *__restrict__ label_logit, float *__restrict__ lse,
+                                                    const float *__restrict__ label_logit, float *__restrict__ log_sum,
                                                     float *__restrict__ row_loss, const float *__restrict__ inv_count,
                                                     float *__restrict__ loss) {
     __shared__ double part[16];
@@ -186,13 +190,14 @@ __global__ __launch_bounds__(1024) void loss_kernel(int32_t n, int32_t C, const 
         if (tiles > 0) {
             m = -INFINITY, s = 0.0f;
             for (int32_t k = 0; k < tiles; ++k) join(m, s, tile_max[(int64_t)k * n + i], tile_sum[(int64_t)k * n + i]);
+            run_max[i] = m;
         } else {
             m = run_max[i], s = run_sum[i];
         }
-        const float z = m + logf(s);
-        lse[i] = z;
+        const float ls = logf(s);
+        log_sum[i] = ls;
         const bool has = has_label(labels[i], C);
-        const float v = has ? z - label_logit[i] : 0.0f;
+        const float v = has ? (m - label_logit[i]) + ls : 0.0f;
         if (row_loss) row_loss[i] = v;
         t += v;
     }
@@ -228,7 +233,7 @@ struct Plan {
 };
 template <class T>
 struct Buffers {
-    float *inv_count, *run_max, *run_sum, *label_logit, *lse, *tile_max, *tile_sum, *colpart, *acc, *part;
+    float *inv_count, *run_max, *run_sum, *label_logit, *log_sum, *tile_max, *tile_sum, *colpart, *acc, *part;
     T *H, *W, *G;              // (float32: G holds the logits first)
 };
 
@@ -255,7 +260,7 @@ Plan plan_of(int32_t n, int32_t f, int32_t C, bool grad, const void *W, void *ws
     b.run_max = ar.take<float>(rows);
     b.run_sum = ar.take<float>(rows);
     b.label_logit = ar.take<float>(rows);
-    b.lse = ar.take<float>(rows);
+    b.log_sum = ar.take<float>(rows);
     // (sized for the smallest tiles: a last, smaller piece may run on them)
     const int64_t tn = (p.piece + kSmallTile - 1) / kSmallTile;
     b.tile_max = ar.take<float>(tn * rows);
@@ -364,7 +369,7 @@ int class_loss(const Plan &p, const Buffers<T> &b, const T *HL, int32_t n, int32
         GCN_LAUNCH_CHECK("join_kernel");
     }
     hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, s, n, C, labels, tiles, b.tile_max, b.tile_sum, b.run_max,
-                       b.run_sum, b.label_logit, b.lse, row_loss, b.inv_count, loss);
+                       b.run_sum, b.label_logit, b.log_sum, row_loss, b.inv_count, loss);
     GCN_LAUNCH_CHECK("loss_kernel");
     if (!dHL) return GCN_OK;
     const float *const factor = bf ? b.inv_count : nullptr;   // (float32 G has it already)
@@ -374,7 +379,8 @@ int class_loss(const Plan &p, const Buffers<T> &b, const T *HL, int32_t n, int32
         if ((rc = weights(c0, P))) return rc;
         TileProduct t = logits(c0, P);
         if constexpr (bf) {
-            t.lse = b.lse;
+            t.row_max = b.run_max;
+            t.log_sum = b.log_sum;
             t.scale = b.inv_count;
             t.G = b.G;
             t.ldg = pp;
@@ -394,8 +400,8 @@ int class_loss(const Plan &p, const Buffers<T> &b, const T *HL, int32_t n, int32
                 t.ldc = pp;
                 if (p.pieces > 1 && (rc = tile_product(kNN, TILE_STORE_F32, t, s))) return rc;
                 const dim3 g((unsigned)((pp + kTB - 1) / kTB), (unsigned)std::min(65535, strips));
-                hipLaunchKernelGGL(grad_rows_kernel, g, dim3(kTB), 0, s, n, P, b.G, pp, labels, c0, C, b.lse,
-                                   b.inv_count, strips == 1 ? db + c0 : b.colpart);
+                hipLaunchKernelGGL(grad_rows_kernel, g, dim3(kTB), 0, s, n, P, b.G, pp, labels, c0, C, b.run_max,
+                                   b.log_sum, b.inv_count, strips == 1 ? db + c0 : b.colpart);
                 GCN_LAUNCH_CHECK("grad_rows_kernel");
             }
             if (strips > 1 && (rc = colsum_reduce_rows(strips, P, b.colpart, db + c0, s))) return rc;

@@ -180,8 +180,9 @@ struct Extras {
     float bias[FN][4];
     float scale;
     int lab[FM];
-    float lse[FM];
+    float top[FM], log2_sum[FM];
 };
+constexpr float kLog2e = 1.44269504088896340736f;
 template <int EPI, int BM, int BN, int WM, int WN, int FM, int FN>
 __device__ __forceinline__ void load_extras(const TileProduct &p, const Coord &c, Extras<FM, FN> &x) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -205,7 +206,11 @@ __device__ __forceinline__ void load_extras(const TileProduct &p, const Coord &c
     }
     if constexpr (EPI == TILE_GRAD) {
 #pragma unroll
-        for (int i = 0; i < FM; ++i) x.lse[i] = r0 + 16 * i < p.M ? p.lse[r0 + 16 * i] : 0.0f;
+        for (int i = 0; i < FM; ++i) {
+            const bool in = r0 + 16 * i < p.M;
+            x.top[i] = in ? p.row_max[r0 + 16 * i] : 0.0f;
+            x.log2_sum[i] = in ? p.log_sum[r0 + 16 * i] * kLog2e : 0.0f;
+        }
     }
 }
 
@@ -288,7 +293,6 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, const Extr
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[i][j][e] += x.bias[j][e];
         if constexpr (EPI == TILE_STATS_STORE) store_f32<FM, FN>(acc, p, r0, c0);
-        constexpr float kLog2e = 1.44269504088896340736f;
         const int w0 = c.tn * BN + wn * (BN / WN);   // the wavefront's first column
         if constexpr (is_stats(EPI)) {
             // a row's columns lie in 4 lanes of WN wavefronts: maximum and sum
@@ -347,13 +351,13 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, const Extr
                 for (int e = 0; e < 4; ++e) cs[j][e] = 0.0f;
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
-                const float lse = x.lse[i];
+                const float top = x.top[i], log2_sum = x.log2_sum[i];
                 const int lab = x.lab[i];
 #pragma unroll
                 for (int j = 0; j < FN; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        acc[i][j][e] = __builtin_amdgcn_exp2f((acc[i][j][e] - lse) * kLog2e);
+                        acc[i][j][e] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e] - top, kLog2e, -log2_sum));
                 if (__any(lab >= w0 && lab < w0 + BN / WN)) {
 #pragma unroll
                     for (int j = 0; j < FN; ++j)

@@ -70,7 +70,7 @@ struct TileProduct {
     int32_t class0, classes;
     float *tile_max, *tile_sum;     // [tiles_n x M]
     float *label_logit;             // [M]
-    const float *lse;               // [M]
+    const float *row_max, *log_sum; // [M]: a row's softmax is exp((x - row_max) - log_sum)
     uint16_t *G;                    // [g_rows x ldg] bfloat16, zeros past M and N
     int64_t ldg, g_rows;
     float *colpart;                 // [tiles_m x N]
