@@ -444,7 +444,7 @@ GradPlan plan_grad(int32_t n, int32_t f, int32_t N, void *ws, size_t ws_bytes, G
 }  // namespace
 
 size_t gcn_rows8_weight_grad_workspace_bytes(int32_t n, int32_t f, int32_t N) {
-    if (n < 0 || f <= 0 || N <= 0 || n > kMostRows) return 0;
+    if (n < 0 || f <= 0 || N <= 0 || std::max({n, f, N}) > kMostRows) return 0;
     GradBuffers b;
     return plan_grad(n, f, N, nullptr, 0, b).total;
 }
