@@ -8,6 +8,7 @@ LOSS and the backward pass that ADAM consumes).  No arithmetic happens here.
 """
 from __future__ import annotations
 
+import functools
 from typing import List, Optional
 
 import numpy as np
@@ -230,6 +231,16 @@ class StepRunner:
                          self.spec.classes if self.head is not None else 0)
 
 
+def _on_its_device(method):
+    """The method with the buffers' device as the current one, which gives calls without a stream theirs: the step's
+    calls follow one another on one stream."""
+    @functools.wraps(method)
+    def call(self, stream=None):
+        with torch.cuda.device(self.H0.device):
+            return method(self, stream)
+    return call
+
+
 class StepRunner8:
     """The fwd+bwd step of an L-layer GCN with a softmax cross entropy head that
     keeps its activations as 8-bit rows and no logits (gcn_rows8.h,
@@ -295,6 +306,7 @@ class StepRunner8:
         """Bytes that stay from the forward to the backward pass."""
         return sum(t.values.shape[0] * t.struct.ldq + t.scale.numel() for t in self.X8 + self.G8 + [self.Y8])
 
+    @_on_its_device
     def forward(self, stream=None):
         H = self.H0
         for li, (fi, h) in enumerate(self.dims):
@@ -313,10 +325,12 @@ class StepRunner8:
             H = Y
         B.gcn_rows8_pack(self.HL, self.Y8, stream)
 
+    @_on_its_device
     def head(self, stream=None):
         B.gcn_class_loss(self.HL, self.W_pred, self.b_pred, self.labels, self.loss, self.ws, row_loss=self.row_loss,
                          dHL=self.dHL, dW_pred=self.dW_pred, db_pred=self.db_pred, stream=stream)
 
+    @_on_its_device
     def backward(self, stream=None):
         if self.symmetric:
             B.gcn_csr_transpose_symmetric(self.A, self.ws, self.AT.vals, stream)
@@ -339,6 +353,7 @@ class StepRunner8:
             B.gcn_rows8_pack(Z, self.Z8[li], stream)
             dY = B.gcn_rows8_product(self.Z8[li], self.W8[li][2], self.dH[li], self.ws, transpose=True, stream=stream)
 
+    @_on_its_device
     def step(self, stream=None):
         self.forward(stream)
         self.head(stream)
