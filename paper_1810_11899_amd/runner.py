@@ -247,18 +247,22 @@ class StepRunner8:
     gcn_classes.h).
 
     Per layer the 8-bit rows of its input H and of A H are all that stays for
-    the backward pass, a quarter of their float32 size; the layer's float32
-    output lives in one of two buffers that the layers share.  With X8, G8 the
-    8-bit rows and Ws8, Wn8 the 8-bit weights:
+    the backward pass, a quarter of their float32 size.  With X8, G8 the 8-bit
+    rows and Ws8, Wn8 the 8-bit weights:
 
         Y  = max([X8 Ws8 || G8 Wn8] + b, 0),  G8 = rows8(A H)
         dW_self = X8^T dZs,  dW_neigh = G8^T dZn,  dZ = dY [Y8 > 0]
         dH = Z8 [Ws8 || Wn8]^T,  Z8 = rows8([dZs || A^T dZn])
 
     the last line by linearity, so that the input gradient is one product.  The
-    head reads the last layer's output and W_pred as bfloat16."""
+    head reads the last layer's output and W_pred as bfloat16.
 
-    def __init__(self, wl, device: str = "cuda"):
+    What a layer leaves besides, its float32 input gradient dH and the 8-bit
+    rows dZs8, dZn8 and Z8, is dead once the layer below is through.  With
+    keep_gradients it stays, layer by layer, until the next forward pass;
+    without, the layers share one set, which then holds that of layer 1."""
+
+    def __init__(self, wl, device: str = "cuda", keep_gradients: bool = True):
         if wl.spec.head != "ce":
             raise ValueError("the 8-bit step has a softmax cross entropy head")
         d = self.dev = torch.device(device)
@@ -287,12 +291,21 @@ class StepRunner8:
         self.G8 = [B.Rows8(n, fi, d) for fi, _ in self.dims]
         hl = 2 * self.dims[-1][1]
         self.Y8 = B.Rows8(n, hl, d)           # the last layer's output, for its ReLU derivative
-        self.Z8 = [None] + [B.Rows8(n, 2 * h, d) for _, h in self.dims[1:]]
-        self.dZs8 = [B.Rows8(n, h, d) for _, h in self.dims]
-        self.dZn8 = [B.Rows8(n, h, d) for _, h in self.dims]
-        width = max(max(fi, 2 * h) for fi, h in self.dims)
-        self._rows = [empty(n, width), empty(n, width)]
-        self._agg = empty(n, width)
+        upper = self.dims[1:]
+        if keep_gradients:
+            rows8 = lambda cols: [None] + [B.Rows8(n, c, d) for c in cols]
+            self._low = [None] + [empty(n, max(fi, h)) for fi, h in upper]
+        else:
+            rows8 = lambda cols: [None] + self._rows8_in_one(n, cols, d)
+            low = empty(n, max((max(dim) for dim in upper), default=0))
+            self._low = [None] + [low[:, :max(dim)] for dim in upper]
+        self.Z8 = rows8([2 * h for _, h in upper])
+        self.dZs8, self.dZn8 = rows8([h for _, h in upper]), rows8([h for _, h in upper])
+        # Float32 rows of a layer: what comes from below and goes back there, the
+        # layer's input H, then dZ's neighbour half, then dH (_low, above layer 0);
+        # and A H, then [dZs || A^T dZn] (_wide)
+        self._wide = empty(n, max([fi for fi, _ in self.dims] + [2 * h for _, h in upper]))
+        self.dH = [None] + [low[:, :fi] for low, (fi, _) in zip(self._low[1:], upper)]
         self.HL, self.dHL = empty(n, hl, dtype=torch.bfloat16), empty(n, hl, dtype=torch.bfloat16)
         self.W_pred, self.b_pred = f(wl.W_pred).to(torch.bfloat16), f(wl.b_pred)
         self.loss, self.row_loss = empty(1), empty(n)
@@ -300,7 +313,16 @@ class StepRunner8:
         self.dWs = [empty(fi, h) for fi, h in self.dims]
         self.dWn = [empty(fi, h) for fi, h in self.dims]
         self.db = [empty(2 * h) for _, h in self.dims]
-        self.dH = [None] + [empty(n, fi) for fi, _ in self.dims[1:]]
+
+    @staticmethod
+    def _rows8_in_one(n: int, cols: List[int], device) -> List[B.Rows8]:
+        """8-bit rows of these widths over one piece of memory, for uses one after another (what is packed there
+        writes its blocks' last columns too)."""
+        blocks = [-(-c // B.ROWS8_BLOCK) for c in cols]
+        kept = torch.zeros(n * max(blocks, default=0) * B.ROWS8_BLOCK, dtype=torch.uint8, device=device)
+        scale = torch.empty(n * max(blocks, default=0), dtype=torch.uint8, device=device)
+        return [B.Rows8.of(kept[:n * b * B.ROWS8_BLOCK].view(n, b * B.ROWS8_BLOCK).view(torch.float8_e4m3fn)[:, :c],
+                           scale[:n * b].view(n, b)) for c, b in zip(cols, blocks)]
 
     def kept_bytes(self) -> int:
         """Bytes that stay from the forward to the backward pass."""
@@ -317,9 +339,9 @@ class StepRunner8:
             if Wb8 is not None:
                 B.gcn_weights8_pack(self.Wb[li], Wb8, stream)
             B.gcn_rows8_pack(H, self.X8[li], stream)
-            agg = B.gcn_aggregate(self.A, H, self._agg[:, :fi], self.ws, B.GCN_BF16, stream)
+            agg = B.gcn_aggregate(self.A, H, self._wide[:, :fi], self.ws, B.GCN_BF16, stream)
             B.gcn_rows8_pack(agg, self.G8[li], stream)
-            Y = self.HL if li == self.L - 1 else self._rows[li % 2][:, :2 * h]
+            Y = self.HL if li == self.L - 1 else self.dH[li + 1]   # (over H, which is packed, where they share)
             B.gcn_rows8_product(self.X8[li], Ws8, Y[:, :h], self.ws, bias=b[:h], relu=True, stream=stream)
             B.gcn_rows8_product(self.G8[li], Wn8, Y[:, h:], self.ws, bias=b[h:], relu=True, stream=stream)
             H = Y
@@ -346,9 +368,9 @@ class StepRunner8:
                                         dZ8=dZ8[li] if li else None, stream=stream)
             if li == 0:
                 break
-            Z = self._rows[0][:, :2 * h]
+            Z = self._wide[:, :2 * h]
             B.gcn_rows8_unpack(self.dZs8[li], Z[:, :h], stream)
-            dZn = B.gcn_rows8_unpack(self.dZn8[li], self._agg[:, :h], stream)
+            dZn = B.gcn_rows8_unpack(self.dZn8[li], self._low[li][:, :h], stream)   # (over dY where they share)
             B.gcn_aggregate(self.AT, dZn, Z[:, h:], self.ws, B.GCN_BF16, stream)
             B.gcn_rows8_pack(Z, self.Z8[li], stream)
             dY = B.gcn_rows8_product(self.Z8[li], self.W8[li][2], self.dH[li], self.ws, transpose=True, stream=stream)

@@ -36,7 +36,7 @@ def test_every_call_of_a_step_is_made_on_the_buffers_device(monkeypatch, method)
         L=2, dims=[(8, 8), (16, 8)], H0=SimpleNamespace(device=torch.device("cuda", 1)), A=SimpleNamespace(),
         AT=SimpleNamespace(vals=None, indptr=None, indices=None), symmetric=True, ws=None,
         W=[(part(8, 8), part(8, 8), part(16))] * 2, Wb=[part(8, 16)] * 2, W8=[(None, None, rows)] * 2, X8=[rows] * 2,
-        G8=[rows] * 2, Y8=rows, Z8=[rows] * 2, dZs8=[rows] * 2, dZn8=[rows] * 2, _rows=[part(4, 16)] * 2, _agg=part(4, 16),
+        G8=[rows] * 2, Y8=rows, Z8=[rows] * 2, dZs8=[rows] * 2, dZn8=[rows] * 2, _wide=part(4, 16), _low=[part(4, 16)] * 2,
         HL=part(4, 16), dHL=part(4, 16), W_pred=None, b_pred=None, labels=None, loss=None, row_loss=None, dW_pred=None,
         db_pred=None, dWs=[None] * 2, dWn=[None] * 2, db=[part(16)] * 2, dH=[part(4, 16)] * 2)
     getattr(r, method)()
