@@ -251,11 +251,16 @@ class StepRunner8:
     rows and Ws8, Wn8 the 8-bit weights:
 
         Y  = max([X8 Ws8 || G8 Wn8] + b, 0),  G8 = rows8(A H)
-        dW_self = X8^T dZs,  dW_neigh = G8^T dZn,  dZ = dY [Y8 > 0]
-        dH = Z8 [Ws8 || Wn8]^T,  Z8 = rows8([dZs || A^T dZn])
+        dW_self = X8^T dZs,  dW_neigh = G8^T dZn,  dZ = bf16(dY) [Y8 > 0]
+        dH = Z8 [Ws || Wn]8^T,  Z8 = rows8([dZs8 || A^T dZn8])
 
-    the last line by linearity, so that the input gradient is one product.  The
-    head reads the last layer's output and W_pred as bfloat16.
+    the last line by linearity, so that the input gradient is one product; its
+    weights are packed side by side, in blocks of their own.  What is rounded: A
+    H and A^T dZn8 are sums in float32 of rows in bfloat16 (which holds dZn8
+    exactly), and dZn reaches dH through two roundings to 8 bits, before and
+    after A^T, dZs through two as well (the second changes it only where its
+    block's scale is another).  The head reads the last layer's output and
+    W_pred as bfloat16.
 
     What a layer leaves besides, its float32 input gradient dH and the 8-bit
     rows dZs8, dZn8 and Z8, is dead once the layer below is through.  With

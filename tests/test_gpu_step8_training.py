@@ -1,5 +1,6 @@
 """The 8-bit step as a training loop runs it: weights that change between the
-steps."""
+steps, the memory it takes, and its input gradients against unrounded ones."""
+import numpy as np
 import pytest
 import torch
 
@@ -77,3 +78,46 @@ def test_memory_beside_the_float32_step():
     # beyond one set, a layer keeps dH (4 128) and the rows dZs8, dZn8 (128 each: whole blocks) and Z8 (128)
     assert kept - shared >= 4 * (4 * 128 + 3 * 128 - 16)
     assert shared < 0.75 * plain
+
+
+def np64(t):
+    return t.detach().to(torch.float64).cpu().numpy()
+
+
+def rounding8(x, rows=1):
+    """How far 8-bit values of x may be off it: half a step, 2^-4 of the value, or where that is below the format's
+    smallest value up to the whole of that one, 2^-9 of the block's scale, which is below 2^-7 / 1.75 of the block's
+    largest magnitude (448 = 1.75 2^8 holds at least half of the range)."""
+    n, f = x.shape
+    top = np.pad(np.abs(x), ((0, -n % rows), (0, -f % 128))).reshape(-(-n // rows), rows, -1, 128).max((1, 3))
+    top = np.repeat(np.repeat(top, rows, 0), 128, 1)[:n, :f]
+    return 2.0 ** -4 * np.abs(x) + 2.0 ** -16 / 1.75 * top
+
+
+def test_input_gradients_against_unrounded_ones():
+    """dH of every layer against [dZs || A^T dZn] [Ws || Wn]^T in float64 from dZ before it is rounded: what the two
+    roundings of dZ and that of the weights may add up to, element by element, and the float32 sums'."""
+    n = 400
+    wl = workload()
+    r = StepRunner8(wl)
+    r.step()
+    torch.cuda.synchronize()
+    AT = torch.sparse_csr_tensor(r.AT.indptr.long(), r.AT.indices.long(), r.AT.vals.double(), (n, n)).to_dense().cpu().numpy()
+    for li in range(r.L - 1, 0, -1):
+        fi, h = r.dims[li]
+        dY = np64(r.dHL if li == r.L - 1 else r.dH[li + 1].to(torch.bfloat16))
+        q = (r.Y8 if li == r.L - 1 else r.X8[li + 1]).values.view(torch.uint8).cpu().numpy()
+        z = np.where((q >= 1) & (q <= 126), dY, 0.0)
+        W = np64(r.Wb[li])
+        e = np.concatenate([rounding8(z[:, :h]), np.abs(AT) @ rounding8(z[:, h:])], 1)
+        Z = np.concatenate([z[:, :h], AT @ z[:, h:]], 1)
+        mag = np.concatenate([np.abs(z[:, :h]), np.abs(AT) @ np.abs(z[:, h:])], 1)
+        e = e + n * 2.0 ** -23 * mag
+        e = e + rounding8(np.abs(Z) + e)
+        tol = e @ np.abs(W).T + (np.abs(Z) + e) @ rounding8(W, 128).T
+        tol += (2 * h + 2) * 2.0 ** -22 * (mag @ np.abs(W).T) + 1e-37
+        err = np.abs(np64(r.dH[li]) - Z @ W.T)
+        assert np.all(err <= tol), float(np.max(err / tol))
+        # a rounding's root mean square is 2^-4 / sqrt(3) of its value at most; three independent ones, and terms of
+        # independent signs (the weights are random): 2^-4 in the 2-norm
+        assert np.linalg.norm(err) <= 2.0 ** -4 * np.linalg.norm(Z @ W.T), np.linalg.norm(err) / np.linalg.norm(Z @ W.T)
