@@ -286,10 +286,10 @@ class StepRunner8:
                                   empty(max(g.nnz, 1))[:g.nnz])
         self.H0 = f(wl.H)
         self.labels = torch.as_tensor(wl.labels, dtype=torch.int32).to(d)
-        # [W_self || W_neigh] side by side, as the input gradient reads them; W's
-        # two are its column ranges, so that both directions see an update
-        self.Wb = [torch.cat((f(l.W_self), f(l.W_neigh)), dim=1) for l in wl.layers]
-        self.W = [(wb[:, :l.h], wb[:, l.h:], f(l.bias)) for wb, l in zip(self.Wb, wl.layers)]
+        self.W = [(f(l.W_self), f(l.W_neigh), f(l.bias)) for l in wl.layers]
+        # [W_self || W_neigh] side by side, as the input gradient reads them: laid
+        # out again by every forward pass, which sees the weights as they are now
+        self.Wb = [None] + [empty(fi, 2 * h) for fi, h in self.dims[1:]]
         self.W8 = [(B.Weights8(fi, h, d), B.Weights8(fi, h, d), B.Weights8(fi, 2 * h, d) if li else None)
                    for li, (fi, h) in enumerate(self.dims)]
         self.X8 = [B.Rows8(n, fi, d) for fi, _ in self.dims]
@@ -342,6 +342,8 @@ class StepRunner8:
             B.gcn_weights8_pack(Ws, Ws8, stream)
             B.gcn_weights8_pack(Wn, Wn8, stream)
             if Wb8 is not None:
+                with torch.cuda.stream(stream):
+                    torch.cat((Ws, Wn), dim=1, out=self.Wb[li])
                 B.gcn_weights8_pack(self.Wb[li], Wb8, stream)
             B.gcn_rows8_pack(H, self.X8[li], stream)
             agg = B.gcn_aggregate(self.A, H, self._wide[:, :fi], self.ws, B.GCN_BF16, stream)

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from tests.gpu_util import require_gpu
+from paper_1810_11899_amd import binding as B
 from paper_1810_11899_amd import synth
 from paper_1810_11899_amd.runner import StepRunner, StepRunner8
 
@@ -41,6 +42,31 @@ def test_updated_weights_reach_both_directions():
     torch.cuda.synchronize()
     for a, b in zip(outputs(r), outputs(fresh)):
         assert torch.equal(a, b)
+
+
+def test_adam_on_the_steps_own_weights():
+    """The layers' tensors go into the optimizer as they are, on a stream of the caller's: two training steps give what
+    runners built from the updated weights give."""
+    wl = workload()
+    r = StepRunner8(wl)
+    r.ws.get(64 << 20)
+    moments = [[(torch.zeros_like(p), torch.zeros_like(p)) for p in w] for w in r.W]
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for k in (1, 2):
+        r.step(stream)
+        stream.synchronize()
+        fresh = StepRunner8(wl)
+        fresh.step()
+        torch.cuda.synchronize()
+        for a, b in zip(outputs(r), outputs(fresh)):
+            assert torch.equal(a, b)
+        for w, g, mv in zip(r.W, zip(r.dWs, r.dWn, r.db), moments):
+            for p, d, (m, v) in zip(w, g, mv):
+                B.gcn_adam_update(p, d, m, v, 0.05, k, stream=stream)
+        stream.synchronize()
+        for l, w in zip(wl.layers, r.W):
+            l.W_self, l.W_neigh, l.bias = [p.cpu().numpy() for p in w]
 
 
 @pytest.mark.parametrize("layers", [[(30, 40)], [(30, 40), (80, 64)], [(30, 40), (80, 150), (300, 24), (48, 33)]])

@@ -32,6 +32,7 @@ def test_every_call_of_a_step_is_made_on_the_buffers_device(monkeypatch, method)
     r = StepRunner8.__new__(StepRunner8)
     part = lambda *s: torch.zeros(s)
     rows = SimpleNamespace(values=part(4, 16))
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
     r.__dict__.update(
         L=2, dims=[(8, 8), (16, 8)], H0=SimpleNamespace(device=torch.device("cuda", 1)), A=SimpleNamespace(),
         AT=SimpleNamespace(vals=None, indptr=None, indices=None), symmetric=True, ws=None,
