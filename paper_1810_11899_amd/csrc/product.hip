@@ -413,10 +413,10 @@ __device__ __forceinline__ void finish(const Args &a, const Coord &c, const Extr
 // register result that could be taken for written, its operands are read as it
 // is issued, and the kernel waits by wait_copies and a barrier.
 __device__ __forceinline__ void copy_to_lds(const uint8_t *base, uint32_t off, uint32_t dst) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ void copy_to_lds(const uint8_t *from, uint32_t dst) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(from) : "memory", "m0");
 }
 template <int N>
 __device__ __forceinline__ void wait_copies() {
