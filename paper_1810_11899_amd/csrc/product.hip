@@ -1023,6 +1023,11 @@ TileShape tile_shape(TileType type, const TileProduct &p) {
     if (splits > 1 && (type == TILE_FP8 || type == TILE_FP8_EXACT)) return TileShape{64, 64};   // (split8)
     const bool big = type != TILE_FP8_EXACT && !is_f32(type) && tiles_of(p.M, p.N, kBigT) * splits >= 160 && per >= 4 &&
                      (type != TILE_FP8 || per <= kBigPieces) && std::max(p.lda, p.ldb) < (1 << 24);
+    // (The count of tiles alone: where the rows fill a part of one tile row only, the other
+    // sizes are up to a sixth faster.  The bfloat16 loss with gradients, us, 256 / 128 / 32
+    // rows a tile: 17 x 256, 65,536 classes 75 / 67 / 64, 131,072 classes 130 / 115 /
+    // 106; 17 x 1024, 131,072 classes 338 / 313 / 323; 128 x 256, 131,072 classes 140 /
+    // 127 / 159; but 256 x 256, 131,072 classes 160 / 187 / 222.)
     if (big) return TileShape{kBigT, kBigT};
     if (type == TILE_FP8 || type == TILE_FP8_EXACT) {
         // Few rows (us, few rows / 64 x 64, 4096 x 4096): 1 row 5.0 / 14.7, 16 7.4 /
@@ -1034,13 +1039,16 @@ TileShape tile_shape(TileType type, const TileProduct &p) {
         // 8000 x 512 x 640 10.3 / 9.4, but 8000 x 1024 x 512 (504 blocks) 12.1 /
         // 13.8; float32 results 50 / 35, 16.4 / 9.0, 14.3 / 14.9 (6205 x 512 x
         // 640), 8000 x 2048 x 2048 88 / 118.
-        // 64 x 128 tiles for float32 results widen fewer operands a product; where two
-        // of them a CU replace four 64 x 64 ones (us, 64 / 64 x 128): 6205 x 602 x 512
-        // 15.1 / 12.8, 8000 x 2048 x 512 30.0 / 26.3, 7000 x 512 x 512 12.3 / 10.8; but
-        // 1500 x 4096 x 2048 (three and one and a half) 40 / 45, 8000 x 1024 x 1024 (128 x
-        // 128 ones) 27 / 29, and bfloat16 results 1000 x 4096 x 2048 18.7 / 21.8.
+        // 64 x 128 tiles for float32 results widen fewer operands a product.  They take
+        // the place of 64 x 64 ones past one and a half a CU (us, 64 x 64 / 64 x 128:
+        // K = 1024 at 384 of them 14.8 / 16.5, at 400 18.6 / 16.3; K = 128 7.6 / 8.1
+        // and 8.9 / 8.0; K = 4096 41.6 / 45 and 53 / 45) and of the second round of 128 x
+        // 128 ones while they need three rounds themselves (128 x 128 / 64 x 128: K =
+        // 1024 at 513 .. 768 24.5 / 20.8, 772 .. 1024 25.0 / 26.8; K = 4096 71 / 60-64 and
+        // 72 / 80; K = 128 10.5 / 9.2 and 10.8 / 12.0).  bfloat16 results: 1000 x 4096 x
+        // 2048 (64 x 64 / 64 x 128) 18.7 / 21.8.
         const int64_t wide = ((int64_t)p.M + 63) / 64 * (((int64_t)p.N + 127) / 128);
-        if (type == TILE_FP8_EXACT && splits == 1 && wide > 384 && wide <= 512) return TileShape{64, 128};
+        if (type == TILE_FP8_EXACT && splits == 1 && wide > 384 && wide <= 768) return TileShape{64, 128};
         if (tiles_of(p.M, p.N, 128) < 256) return TileShape{64, 64};
     }
     if ((type == TILE_BF16_NN || type == TILE_F32_NN) && tiles_of(p.M, p.N, 128) < 256) return TileShape{32, 128};

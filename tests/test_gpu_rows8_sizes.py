@@ -7,6 +7,7 @@ import torch
 
 from oracle import rows8 as R
 from tests.gpu_util import require_gpu
+from tests import test_gpu_rows8 as small
 from tests.test_gpu_rows8 import DT, bytes_of, gen, product_bound, rows_of, spread, to_dev, weights_of
 from paper_1810_11899_amd import binding as B
 
@@ -83,3 +84,10 @@ def test_weight_grad_of_large_subgraphs(n, f, N, dtype, mask):
     v = B.gcn_rows8_unpack(dZ8, torch.empty((n, N), device="cuda")).double()
     scale = torch.exp2(dZ8.scale.double() - 127).repeat_interleave(128, 1)[:, :N]
     assert bool(((v - z).abs() <= 2.0 ** -4 * z.abs() + 2.0 ** -9 * scale).all())
+
+
+@pytest.mark.parametrize("n, K, N, transpose", [(6400, 700, 500, False), (6145, 300, 1000, True), (12288, 129, 512, False),
+                                                (12300, 260, 512, False), (6400, 4096, 512, False)])
+def test_product_about_the_edges_of_a_tile_size(n, K, N, transpose):
+    """From 384 to 768 tiles of 64 x 128, and one row of tiles more."""
+    small.test_product_of_many_tiles(n, K, N, transpose)
