@@ -16,9 +16,9 @@
 // float32 operands: pass 1 keeps the logits of a single piece where G will be,
 // and pass 2 turns them into G (1 / n_l included, no rounding to fewer bits) by an
 // elementwise pass; with several pieces it computes them again.  The products
-// run at 100-110 TFLOP/s (peak 157) and are nine tenths of the time at 2000 x 256,
+// run at 87-113 TFLOP/s (peak 157) and are nine tenths of the time at 2000 x 256,
 // 10,007 classes (349 us; 17 x 128, 1009 classes: 36 us of launches).  bfloat16:
-// 16,384 x 1024, 131,072 classes 15.6 ms, four products of 1080-1330 TFLOP/s.
+// 16,384 x 1024, 131,072 classes 15.4 ms, four products of 1080-1330 TFLOP/s.
 #include <algorithm>
 
 #include "gcn_classes.h"

@@ -206,7 +206,8 @@ __global__ __launch_bounds__(kTB) void pack_weights_kernel(int32_t K, int32_t N,
 
 // The elementwise half of the backward pass: dZ = bf16(dY) where the mask byte
 // is a positive e4m3 value (1 .. 0x7E), zero elsewhere, as bfloat16 rows; the
-// column sums of a strip of rows; and, when wanted, dZ's 8-bit rows.  One
+// column sums of a strip of rows; and, when wanted, dZ's 8-bit rows.  All three,
+// and dW, are of the rounded dZ: db belongs to the dW beside it.  One
 // block of 128 columns and a strip of rows to a workgroup, 16 lanes a row, so
 // that one pass over dY and the mask serves all three.  The rows from n to nz
 // are zeros.  The workgroups past the strips widen X8 to bfloat16 rows.  Bound by
