@@ -179,9 +179,16 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # (not part of torch's documented interface)
+
+
 def _stream(stream=None):
-    # (the current stream's handle without its Python object: a call's largest cost on the host)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
+    if stream is None:
+        # (the handle without its Python object, where torch gives it: the object is a call's largest cost on the host)
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
+        stream = torch.cuda.current_stream()
+    return stream.cuda_stream
 
 
 def _ld(t: torch.Tensor) -> int:

@@ -96,3 +96,19 @@ def test_parts_on_different_devices_are_refused():
     for at in ((1, 0, 0), (0, 1, 0), (0, 0, 1)):
         with pytest.raises(ValueError, match="one device"):
             B.Weights8.of(kept(128, 128, at[0]), kept(128, 128, at[1]), scale(1, 1, at[2]))
+
+
+# ------------------------------------------------------------------- streams
+def test_the_current_stream_without_torchs_undocumented_call(monkeypatch):
+    """Every call's stream: the documented one where torch does not give the handle alone."""
+    class Current:
+        cuda_stream = 0x1234
+
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: Current)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(B, "_raw_stream", None)
+    assert B._stream() == 0x1234
+    monkeypatch.setattr(B, "_raw_stream", lambda device: 0x5000 + device)
+    assert B._stream() == 0x5003
+    Current.cuda_stream = 0x77
+    assert B._stream(Current) == 0x77
