@@ -91,3 +91,20 @@ def test_weight_grad_of_large_subgraphs(n, f, N, dtype, mask):
 def test_product_about_the_edges_of_a_tile_size(n, K, N, transpose):
     """From 384 to 768 tiles of 64 x 128, and one row of tiles more."""
     small.test_product_of_many_tiles(n, K, N, transpose)
+
+
+@pytest.mark.parametrize("shift", [-149, -140, -134, -127, -118, 120])
+def test_pack_and_unpack_at_the_ends_of_the_types(shift):
+    """Blocks from float32's smallest subnormal to its largest values: bytes, scales and what comes back, in float32
+    exactly and in bfloat16 rounded once."""
+    g = gen(shift + 1000)
+    x = np.ldexp(g.integers(-15, 16, size=(6, 300)).astype(np.float64), shift)
+    x[0, :128], x[1, 5], x[2, 7] = 0.0, -0.0, np.ldexp(1.0, -149)
+    r = B.gcn_rows8_pack(to_dev(x), B.Rows8(6, 300))
+    q, s = R.pack_rows(x)
+    assert np.array_equal(bytes_of(r.values), q) and np.array_equal(bytes_of(r.scale), s)
+    v = R.values(q, s)
+    out = B.gcn_rows8_unpack(r, torch.empty((6, 300), device="cuda"))
+    assert np.array_equal(out.cpu().numpy().astype(np.float64), v)
+    out = B.gcn_rows8_unpack(r, torch.empty((6, 300), dtype=torch.bfloat16, device="cuda"))
+    assert torch.equal(out.cpu(), torch.from_numpy(v.astype(np.float32)).to(torch.bfloat16))
