@@ -1045,8 +1045,10 @@ TileShape tile_shape(TileType type, const TileProduct &p) {
         // and 8.9 / 8.0; K = 4096 41.6 / 45 and 53 / 45) and of the second round of 128 x
         // 128 ones while they need three rounds themselves (128 x 128 / 64 x 128: K =
         // 1024 at 513 .. 768 24.5 / 20.8, 772 .. 1024 25.0 / 26.8; K = 4096 71 / 60-64 and
-        // 72 / 80; K = 128 10.5 / 9.2 and 10.8 / 12.0).  bfloat16 results: 1000 x 4096 x
-        // 2048 (64 x 64 / 64 x 128) 18.7 / 21.8.
+        // 72 / 80; K = 128 10.5 / 9.2 and 10.8 / 12.0).  Whole columns of tiles; where
+        // the last one is at most half full they gain less and 64 x 64 ones would be the
+        // fastest (38,400 x 64, K = 2048: 128 x 128 38, 64 x 128 32, 64 x 64 23).  bfloat16
+        // results: 1000 x 4096 x 2048 (64 x 64 / 64 x 128) 18.7 / 21.8.
         const int64_t wide = ((int64_t)p.M + 63) / 64 * (((int64_t)p.N + 127) / 128);
         if (type == TILE_FP8_EXACT && splits == 1 && wide > 384 && wide <= 768) return TileShape{64, 128};
         if (tiles_of(p.M, p.N, 128) < 256) return TileShape{64, 64};
