@@ -21,6 +21,7 @@ GCN_AGGREGATE_FIRST, GCN_TRANSFORM_FIRST = 0, 1
 GCN_SOFTMAX_CE, GCN_SIGMOID_BCE = 0, 1
 GCN_ROWS_F32, GCN_ROWS_BF16 = 0, 1
 ROWS8_BLOCK = 128                         # columns under one scale of 8-bit rows
+ROWS4_PIECE = 256                         # columns of 4-bit rows that are kept together
 LOSS_KIND = {"ce": GCN_SOFTMAX_CE, "bce": GCN_SIGMOID_BCE}
 GCN_NOALLOC_SCRATCH_BYTES = 64 << 20      # the static scratch array of gcn_aggregate_noalloc
 PREC = {"f32": GCN_F32, "fp32": GCN_F32, "bf16": GCN_BF16}
@@ -46,6 +47,11 @@ class gcn_rows8(ctypes.Structure):
 class gcn_weights8(ctypes.Structure):
     _fields_ = [("K", ctypes.c_int32), ("N", ctypes.c_int32), ("ldq", ctypes.c_int32), ("ldqT", ctypes.c_int32),
                 ("ldscale", ctypes.c_int32), ("q", ctypes.c_void_p), ("qT", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p)]
+
+
+class gcn_rows4(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("f", ctypes.c_int32), ("ldq", ctypes.c_int32), ("q", ctypes.c_void_p),
                 ("scale", ctypes.c_void_p)]
 
 
@@ -79,6 +85,7 @@ _SZ = ctypes.c_size_t
 _CSRP = ctypes.POINTER(gcn_csr)
 _R8P = ctypes.POINTER(gcn_rows8)
 _W8P = ctypes.POINTER(gcn_weights8)
+_R4P = ctypes.POINTER(gcn_rows4)
 
 _SIGNATURES = {
     "gcn_last_error": (ctypes.c_char_p, []),
@@ -135,6 +142,12 @@ _SIGNATURES = {
     "gcn_rows8_weight_grad_workspace_bytes": (_SZ, [_I32, _I32, _I32]),
     "gcn_rows8_weight_grad": (ctypes.c_int, [_R8P, _P, _I32, _P, ctypes.c_int, _I32, _I32, _P, _I32, _P, _R8P, _P, _SZ,
                                              _P]),
+    # gcn_rows4.h
+    "gcn_rows4_pack_workspace_bytes": (_SZ, [_I32, _I32]),
+    "gcn_rows4_pack": (ctypes.c_int, [_P, ctypes.c_int, _I32, _I32, _I32, _P, _I32, _R4P, _R4P, _P, _P, _SZ, _P]),
+    "gcn_rows4_unpack": (ctypes.c_int, [_R4P, _P, ctypes.c_int, _I32, _P]),
+    "gcn_rows4_product_workspace_bytes": (_SZ, [_I32, _I32, _I32]),
+    "gcn_rows4_product": (ctypes.c_int, [_R4P, _R4P, _P, ctypes.c_int, _P, ctypes.c_int, _I32, _P, _SZ, _P]),
     # gcn_classes.h
     "gcn_class_loss_workspace_bytes": (_SZ, [_I32, _I32, _I32, ctypes.c_int, ctypes.c_int]),
     "gcn_class_loss": (ctypes.c_int, [_P, _I32, _I32, _I32, _P, _P, _I32, _P, ctypes.c_int, _P, _P, _P, _I32, _P, _P,
@@ -744,6 +757,108 @@ def gcn_rows8_weight_grad(X8: Rows8, dY: torch.Tensor, dW: torch.Tensor, ws: Wor
             _one_device(dW, X8.values, dY, db, mask, None if dZ8 is None else dZ8.values, ws.buf), stream, X8.ref,
             _ptr(mask), ldm, dY.data_ptr(), _rows_type(dY, "dY"), _ld(dY), N, dW.data_ptr(), _ld(dW), _ptr(db),
             None if dZ8 is None else dZ8.ref, w, wb)
+
+
+# ---------------------------------------------------------------- 4-bit rows
+def _pieces4(f: int) -> int:
+    return (f + ROWS4_PIECE - 1) // ROWS4_PIECE
+
+
+class Rows4:
+    """n x f values in 4 bits: `values` (uint8, n x 128 ceil(f / 256), two
+    values a byte, the first in the low bits, zeros past f) and `scale` (uint8,
+    ceil(f / 256) x ceil(n / 64) x 512, in the order of gcn_rows4.h; see
+    rows4_scales)."""
+
+    def __init__(self, n: int, f: int, device="cuda"):
+        d = torch.device(device)
+        # (scales: 2^-127 behind the last row, where nothing is written)
+        self._set(torch.zeros((n, _pieces4(f) * ROWS4_PIECE // 2), dtype=torch.uint8, device=d),
+                  torch.zeros((_pieces4(f), (n + 63) // 64, 512), dtype=torch.uint8, device=d), f)
+
+    @classmethod
+    def of(cls, values: torch.Tensor, scale: torch.Tensor, f: int) -> "Rows4":
+        """Rows kept elsewhere, f columns: `values` row-major with rows of whole 128-byte pieces."""
+        self = cls.__new__(cls)
+        self._set(values, scale, f)
+        return self
+
+    def _set(self, values, scale, f):
+        self.n, self.f = int(values.shape[0]), int(f)
+        self.values, self.scale = values, scale
+        row = _pieces4(self.f) * ROWS4_PIECE // 2
+        if values.dim() != 2 or values.dtype != torch.uint8 or not values.is_cuda or values.shape[1] < row:
+            raise TypeError("values must be a uint8 CUDA/HIP tensor with rows of whole 128-byte pieces")
+        ld = row
+        if self.n and row:
+            if values.stride(1) != 1:
+                raise ValueError("values must have unit column stride")
+            if self.n > 1:
+                ld = int(values.stride(0))
+        _want(scale, "scale", torch.uint8, (_pieces4(self.f), (self.n + 63) // 64, 512))
+        if not scale.is_contiguous():
+            raise ValueError("scale must be contiguous")
+        _one_device(values, scale)
+        self.struct = gcn_rows4(self.n, self.f, ld, values.data_ptr(), scale.data_ptr())
+        self.ref = ctypes.byref(self.struct)
+
+
+def rows4_scales(scale: torch.Tensor) -> torch.Tensor:
+    """Scale bytes n x ceil(f / 32), a row's one after another, in the order that Rows4 keeps them."""
+    n, b = int(scale.shape[0]), int(scale.shape[1])
+    pieces, groups = (b + 7) // 8, (n + 63) // 64
+    s = torch.nn.functional.pad(scale, (0, pieces * 8 - b, 0, groups * 64 - n), value=127)
+    # [group, row block, row, piece, half, block] -> [piece, group, half, block, row, row block]
+    return s.view(groups, 4, 16, pieces, 2, 4).permute(3, 0, 4, 5, 2, 1).reshape(pieces, groups, 512).contiguous()
+
+
+def gcn_rows4_pack(X: torch.Tensor, ws: Workspace, out: Optional[Rows4] = None, out_t: Optional[Rows4] = None,
+                   mask: Optional[torch.Tensor] = None, colsum: Optional[torch.Tensor] = None, stream=None):
+    """out, out_t = the 4-bit rows of Z and of Z^T, colsum = the column sums of
+    Z, with Z = X where mask is positive and zero elsewhere, or X without one."""
+    t = _rows_type(X, "X")
+    ldx = _ld(X)
+    n, f = int(X.shape[0]), int(X.shape[1])
+    if out is not None and (out.n, out.f) != (n, f):
+        raise ValueError("X and out differ in shape")
+    if out_t is not None and (out_t.n, out_t.f) != (f, n):
+        raise ValueError("out_t must be f x n")
+    if mask is not None:
+        _want(mask, "mask", X.dtype, (n, f))
+    w = wb = None
+    if colsum is not None:
+        _want(colsum, "colsum", torch.float32, (f,))
+        if not colsum.is_contiguous():
+            raise ValueError("colsum must be contiguous")
+        w, wb = ws.args(lib().gcn_rows4_pack_workspace_bytes(n, f))
+    _launch("gcn_rows4_pack",
+            _one_device(X, mask, None if out is None else out.values, None if out_t is None else out_t.values, colsum,
+                        None if w is None else ws.buf), stream, X.data_ptr(), t, n, f, ldx, _ptr(mask),
+            0 if mask is None else _ld(mask), None if out is None else out.ref, None if out_t is None else out_t.ref,
+            _ptr(colsum), w, wb or 0)
+
+
+def gcn_rows4_unpack(rows: Rows4, out: torch.Tensor, stream=None) -> torch.Tensor:
+    if tuple(out.shape) != (rows.n, rows.f):
+        raise ValueError("out and the 4-bit rows differ in shape")
+    _launch("gcn_rows4_unpack", _one_device(out, rows.values), stream, rows.ref, out.data_ptr(), _rows_type(out, "out"),
+            _ld(out))
+    return out
+
+
+def gcn_rows4_product(A4: Rows4, B4: Rows4, Y: torch.Tensor, ws: Workspace, bias: Optional[torch.Tensor] = None,
+                      relu: bool = False, stream=None) -> torch.Tensor:
+    """Y [A4.n x B4.n] = act(A4 B4^T + bias)."""
+    if tuple(Y.shape) != (A4.n, B4.n):
+        raise ValueError("Y's shape does not fit the operands")
+    if bias is not None:
+        _dev_f32(bias, "bias")
+        if bias.numel() != B4.n or not bias.is_contiguous():
+            raise ValueError("bias needs one contiguous element per column of Y")
+    w, wb = ws.args(lib().gcn_rows4_product_workspace_bytes(A4.n, B4.n, A4.f))
+    _launch("gcn_rows4_product", _one_device(Y, A4.values, B4.values, bias, ws.buf), stream, A4.ref, B4.ref, _ptr(bias),
+            int(bool(relu)), Y.data_ptr(), _rows_type(Y, "Y"), _ld(Y), w, wb)
+    return Y
 
 
 # ------------------------------------------------------------- many classes

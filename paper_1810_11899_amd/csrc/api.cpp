@@ -39,7 +39,8 @@ static const char *kClassNames[K_CLASS_COUNT] = {
     "transpose_sort", "transpose_final", "cvt_bf16", "gemm_nn_bf16", "gemm_tn_bf16", "gemm_nt_bf16",
     "spmm_bf16", "transpose_bf16", "frontier_sample", "induce_subgraphs", "gather_rows", "adam", "transpose_symmetric",
     "gemm_nt_bf16_big", "gemm_nt_bf16_big_masked", "gemm_tn_bf16_big", "rows8_pack", "rows8_product",
-    "rows8_mask", "rows8_weight_grad", "class_prep", "class_stats", "class_grad", "class_product"};
+    "rows8_mask", "rows8_weight_grad", "class_prep", "class_stats", "class_grad", "class_product",
+    "rows4_pack", "rows4_product", "muon_prep", "muon_product", "muon_update"};
 
 const char *class_name(int cls) {
     return (cls >= 0 && cls < K_CLASS_COUNT) ? kClassNames[cls] : "";

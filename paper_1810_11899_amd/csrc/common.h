@@ -97,6 +97,11 @@ enum KernelClass {
     K_CLASS_STATS,              // logits of a piece joined into the running maximum and sum
     K_CLASS_GRAD,               // logits of a piece to their gradient
     K_CLASS_PRODUCT,            // the gradient's two products
+    K_ROWS4_PACK,               // 4-bit rows: packing, unpacking
+    K_ROWS4_PRODUCT,
+    K_MUON_PREP,                // orthogonalised update: momentum and norm, operands
+    K_MUON_PRODUCT,
+    K_MUON_UPDATE,
     K_CLASS_COUNT
 };
 const char *class_name(int cls);

@@ -408,6 +408,53 @@ __global__ __launch_bounds__(64 * kThinWaves) void thin_kernel(TileProduct p) {
     }
 }
 
+// The same of 4-bit rows: a wavefront takes every eighth piece of 256 columns.
+template <int EPI, int FM>
+__global__ __launch_bounds__(64 * kThinWaves) void thin4_kernel(TileProduct p) {
+    __shared__ f32x4 part[kThinWaves][FM][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * 16;
+    const uint8_t *const b = p.B + (int64_t)min(n0 + fr, p.N - 1) * p.ldb + g * 16;
+    const uint8_t *const sbp = p.sb + (int64_t)(n0 / 64) * 512 + lane * 4;
+    const int by = n0 % 64 / 16 * 8;
+    const uint8_t *a[FM];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) a[i] = p.A + (int64_t)min(16 * i + fr, p.M - 1) * p.lda + g * 16;
+    f32x4 acc[FM];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int t = wave; t < p.kt; t += kThinWaves) {
+        const int64_t o = (int64_t)t * kPiece;
+        const Frag fb = {*(const uint4 *)(b + o), *(const uint4 *)(b + o + 64)};
+        const uint8_t *sbt = sbp + (int64_t)t * p.groups_b * 512, *sat = p.sa + (int64_t)t * p.groups_a * 512 + lane * 4;
+        const int b4[2] = {*(const int *)sbt >> by, *(const int *)(sbt + 256) >> by};
+        const int a4[2] = {*(const int *)sat, *(const int *)(sat + 256)};
+        static_for<FM>([&](auto i) {
+            const Frag fa = {*(const uint4 *)(a[i.value] + o), *(const uint4 *)(a[i.value] + o + 64)};
+            mma4<i.value, 0>(acc[i.value], fa, fb, a4, b4);
+        });
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i) part[wave][i][lane] = acc[i];
+    __syncthreads();
+    if (wave >= FM) return;
+    f32x4 v = part[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < kThinWaves; ++w) v += part[w][wave][lane];
+    const int row = 16 * wave + fr;
+    if (row >= p.M) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int col = n0 + 4 * g + e;
+        if (col >= p.N) break;
+        float x = v[e] + (p.bias ? p.bias[col] : 0.0f);
+        if (p.relu) x = x < 0.0f ? 0.0f : x;   // (NaN stays)
+        const int64_t at = (int64_t)row * p.ldc + col;
+        if constexpr (EPI == TILE_STORE) ((uint16_t *)p.C)[at] = to_bf16(x);
+        else ((float *)p.C)[at] = x;
+    }
+}
+
 template <int V>
 __device__ __forceinline__ auto load_bias(const float *b) {
     typedef float vec __attribute__((ext_vector_type(V)));
@@ -463,6 +510,19 @@ __global__ __launch_bounds__(256) void reduce_kernel(int32_t splits, int64_t cou
 
 template <int TYPE, int EPI>
 void launch(TileShape t, const Args &a, unsigned grid, hipStream_t s) {
+    if constexpr (TYPE == TILE_FP4) {
+        if constexpr (EPI != TILE_PARTIAL) if (t.n == 16) {
+            const dim3 g((unsigned)((a.p.N + 15ll) / 16)), b(64 * kThinWaves);
+            if (a.p.M <= 16) hipLaunchKernelGGL((thin4_kernel<EPI, 1>), g, b, 0, s, a.p);
+            else if (a.p.M <= 32) hipLaunchKernelGGL((thin4_kernel<EPI, 2>), g, b, 0, s, a.p);
+            else hipLaunchKernelGGL((thin4_kernel<EPI, 4>), g, b, 0, s, a.p);
+            return;
+        }
+        if (t.m == 64) {
+            hipLaunchKernelGGL((tile_kernel<TYPE, EPI, 64, 64, 4, 1>), dim3(grid), dim3(256), 0, s, a);
+            return;
+        }
+    }
     if constexpr (TYPE == TILE_FP8 || TYPE == TILE_FP8_EXACT) {
         if constexpr (EPI != TILE_PARTIAL) if (t.n == 16) {
             const dim3 g((unsigned)((a.p.N + 15) / 16)), b(64 * kThinWaves);
@@ -508,6 +568,13 @@ int64_t tiles_of(int64_t M, int64_t N, int64_t t) { return ((M + t - 1) / t) * (
 
 TileShape tile_shape(TileType type, const TileProduct &p) {
     const int32_t splits = std::max(1, p.splits), per = (p.kt + splits - 1) / splits;
+    if (type == TILE_FP4) {
+        if (p.M <= kThin && splits == 1) return TileShape{kThin, 16};
+        if (tiles_of(p.M, p.N, kBigT) * splits >= 160 && per >= 4 && std::max(p.lda, p.ldb) < (1 << 24))
+            return TileShape{kBigT, kBigT};
+        if (tiles_of(p.M, p.N, 128) * splits < 256) return TileShape{64, 64};
+        return TileShape{128, 128};
+    }
     if (splits > 1 && (type == TILE_FP8 || type == TILE_FP8_EXACT)) return TileShape{64, 64};   // (split8)
     const bool big = type != TILE_FP8_EXACT && !is_f32(type) && tiles_of(p.M, p.N, kBigT) * splits >= 160 && per >= 4 &&
                      (type != TILE_FP8 || per <= kBigPieces) && std::max(p.lda, p.ldb) < (1 << 24);
@@ -625,6 +692,9 @@ int tile_product(TileType type, TileEpilogue epi, const TileProduct &p, hipStrea
     else if (type == TILE_BF16 && epi == TILE_PARTIAL) launch<TILE_BF16, TILE_PARTIAL>(t, a, grid, s);
     else if (type == TILE_BF16_TN && epi == TILE_STORE) launch<TILE_BF16_TN, TILE_STORE>(t, a, grid, s);
     else if (type == TILE_BF16_TN && epi == TILE_PARTIAL) launch<TILE_BF16_TN, TILE_PARTIAL>(t, a, grid, s);
+    else if (type == TILE_FP4 && epi == TILE_STORE) launch<TILE_FP4, TILE_STORE>(t, a, grid, s);
+    else if (type == TILE_FP4 && epi == TILE_STORE_F32) launch<TILE_FP4, TILE_STORE_F32>(t, a, grid, s);
+    else if (type == TILE_FP4 && epi == TILE_PARTIAL) launch<TILE_FP4, TILE_PARTIAL>(t, a, grid, s);
     else if (type == TILE_FP8 && epi == TILE_STORE) launch<TILE_FP8, TILE_STORE>(t, a, grid, s);
     else if (type == TILE_FP8 && epi == TILE_PARTIAL) launch<TILE_FP8, TILE_PARTIAL>(t, a, grid, s);
     else if (type == TILE_FP8_EXACT && epi == TILE_PARTIAL) launch<TILE_FP8_EXACT, TILE_PARTIAL>(t, a, grid, s);

@@ -36,7 +36,12 @@ enum TileType {
     TILE_BF16_NN = 4,    // C = A B, A bfloat16 rows and B stored K x N
     TILE_F32 = 5,        // the three for float32 operands and products
     TILE_F32_TN = 6,
-    TILE_F32_NN = 7
+    TILE_F32_NN = 7,
+    TILE_F16 = 8,        // float16 operands
+    TILE_F16_NN = 9,     // C = A B, A float16 rows and B stored K x N
+    TILE_PAIR = 10,      // float16 pairs, three part products (muon.hip)
+    TILE_PAIR_NN = 11,   // C = A B of pairs: B's rows are pairs along its columns too
+    TILE_FP4 = 12        // e2m1 operands with scales, 4-bit matrix instructions
 };
 enum TileEpilogue {
     TILE_STORE = 0,    // C as bfloat16, bias, ReLU
@@ -55,6 +60,9 @@ struct TileProduct {
     // of row j, piece k at sb[(j / 128) * sb_n + k * sb_k]
     const uint8_t *sa, *sb;
     int64_t ldsa, sb_n, sb_k;
+    // of 4-bit operands: scales of 64 rows and a piece in 512 bytes, those of
+    // piece k and row group r at sa[(k * groups_a + r) * 512], B's likewise
+    int32_t groups_a, groups_b;
     // TILE_STORE, TILE_STORE_F32, TILE_STATS_STORE
     void *C;
     int64_t ldc;             // elements

@@ -27,6 +27,7 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16v8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16v8 __attribute__((ext_vector_type(8)));
 
 constexpr int kPiece = 128;   // bytes of a row in one stage
 
@@ -61,15 +62,37 @@ struct Frag {
     uint4 lo, hi;
 };
 
+// byte of column c's high part in a row of pairs: 32 high parts, then their 32
+// low ones, 64 bytes on
+__host__ __device__ __forceinline__ int64_t pair_place(int64_t c) { return c / 32 * 128 + c % 32 * 2; }
+
 constexpr bool is_fp8(int type) { return type == TILE_FP8 || type == TILE_FP8_EXACT; }
 constexpr bool is_f32(int type) { return type == TILE_F32 || type == TILE_F32_TN || type == TILE_F32_NN; }
 // which operands are stored along the other way
 constexpr bool km_a(int type) { return type == TILE_BF16_TN || type == TILE_F32_TN; }
-constexpr bool km_b(int type) { return km_a(type) || type == TILE_BF16_NN || type == TILE_F32_NN; }
+constexpr bool km_b(int type) {
+    return km_a(type) || type == TILE_BF16_NN || type == TILE_F32_NN || type == TILE_F16_NN || type == TILE_PAIR_NN;
+}
+constexpr bool is_f16(int type) { return type == TILE_F16 || type == TILE_F16_NN; }
+constexpr bool is_pair(int type) { return type == TILE_PAIR || type == TILE_PAIR_NN; }
 
 template <int TYPE>
 __device__ __forceinline__ void mma(f32x4 &acc, const Frag &a, const Frag &b, int sa, int sb) {
-    if constexpr (!is_fp8(TYPE)) {
+    if constexpr (is_f16(TYPE)) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16v8, b.lo), __builtin_bit_cast(f16v8, a.lo),
+                                                     acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16v8, b.hi), __builtin_bit_cast(f16v8, a.hi),
+                                                     acc, 0, 0, 0);
+    } else if constexpr (is_pair(TYPE)) {
+        // 32 columns: their high parts in the first chunks, their low parts in the
+        // others; the product of the low parts is below the sum's last bit
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16v8, b.lo), __builtin_bit_cast(f16v8, a.hi),
+                                                     acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16v8, b.hi), __builtin_bit_cast(f16v8, a.lo),
+                                                     acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16v8, b.lo), __builtin_bit_cast(f16v8, a.lo),
+                                                     acc, 0, 0, 0);
+    } else if constexpr (!is_fp8(TYPE)) {
         acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16v8, b.lo),
                                                       __builtin_bit_cast(bf16v8, a.lo), acc, 0, 0, 0);
         acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16v8, b.hi),
@@ -78,6 +101,19 @@ __device__ __forceinline__ void mma(f32x4 &acc, const Frag &a, const Frag &b, in
         acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i32x8, b),
                                                                __builtin_bit_cast(i32x8, a), acc, 0, 0, 0, sb, 0, sa);
     }
+}
+
+// 4-bit operands: a chunk is one block of 32 values, which one lane of the
+// instruction holds, so that the chunks g and g + 4 are two instructions' shares.
+// sa, sb: words of the scales of four 16-row blocks for the first and the second
+// half of the piece; the instruction picks byte I of A's and J of B's.
+__device__ __forceinline__ i32x8 four_words(uint4 v) {
+    return i32x8{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
+}
+template <int I, int J>
+__device__ __forceinline__ void mma4(f32x4 &acc, const Frag &a, const Frag &b, const int (&sa)[2], const int (&sb)[2]) {
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(four_words(b.lo), four_words(a.lo), acc, 4, 4, J, sb[0], I, sa[0]);
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(four_words(b.hi), four_words(a.hi), acc, 4, 4, J, sb[1], I, sa[1]);
 }
 
 // Operands stored along the other way (KM: K x rows): a stage holds 64 k-rows
@@ -141,6 +177,14 @@ __device__ __forceinline__ void copy_to_lds(const uint8_t *base, uint32_t off, u
 __device__ __forceinline__ void copy_to_lds(const uint8_t *from, uint32_t dst) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(from) : "memory", "m0");
 }
+// f(0), f(1) .. f(N - 1) of compile-time numbers
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void static_for(F &&f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        static_for<N, I + 1>(f);
+    }
+}
 template <int N>
 __device__ __forceinline__ void wait_copies() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
@@ -164,7 +208,7 @@ __device__ __forceinline__ void turn() {
 // kScalePieces pieces at a time.
 constexpr int kScalePieces = 64;
 constexpr int small_lds(int type, int BM, int BN) {
-    return 2 * (BM + BN) * kPiece + (is_fp8(type) ? kScalePieces * (BM + 1) : 0);
+    return 2 * (BM + BN) * kPiece + (is_fp8(type) ? kScalePieces * (BM + 1) : type == TILE_FP4 ? 16 * (BM + BN) : 0);
 }
 // `lds`: small_lds bytes; behind the loop they are free again.
 template <int TYPE, int BM, int BN, int WM, int WN>
@@ -174,15 +218,17 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
     constexpr int kStage = (BM + BN) * kPiece;
     constexpr int LA = BM * kPiece / 16 / T, LB = BN * kPiece / 16 / T;
     static_assert(LA * T * 16 == BM * kPiece && LB * T * 16 == BN * kPiece, "whole chunks per lane");
-    static_assert(kRows8Block % BN == 0, "a tile's columns share a scale");
     constexpr bool SCALED = is_fp8(TYPE);
+    static_assert(!SCALED || kRows8Block % BN == 0, "a tile's columns share a scale");
+    static_assert(TYPE != TILE_FP4 || (BM % 64 == 0 && BN % 64 == 0 && FN == 4), "scales come in groups of 64 rows");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const int m0 = c.tm * BM, n0 = c.tn * BN;
     constexpr bool KA = km_a(TYPE), KB = km_b(TYPE);
     static_assert((!KA || BM == 128) && (!KB || BN == 128), "k-rows of 128 elements");
     constexpr int E = is_f32(TYPE) ? 4 : 2, V = 16 / E, CH = 128 / V;   // of k-major operands: bytes, elements a chunk, chunks a row
-    const int64_t step_a = KA ? kPiece / E * p.lda : kPiece, step_b = KB ? kPiece / E * p.ldb : kPiece;
+    // (pairs along the columns: a stage holds 32 rows' high parts, then their low ones)
+    const int64_t step_a = KA ? kPiece / E * p.lda : kPiece, step_b = KB ? kPiece / (is_pair(TYPE) ? 4 : E) * p.ldb : kPiece;
     // Copy u of a thread: tile row (u T + thread) / 8, stored chunk thread % 8,
     // which holds the row's chunk (thread % 8) ^ (row % 8); rows past the extent
     // are clamped (their products are dropped).  k-major: k-row (u T + thread) /
@@ -190,6 +236,7 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
     const int lr = threadIdx.x >> 3, chunk = ((threadIdx.x & 7) ^ (lr & 7)) * 16;
     auto km_at = [&](int64_t ld, int x0, int extent, int u) {
         const int k = (u * T + threadIdx.x) / CH, ch = V * ((threadIdx.x % CH) ^ (4 * ((is_f32(TYPE) ? k >> 2 : k) & 3)));
+        if constexpr (is_pair(TYPE)) return (k & 31) * ld + pair_place(min(x0 + ch, ((extent + 31) & -32) - 8)) + (k >> 5) * 64;
         return k * ld + E * (int64_t)min(x0 + ch, ((extent + V - 1) & -V) - V);
     };
     const uint8_t *ga[LA], *gb[LB];
@@ -202,12 +249,26 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
         gb[u] = p.B + kt0 * step_b +
                 (KB ? km_at(p.ldb, n0, p.N, u) : (int64_t)min(n0 + u * (T / 8) + lr, p.N - 1) * p.ldb + chunk);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * 1024;
+    // 4-bit operands: the piece's scales, 32 lanes a group of 64 rows, A's groups first
+    const uint8_t *g4 = nullptr;
+    int64_t step4 = 0;
+    if constexpr (TYPE == TILE_FP4) {
+        const int r = threadIdx.x >> 5, nb = BM / 64;
+        const bool of_a = r < nb;
+        step4 = (int64_t)(of_a ? p.groups_a : p.groups_b) * 512;
+        g4 = (of_a ? p.sa + (int64_t)min(m0 / 64 + r, p.groups_a - 1) * 512
+                   : p.sb + (int64_t)min(n0 / 64 + r - nb, p.groups_b - 1) * 512) +
+             kt0 * step4 + (threadIdx.x & 31) * 16;
+    }
     auto copy = [&](int t, int stage) {
         const uint32_t d = lds0 + stage * kStage;
 #pragma unroll
         for (int u = 0; u < LA; ++u) copy_to_lds(ga[u] + t * step_a, d + u * T * 16);
 #pragma unroll
         for (int u = 0; u < LB; ++u) copy_to_lds(gb[u] + t * step_b, d + BM * kPiece + u * T * 16);
+        if constexpr (TYPE == TILE_FP4) {
+            if (threadIdx.x < (BM + BN) / 2) copy_to_lds(g4 + t * step4, lds0 + 2 * kStage + stage * 8 * (BM + BN));
+        }
     };
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -257,6 +318,17 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
         Frag fb[FN];
 #pragma unroll
         for (int j = 0; j < FN; ++j) fb[j] = frag(tb, wn * (BN / WN) + 16 * j, KB);
+        if constexpr (TYPE == TILE_FP4) {
+            const char *s4 = lds + 2 * kStage + (t & 1) * 8 * (BM + BN) + lane * 4;
+            const char *qb = s4 + (BM / 64 + wn) * 512, *qa = s4 + wm * (BM / WM) / 64 * 512;
+            const int b4[2] = {*(const int *)qb, *(const int *)(qb + 256)};
+            const int by = wm * (BM / WM) % 64 / 16 * 8;   // (a wavefront with fewer rows than 64: its first block to byte 0)
+            const int a4[2] = {*(const int *)qa >> by, *(const int *)(qa + 256) >> by};
+            static_for<FM>([&](auto i) {
+                const Frag fa = frag(ta, wm * (BM / WM) + 16 * i.value, false);
+                static_for<FN>([&](auto j) { mma4<i.value, j.value>(acc[i.value][j.value], fa, fb[j.value], a4, b4); });
+            });
+        } else
         if constexpr (TYPE == TILE_FP8_EXACT) {
             bf16v8 wb[FN][4];
 #pragma unroll
@@ -357,7 +429,10 @@ __device__ __forceinline__ void mma_big(f32x4 &acc, const Frag &a, const Frag &b
         mma<TYPE>(acc, a, b, 0, 0);
 }
 
-constexpr int big_lds(int type) { return 2 * kBuffer + (type == TILE_FP8 ? kScaleA + kScaleB : 0); }
+constexpr int kScales4 = 16 * 2 * kBigT / 2;   // of the 512 rows of a 4-bit piece, 8 a row
+constexpr int big_lds(int type) {
+    return 2 * kBuffer + (type == TILE_FP8 ? kScaleA + kScaleB : type == TILE_FP4 ? 2 * kScales4 : 0);
+}
 // `lds`: big_lds bytes.
 template <int TYPE>
 __device__ __forceinline__ void big_loop(const TileProduct &p, const Coord &c, int kt0, int nt, char *lds,
@@ -372,9 +447,10 @@ __device__ __forceinline__ void big_loop(const TileProduct &p, const Coord &c, i
     // of the 8 of A's first or second half's columns in the region, or of the 4
     // of B's four quarters'; chunks past the extent are clamped to the last.
     constexpr bool KA = km_a(TYPE), KB = km_b(TYPE);
-    const int64_t step_a = KA ? 64 * p.lda : kPiece, step_b = KB ? 64 * p.ldb : kPiece;
+    constexpr bool PB = TYPE == TILE_PAIR_NN;   // (a stage: 32 rows' high parts, then their low ones)
+    const int64_t step_a = KA ? 64 * p.lda : kPiece, step_b = KB ? (PB ? 32 : 64) * p.ldb : kPiece;
     const uint8_t *const ba = p.A + (KA ? (int64_t)m0 * 2 : (int64_t)m0 * p.lda) + kt0 * step_a;
-    const uint8_t *const bb = p.B + (KB ? (int64_t)n0 * 2 : (int64_t)n0 * p.ldb) + kt0 * step_b;
+    const uint8_t *const bb = p.B + (KB ? (int64_t)n0 * (PB ? 4 : 2) : (int64_t)n0 * p.ldb) + kt0 * step_b;
     uint32_t oa[2][2], ob[2][2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -388,12 +464,23 @@ __device__ __forceinline__ void big_loop(const TileProduct &p, const Coord &c, i
                            2 * (uint32_t)min((gc >> 3) * 128 + 64 * h + (gc & 7) * 8, ((p.M + 7) & ~7) - 8 - m0);
             else
                 oa[h][u] = (uint32_t)min((rr >> 6) * 128 + (rr & 63) + 64 * h, p.M - 1 - m0) * (uint32_t)p.lda + ch;
-            if constexpr (KB)
+            if constexpr (PB)
+                ob[h][u] = (uint32_t)(k & 31) * (uint32_t)p.ldb + 64 * (uint32_t)(k >> 5) +
+                           (uint32_t)pair_place(min((gc >> 2) * 64 + 32 * h + (gc & 3) * 8, ((p.N + 31) & ~31) - 8 - n0));
+            else if constexpr (KB)
                 ob[h][u] = (uint32_t)k * (uint32_t)p.ldb +
                            2 * (uint32_t)min((gc >> 2) * 64 + 32 * h + (gc & 3) * 8, ((p.N + 7) & ~7) - 8 - n0);
             else
                 ob[h][u] = (uint32_t)min((rr >> 5) * 64 + (rr & 31) + 32 * h, p.N - 1 - n0) * (uint32_t)p.ldb + ch;
         }
+    }
+    const uint8_t *g4 = nullptr;
+    int64_t step4 = 0;
+    if constexpr (TYPE == TILE_FP4) {
+        step4 = (int64_t)(wave < 4 ? p.groups_a : p.groups_b) * 512;
+        g4 = (wave < 4 ? p.sa + (int64_t)min(m0 / 64 + wave, p.groups_a - 1) * 512
+                       : p.sb + (int64_t)min(n0 / 64 + wave - 4, p.groups_b - 1) * 512) +
+             kt0 * step4 + lane * 16;
     }
     // region 0, 1: A-lo, A-hi; 2, 3: B-lo, B-hi
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * 1024;
@@ -402,6 +489,10 @@ __device__ __forceinline__ void big_loop(const TileProduct &p, const Coord &c, i
         const uint32_t d = lds0 + (t & 1) * kBuffer + region * kRegion;
 #pragma unroll
         for (int u = 0; u < 2; ++u) copy_to_lds(g, region < 2 ? oa[region & 1][u] : ob[region & 1][u], d + u * 8192);
+        if constexpr (TYPE == TILE_FP4) {
+            // the piece's scales go with its first region, a group of 64 rows to half a wavefront
+            if (region == 0 && lane < 32) copy_to_lds(g4 + t * step4, lds0 + 2 * kBuffer - wave * 512 + (t & 1) * kScales4);
+        }
     };
 
 #pragma unroll
@@ -442,8 +533,17 @@ __device__ __forceinline__ void big_loop(const TileProduct &p, const Coord &c, i
     int sa[2] = {0, 0}, sb = 0;
 
     Frag fa[4], bl[2], bh[2], bn[2];
-    auto quarter = [&](int h, int k, const Frag (&b)[2]) {   // rows half h, columns half k
+    int a4[2][2] = {}, b4[2] = {};   // 4-bit operands: the scales of A's two halves and of B, by halves of the piece
+    auto quarter = [&](auto hh, auto kk, const Frag (&b)[2]) {   // rows half h, columns half k
+        constexpr int h = decltype(hh)::value, k = decltype(kk)::value;
         __builtin_amdgcn_s_setprio(1);
+        if constexpr (TYPE == TILE_FP4)
+            static_for<2>([&](auto j) {
+                static_for<4>([&](auto i) {
+                    mma4<i.value, 2 * k + j.value>(acc[4 * h + i.value][2 * k + j.value], fa[i.value], b[j.value], a4[h], b4);
+                });
+            });
+        else
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             mma_big<TYPE, 0>(acc[4 * h + 0][2 * k + j], fa[0], b[j], sa[h], sb);
@@ -465,6 +565,7 @@ __device__ __forceinline__ void big_loop(const TileProduct &p, const Coord &c, i
         else wait_copies<decltype(n0)::value>();
     };
     using std::integral_constant;
+    constexpr int X = TYPE == TILE_FP4;   // (region 0 takes one copy more)
     auto piece = [&](int t) {
         const int left = nt - 1 - t;
         // quarter 0
@@ -474,32 +575,41 @@ __device__ __forceinline__ void big_loop(const TileProduct &p, const Coord &c, i
             sa[1] = (int)wsa[t * 64 + 16];
             sb = wsb[t * 2];
         }
+        if constexpr (TYPE == TILE_FP4) {
+            const char *s4 = lds + 2 * kBuffer + (t & 1) * kScales4 + lane * 4;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                a4[0][q] = *(const int *)(s4 + (2 * wm) * 512 + q * 256);
+                a4[1][q] = *(const int *)(s4 + (2 * wm + 1) * 512 + q * 256);
+                b4[q] = *(const int *)(s4 + (4 + wn) * 512 + q * 256);
+            }
+        }
         if (left >= 1) copy(1, t + 1);
-        wait_for(left, integral_constant<int, 10>{}, integral_constant<int, 10>{}, integral_constant<int, 2>{});
+        wait_for(left, integral_constant<int, 10 + X>{}, integral_constant<int, 10 + X>{}, integral_constant<int, 2>{});
         turn();
-        quarter(0, 0, bl);
+        quarter(integral_constant<int, 0>{}, integral_constant<int, 0>{}, bl);
         turn();
         // quarter 1
         read_b(bh, t, 1);
         if (left >= 2) copy(2, t + 2);
-        wait_for(left, integral_constant<int, 10>{}, integral_constant<int, 8>{}, integral_constant<int, 0>{});
+        wait_for(left, integral_constant<int, 10 + X>{}, integral_constant<int, 8 + X>{}, integral_constant<int, 0>{});
         turn();
-        quarter(0, 1, bh);
+        quarter(integral_constant<int, 0>{}, integral_constant<int, 1>{}, bh);
         turn();
         // quarter 2
         read_a(fa, t, 1);
         if (left >= 2) copy(0, t + 2);
-        wait_for(left, integral_constant<int, 10>{}, integral_constant<int, 6>{}, integral_constant<int, 0>{});
+        wait_for(left, integral_constant<int, 10 + 2 * X>{}, integral_constant<int, 6 + X>{}, integral_constant<int, 0>{});
         turn();
-        quarter(1, 1, bh);
+        quarter(integral_constant<int, 1>{}, integral_constant<int, 1>{}, bh);
         turn();
         // quarter 3 (behind the last piece the read is of a stale one, unused)
         read_b(bn, t + 1, 0);
         if (left >= 2) copy(3, t + 2);
-        wait_for(left, integral_constant<int, 10>{}, integral_constant<int, 4>{}, integral_constant<int, 0>{});
+        wait_for(left, integral_constant<int, 10 + X>{}, integral_constant<int, 4>{}, integral_constant<int, 0>{});
         turn();
         wait_reads();   // bn's: its region is refilled in quarter 1, before bn is used
-        quarter(1, 0, bl);
+        quarter(integral_constant<int, 1>{}, integral_constant<int, 0>{}, bl);
         turn();
         bl[0] = bn[0];
         bl[1] = bn[1];
@@ -526,7 +636,7 @@ __device__ __forceinline__ void big_loop(const TileProduct &p, const Coord &c, i
             copy(2, 1);
             copy(0, 1);
             copy(3, 1);
-            wait_copies<10>();
+            wait_copies<10 + X>();
         } else {
             wait_copies<4>();
         }
