@@ -55,6 +55,12 @@ class gcn_rows4(ctypes.Structure):
                 ("scale", ctypes.c_void_p)]
 
 
+class gcn_muon_matrix(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("ldw", ctypes.c_int32), ("ldg", ctypes.c_int32),
+                ("ldm", ctypes.c_int32), ("W", ctypes.c_void_p), ("G", ctypes.c_void_p), ("M", ctypes.c_void_p),
+                ("scale", ctypes.c_double)]
+
+
 class gcn_sampler_params(ctypes.Structure):
     _fields_ = [("m", ctypes.c_int32), ("n", ctypes.c_int32), ("db_entries", ctypes.c_int32),
                 ("ia_slots", ctypes.c_int32), ("cap", ctypes.c_int32), ("seed", ctypes.c_uint64)]
@@ -155,6 +161,12 @@ _SIGNATURES = {
     # gcn_optim.h
     "gcn_adam_update": (ctypes.c_int, [_P, _P, _P, _P, _I64, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                                        ctypes.c_double, _I32, _P]),
+    # gcn_muon.h
+    "gcn_orthogonalise_workspace_bytes": (_SZ, [_I32, _I32, ctypes.c_int]),
+    "gcn_orthogonalise": (ctypes.c_int, [_P, ctypes.c_int, _I32, _I32, _I32, _P, _I32, _I32, ctypes.c_int, _P, _SZ, _P]),
+    "gcn_muon_workspace_bytes": (_SZ, [_I32, ctypes.POINTER(gcn_muon_matrix), ctypes.c_int]),
+    "gcn_muon_update": (ctypes.c_int, [_I32, ctypes.POINTER(gcn_muon_matrix), ctypes.c_int, ctypes.c_double,
+                                       ctypes.c_double, ctypes.c_int, ctypes.c_double, _I32, ctypes.c_int, _P, _SZ, _P]),
     # gcn_peaks.h
     "gcn_peak_stream_read": (ctypes.c_int, [_P, _I64, _P, _I32, _P]),
     "gcn_peak_mfma": (ctypes.c_int, [ctypes.c_int, _I32, _I32, _P, ctypes.POINTER(ctypes.c_double), _P]),
@@ -899,6 +911,62 @@ def gcn_adam_update(params, grads, m, v, lr: float, step: int, beta1: float = 0.
             raise ValueError(f"{nm} must be contiguous with as many elements as params")
     _check(lib().gcn_adam_update(_ptr(params), _ptr(grads), _ptr(m), _ptr(v), params.numel(), lr, beta1, beta2,
                                  eps, int(step), _stream(stream)), "gcn_adam_update")
+
+
+def gcn_orthogonalise(X: torch.Tensor, out: torch.Tensor, ws: Workspace, steps: int = 5, prec: int = GCN_F32,
+                      stream=None) -> torch.Tensor:
+    """out = X with its singular values moved to about one; out may be X."""
+    t = _rows_type(X, "X")
+    _want(out, "out", X.dtype, X.shape)
+    rows, cols = int(X.shape[0]), int(X.shape[1])
+    w, wb = ws.args(lib().gcn_orthogonalise_workspace_bytes(rows, cols, prec))
+    _launch("gcn_orthogonalise", _one_device(X, out, ws.buf), stream, X.data_ptr(), t, rows, cols, _ld(X),
+            out.data_ptr(), _ld(out), int(steps), prec, w, wb)
+    return out
+
+
+class MuonStep:
+    """gcn_muon_update with the matrices' descriptors built once: lists of
+    weight matrices (float32, updated), their gradients (all float32 or all
+    bfloat16) and momenta (float32, zeros before the first step, updated).
+    scales: the factor of each matrix's updates (0.2 sqrt(max(rows, cols)), the
+    size of an Adam step, where None).  The tensors must stay alive and in place."""
+
+    def __init__(self, params, grads, momenta, scales=None, momentum: float = 0.95, nesterov: bool = True,
+                 weight_decay: float = 0.0, steps: int = 5, prec: int = GCN_F32):
+        params, grads, momenta = list(params), list(grads), list(momenta)
+        if not params or len(params) != len(grads) or len(params) != len(momenta):
+            raise ValueError("as many gradients and momenta as weight matrices are needed, one at least")
+        if scales is None:
+            scales = [0.2 * max(W.shape) ** 0.5 for W in params]
+        scales = list(scales)
+        if len(scales) != len(params):
+            raise ValueError("one scale for each matrix is needed")
+        self.count = len(params)
+        self.arr = (gcn_muon_matrix * self.count)()
+        self._keep = (params, grads, momenta)
+        self.type = _rows_type(grads[0], "a gradient")
+        for i, (W, G, M, s) in enumerate(zip(params, grads, momenta, scales)):
+            if W.dim() != 2:
+                raise ValueError("weights must be matrices")
+            _want(W, "a weight matrix", torch.float32, W.shape)
+            _want(M, "a momentum", torch.float32, W.shape)
+            _want(G, "a gradient", grads[0].dtype, W.shape)
+            self.arr[i] = gcn_muon_matrix(int(W.shape[0]), int(W.shape[1]), _ld(W), _ld(G), _ld(M), W.data_ptr(),
+                                          G.data_ptr(), M.data_ptr(), float(s))
+        self.device = _one_device(params[0], *params[1:], *grads, *momenta)
+        self.momentum, self.nesterov, self.weight_decay = float(momentum), bool(nesterov), float(weight_decay)
+        self.steps, self.prec = int(steps), int(prec)
+
+    def workspace_bytes(self) -> int:
+        return int(lib().gcn_muon_workspace_bytes(self.count, self.arr, self.prec))
+
+    def __call__(self, lr: float, ws: Workspace, stream=None):
+        w, wb = ws.args(self.workspace_bytes())
+        if ws.buf.get_device() != self.device:
+            raise ValueError("all tensors of a call must be on one device")
+        _launch("gcn_muon_update", self.device, stream, self.count, self.arr, self.type, float(lr), self.momentum,
+                int(self.nesterov), self.weight_decay, self.steps, self.prec, w, wb)
 
 
 # ---------------------------------------------------------------- profiling

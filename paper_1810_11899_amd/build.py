@@ -18,7 +18,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(PKG, "_build")
 LIB_PATH = os.path.join(PKG, "libgcnlayer.so")
 SOURCES = ["api.cpp", "spmm.hip", "gemm.hip", "elementwise.hip", "transpose.hip", "peaks.hip", "sampler.hip", "optim.hip", "noalloc.hip",
-           "rows8.hip", "product.hip", "classes.hip", "rows4.hip"]
+           "rows8.hip", "product.hip", "classes.hip", "rows4.hip", "muon.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
