@@ -40,7 +40,7 @@ static const char *kClassNames[K_CLASS_COUNT] = {
     "spmm_bf16", "transpose_bf16", "frontier_sample", "induce_subgraphs", "gather_rows", "adam", "transpose_symmetric",
     "gemm_nt_bf16_big", "gemm_nt_bf16_big_masked", "gemm_tn_bf16_big", "rows8_pack", "rows8_product",
     "rows8_mask", "rows8_weight_grad", "class_prep", "class_stats", "class_grad", "class_product",
-    "rows4_pack", "rows4_product", "muon_prep", "muon_product", "muon_update"};
+    "rows4_pack", "rows4_product", "muon_prep", "muon_product", "muon_small"};
 
 const char *class_name(int cls) {
     return (cls >= 0 && cls < K_CLASS_COUNT) ? kClassNames[cls] : "";

@@ -101,7 +101,7 @@ enum KernelClass {
     K_ROWS4_PRODUCT,
     K_MUON_PREP,                // orthogonalised update: momentum and norm, operands
     K_MUON_PRODUCT,
-    K_MUON_UPDATE,
+    K_MUON_SMALL,               // whole updates of matrices that fit in LDS
     K_CLASS_COUNT
 };
 const char *class_name(int cls);

@@ -32,7 +32,7 @@ namespace {
 
 constexpr int kTB = 256;
 constexpr int kGroup = 16;        // matrices of a launch
-constexpr int kMostParts = 512;   // of a matrix's sum of squares
+constexpr int kMostParts = 1024;  // of a matrix's sum of squares
 constexpr int kXBits = 15, kABits = 14, kBBits = 13;   // what X, A and B are scaled by
 constexpr float kCoefA = 3.4445f, kCoefB = -4.7750f, kCoefC = 2.0315f;
 
@@ -63,43 +63,89 @@ struct Group {
     uint32_t first[kGroup + 1];   // a launch's blocks by job
     int32_t count;
     int32_t tile_m, tile_n;
+    uint32_t per_xcd, band;       // of a product's tiles
+    int full;                     // A and B: all of their tiles, not those on and below the diagonal alone
     float momentum, decay;
     int nesterov, grad_bf16, out_bf16;
 };
-__device__ __forceinline__ int job_of(const Group &g) {
+__device__ __forceinline__ int job_of(const Group &g, uint32_t block) {
     int j = 0;
-    while (j + 1 < g.count && blockIdx.x >= g.first[j + 1]) ++j;
+    while (j + 1 < g.count && block >= g.first[j + 1]) ++j;
     return j;
 }
 
-__device__ __forceinline__ float grad_at(const Group &g, const Job &J, int64_t r, int64_t c) {
-    return g.grad_bf16 ? __uint_as_float((uint32_t)((const uint16_t *)J.G)[r * J.ldg + c] << 16)
-                       : ((const float *)J.G)[r * J.ldg + c];
+// Four consecutive columns of U from c of row r (zeros past the last), M updated on
+// the way with UPDATE.
+template <bool UPDATE>
+__device__ __forceinline__ f32x4 four_of_u(const Group &g, const Job &J, int64_t r, int32_t c) {
+    f32x4 u = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (r >= J.rows || c >= J.cols) return u;
+    const bool whole = c + 4 <= J.cols;
+    if (g.grad_bf16) {
+        const uint16_t *p = (const uint16_t *)J.G + r * J.ldg + c;
+        if (whole) {
+            uint2 w;
+            __builtin_memcpy(&w, p, 8);
+            u = f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
+                      __uint_as_float(w.y & 0xFFFF0000u)};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < J.cols) u[e] = __uint_as_float((uint32_t)p[e] << 16);
+        }
+    } else {
+        const float *p = (const float *)J.G + r * J.ldg + c;
+        if (whole) {
+            u = __builtin_bit_cast(f32x4, load16(p));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < J.cols) u[e] = p[e];
+        }
+    }
+    if (!J.M) return u;
+    float *p = J.M + r * J.ldm + c;
+    f32x4 m = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (whole) {
+        m = __builtin_bit_cast(f32x4, load16(p));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < J.cols) m[e] = p[e];
+    }
+    if constexpr (UPDATE) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[e] = fmaf(g.momentum, m[e], u[e]);
+        if (whole) {
+            store16(p, __builtin_bit_cast(uint4, m));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < J.cols) p[e] = m[e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = g.nesterov ? fmaf(g.momentum, m[e], u[e]) : m[e];
+    return u;
 }
-// U's element from the gradient and the updated momentum
-__device__ __forceinline__ float update_of(const Group &g, float grad, float m) {
-    return g.nesterov ? fmaf(g.momentum, m, grad) : m;
+__device__ __forceinline__ double squares(f32x4 u) {
+    return ((double)u[0] * u[0] + (double)u[1] * u[1]) + ((double)u[2] * u[2] + (double)u[3] * u[3]);
 }
+// the factor that makes X0 of U: of a matrix of zeros 0
+__device__ __forceinline__ double inverse_norm(double sum) { return sum > 0.0 ? (double)(1 << kXBits) / sqrt(sum) : 0.0; }
 
 // M <- momentum M + G, and U's sum of squares in float64 (no overflow, and the norm
 // of millions of elements to float32's last bit): a block's share of the
 // elements, in order.
 __global__ __launch_bounds__(kTB) void momentum_kernel(Group g) {
     __shared__ double red[kTB / 64];
-    const Job &J = g.job[job_of(g)];
-    const uint32_t block = blockIdx.x - g.first[job_of(g)];
-    const int64_t total = (int64_t)J.rows * J.cols, step = (int64_t)J.parts * kTB;
+    const int j = job_of(g, blockIdx.x);
+    const Job &J = g.job[j];
+    const uint32_t block = blockIdx.x - g.first[j], per_row = ((uint32_t)J.cols + 3) / 4;
+    const uint32_t total = (uint32_t)J.rows * per_row, step = (uint32_t)J.parts * kTB;   // (sides up to 2^16: below 2^31)
     double sum = 0.0;
-    for (int64_t i = (int64_t)block * kTB + threadIdx.x; i < total; i += step) {
-        const int64_t r = i / J.cols, c = i - r * J.cols;
-        float u = grad_at(g, J, r, c);
-        if (J.M) {
-            const float m = fmaf(g.momentum, J.M[r * J.ldm + c], u);
-            J.M[r * J.ldm + c] = m;
-            u = update_of(g, u, m);
-        }
-        sum += (double)u * u;
-    }
+    for (uint32_t i = block * kTB + threadIdx.x; i < total; i += step)
+        sum += squares(four_of_u<true>(g, J, i / per_row, 4 * (i % per_row)));
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x / 64] = sum;
@@ -142,79 +188,135 @@ template <bool PAIR>
 __global__ __launch_bounds__(kTB) void operand_kernel(Group g) {
     __shared__ float tile[64][65];
     __shared__ double red[kTB / 64];
-    const int j = job_of(g);
+    const int j = job_of(g, blockIdx.x);
     const Job &J = g.job[j];
     const uint32_t block = blockIdx.x - g.first[j], across = (uint32_t)((J.np + 63) / 64);
     const int64_t i0 = (int64_t)(block / across) * 64, j0 = (int64_t)(block % across) * 64;   // X's rows, columns
+    const bool tall = J.rows > J.cols;
+    const int64_t r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;   // U's
+    const int tr = (int)(threadIdx.x >> 4), tc = 4 * (int)(threadIdx.x & 15);
+    f32x4 u[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) u[k] = four_of_u<false>(g, J, r0 + 16 * k + tr, (int32_t)c0 + tc);
     double sum = 0.0;
     for (int i = threadIdx.x; i < J.parts; i += kTB) sum += J.part[i];
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x / 64] = sum;
     __syncthreads();
-    sum = (red[0] + red[1]) + (red[2] + red[3]);
-    const double inv = sum > 0.0 ? (double)(1 << kXBits) / sqrt(sum) : 0.0;
-    const bool tall = J.rows > J.cols;
-    const int64_t r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;   // U's
-#pragma unroll 4
-    for (int k = 0; k < 16; ++k) {
-        const int rl = 4 * k + (int)(threadIdx.x >> 6), cl = threadIdx.x & 63;
-        const int64_t r = r0 + rl, c = c0 + cl;
-        float u = 0.0f;
-        if (r < J.rows && c < J.cols) {
-            u = grad_at(g, J, r, c);
-            if (J.M) u = update_of(g, u, J.M[r * J.ldm + c]);
-        }
-        (tall ? tile[cl][rl] : tile[rl][cl]) = (float)((double)u * inv);
+    const double inv = inverse_norm((red[0] + red[1]) + (red[2] + red[3]));
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[k][e] = (float)((double)u[k][e] * inv);
+    if (tall) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) tile[tc + e][16 * k + tr] = u[k][e];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[k][e] = tile[16 * k + tr][tc + e];
     }
-    __syncthreads();
     const int64_t bytes = row_bytes<PAIR>(J.np), low = PAIR ? 64 : 2 * (int64_t)J.mp * J.np;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int i = 16 * k + (int)(threadIdx.x >> 4), c = 4 * (int)(threadIdx.x & 15);
-        if (i0 + i < J.mp && j0 + c < J.np)
-            store_parts(J.X0 + place<PAIR>(i0 + i, bytes, j0 + c), low,
-                        f32x4{tile[i][c], tile[i][c + 1], tile[i][c + 2], tile[i][c + 3]});
-    }
+    for (int k = 0; k < 4; ++k)
+        if (i0 + 16 * k + tr < J.mp && j0 + tc < J.np)
+            store_parts(J.X0 + place<PAIR>(i0 + 16 * k + tr, bytes, j0 + tc), low, u[k]);
 }
 
 enum Stage { GRAM = 0, POLY = 1, NEXT = 2, LAST = 3 };
 
-// The sums of a product to what it forms.  acc[i][j]: row r0 + 16 i, columns c0 +
-// 16 j .. + 3.
-template <bool PAIR, int STAGE, int FM>
-__device__ __forceinline__ void finish(const Job &J, const uint8_t *X, uint8_t *next, int r0, int c0, f32x4 (&acc)[FM][4]) {
+// What a product's epilogue reads beside four sums: A's or X's elements at their place.
+template <bool PAIR, int STAGE>
+__device__ __forceinline__ f32x4 old_at(const Job &J, const uint8_t *X, int row, int col) {
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if constexpr (STAGE == GRAM) return v;
+    const int32_t cols = STAGE == POLY ? J.mp : J.np;
+    if (row < J.mp && col < cols) {
+        const uint8_t *p = (STAGE == POLY ? J.A : X) + place<PAIR>(row, row_bytes<PAIR>(cols), col);
+        v = four_of(p);
+        // (A of the single products is its high parts alone)
+        if constexpr (PAIR) v += four_of(p + 64);
+        else if (STAGE != POLY) v += four_of(p + 2 * (int64_t)J.mp * J.np);
+    }
+    return v;
+}
+
+// W <- decay W - step O, or out = O, for four consecutive columns of a row of O.
+__device__ __forceinline__ void apply(const Group &g, const Job &J, int row, int col, f32x4 o) {
+    if (J.rows > J.cols) {   // O lies transposed
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (row >= J.cols || col + e >= J.rows) continue;
+            const int64_t at = (int64_t)(col + e) * J.ldw + row;
+            if (J.W) J.W[at] = g.decay * J.W[at] - J.step * o[e];
+            else if (g.out_bf16) ((uint16_t *)J.out)[at] = to_bf16(o[e]);
+            else ((float *)J.out)[at] = o[e];
+        }
+        return;
+    }
+    if (row >= J.rows) return;
+    const int64_t at = (int64_t)row * J.ldw + col;
+    if (col + 4 <= J.cols) {
+        if (J.W) {
+            const f32x4 w = __builtin_bit_cast(f32x4, load16(J.W + at));
+            store16(J.W + at, __builtin_bit_cast(uint4, g.decay * w - J.step * o));
+        } else if (g.out_bf16) {
+            const uint2 v = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+            __builtin_memcpy((uint16_t *)J.out + at, &v, 8);
+        } else {
+            store16((float *)J.out + at, __builtin_bit_cast(uint4, o));
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (col + e >= J.cols) continue;
+        if (J.W) J.W[at + e] = g.decay * J.W[at + e] - J.step * o[e];
+        else if (g.out_bf16) ((uint16_t *)J.out)[at + e] = to_bf16(o[e]);
+        else ((float *)J.out)[at + e] = o[e];
+    }
+}
+
+// v of four consecutive columns of a row to four consecutive rows of a column: lane
+// 4 q + k of a row of 16 gives element e to lane 4 q + e and takes element k of
+// it.  In two exchanges, of single columns and of pairs.
+__device__ __forceinline__ f32x4 turned(f32x4 v) {
+    const bool odd = threadIdx.x & 1, up = threadIdx.x & 2;
+    const float a = __shfl_xor(odd ? v[0] : v[1], 1), b = __shfl_xor(odd ? v[2] : v[3], 1);
+    v = odd ? f32x4{a, v[1], b, v[3]} : f32x4{v[0], a, v[2], b};
+    const float c = __shfl_xor(up ? v[0] : v[2], 2), d = __shfl_xor(up ? v[1] : v[3], 2);
+    return up ? f32x4{c, d, v[2], v[3]} : f32x4{v[0], v[1], c, d};
+}
+
+// Four sums to what the product forms.  mirror: of a tile below the diagonal of A or
+// B, whose other half they are too.
+template <bool PAIR, int STAGE>
+__device__ __forceinline__ void finish(const Group &g, const Job &J, uint8_t *next, int row, int col, bool mirror, f32x4 old,
+                                       f32x4 v) {
     const int32_t cols = STAGE <= POLY ? J.mp : J.np;
     const int64_t bytes = row_bytes<PAIR>(cols);
     // (A and B of the single products are their high parts alone)
     const int64_t low = PAIR ? 64 : STAGE <= POLY ? 0 : 2 * (int64_t)J.mp * J.np;
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int row = r0 + 16 * i, col = c0 + 16 * j;
-            if (row >= J.mp || col >= cols) continue;
-            const int64_t at = place<PAIR>(row, bytes, col);
-            f32x4 v = acc[i][j];
-            if constexpr (STAGE == GRAM) {
-                v *= two_to(kABits - 2 * kXBits);
-                store_parts(J.A + at, low, v);
-            } else if constexpr (STAGE == POLY) {
-                f32x4 a = four_of(J.A + at);
-                if (low) a += four_of(J.A + at + low);
-                v = v * (kCoefC * two_to(kBBits - 2 * kABits)) + a * (kCoefB * two_to(kBBits - kABits));
-                store_parts(J.B + at, low, v);
-            } else {
-                const f32x4 x = four_of(X + at) + four_of(X + at + low);
-                v = v * two_to(-kBBits) + x * kCoefA;
-                if constexpr (STAGE == NEXT) {
-                    store_parts(next + at, low, v);
-                } else {
-                    v *= two_to(-kXBits);
-                    *(f32x4 *)((float *)next + (int64_t)row * J.np + col) = v;
-                }
-            }
+    const bool in = row < J.mp && col < cols;
+    if constexpr (STAGE <= POLY) {
+        if constexpr (STAGE == GRAM) v *= two_to(kABits - 2 * kXBits);
+        else v = v * (kCoefC * two_to(kBBits - 2 * kABits)) + old * (kCoefB * two_to(kBBits - kABits));
+        uint8_t *const to = STAGE == GRAM ? J.A : J.B;
+        if (in) store_parts(to + place<PAIR>(row, bytes, col), low, v);
+        if (mirror) {   // (all lanes exchange; mp is a multiple of 32: a block of 16 x 16 is in or out)
+            v = turned(v);
+            if (in) store_parts(to + place<PAIR>(col + (row & 3), bytes, row & ~3), low, v);
         }
+    } else {
+        if (!in) return;
+        v = v * two_to(-kBBits) + old * kCoefA;
+        if constexpr (STAGE == NEXT) store_parts(next + place<PAIR>(row, bytes, col), low, v);
+        else apply(g, J, row, col, v * two_to(-kXBits));
+    }
 }
 
 template <bool PAIR, int STAGE>
@@ -222,108 +324,130 @@ constexpr int type_of() {
     return STAGE <= POLY ? (PAIR ? TILE_PAIR : TILE_F16) : (PAIR ? TILE_PAIR_NN : TILE_F16_NN);
 }
 
-// A tile of a product of one of the group's matrices.  odd: X is in X1.
+// A tile of a product of one of the group's matrices.  odd: X is in X1.  The
+// group's tiles are numbered matrix by matrix and dealt to the XCDs in eight
+// runs, so that a matrix is read by as few L2s as can be; within a matrix in
+// bands of `band` row tiles (A and B: tiles on and below the diagonal, row by row).
 template <bool PAIR, int STAGE>
-__device__ __forceinline__ bool product_of(const Group &g, int odd, const Job *&J, TileProduct &p, Coord &c, const uint8_t *&X,
-                                           uint8_t *&next) {
-    const int j = job_of(g);
-    J = &g.job[j];
-    X = odd ? J->X1 : J->X0;
-    next = odd ? J->X0 : J->X1;
+__device__ __forceinline__ void product_of(const Group &g, const Job &J, const uint8_t *X, uint32_t at, TileProduct &p,
+                                           Coord &c) {
     constexpr int kUnit = PAIR ? 32 : 64;   // columns of a piece
-    p.M = J->mp;
+    p.M = J.mp;
     if constexpr (STAGE == GRAM) {
         p.A = p.B = X;
-        p.lda = p.ldb = row_bytes<PAIR>(J->np);
-        p.N = J->mp;
-        p.kt = J->np / kUnit;
+        p.lda = p.ldb = row_bytes<PAIR>(J.np);
+        p.N = J.mp;
+        p.kt = J.np / kUnit;
     } else if constexpr (STAGE == POLY) {
-        p.A = p.B = J->A;
-        p.lda = p.ldb = row_bytes<PAIR>(J->mp);
-        p.N = J->mp;
-        p.kt = J->mp / kUnit;
+        p.A = p.B = J.A;
+        p.lda = p.ldb = row_bytes<PAIR>(J.mp);
+        p.N = J.mp;
+        p.kt = J.mp / kUnit;
     } else {
-        p.A = J->B;
-        p.lda = row_bytes<PAIR>(J->mp);
+        p.A = J.B;
+        p.lda = row_bytes<PAIR>(J.mp);
         p.B = X;
-        p.ldb = row_bytes<PAIR>(J->np);
-        p.N = J->np;
-        p.kt = J->mp / kUnit;
+        p.ldb = row_bytes<PAIR>(J.np);
+        p.N = J.np;
+        p.kt = J.mp / kUnit;
     }
-    Args a;
-    a.tiles_m = (p.M + g.tile_m - 1) / g.tile_m;
-    a.tiles_n = (p.N + g.tile_n - 1) / g.tile_n;
-    a.band = 8;
-    a.total = (uint32_t)a.tiles_m * a.tiles_n;
-    a.per_xcd = (a.total + 7) / 8;
-    return coord_of(a, blockIdx.x - g.first[j], c);
+    c.split = 0;
+    if (STAGE <= POLY && !g.full) {
+        // row t of the triangle starts at t (t + 1) / 2
+        int t = (int)((sqrtf(8.0f * (float)at + 1.0f) - 1.0f) * 0.5f);
+        while ((uint32_t)(t + 1) * (t + 2) / 2 <= at) ++t;
+        while ((uint32_t)t * (t + 1) / 2 > at) --t;
+        c.tm = t;
+        c.tn = (int)(at - (uint32_t)t * (t + 1) / 2);
+    } else {
+        const uint32_t tiles_m = (uint32_t)((p.M + g.tile_m - 1) / g.tile_m), tiles_n = (uint32_t)((p.N + g.tile_n - 1) / g.tile_n);
+        const uint32_t b = at / (g.band * tiles_n), q = at - b * g.band * tiles_n, h = min(g.band, tiles_m - b * g.band);
+        c.tn = (int)(q / h);
+        c.tm = (int)(b * g.band + (q - c.tn * h));
+    }
+    // (the same in every lane, and the copies take their bases in scalar registers)
+    c.tm = __builtin_amdgcn_readfirstlane(c.tm);
+    c.tn = __builtin_amdgcn_readfirstlane(c.tn);
 }
 
-template <bool PAIR, int STAGE, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM *WN) void muon_kernel(Group g, int odd) {
-    constexpr int TYPE = type_of<PAIR, STAGE>(), FM = BM / WM / 16;
-    __shared__ __attribute__((aligned(16))) char lds[small_lds(TYPE, BM, BN)];
-    const Job *J;
-    TileProduct p{};
-    Coord c;
-    const uint8_t *X;
-    uint8_t *next;
-    if (!product_of<PAIR, STAGE>(g, odd, J, p, c, X, next)) return;
+// The block's tile, or the end of the block where it has none.
+#define GCN_MUON_TILE                                                          \
+    const uint32_t L = (blockIdx.x & 7) * g.per_xcd + (blockIdx.x >> 3);       \
+    if (L >= g.first[g.count]) return;                                         \
+    const int job = job_of(g, L);                                              \
+    const Job &J = g.job[job];                                                 \
+    const uint8_t *const X = odd ? J.X1 : J.X0;                                \
+    uint8_t *const next = odd ? J.X0 : J.X1;                                   \
+    TileProduct p{};                                                           \
+    Coord c;                                                                   \
+    product_of<PAIR, STAGE>(g, J, X, L - g.first[job], p, c);                  \
+    const bool mirror = STAGE <= POLY && !g.full && c.tm != c.tn
+
+// KG groups of WM x WN wavefronts take a KG-th of the sum each, and share the tile's
+// epilogue: a launch of fewer tiles than CUs has one wavefront a SIMD and group,
+// which waits for its own copies, reads and products in turn.
+template <bool PAIR, int STAGE, int BM, int BN, int WM, int WN, int KG>
+__global__ __launch_bounds__(64 * WM *WN *KG) void muon_kernel(Group g, int odd) {
+    constexpr int TYPE = type_of<PAIR, STAGE>(), FM = BM / WM / 16, kOwn = FM * 4 / KG, T = 64 * WM * WN;
+    constexpr int kLds = small_lds(TYPE, BM, BN);
+    static_assert(KG == 1 || KG * FM * 4 * T * 16 <= KG * kLds, "the groups' sums fit where the operands were");
+    __shared__ __attribute__((aligned(16))) char lds[KG * kLds];
+    GCN_MUON_TILE;
+    const uint32_t tid = threadIdx.x % T;
+    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / T), lane = tid & 63, wave = tid >> 6;
+    const int r0 = c.tm * BM + wave / WN * (BM / WM) + (lane & 15), c0 = c.tn * BN + wave % WN * (BN / WN) + 4 * (lane >> 4);
+    f32x4 old[kOwn];
+    if constexpr (kOwn <= 4) {   // (a few registers: ahead of the loop)
+#pragma unroll
+        for (int u = 0; u < kOwn; ++u) {
+            const int b = u * KG + group;
+            old[u] = old_at<PAIR, STAGE>(J, X, r0 + 16 * (b / 4), c0 + 16 * (b % 4));
+        }
+    }
     f32x4 acc[FM][4];
-    small_loop<TYPE, BM, BN, WM, WN>(p, c, 0, p.kt, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    finish<PAIR, STAGE, FM>(*J, X, next, c.tm * BM + wave / WN * (BM / WM) + (lane & 15),
-                            c.tn * BN + wave % WN * (BN / WN) + 4 * (lane >> 4), acc);
+    const int per = (p.kt + KG - 1) / KG, k0 = min(group * per, p.kt);
+    small_loop<TYPE, BM, BN, WM, WN, 2>(p, c, k0, min(per, p.kt - k0), lds + group * kLds, acc, tid, per);
+    if constexpr (KG > 1) {
+        f32x4 *const part = (f32x4 *)lds;   // [block][group][thread]
+#pragma unroll
+        for (int b = 0; b < FM * 4; ++b) part[(b * KG + group) * T + tid] = acc[b / 4][b % 4];
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kOwn; ++u) {
+            const int b = u * KG + group;
+            f32x4 v = part[b * KG * T + tid];
+#pragma unroll
+            for (int q = 1; q < KG; ++q) v += part[(b * KG + q) * T + tid];
+            finish<PAIR, STAGE>(g, J, next, r0 + 16 * (b / 4), c0 + 16 * (b % 4), mirror, old[u], v);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x4 o = kOwn <= 4 ? old[kOwn <= 4 ? i * 4 + j : 0] : old_at<PAIR, STAGE>(J, X, r0 + 16 * i, c0 + 16 * j);
+                finish<PAIR, STAGE>(g, J, next, r0 + 16 * i, c0 + 16 * j, mirror, o, acc[i][j]);
+            }
+    }
 }
 template <bool PAIR, int STAGE>
 __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void muon_big_kernel(Group g, int odd) {
     constexpr int TYPE = type_of<PAIR, STAGE>();
     __shared__ __attribute__((aligned(16))) char lds[big_lds(TYPE)];
-    const Job *J;
-    TileProduct p{};
-    Coord c;
-    const uint8_t *X;
-    uint8_t *next;
-    if (!product_of<PAIR, STAGE>(g, odd, J, p, c, X, next)) return;
+    GCN_MUON_TILE;
     f32x4 acc[8][4];
     big_loop<TYPE>(p, c, 0, p.kt, lds, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    finish<PAIR, STAGE, 8>(*J, X, next, c.tm * kBigT + (wave >> 2) * 128 + (lane & 15),
-                           c.tn * kBigT + (wave & 3) * 64 + 4 * (lane >> 4), acc);
-}
-
-// W <- decay W - step O, or out = O, from O [m x n] (rows of np float32), through LDS
-// where it lies transposed.
-__global__ __launch_bounds__(kTB) void update_kernel(Group g, int odd) {
-    __shared__ float tile[64][65];
-    const int j = job_of(g);
-    const Job &J = g.job[j];
-    const uint32_t block = blockIdx.x - g.first[j], across = (uint32_t)((J.cols + 63) / 64);
-    const int64_t r0 = (int64_t)(block / across) * 64, c0 = (int64_t)(block % across) * 64;
-    const bool tall = J.rows > J.cols;
-    const float *O = (const float *)(odd ? J.X0 : J.X1);
-    if (tall) {
-#pragma unroll 4
-        for (int k = 0; k < 16; ++k) {
-            const int i = 4 * k + (int)(threadIdx.x >> 6), c = threadIdx.x & 63;   // O's row c0 + i, column r0 + c
-            if (c0 + i < J.cols && r0 + c < J.rows) tile[c][i] = O[(c0 + i) * J.np + r0 + c];
-        }
-        __syncthreads();
-    }
-#pragma unroll 4
-    for (int k = 0; k < 16; ++k) {
-        const int rl = 4 * k + (int)(threadIdx.x >> 6), cl = threadIdx.x & 63;
-        const int64_t r = r0 + rl, c = c0 + cl;
-        if (r >= J.rows || c >= J.cols) continue;
-        const float o = tall ? tile[rl][cl] : O[r * J.np + c];
-        if (J.W) {
-            float *w = J.W + r * J.ldw + c;
-            *w = g.decay * *w - J.step * o;
-        } else if (g.out_bf16) {
-            ((uint16_t *)J.out)[r * J.ldw + c] = to_bf16(o);
-        } else {
-            ((float *)J.out)[r * J.ldw + c] = o;
-        }
+    const int r0 = c.tm * kBigT + (wave >> 2) * 128 + (lane & 15), c0 = c.tn * kBigT + (wave & 3) * 64 + 4 * (lane >> 4);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {   // (two rows' reads at a time)
+        f32x4 old[2][4];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) old[k / 4][k % 4] = old_at<PAIR, STAGE>(J, X, r0 + 16 * (i + k / 4), c0 + 16 * (k % 4));
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            finish<PAIR, STAGE>(g, J, next, r0 + 16 * (i + k / 4), c0 + 16 * (k % 4), mirror, old[k / 4][k % 4],
+                                acc[i + k / 4][k % 4]);
     }
 }
 
@@ -345,7 +469,6 @@ void plan_job(Job &J, bool pair, Arena &ar) {
     const int32_t unit = pair ? 32 : 64;
     J.mp = up(J.m, unit);
     J.np = up(J.n, unit);
-    // (X1 also takes the result, four bytes an element)
     J.X0 = ar.take<uint8_t>(4 * (size_t)J.mp * J.np);
     J.X1 = ar.take<uint8_t>(4 * (size_t)J.mp * J.np);
     J.A = ar.take<uint8_t>((pair ? 4 : 2) * (size_t)J.mp * J.mp);
@@ -374,35 +497,51 @@ int64_t tiles(int32_t m, int32_t n, int32_t tm, int32_t tn) {
 template <bool PAIR, int STAGE>
 int product(Group &g, int odd, hipStream_t s) {
     auto cols = [](const Job &J) { return STAGE <= POLY ? J.mp : J.np; };
-    int64_t big = 0, mid = 0;
+    auto count = [&](const Job &J, int32_t tm, int32_t tn) {
+        const int64_t t = (J.mp + tm - 1) / tm;
+        return STAGE <= POLY && !g.full ? t * (t + 1) / 2 : t * ((cols(J) + tn - 1) / tn);
+    };
+    auto all = [&](int32_t tm, int32_t tn) {
+        int64_t n = 0;
+        for (int j = 0; j < g.count; ++j) n += count(g.job[j], tm, tn);
+        return n;
+    };
     double flops = 0.0;
     bool deep = true;
     for (int j = 0; j < g.count; ++j) {
         const Job &J = g.job[j];
-        big += tiles(J.mp, cols(J), kBigT, kBigT);
-        mid += tiles(J.mp, cols(J), 128, 128);
         deep = deep && J.mp >= 256 && J.np < (1 << 22);   // (a large tile's row offsets within it: 32 bits)
-        flops += 2.0 * J.m * J.m * (STAGE == POLY ? J.m : J.n);
+        flops += STAGE == GRAM ? (double)J.m * J.m * J.n : STAGE == POLY ? (double)J.m * J.m * J.m : 2.0 * J.m * J.m * J.n;
     }
     ProfScope prof(K_MUON_PRODUCT, s, flops, 0.0);
+    g.full = 1;
+    if (STAGE <= POLY && all(64, 64) > 128) g.full = 0;
     auto grid = [&](int32_t tm, int32_t tn) {
         g.tile_m = tm;
         g.tile_n = tn;
-        return dim3(blocks_of(g, [&](const Job &J) { return (uint64_t)(tiles(J.mp, cols(J), tm, tn) + 7) / 8 * 8; }));
+        const uint32_t total = blocks_of(g, [&](const Job &J) { return (uint64_t)count(J, tm, tn); });
+        g.per_xcd = (total + 7) / 8;
+        g.band = (uint32_t)std::max(1, std::min(8, (int)std::lround(std::sqrt((double)g.per_xcd))));
+        return dim3(8 * g.per_xcd);
     };
-    if (deep && big >= 160) {
+#define GCN_MUON(BM, BN, WM, WN, KG)                                                                             \
+    do {                                                                                                         \
+        const dim3 b = grid(BM, BN);                                                                             \
+        hipLaunchKernelGGL((muon_kernel<PAIR, STAGE, BM, BN, WM, WN, KG>), b, dim3(64 * WM * WN * KG), 0, s, g, odd); \
+    } while (0)
+    if (deep && all(kBigT, kBigT) >= (STAGE <= POLY ? 120 : 160)) {
         const dim3 b = grid(kBigT, kBigT);
         hipLaunchKernelGGL((muon_big_kernel<PAIR, STAGE>), b, dim3(kBigThreads), 0, s, g, odd);
-    } else if (mid >= 256) {
-        const dim3 b = grid(128, 128);
-        hipLaunchKernelGGL((muon_kernel<PAIR, STAGE, 128, 128, 2, 2>), b, dim3(256), 0, s, g, odd);
     } else if constexpr (STAGE <= POLY) {
-        const dim3 b = grid(64, 64);
-        hipLaunchKernelGGL((muon_kernel<PAIR, STAGE, 64, 64, 4, 1>), b, dim3(256), 0, s, g, odd);
+        if (all(128, 128) >= 256) GCN_MUON(128, 128, 2, 2, 1);
+        else if (all(64, 64) > 256) GCN_MUON(64, 64, 4, 1, 1);
+        else GCN_MUON(64, 64, 4, 1, 4);
     } else {
-        const dim3 b = grid(32, 128);
-        hipLaunchKernelGGL((muon_kernel<PAIR, STAGE, 32, 128, 2, 2>), b, dim3(256), 0, s, g, odd);
+        if (all(128, 128) >= 192) GCN_MUON(128, 128, 2, 2, 1);
+        else if (all(32, 128) > 256) GCN_MUON(64, 128, 2, 2, 2);
+        else GCN_MUON(32, 128, 2, 2, 4);
     }
+#undef GCN_MUON
     GCN_LAUNCH_CHECK("muon_kernel");
     return GCN_OK;
 }
@@ -426,12 +565,6 @@ int run_group(Group &g, int32_t steps, hipStream_t s) {
         if ((rc = product<PAIR, GRAM>(g, odd, s)) || (rc = product<PAIR, POLY>(g, odd, s))) return rc;
         if ((rc = k + 1 < steps ? product<PAIR, NEXT>(g, odd, s) : product<PAIR, LAST>(g, odd, s))) return rc;
     }
-    double bytes = 0.0;
-    for (int j = 0; j < g.count; ++j) bytes += 12.0 * g.job[j].rows * g.job[j].cols;
-    ProfScope prof(K_MUON_UPDATE, s, 0.0, bytes);
-    const dim3 b(blocks_of(g, [](const Job &J) { return (uint64_t)tiles(J.rows, J.cols, 64, 64); }));
-    hipLaunchKernelGGL(update_kernel, b, dim3(kTB), 0, s, g, (int)((steps - 1) & 1));
-    GCN_LAUNCH_CHECK("update_kernel");
     return GCN_OK;
 }
 int run_group(Group &g, int32_t steps, bool pairs, hipStream_t s) {

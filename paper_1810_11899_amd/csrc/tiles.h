@@ -207,21 +207,26 @@ __device__ __forceinline__ void turn() {
 // them, were no faster at any of the sizes below).  Scales are staged for
 // kScalePieces pieces at a time.
 constexpr int kScalePieces = 64;
-constexpr int small_lds(int type, int BM, int BN) {
-    return 2 * (BM + BN) * kPiece + (is_fp8(type) ? kScalePieces * (BM + 1) : type == TILE_FP4 ? 16 * (BM + BN) : 0);
+constexpr int small_lds(int type, int BM, int BN, int stages = 2) {
+    return stages * (BM + BN) * kPiece + (is_fp8(type) ? kScalePieces * (BM + 1) : type == TILE_FP4 ? 8 * stages * (BM + BN) : 0);
 }
-// `lds`: small_lds bytes; behind the loop they are free again.
-template <int TYPE, int BM, int BN, int WM, int WN>
+// `lds`: small_lds bytes; behind the loop they are free again.  S stages, a power
+// of two: more than two where a CU has one workgroup and nothing else hides what
+// a copy takes.  `tid`: the thread's number among the loop's 64 WM WN, where a workgroup
+// runs several of them side by side, with LDS of their own; then `turns` is the
+// largest nt among them (they share their barriers).
+template <int TYPE, int BM, int BN, int WM, int WN, int S>
 __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c, int kt0, int nt, char *lds,
-                                           f32x4 (&acc)[BM / WM / 16][BN / WN / 16]) {
+                                           f32x4 (&acc)[BM / WM / 16][BN / WN / 16], uint32_t tid, int turns) {
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16, T = 64 * WM * WN;
     constexpr int kStage = (BM + BN) * kPiece;
+    static_assert((S & (S - 1)) == 0 && (S == 2 || !is_fp8(TYPE)), "stages");
     constexpr int LA = BM * kPiece / 16 / T, LB = BN * kPiece / 16 / T;
     static_assert(LA * T * 16 == BM * kPiece && LB * T * 16 == BN * kPiece, "whole chunks per lane");
     constexpr bool SCALED = is_fp8(TYPE);
     static_assert(!SCALED || kRows8Block % BN == 0, "a tile's columns share a scale");
     static_assert(TYPE != TILE_FP4 || (BM % 64 == 0 && BN % 64 == 0 && FN == 4), "scales come in groups of 64 rows");
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const int m0 = c.tm * BM, n0 = c.tn * BN;
     constexpr bool KA = km_a(TYPE), KB = km_b(TYPE);
@@ -233,9 +238,9 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
     // which holds the row's chunk (thread % 8) ^ (row % 8); rows past the extent
     // are clamped (their products are dropped).  k-major: k-row (u T + thread) /
     // CH, its chunks clamped to the last whole one.
-    const int lr = threadIdx.x >> 3, chunk = ((threadIdx.x & 7) ^ (lr & 7)) * 16;
+    const int lr = tid >> 3, chunk = ((tid & 7) ^ (lr & 7)) * 16;
     auto km_at = [&](int64_t ld, int x0, int extent, int u) {
-        const int k = (u * T + threadIdx.x) / CH, ch = V * ((threadIdx.x % CH) ^ (4 * ((is_f32(TYPE) ? k >> 2 : k) & 3)));
+        const int k = (u * T + tid) / CH, ch = V * ((tid % CH) ^ (4 * ((is_f32(TYPE) ? k >> 2 : k) & 3)));
         if constexpr (is_pair(TYPE)) return (k & 31) * ld + pair_place(min(x0 + ch, ((extent + 31) & -32) - 8)) + (k >> 5) * 64;
         return k * ld + E * (int64_t)min(x0 + ch, ((extent + V - 1) & -V) - V);
     };
@@ -253,12 +258,12 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
     const uint8_t *g4 = nullptr;
     int64_t step4 = 0;
     if constexpr (TYPE == TILE_FP4) {
-        const int r = threadIdx.x >> 5, nb = BM / 64;
+        const int r = tid >> 5, nb = BM / 64;
         const bool of_a = r < nb;
         step4 = (int64_t)(of_a ? p.groups_a : p.groups_b) * 512;
         g4 = (of_a ? p.sa + (int64_t)min(m0 / 64 + r, p.groups_a - 1) * 512
                    : p.sb + (int64_t)min(n0 / 64 + r - nb, p.groups_b - 1) * 512) +
-             kt0 * step4 + (threadIdx.x & 31) * 16;
+             kt0 * step4 + (tid & 31) * 16;
     }
     auto copy = [&](int t, int stage) {
         const uint32_t d = lds0 + stage * kStage;
@@ -267,7 +272,7 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
 #pragma unroll
         for (int u = 0; u < LB; ++u) copy_to_lds(gb[u] + t * step_b, d + BM * kPiece + u * T * 16);
         if constexpr (TYPE == TILE_FP4) {
-            if (threadIdx.x < (BM + BN) / 2) copy_to_lds(g4 + t * step4, lds0 + 2 * kStage + stage * 8 * (BM + BN));
+            if (tid < (BM + BN) / 2) copy_to_lds(g4 + t * step4, lds0 + S * kStage + stage * 8 * (BM + BN));
         }
     };
 #pragma unroll
@@ -284,17 +289,19 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
     uint8_t *const s8 = (uint8_t *)lds + 2 * kStage;   // [piece][BM rows], then [piece]
     auto scales = [&](int t) {
         const int w = min(kScalePieces, nt - t);
-        for (int i = threadIdx.x; i < BM * w; i += T) {
+        for (int i = tid; i < BM * w; i += T) {
             const int r = i / w, k = i - r * w;
             s8[k * BM + r] = p.sa[(int64_t)min(m0 + r, p.M - 1) * p.ldsa + kt0 + t + k];
         }
-        for (int k = threadIdx.x; k < w; k += T)
+        for (int k = tid; k < w; k += T)
             s8[kScalePieces * BM + k] = p.sb[(int64_t)(n0 / kRows8Block) * p.sb_n + (int64_t)(kt0 + t + k) * p.sb_k];
     };
     if constexpr (SCALED) {
         if (nt > 0) scales(0);
     }
-    if (nt > 0) copy(0, 0);
+#pragma unroll
+    for (int u = 0; u < S - 1; ++u)
+        if (u < nt) copy(u, u);
     for (int t = 0; t < nt; ++t) {
         if constexpr (SCALED) {
             if (t % kScalePieces == 0 && t) {
@@ -303,11 +310,17 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
             }
             wait_reads();   // the scales' LDS writes, ahead of the barrier
         }
-        wait_copies<0>();   // piece t has landed
+        // piece t has landed (the copies behind it: those of S - 2 pieces)
+        if (S > 2 && nt - 1 - t >= S - 2) {
+            if (TYPE == TILE_FP4 && wave * 64 < (BM + BN) / 2) wait_copies<(S - 2) * (LA + LB + 1)>();
+            else wait_copies<(S - 2) * (LA + LB)>();
+        } else {
+            wait_copies<0>();
+        }
         turn();
         // (every wavefront has used what it read of piece t - 1: its stage is free)
-        if (t + 1 < nt) copy(t + 1, (t + 1) & 1);
-        const char *ta = lds + (t & 1) * kStage, *tb = ta + BM * kPiece;
+        if (t + S - 1 < nt) copy(t + S - 1, (t + S - 1) & (S - 1));
+        const char *ta = lds + (t & (S - 1)) * kStage, *tb = ta + BM * kPiece;
         int sa[FM], sb = 0;
         if constexpr (SCALED) {
             const int k = t % kScalePieces;
@@ -319,7 +332,7 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
 #pragma unroll
         for (int j = 0; j < FN; ++j) fb[j] = frag(tb, wn * (BN / WN) + 16 * j, KB);
         if constexpr (TYPE == TILE_FP4) {
-            const char *s4 = lds + 2 * kStage + (t & 1) * 8 * (BM + BN) + lane * 4;
+            const char *s4 = lds + S * kStage + (t & (S - 1)) * 8 * (BM + BN) + lane * 4;
             const char *qb = s4 + (BM / 64 + wn) * 512, *qa = s4 + wm * (BM / WM) / 64 * 512;
             const int b4[2] = {*(const int *)qb, *(const int *)(qb + 256)};
             const int by = wm * (BM / WM) % 64 / 16 * 8;   // (a wavefront with fewer rows than 64: its first block to byte 0)
@@ -385,8 +398,15 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
                 else asm volatile("" : "+a"(acc[i][j]));   // (where the products leave them: pinned elsewhere they are moved there and back)
             }
     }
+    for (int t = nt; t < turns; ++t) turn();
     __syncthreads();
 }
+template <int TYPE, int BM, int BN, int WM, int WN, int S = 2>
+__device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c, int kt0, int nt, char *lds,
+                                           f32x4 (&acc)[BM / WM / 16][BN / WN / 16]) {
+    small_loop<TYPE, BM, BN, WM, WN, S>(p, c, kt0, nt, lds, acc, threadIdx.x, nt);
+}
+
 
 // ------------------------------------------------------------ large tiles
 // 256 x 256 tiles of 8 wavefronts (2 along M, 4 along N; 128 x 64 each), one
