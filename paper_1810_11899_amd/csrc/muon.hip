@@ -45,32 +45,37 @@ constexpr float two_to(int k) {
 // A matrix of the group.  X0 and X1 [mp x np], A and B [mp x mp] in the workspace:
 // pairs in rows of 4 np bytes (32 high parts, 32 low ones, ..), or float16 rows,
 // X's low parts in a second plane mp np elements on.
-struct Job {
+// (What a product needs first stands in its first 64 bytes.)
+struct alignas(64) Job {
+    uint8_t *X0, *X1, *A, *B;
+    int32_t mp, np;
+    int32_t rows, cols;
+    int64_t ldw;             // of out too
+    float step;              // lr * scale
+    int32_t parts;
     float *W;                // updated, or null
+    void *out;               // orthogonalise's result, or null
     const void *G;           // the gradient, or what is orthogonalised
     float *M;                // momentum, or null
-    void *out;               // orthogonalise's result, or null
-    int64_t ldw, ldg, ldm;   // ldw: of out too
-    int32_t rows, cols;
-    int32_t m, n, mp, np;
-    uint8_t *X0, *X1, *A, *B;
+    int64_t ldg, ldm;
     double *part;            // sums of squares
-    int32_t parts;
-    float step;              // lr * scale
 };
-struct Group {
-    Job job[kGroup];
-    uint32_t first[kGroup + 1];   // a launch's blocks by job
+// A launch's arguments.  The chain of loads from its number to a block's operands is a
+// good part of a small launch: the table of first blocks is one line, read
+// whole.
+struct alignas(64) Group {
+    uint32_t first[kGroup];       // a launch's first block of each job, of no job 2^32 - 1
+    uint32_t total, per_xcd, band;
     int32_t count;
-    int32_t tile_m, tile_n;
-    uint32_t per_xcd, band;       // of a product's tiles
     int full;                     // A and B: all of their tiles, not those on and below the diagonal alone
     float momentum, decay;
     int nesterov, grad_bf16, out_bf16;
+    Job job[kGroup];
 };
 __device__ __forceinline__ int job_of(const Group &g, uint32_t block) {
     int j = 0;
-    while (j + 1 < g.count && block >= g.first[j + 1]) ++j;
+#pragma unroll
+    for (int k = 1; k < kGroup; ++k) j += block >= g.first[k];
     return j;
 }
 
@@ -328,7 +333,7 @@ constexpr int type_of() {
 // group's tiles are numbered matrix by matrix and dealt to the XCDs in eight
 // runs, so that a matrix is read by as few L2s as can be; within a matrix in
 // bands of `band` row tiles (A and B: tiles on and below the diagonal, row by row).
-template <bool PAIR, int STAGE>
+template <bool PAIR, int STAGE, int BM, int BN>
 __device__ __forceinline__ void product_of(const Group &g, const Job &J, const uint8_t *X, uint32_t at, TileProduct &p,
                                            Coord &c) {
     constexpr int kUnit = PAIR ? 32 : 64;   // columns of a piece
@@ -360,7 +365,7 @@ __device__ __forceinline__ void product_of(const Group &g, const Job &J, const u
         c.tm = t;
         c.tn = (int)(at - (uint32_t)t * (t + 1) / 2);
     } else {
-        const uint32_t tiles_m = (uint32_t)((p.M + g.tile_m - 1) / g.tile_m), tiles_n = (uint32_t)((p.N + g.tile_n - 1) / g.tile_n);
+        const uint32_t tiles_m = (uint32_t)(p.M + BM - 1) / BM, tiles_n = (uint32_t)(p.N + BN - 1) / BN;
         const uint32_t b = at / (g.band * tiles_n), q = at - b * g.band * tiles_n, h = min(g.band, tiles_m - b * g.band);
         c.tn = (int)(q / h);
         c.tm = (int)(b * g.band + (q - c.tn * h));
@@ -371,16 +376,16 @@ __device__ __forceinline__ void product_of(const Group &g, const Job &J, const u
 }
 
 // The block's tile, or the end of the block where it has none.
-#define GCN_MUON_TILE                                                          \
+#define GCN_MUON_TILE(BM, BN)                                                     \
     const uint32_t L = (blockIdx.x & 7) * g.per_xcd + (blockIdx.x >> 3);       \
-    if (L >= g.first[g.count]) return;                                         \
+    if (L >= g.total) return;                                                  \
     const int job = job_of(g, L);                                              \
     const Job &J = g.job[job];                                                 \
     const uint8_t *const X = odd ? J.X1 : J.X0;                                \
     uint8_t *const next = odd ? J.X0 : J.X1;                                   \
     TileProduct p{};                                                           \
     Coord c;                                                                   \
-    product_of<PAIR, STAGE>(g, J, X, L - g.first[job], p, c);                  \
+    product_of<PAIR, STAGE, BM, BN>(g, J, X, L - g.first[job], p, c);          \
     const bool mirror = STAGE <= POLY && !g.full && c.tm != c.tn
 
 // KG groups of WM x WN wavefronts take a KG-th of the sum each, and share the tile's
@@ -392,7 +397,7 @@ __global__ __launch_bounds__(64 * WM *WN *KG) void muon_kernel(Group g, int odd)
     constexpr int kLds = small_lds(TYPE, BM, BN);
     static_assert(KG == 1 || KG * FM * 4 * T * 16 <= KG * kLds, "the groups' sums fit where the operands were");
     __shared__ __attribute__((aligned(16))) char lds[KG * kLds];
-    GCN_MUON_TILE;
+    GCN_MUON_TILE(BM, BN);
     const uint32_t tid = threadIdx.x % T;
     const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / T), lane = tid & 63, wave = tid >> 6;
     const int r0 = c.tm * BM + wave / WN * (BM / WM) + (lane & 15), c0 = c.tn * BN + wave % WN * (BN / WN) + 4 * (lane >> 4);
@@ -434,7 +439,7 @@ template <bool PAIR, int STAGE>
 __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void muon_big_kernel(Group g, int odd) {
     constexpr int TYPE = type_of<PAIR, STAGE>();
     __shared__ __attribute__((aligned(16))) char lds[big_lds(TYPE)];
-    GCN_MUON_TILE;
+    GCN_MUON_TILE(kBigT, kBigT);
     f32x4 acc[8][4];
     big_loop<TYPE>(p, c, 0, p.kt, lds, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -451,6 +456,169 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
     }
 }
 
+// ------------------------------------------------------------- small matrices
+// A whole update of a matrix whose X and A fit in LDS as pairs, by one workgroup: no
+// launches between the products.  X and A lie as pieces of 32 columns, a
+// row's 128 bytes (high parts, low parts) beside the next row's, chunk c of row r at
+// c ^ (r % 8), so that 16 rows' chunks are on different banks.  B takes A's place.  A and B: a wavefront has one block of
+// 16 TS x 16 TS.  a X + B X: a wavefront has 16 columns of X at a time, which no
+// other reads, and writes them back in place.  50 x 64: 80 us in launches of their
+// own, 19 here; 64 x 560 102 and 54, 128 x 192 98 and 62, sixteen of 128 x 128 96 and 56.
+constexpr int kSmallLds = 160 << 10, kSmallThreads = 1024, kSmallSide = 128;
+bool fits_lds(int64_t mp, int64_t np) { return mp <= kSmallSide && 4 * mp * (mp + np) <= kSmallLds; }
+
+struct Resident {
+    char *base;
+    int step;     // bytes from a piece of 32 columns to the next, 128 a row
+    // of column c's high part in row r; its low part lies at the place of chunk + 4
+    __device__ __forceinline__ char *at(int r, int c, int part) const {
+        return base + c / 32 * step + r * 128 + (((c % 32 / 8 + 4 * part) ^ (r & 7)) * 16) + c % 8 * 2;
+    }
+    // 16 rows against a piece of 32 columns
+    __device__ __forceinline__ Frag rows(int r0, int piece, int lane) const {
+        const int fr = lane & 15, g = lane >> 4;
+        const char *q = base + piece * step + (r0 + fr) * 128;
+        return Frag{*(const uint4 *)(q + (g ^ (fr & 7)) * 16), *(const uint4 *)(q + ((g + 4) ^ (fr & 7)) * 16)};
+    }
+    // 16 columns from c0 against 32 rows
+    __device__ __forceinline__ Frag columns(int piece, int c0, int lane) const {
+        const int r = 32 * piece + 8 * (lane >> 4) + ((lane & 15) >> 2), c = c0 + 4 * (lane & 3);
+        const uint2 a = km_read(at(r, c, 0)), b = km_read(at(r + 4, c, 0)), d = km_read(at(r, c, 1)), e = km_read(at(r + 4, c, 1));
+        return Frag{make_uint4(a.x, a.y, b.x, b.y), make_uint4(d.x, d.y, e.x, e.y)};
+    }
+    __device__ __forceinline__ f32x4 four(int r, int c) const {
+        return four_of((const uint8_t *)at(r, c, 0)) + four_of((const uint8_t *)at(r, c, 1));
+    }
+    __device__ __forceinline__ void put(int r, int c, f32x4 v) const {
+        const uint2 h = four_halves(v);
+        *(uint2 *)at(r, c, 0) = h;
+        const f32x4 hi = {half_value(h.x & 0xFFFFu), half_value(h.x >> 16), half_value(h.y & 0xFFFFu), half_value(h.y >> 16)};
+        *(uint2 *)at(r, c, 1) = four_halves(v - hi);
+    }
+    __device__ __forceinline__ void put_one(int r, int c, float v) const {
+        const uint16_t h = half_bits(v);
+        *(uint16_t *)at(r, c, 0) = h;
+        *(uint16_t *)at(r, c, 1) = half_bits(v - half_value(h));
+    }
+};
+
+// The wavefront's block of P P^T, P's rows against each other over `pieces`.
+template <int TS>
+__device__ __forceinline__ void block_of(const Resident &P, int pieces, int i0, int j0, int lane, f32x4 (&acc)[TS][TS]) {
+#pragma unroll
+    for (int i = 0; i < TS; ++i)
+#pragma unroll
+        for (int j = 0; j < TS; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int t = 0; t < pieces; ++t) {
+        Frag b[TS];
+#pragma unroll
+        for (int j = 0; j < TS; ++j) b[j] = P.rows(j0 + 16 * j, t, lane);
+#pragma unroll
+        for (int i = 0; i < TS; ++i) {
+            const Frag a = P.rows(i0 + 16 * i, t, lane);
+#pragma unroll
+            for (int j = 0; j < TS; ++j) mma<TILE_PAIR>(acc[i][j], a, b[j], 0, 0);
+        }
+    }
+}
+// A = X X^T, then B in A's place; every wavefront calls it
+template <int TS>
+__device__ __forceinline__ void gram_and_poly(const Resident &X, const Resident &A, int mp, int np, int lane, int wave) {
+    const int across = mp / (16 * TS), i0 = wave / across * 16 * TS, j0 = wave % across * 16 * TS;
+    const bool mine = wave < across * across;
+    f32x4 acc[TS][TS];
+    const int r0 = i0 + (lane & 15), c0 = j0 + 4 * (lane >> 4);
+    if (mine) {
+        block_of<TS>(X, np / 32, i0, j0, lane, acc);
+#pragma unroll
+        for (int i = 0; i < TS; ++i)
+#pragma unroll
+            for (int j = 0; j < TS; ++j) A.put(r0 + 16 * i, c0 + 16 * j, acc[i][j] * two_to(kABits - 2 * kXBits));
+    }
+    __syncthreads();
+    if (mine) {
+        block_of<TS>(A, mp / 32, i0, j0, lane, acc);
+#pragma unroll
+        for (int i = 0; i < TS; ++i)
+#pragma unroll
+            for (int j = 0; j < TS; ++j)
+                acc[i][j] = acc[i][j] * (kCoefC * two_to(kBBits - 2 * kABits)) +
+                            A.four(r0 + 16 * i, c0 + 16 * j) * (kCoefB * two_to(kBBits - kABits));
+    }
+    __syncthreads();   // A is read
+    if (mine) {
+#pragma unroll
+        for (int i = 0; i < TS; ++i)
+#pragma unroll
+            for (int j = 0; j < TS; ++j) A.put(r0 + 16 * i, c0 + 16 * j, acc[i][j]);
+    }
+    __syncthreads();
+}
+
+__global__ __launch_bounds__(kSmallThreads) void resident_kernel(Group g, int steps) {
+    __shared__ __attribute__((aligned(16))) char lds[kSmallLds];
+    const Job &J = g.job[blockIdx.x];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mp = J.mp, np = J.np;
+    const Resident A{lds, 128 * mp}, X{lds + 4 * mp * mp, 128 * mp};
+    // M and the norm, then X, each of a thread's own elements of U both times
+    const uint32_t per_row = ((uint32_t)J.cols + 3) / 4, total = (uint32_t)J.rows * per_row;
+    double sum = 0.0;
+    for (uint32_t i = threadIdx.x; i < total; i += kSmallThreads)
+        sum += squares(four_of_u<true>(g, J, i / per_row, 4 * (i % per_row)));
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    double *const red = (double *)lds;   // (A's place)
+    if (lane == 0) red[wave] = sum;
+    for (int i = threadIdx.x; i < mp * np / 4; i += kSmallThreads) *(uint4 *)(X.base + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < kSmallThreads / 64; ++w) sum += red[w];
+    const double inv = inverse_norm(sum);
+    const bool tall = J.rows > J.cols;
+    for (uint32_t i = threadIdx.x; i < total; i += kSmallThreads) {
+        const int r = (int)(i / per_row), c = 4 * (int)(i % per_row);
+        f32x4 u = four_of_u<false>(g, J, r, c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = (float)((double)u[e] * inv);
+        if (tall) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < J.cols) X.put_one(c + e, r, u[e]);
+        } else {
+            X.put(r, c, u);
+        }
+    }
+    __syncthreads();
+    for (int k = 0; k < steps; ++k) {
+        if (mp > 64) gram_and_poly<2>(X, A, mp, np, lane, wave);
+        else gram_and_poly<1>(X, A, mp, np, lane, wave);
+        const bool last = k + 1 == steps;
+        for (int c0 = 16 * wave; c0 < np; c0 += 16 * (kSmallThreads / 64)) {
+            f32x4 acc[kSmallSide / 16];
+#pragma unroll
+            for (int i = 0; i < kSmallSide / 16; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+            for (int t = 0; t < mp / 32; ++t) {
+                const Frag x = X.columns(t, c0, lane);
+#pragma unroll
+                for (int i = 0; i < kSmallSide / 16; ++i)
+                    if (16 * i < mp) mma<TILE_PAIR>(acc[i], A.rows(16 * i, t, lane), x, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < kSmallSide / 16; ++i) {
+                if (16 * i >= mp) break;
+                const int row = 16 * i + (lane & 15), col = c0 + 4 * (lane >> 4);
+                const f32x4 v = acc[i] * two_to(-kBBits) + X.four(row, col) * kCoefA;
+                if (last) apply(g, J, row, col, v * two_to(-kXBits));
+                else X.put(row, col, v);
+            }
+        }
+        __syncthreads();
+    }
+}
+
 // Whether a matrix takes pairs.  GCN_BF16 does so too for matrices with a short side: a
 // single product's roundings average out over many singular values only (one row:
 // 4e-3 off, 128 rows 1.7e-3), and their time is launches, not products.
@@ -464,11 +632,9 @@ int32_t up(int32_t x, int32_t to) { return (x + to - 1) / to * to; }
 
 // The job's places in the workspace.
 void plan_job(Job &J, bool pair, Arena &ar) {
-    J.m = std::min(J.rows, J.cols);
-    J.n = std::max(J.rows, J.cols);
     const int32_t unit = pair ? 32 : 64;
-    J.mp = up(J.m, unit);
-    J.np = up(J.n, unit);
+    J.mp = up(std::min(J.rows, J.cols), unit);
+    J.np = up(std::max(J.rows, J.cols), unit);
     J.X0 = ar.take<uint8_t>(4 * (size_t)J.mp * J.np);
     J.X1 = ar.take<uint8_t>(4 * (size_t)J.mp * J.np);
     J.A = ar.take<uint8_t>((pair ? 4 : 2) * (size_t)J.mp * J.mp);
@@ -486,7 +652,8 @@ unsigned blocks_of(Group &g, F &&blocks) {
         g.first[j] = (uint32_t)at;
         at += blocks(g.job[j]);
     }
-    g.first[g.count] = (uint32_t)at;
+    for (int j = g.count; j < kGroup; ++j) g.first[j] = 0xFFFFFFFFu;
+    g.total = (uint32_t)at;
     return (unsigned)at;
 }
 
@@ -511,14 +678,13 @@ int product(Group &g, int odd, hipStream_t s) {
     for (int j = 0; j < g.count; ++j) {
         const Job &J = g.job[j];
         deep = deep && J.mp >= 256 && J.np < (1 << 22);   // (a large tile's row offsets within it: 32 bits)
-        flops += STAGE == GRAM ? (double)J.m * J.m * J.n : STAGE == POLY ? (double)J.m * J.m * J.m : 2.0 * J.m * J.m * J.n;
+        const double m = std::min(J.rows, J.cols), n = std::max(J.rows, J.cols);
+        flops += STAGE == GRAM ? m * m * n : STAGE == POLY ? m * m * m : 2.0 * m * m * n;
     }
     ProfScope prof(K_MUON_PRODUCT, s, flops, 0.0);
     g.full = 1;
     if (STAGE <= POLY && all(64, 64) > 128) g.full = 0;
     auto grid = [&](int32_t tm, int32_t tn) {
-        g.tile_m = tm;
-        g.tile_n = tn;
         const uint32_t total = blocks_of(g, [&](const Job &J) { return (uint64_t)count(J, tm, tn); });
         g.per_xcd = (total + 7) / 8;
         g.band = (uint32_t)std::max(1, std::min(8, (int)std::lround(std::sqrt((double)g.per_xcd))));
@@ -548,6 +714,21 @@ int product(Group &g, int odd, hipStream_t s) {
 
 template <bool PAIR>
 int run_group(Group &g, int32_t steps, hipStream_t s) {
+    if constexpr (PAIR) {
+        bool small = true;
+        double flops = 0.0;
+        for (int j = 0; j < g.count; ++j) {
+            const Job &J = g.job[j];
+            small = small && fits_lds(J.mp, J.np);
+            flops += (3.0 * J.np + J.mp) * J.mp * J.mp * steps;
+        }
+        if (small) {
+            ProfScope prof(K_MUON_SMALL, s, flops, 0.0);
+            hipLaunchKernelGGL(resident_kernel, dim3((unsigned)g.count), dim3(kSmallThreads), 0, s, g, (int)steps);
+            GCN_LAUNCH_CHECK("resident_kernel");
+            return GCN_OK;
+        }
+    }
     {
         double bytes = 0.0;
         for (int j = 0; j < g.count; ++j) bytes += 12.0 * g.job[j].rows * g.job[j].cols;
