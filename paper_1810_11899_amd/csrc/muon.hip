@@ -411,7 +411,7 @@ __global__ __launch_bounds__(64 * WM *WN *KG) void muon_kernel(Group g, int odd)
     }
     f32x4 acc[FM][4];
     const int per = (p.kt + KG - 1) / KG, k0 = min(group * per, p.kt);
-    small_loop<TYPE, BM, BN, WM, WN, 2>(p, c, k0, min(per, p.kt - k0), lds + group * kLds, acc, tid, per);
+    small_loop<TYPE, BM, BN, WM, WN>(p, c, k0, min(per, p.kt - k0), lds + group * kLds, acc, tid, per);
     if constexpr (KG > 1) {
         f32x4 *const part = (f32x4 *)lds;   // [block][group][thread]
 #pragma unroll

@@ -253,12 +253,23 @@ int check_rows4(const gcn_rows4 *r, const char *who) {
     return GCN_OK;
 }
 
-// Parts of a product's sum, for products with few tiles.
+// Parts of a product's sum, for products with few tiles and long sums (weight
+// gradients): 128 x 128 tiles, two a CU and 16 pieces a part or more, where they fill the
+// CUs, else 64 x 64 ones of 8 pieces.  Parts are written and read again, which
+// costs about 3 us and 0.4 us a megabyte (us, in 1 / 2 / 4 / 8 / 16 parts, float32 results;
+// 64 x 64: 1024 x 512 x 8000 12.6 / 12.0 / 13.3, 512 x 256 x 8000 12.2 / 9.9 / 9.5 / 9.7,
+// 256 x 256 x 32,000 38 / 22 / 14.5 / 11.7 / 11.5, 1024 x 1024 x 8192 13.3 / 16.4; 128 x 128:
+// 1024 x 512 x 65,536 151 / 84 / 48 / 32 / 33, 1024 x 1024 x 65,536 156 / 85 / 52 / 45 / 61, 64 x 64
+// 116 / 67 / 61 / 65; 256 x 256 tiles 363 / 192 / 105 / 63 / 44 and 364 / 193 / 107 / 66 / 54).
+// Few rows take thin4_kernel unless it has few workgroups and a long sum.
 int32_t split4(int32_t M, int32_t N, int32_t kt) {
-    if (M <= 64 || kt < 8) return 1;
-    const int64_t tiles = ((M + 127ll) / 128) * ((N + 127ll) / 128);
-    if (tiles >= 128) return 1;
-    return tile_splits(M, N, kt, false);
+    if (kt < 24 || (M <= 64 && N > 2048)) return 1;
+    const int64_t t64 = ((M + 63ll) / 64) * ((N + 63ll) / 64), t128 = ((M + 127ll) / 128) * ((N + 127ll) / 128);
+    int64_t sp = std::min<int64_t>(512 / t128, kt / 16);
+    if (t128 * sp < 192) sp = std::min<int64_t>({(kt < 64 ? 256 : 512) / t64, kt / 8, 32});
+    if (sp <= 1) return 1;
+    const int32_t per = (int32_t)((kt + sp - 1) / sp);
+    return (kt + per - 1) / per;
 }
 
 }  // namespace

@@ -207,20 +207,17 @@ __device__ __forceinline__ void turn() {
 // them, were no faster at any of the sizes below).  Scales are staged for
 // kScalePieces pieces at a time.
 constexpr int kScalePieces = 64;
-constexpr int small_lds(int type, int BM, int BN, int stages = 2) {
-    return stages * (BM + BN) * kPiece + (is_fp8(type) ? kScalePieces * (BM + 1) : type == TILE_FP4 ? 8 * stages * (BM + BN) : 0);
+constexpr int small_lds(int type, int BM, int BN) {
+    return 2 * (BM + BN) * kPiece + (is_fp8(type) ? kScalePieces * (BM + 1) : type == TILE_FP4 ? 16 * (BM + BN) : 0);
 }
-// `lds`: small_lds bytes; behind the loop they are free again.  S stages, a power
-// of two: more than two where a CU has one workgroup and nothing else hides what
-// a copy takes.  `tid`: the thread's number among the loop's 64 WM WN, where a workgroup
+// `lds`: small_lds bytes; behind the loop they are free again.  `tid`: the thread's number among the loop's 64 WM WN, where a workgroup
 // runs several of them side by side, with LDS of their own; then `turns` is the
 // largest nt among them (they share their barriers).
-template <int TYPE, int BM, int BN, int WM, int WN, int S>
+template <int TYPE, int BM, int BN, int WM, int WN>
 __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c, int kt0, int nt, char *lds,
                                            f32x4 (&acc)[BM / WM / 16][BN / WN / 16], uint32_t tid, int turns) {
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16, T = 64 * WM * WN;
     constexpr int kStage = (BM + BN) * kPiece;
-    static_assert((S & (S - 1)) == 0 && (S == 2 || !is_fp8(TYPE)), "stages");
     constexpr int LA = BM * kPiece / 16 / T, LB = BN * kPiece / 16 / T;
     static_assert(LA * T * 16 == BM * kPiece && LB * T * 16 == BN * kPiece, "whole chunks per lane");
     constexpr bool SCALED = is_fp8(TYPE);
@@ -272,7 +269,7 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
 #pragma unroll
         for (int u = 0; u < LB; ++u) copy_to_lds(gb[u] + t * step_b, d + BM * kPiece + u * T * 16);
         if constexpr (TYPE == TILE_FP4) {
-            if (tid < (BM + BN) / 2) copy_to_lds(g4 + t * step4, lds0 + S * kStage + stage * 8 * (BM + BN));
+            if (tid < (BM + BN) / 2) copy_to_lds(g4 + t * step4, lds0 + 2 * kStage + stage * 8 * (BM + BN));
         }
     };
 #pragma unroll
@@ -299,9 +296,7 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
     if constexpr (SCALED) {
         if (nt > 0) scales(0);
     }
-#pragma unroll
-    for (int u = 0; u < S - 1; ++u)
-        if (u < nt) copy(u, u);
+    if (nt > 0) copy(0, 0);
     for (int t = 0; t < nt; ++t) {
         if constexpr (SCALED) {
             if (t % kScalePieces == 0 && t) {
@@ -310,17 +305,11 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
             }
             wait_reads();   // the scales' LDS writes, ahead of the barrier
         }
-        // piece t has landed (the copies behind it: those of S - 2 pieces)
-        if (S > 2 && nt - 1 - t >= S - 2) {
-            if (TYPE == TILE_FP4 && wave * 64 < (BM + BN) / 2) wait_copies<(S - 2) * (LA + LB + 1)>();
-            else wait_copies<(S - 2) * (LA + LB)>();
-        } else {
-            wait_copies<0>();
-        }
+        wait_copies<0>();   // piece t has landed
         turn();
         // (every wavefront has used what it read of piece t - 1: its stage is free)
-        if (t + S - 1 < nt) copy(t + S - 1, (t + S - 1) & (S - 1));
-        const char *ta = lds + (t & (S - 1)) * kStage, *tb = ta + BM * kPiece;
+        if (t + 1 < nt) copy(t + 1, (t + 1) & 1);
+        const char *ta = lds + (t & 1) * kStage, *tb = ta + BM * kPiece;
         int sa[FM], sb = 0;
         if constexpr (SCALED) {
             const int k = t % kScalePieces;
@@ -332,7 +321,7 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
 #pragma unroll
         for (int j = 0; j < FN; ++j) fb[j] = frag(tb, wn * (BN / WN) + 16 * j, KB);
         if constexpr (TYPE == TILE_FP4) {
-            const char *s4 = lds + S * kStage + (t & (S - 1)) * 8 * (BM + BN) + lane * 4;
+            const char *s4 = lds + 2 * kStage + (t & 1) * 8 * (BM + BN) + lane * 4;
             const char *qb = s4 + (BM / 64 + wn) * 512, *qa = s4 + wm * (BM / WM) / 64 * 512;
             const int b4[2] = {*(const int *)qb, *(const int *)(qb + 256)};
             const int by = wm * (BM / WM) % 64 / 16 * 8;   // (a wavefront with fewer rows than 64: its first block to byte 0)
@@ -401,10 +390,10 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
     for (int t = nt; t < turns; ++t) turn();
     __syncthreads();
 }
-template <int TYPE, int BM, int BN, int WM, int WN, int S = 2>
+template <int TYPE, int BM, int BN, int WM, int WN>
 __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c, int kt0, int nt, char *lds,
                                            f32x4 (&acc)[BM / WM / 16][BN / WN / 16]) {
-    small_loop<TYPE, BM, BN, WM, WN, S>(p, c, kt0, nt, lds, acc, threadIdx.x, nt);
+    small_loop<TYPE, BM, BN, WM, WN>(p, c, kt0, nt, lds, acc, threadIdx.x, nt);
 }
 
 

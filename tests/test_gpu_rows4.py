@@ -207,7 +207,8 @@ def test_product(M, N, K, dtype, ws):
 
 def test_product_of_whole_numbers_is_exact(ws):
     """Small whole numbers: every sum below 2^24 is exact in any order, on every tile shape."""
-    for M, N, K in ((40, 500, 1024), (300, 300, 512), (1500, 1600, 640), (4100, 4096, 1024), (600, 520, 40000)):
+    for M, N, K in ((40, 500, 1024), (300, 300, 512), (1500, 1600, 640), (4100, 4096, 1024), (600, 520, 40000),
+                    (50, 130, 30000), (200, 130, 6500), (1024, 512, 65536)):
         g = torch.Generator(device="cuda")
         g.manual_seed(M)
         x = torch.randint(-3, 4, (M, K), generator=g, device="cuda").float()
