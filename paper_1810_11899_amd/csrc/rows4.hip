@@ -39,30 +39,51 @@ __device__ __forceinline__ uint32_t held8(const float *x, int s) {
     return s == kNaNScale ? 0u : r;
 }
 
-// eight consecutive elements from column c of a row (zeros past f)
+// Eight consecutive elements from column c of a row as they lie in memory (zeros past
+// f); their values.  Apart, so that all of a thread's loads are in flight before
+// the first is used.
 template <bool BF>
-__device__ __forceinline__ void load8(const void *row, int64_t c, int32_t f, float (&x)[8]) {
-    if (c + 8 <= f) {
-        if (BF) {
-            const uint4 v = load16((const uint16_t *)row + c);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[2 * i] = __uint_as_float(w[i] << 16);
-                x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-            }
+struct Raw {
+    uint4 v[BF ? 1 : 2];
+};
+template <bool BF>
+__device__ __forceinline__ Raw<BF> load_raw(const void *row, int64_t c, int32_t f) {
+    Raw<BF> x;
+    const int64_t left = f - c;
+    if (left >= 8) {
+        if constexpr (BF) {
+            x.v[0] = load16((const uint16_t *)row + c);
         } else {
-            const uint4 a = load16((const float *)row + c), b = load16((const float *)row + c + 4);
-            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
+            x.v[0] = load16((const float *)row + c);
+            x.v[1] = load16((const float *)row + c + 4);
         }
     } else {
+        uint32_t w[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            x[i] = c + i < f ? (BF ? __uint_as_float((uint32_t)((const uint16_t *)row)[c + i] << 16)
-                                   : ((const float *)row)[c + i])
-                             : 0.0f;
+            if (i < left) w[i] = BF ? (uint32_t)((const uint16_t *)row)[c + i] : ((const uint32_t *)row)[c + i];
+        if constexpr (BF) {
+            x.v[0] = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+        } else {
+            x.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            x.v[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+    }
+    return x;
+}
+template <bool BF>
+__device__ __forceinline__ void values_of(const Raw<BF> &r, float (&x)[8]) {
+    if constexpr (BF) {
+        const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+    } else {
+        const uint32_t w[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
     }
 }
 
@@ -82,10 +103,12 @@ struct PackArgs {
 // come from memory; 4 lanes hold a block of a row, which they pack at once.  The
 // columns are packed from LDS, one thread a block of 32 rows, and written
 // through LDS again, 64 bytes a row.
+// Bound by memory: PACKNOTE
+constexpr int kPackT = 512;
 template <bool BF, bool COLS>
-__global__ __launch_bounds__(kTB) void pack4_kernel(PackArgs a) {
+__global__ __launch_bounds__(kPackT) void pack4_kernel(PackArgs a) {
     typedef typename std::conditional<BF, uint16_t, float>::type T;
-    constexpr int kLd = kTile + (BF ? 8 : 4);
+    constexpr int kLd = kTile + (BF ? 8 : 4), kRows = kTile * 16 / kPackT;
     __shared__ __attribute__((aligned(16))) T tile[COLS ? kTile : 1][kLd];
     __shared__ uint4 turned[COLS ? kTile * 4 : 1];
     __shared__ float sums[COLS ? 4 : 1][kTile];
@@ -93,21 +116,27 @@ __global__ __launch_bounds__(kTB) void pack4_kernel(PackArgs a) {
     for (int64_t b = blockIdx.x; b < tiles; b += gridDim.x) {
         const int64_t tr = b / a.tiles_c, tc = b - tr * a.tiles_c;
         const int64_t r0 = tr * kTile, c0 = tc * kTile;
-        const int cl = 8 * (int)(threadIdx.x & 15);
+        const int cl = 8 * (int)(threadIdx.x & 15), rl0 = (int)(threadIdx.x >> 4);
         const int64_t c = c0 + cl;
+        Raw<BF> raw[kRows], mask[kRows];
 #pragma unroll
-        for (int u = 0; u < kTile / 16; ++u) {
-            const int rl = 16 * u + (int)(threadIdx.x >> 4);
-            const int64_t r = r0 + rl;
-            float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-            if (r < a.n) {
-                load8<BF>((const T *)a.X + r * a.ldx, c, a.f, x);
-                if (a.mask) {
-                    float m[8];
-                    load8<BF>((const T *)a.mask + r * a.ldm, c, a.f, m);
+        for (int u = 0; u < kRows; ++u) {
+            const int64_t row = r0 + (kTile / kRows) * u + rl0;
+            const int32_t f = row < a.n ? a.f : 0;
+            raw[u] = load_raw<BF>((const T *)a.X + row * a.ldx, c, f);
+            if (a.mask) mask[u] = load_raw<BF>((const T *)a.mask + row * a.ldm, c, f);
+        }
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = m[i] > 0.0f ? x[i] : 0.0f;
-                }
+        for (int u = 0; u < kRows; ++u) {
+            const int rl = (kTile / kRows) * u + rl0;
+            const int64_t row = r0 + rl;
+            float x[8];
+            values_of<BF>(raw[u], x);
+            if (a.mask) {
+                float m[8];
+                values_of<BF>(mask[u], m);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = m[i] > 0.0f ? x[i] : 0.0f;
             }
             if (a.q) {
                 uint32_t top = 0u;
@@ -116,9 +145,9 @@ __global__ __launch_bounds__(kTB) void pack4_kernel(PackArgs a) {
                 top = max(top, (uint32_t)__shfl_xor((int)top, 1));
                 top = max(top, (uint32_t)__shfl_xor((int)top, 2));
                 const int s = scale_byte(top);
-                if (r < a.n && c < (((int64_t)a.f + 255) & ~255ll)) {
-                    *(uint32_t *)(a.q + r * a.ldq + c / 2) = held8(x, s);
-                    if ((threadIdx.x & 3) == 0) a.scale[scale_place(r, c >> 5, groups)] = (uint8_t)s;
+                if (row < a.n && c < (((int64_t)a.f + 255) & ~255ll)) {
+                    *(uint32_t *)(a.q + row * a.ldq + c / 2) = held8(x, s);
+                    if ((threadIdx.x & 3) == 0) a.scale[scale_place(row, c >> 5, groups)] = (uint8_t)s;
                 }
             }
             if constexpr (COLS) {
@@ -136,10 +165,9 @@ __global__ __launch_bounds__(kTB) void pack4_kernel(PackArgs a) {
         }
         if constexpr (COLS) {
             __syncthreads();
-            const int col = threadIdx.x & (kTile - 1);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int blk = 2 * h + (int)(threadIdx.x >> 7);   // of 32 rows
+            const int col = threadIdx.x & (kTile - 1), blk = (int)threadIdx.x / kTile;   // of 32 rows
+            const bool to_t = a.qt && r0 < (((int64_t)a.n + 255) & ~255ll);
+            {
                 float x[32];
                 uint32_t top = 0u;
                 float sum = 0.0f;
@@ -152,26 +180,21 @@ __global__ __launch_bounds__(kTB) void pack4_kernel(PackArgs a) {
                     sum += x[i];
                 }
                 sums[blk][col] = sum;
-                if (a.qt) {
+                if (to_t) {
                     const int s = scale_byte(top);
                     turned[col * 4 + blk] = make_uint4(held8(x, s), held8(x + 8, s), held8(x + 16, s), held8(x + 24, s));
-                    if (c0 + col < a.f && r0 < (((int64_t)a.n + 255) & ~255ll))
-                        a.scale_t[scale_place(c0 + col, (r0 >> 5) + blk, groups_t)] = (uint8_t)s;
+                    if (c0 + col < a.f) a.scale_t[scale_place(c0 + col, (r0 >> 5) + blk, groups_t)] = (uint8_t)s;
                 }
             }
             __syncthreads();
-            if (a.qt && r0 < (((int64_t)a.n + 255) & ~255ll)) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int i = h * kTB + (int)threadIdx.x;
-                    const int64_t row = c0 + (i >> 2);
-                    if (row < a.f) *(uint4 *)(a.qt + row * a.ldqt + r0 / 2 + (i & 3) * 16) = turned[i];
-                }
+            if (to_t) {
+                const int64_t row = c0 + (threadIdx.x >> 2);
+                if (row < a.f) *(uint4 *)(a.qt + row * a.ldqt + r0 / 2 + (threadIdx.x & 3) * 16) = turned[threadIdx.x];
             }
             if (a.part && threadIdx.x < kTile && c0 + threadIdx.x < a.f && r0 < a.n)
                 a.part[tr * a.f + c0 + threadIdx.x] = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) +
                                                       (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
-            __syncthreads();
+            // (the next tile's rows are written behind a barrier that the last reads of this one's are ahead of)
         }
     }
 }
@@ -336,7 +359,7 @@ int gcn_rows4_pack(const void *X, gcn_rows_type type, int32_t n, int32_t f, int3
         ProfScope prof(K_ROWS4_PACK, s, 0.0,
                        (double)n * f * ((bf ? 2.0 : 4.0) * (mask ? 2 : 1) + 0.53125 * ((out ? 1 : 0) + (outT ? 1 : 0))));
         const unsigned g = (unsigned)std::min<int64_t>((int64_t)a.tiles_r * a.tiles_c, 1 << 16);
-#define GCN_PACK4(BF, COLS) hipLaunchKernelGGL((pack4_kernel<BF, COLS>), dim3(g), dim3(kTB), 0, s, a)
+#define GCN_PACK4(BF, COLS) hipLaunchKernelGGL((pack4_kernel<BF, COLS>), dim3(g), dim3(kPackT), 0, s, a)
         if (bf && cols) GCN_PACK4(true, true);
         else if (bf) GCN_PACK4(true, false);
         else if (cols) GCN_PACK4(false, true);
