@@ -8,6 +8,7 @@ raises instead of falling back to anything else.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -776,6 +777,11 @@ def _pieces4(f: int) -> int:
     return (f + ROWS4_PIECE - 1) // ROWS4_PIECE
 
 
+@functools.lru_cache(maxsize=4096)
+def _product4_bytes(M: int, N: int, K: int) -> int:   # (a call of its own, once per shape: a microsecond on the host)
+    return int(lib().gcn_rows4_product_workspace_bytes(M, N, K))
+
+
 class Rows4:
     """n x f values in 4 bits: `values` (uint8, n x 128 ceil(f / 256), two
     values a byte, the first in the low bits, zeros past f) and `scale` (uint8,
@@ -830,28 +836,31 @@ def gcn_rows4_pack(X: torch.Tensor, ws: Workspace, out: Optional[Rows4] = None, 
     Z, with Z = X where mask is positive and zero elsewhere, or X without one."""
     t = _rows_type(X, "X")
     ldx = _ld(X)
-    n, f = int(X.shape[0]), int(X.shape[1])
-    if out is not None and (out.n, out.f) != (n, f):
+    n, f = X.shape
+    if out is not None and (out.n != n or out.f != f):
         raise ValueError("X and out differ in shape")
-    if out_t is not None and (out_t.n, out_t.f) != (f, n):
+    if out_t is not None and (out_t.n != f or out_t.f != n):
         raise ValueError("out_t must be f x n")
-    if mask is not None:
-        _want(mask, "mask", X.dtype, (n, f))
-    w = wb = None
+    w, wb, buf = None, 0, None
     if colsum is not None:
         _want(colsum, "colsum", torch.float32, (f,))
         if not colsum.is_contiguous():
             raise ValueError("colsum must be contiguous")
-        w, wb = ws.args(lib().gcn_rows4_pack_workspace_bytes(n, f))
+        buf = ws.get(lib().gcn_rows4_pack_workspace_bytes(n, f))
+        w, wb = buf.data_ptr(), buf.numel()
+    m, ldm = None, 0
+    if mask is not None:
+        _want(mask, "mask", X.dtype, (n, f))
+        m, ldm = mask.data_ptr(), _ld(mask)
     _launch("gcn_rows4_pack",
-            _one_device(X, mask, None if out is None else out.values, None if out_t is None else out_t.values, colsum,
-                        None if w is None else ws.buf), stream, X.data_ptr(), t, n, f, ldx, _ptr(mask),
-            0 if mask is None else _ld(mask), None if out is None else out.ref, None if out_t is None else out_t.ref,
-            _ptr(colsum), w, wb or 0)
+            _one_device(X, None if out is None else out.values, None if out_t is None else out_t.values, mask, colsum, buf),
+            stream, X.data_ptr(), t, n, f, ldx, m, ldm, None if out is None else out.ref,
+            None if out_t is None else out_t.ref, None if colsum is None else colsum.data_ptr(), w, wb)
 
 
 def gcn_rows4_unpack(rows: Rows4, out: torch.Tensor, stream=None) -> torch.Tensor:
-    if tuple(out.shape) != (rows.n, rows.f):
+    n, f = out.shape
+    if n != rows.n or f != rows.f:
         raise ValueError("out and the 4-bit rows differ in shape")
     _launch("gcn_rows4_unpack", _one_device(out, rows.values), stream, rows.ref, out.data_ptr(), _rows_type(out, "out"),
             _ld(out))
@@ -861,15 +870,18 @@ def gcn_rows4_unpack(rows: Rows4, out: torch.Tensor, stream=None) -> torch.Tenso
 def gcn_rows4_product(A4: Rows4, B4: Rows4, Y: torch.Tensor, ws: Workspace, bias: Optional[torch.Tensor] = None,
                       relu: bool = False, stream=None) -> torch.Tensor:
     """Y [A4.n x B4.n] = act(A4 B4^T + bias)."""
-    if tuple(Y.shape) != (A4.n, B4.n):
+    M, N = Y.shape
+    if M != A4.n or N != B4.n:
         raise ValueError("Y's shape does not fit the operands")
+    b = None
     if bias is not None:
         _dev_f32(bias, "bias")
-        if bias.numel() != B4.n or not bias.is_contiguous():
+        if bias.numel() != N or not bias.is_contiguous():
             raise ValueError("bias needs one contiguous element per column of Y")
-    w, wb = ws.args(lib().gcn_rows4_product_workspace_bytes(A4.n, B4.n, A4.f))
-    _launch("gcn_rows4_product", _one_device(Y, A4.values, B4.values, bias, ws.buf), stream, A4.ref, B4.ref, _ptr(bias),
-            int(bool(relu)), Y.data_ptr(), _rows_type(Y, "Y"), _ld(Y), w, wb)
+        b = bias.data_ptr()
+    buf = ws.get(_product4_bytes(M, N, A4.f))
+    _launch("gcn_rows4_product", _one_device(Y, A4.values, B4.values, bias, buf), stream, A4.ref, B4.ref, b, 1 if relu else 0,
+            Y.data_ptr(), _rows_type(Y, "Y"), _ld(Y), buf.data_ptr(), buf.numel())
     return Y
 
 
@@ -919,9 +931,9 @@ def gcn_orthogonalise(X: torch.Tensor, out: torch.Tensor, ws: Workspace, steps: 
     t = _rows_type(X, "X")
     _want(out, "out", X.dtype, X.shape)
     rows, cols = int(X.shape[0]), int(X.shape[1])
-    w, wb = ws.args(lib().gcn_orthogonalise_workspace_bytes(rows, cols, prec))
-    _launch("gcn_orthogonalise", _one_device(X, out, ws.buf), stream, X.data_ptr(), t, rows, cols, _ld(X),
-            out.data_ptr(), _ld(out), int(steps), prec, w, wb)
+    buf = ws.get(lib().gcn_orthogonalise_workspace_bytes(rows, cols, prec))
+    _launch("gcn_orthogonalise", _one_device(X, out, buf), stream, X.data_ptr(), t, rows, cols, _ld(X),
+            out.data_ptr(), _ld(out), int(steps), prec, buf.data_ptr(), buf.numel())
     return out
 
 
@@ -962,11 +974,12 @@ class MuonStep:
         return int(lib().gcn_muon_workspace_bytes(self.count, self.arr, self.prec))
 
     def __call__(self, lr: float, ws: Workspace, stream=None):
-        w, wb = ws.args(self.workspace_bytes())
-        if ws.buf.get_device() != self.device:
+        buf = ws.get(self.workspace_bytes())
+        if buf.get_device() != self.device:
             raise ValueError("all tensors of a call must be on one device")
         _launch("gcn_muon_update", self.device, stream, self.count, self.arr, self.type, float(lr), self.momentum,
-                int(self.nesterov), self.weight_decay, self.steps, self.prec, w, wb)
+                int(self.nesterov), self.weight_decay, self.steps, self.prec,
+                buf.data_ptr(), buf.numel())
 
 
 # ---------------------------------------------------------------- profiling
