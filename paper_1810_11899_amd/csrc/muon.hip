@@ -393,29 +393,31 @@ __device__ __forceinline__ void product_of(const Group &g, const Job &J, const u
 // which waits for its own copies, reads and products in turn.
 template <bool PAIR, int STAGE, int BM, int BN, int WM, int WN, int KG>
 __global__ __launch_bounds__(64 * WM *WN *KG) void muon_kernel(Group g, int odd) {
-    constexpr int TYPE = type_of<PAIR, STAGE>(), FM = BM / WM / 16, kOwn = FM * 4 / KG, T = 64 * WM * WN;
+    constexpr int TYPE = type_of<PAIR, STAGE>(), FM = BM / WM / 16, FN = BN / WN / 16, kBlocks = FM * FN, kOwn = kBlocks / KG,
+                  T = 64 * WM * WN;
     constexpr int kLds = small_lds(TYPE, BM, BN);
-    static_assert(KG == 1 || KG * FM * 4 * T * 16 <= KG * kLds, "the groups' sums fit where the operands were");
+    static_assert(KG == 1 || kBlocks * T * 16 <= kLds, "the groups' sums fit where the operands were");
     __shared__ __attribute__((aligned(16))) char lds[KG * kLds];
     GCN_MUON_TILE(BM, BN);
     const uint32_t tid = threadIdx.x % T;
     const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / T), lane = tid & 63, wave = tid >> 6;
     const int r0 = c.tm * BM + wave / WN * (BM / WM) + (lane & 15), c0 = c.tn * BN + wave % WN * (BN / WN) + 4 * (lane >> 4);
-    f32x4 old[kOwn];
-    if constexpr (kOwn <= 4) {   // (a few registers: ahead of the loop)
+    constexpr bool kAhead = kOwn <= 4;   // (a few registers)
+    f32x4 old[kAhead ? kOwn : 1];
+    if constexpr (kAhead) {
 #pragma unroll
         for (int u = 0; u < kOwn; ++u) {
             const int b = u * KG + group;
-            old[u] = old_at<PAIR, STAGE>(J, X, r0 + 16 * (b / 4), c0 + 16 * (b % 4));
+            old[u] = old_at<PAIR, STAGE>(J, X, r0 + 16 * (b / FN), c0 + 16 * (b % FN));
         }
     }
-    f32x4 acc[FM][4];
+    f32x4 acc[FM][FN];
     const int per = (p.kt + KG - 1) / KG, k0 = min(group * per, p.kt);
     small_loop<TYPE, BM, BN, WM, WN>(p, c, k0, min(per, p.kt - k0), lds + group * kLds, acc, tid, per);
     if constexpr (KG > 1) {
         f32x4 *const part = (f32x4 *)lds;   // [block][group][thread]
 #pragma unroll
-        for (int b = 0; b < FM * 4; ++b) part[(b * KG + group) * T + tid] = acc[b / 4][b % 4];
+        for (int b = 0; b < kBlocks; ++b) part[(b * KG + group) * T + tid] = acc[b / FN][b % FN];
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < kOwn; ++u) {
@@ -423,14 +425,15 @@ __global__ __launch_bounds__(64 * WM *WN *KG) void muon_kernel(Group g, int odd)
             f32x4 v = part[b * KG * T + tid];
 #pragma unroll
             for (int q = 1; q < KG; ++q) v += part[(b * KG + q) * T + tid];
-            finish<PAIR, STAGE>(g, J, next, r0 + 16 * (b / 4), c0 + 16 * (b % 4), mirror, old[u], v);
+            finish<PAIR, STAGE>(g, J, next, r0 + 16 * (b / FN), c0 + 16 * (b % FN), mirror,
+                                kAhead ? old[kAhead ? u : 0] : old_at<PAIR, STAGE>(J, X, r0 + 16 * (b / FN), c0 + 16 * (b % FN)), v);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const f32x4 o = kOwn <= 4 ? old[kOwn <= 4 ? i * 4 + j : 0] : old_at<PAIR, STAGE>(J, X, r0 + 16 * i, c0 + 16 * j);
+            for (int j = 0; j < FN; ++j) {
+                const f32x4 o = kAhead ? old[kAhead ? i * FN + j : 0] : old_at<PAIR, STAGE>(J, X, r0 + 16 * i, c0 + 16 * j);
                 finish<PAIR, STAGE>(g, J, next, r0 + 16 * i, c0 + 16 * j, mirror, o, acc[i][j]);
             }
     }
@@ -701,6 +704,7 @@ int product(Group &g, int odd, hipStream_t s) {
     } else if constexpr (STAGE <= POLY) {
         if (all(128, 128) >= 256) GCN_MUON(128, 128, 2, 2, 1);
         else if (all(64, 64) > 256) GCN_MUON(64, 64, 4, 1, 1);
+        else if (all(32, 32) <= 320) GCN_MUON(32, 32, 1, 1, 4);
         else GCN_MUON(64, 64, 4, 1, 4);
     } else {
         if (all(128, 128) >= 192) GCN_MUON(128, 128, 2, 2, 1);

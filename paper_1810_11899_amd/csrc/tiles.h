@@ -296,7 +296,11 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
     if constexpr (SCALED) {
         if (nt > 0) scales(0);
     }
+    // both stages at once: the second piece's copy would wait for the first's otherwise
+    // (8-bit scales pass through registers behind the first copy)
+    constexpr bool kBoth = !SCALED;
     if (nt > 0) copy(0, 0);
+    if (kBoth && nt > 1) copy(1, 1);
     for (int t = 0; t < nt; ++t) {
         if constexpr (SCALED) {
             if (t % kScalePieces == 0 && t) {
@@ -305,10 +309,16 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
             }
             wait_reads();   // the scales' LDS writes, ahead of the barrier
         }
-        wait_copies<0>();   // piece t has landed
+        // piece t has landed
+        if (kBoth && t == 0 && nt > 1) {
+            if (TYPE == TILE_FP4 && wave * 64 < (BM + BN) / 2) wait_copies<LA + LB + 1>();
+            else wait_copies<LA + LB>();
+        } else {
+            wait_copies<0>();
+        }
         turn();
         // (every wavefront has used what it read of piece t - 1: its stage is free)
-        if (t + 1 < nt) copy(t + 1, (t + 1) & 1);
+        if ((t || !kBoth) && t + 1 < nt) copy(t + 1, (t + 1) & 1);
         const char *ta = lds + (t & 1) * kStage, *tb = ta + BM * kPiece;
         int sa[FM], sb = 0;
         if constexpr (SCALED) {
