@@ -685,8 +685,10 @@ int product(Group &g, int odd, hipStream_t s) {
         flops += STAGE == GRAM ? m * m * n : STAGE == POLY ? m * m * m : 2.0 * m * m * n;
     }
     ProfScope prof(K_MUON_PRODUCT, s, flops, 0.0);
+    // Half of A's and B's tiles where all 32 x 32 ones would be more than a round (their
+    // transposed stores cost about half a microsecond otherwise).
     g.full = 1;
-    if (STAGE <= POLY && all(64, 64) > 128) g.full = 0;
+    if (STAGE <= POLY && all(32, 32) > 256) g.full = 0;
     auto grid = [&](int32_t tm, int32_t tn) {
         const uint32_t total = blocks_of(g, [&](const Job &J) { return (uint64_t)count(J, tm, tn); });
         g.per_xcd = (total + 7) / 8;
@@ -698,18 +700,32 @@ int product(Group &g, int odd, hipStream_t s) {
         const dim3 b = grid(BM, BN);                                                                             \
         hipLaunchKernelGGL((muon_kernel<PAIR, STAGE, BM, BN, WM, WN, KG>), b, dim3(64 * WM * WN * KG), 0, s, g, odd); \
     } while (0)
-    if (deep && all(kBigT, kBigT) >= (STAGE <= POLY ? 120 : 160)) {
+    // us a call of five steps, the two ways on either side of each border.  Large tiles for a X + B X: 3000 x 3200
+    // (156 of them) 2185 with 128 x 128 ones, 2121 with large; for A and B 3000 x 3200 (78) 2185 and 2850, 3400 x
+    // 3400 in GCN_BF16 (105) 1099 and 1386.
+    if (deep && all(kBigT, kBigT) >= (STAGE <= POLY ? 120 : 150)) {
         const dim3 b = grid(kBigT, kBigT);
         hipLaunchKernelGGL((muon_big_kernel<PAIR, STAGE>), b, dim3(kBigThreads), 0, s, g, odd);
     } else if constexpr (STAGE <= POLY) {
-        if (all(128, 128) >= 256) GCN_MUON(128, 128, 2, 2, 1);
-        else if (all(64, 64) > 256) GCN_MUON(64, 64, 4, 1, 1);
-        else if (all(32, 32) <= 320) GCN_MUON(32, 32, 1, 1, 4);
-        else GCN_MUON(64, 64, 4, 1, 4);
+        // 32 x 32 tiles while they are few: a CU's own path to its L2 carries 64 bytes a cycle, and few tiles leave
+        // most of the CUs, and their paths, idle (four of 602 x 128 and 256 x 128: 118 with 64 x 64 ones, 93 so; 700 x
+        // 700, 253 of them, 176 and 148; 1024 x 1024, 528, 227 and 234).  64 x 64 in two parts a CU: 1500 x 1500
+        // (300) 487 unsplit, 429 so; unsplit 2000 x 2500 (528) 850, 895 in 128 x 128 ones of two parts; those 2500 x
+        // 2500 (820 or 210) 1267 and 1108.
+        if (all(128, 128) > 256) GCN_MUON(128, 128, 2, 2, 1);
+        else if (all(64, 64) > 640) GCN_MUON(128, 128, 2, 2, 2);
+        else if (all(64, 64) > 512) GCN_MUON(64, 64, 4, 1, 1);
+        else if (all(64, 64) > 256) GCN_MUON(64, 64, 4, 1, 2);
+        else if (all(32, 32) > 400) GCN_MUON(64, 64, 4, 1, 4);
+        else GCN_MUON(32, 32, 1, 1, 4);
     } else {
-        if (all(128, 128) >= 192) GCN_MUON(128, 128, 2, 2, 1);
-        else if (all(32, 128) > 256) GCN_MUON(64, 128, 2, 2, 2);
-        else GCN_MUON(32, 128, 2, 2, 4);
+        // The smallest tiles that one round of a workgroup a CU holds: 512 x 512 and 1024 x 512, two each (416 of 32
+        // rows, 208 of 64) 230 and 206; 1500 x 1500 (288 of 64, 144 of 128) 560 and 487; 1024 x 2048 (256 of 64, 128)
+        // 287 and 321; 2000 x 2500 in GCN_BF16 (320 of 128) in two parts 508, unsplit 454.
+        if (all(32, 128) <= 256) GCN_MUON(32, 128, 2, 2, 4);
+        else if (all(64, 128) <= 256) GCN_MUON(64, 128, 2, 2, 2);
+        else if (all(128, 128) <= 256) GCN_MUON(128, 128, 2, 2, 2);
+        else GCN_MUON(128, 128, 2, 2, 1);
     }
 #undef GCN_MUON
     GCN_LAUNCH_CHECK("muon_kernel");

@@ -110,7 +110,8 @@ def test_spectra_that_fall(rows, cols, kind, ws):
     assert rel2(out.cpu().numpy(), want) <= 2.0 ** -8
 
 
-@pytest.mark.parametrize("rows, cols", [(1024, 1100), (2300, 1030), (4096, 2816)])
+@pytest.mark.parametrize("rows, cols", [(700, 700), (1024, 1100), (1500, 1500), (2300, 1030), (2050, 2300), (2500, 2500),
+                                        (3000, 3300), (4096, 2816), (300, 9000), (4096, 4100)])
 @pytest.mark.parametrize("prec", [B.GCN_F32, B.GCN_BF16])
 def test_large_sides(rows, cols, prec, ws):
     """The other tile shapes, against the iteration in float64 on the GPU."""
