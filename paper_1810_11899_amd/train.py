@@ -56,7 +56,10 @@ class FlatModel:
     the products take 16-byte loads (a width such as 602 is not a multiple of
     four floats)."""
 
-    def __init__(self, dims: List[Tuple[int, int]], classes: int, device, seed: int = 0):
+    def __init__(self, dims: List[Tuple[int, int]], classes: int, device, seed: int = 0, matrices_first: bool = False):
+        """matrices_first: the layers' weight matrices ahead of the biases and the prediction layer, which then
+        are the last `total - tail` elements of the buffers (an optimiser of matrices for the former, one call of
+        an elementwise optimiser for the latter)."""
         self.dims = list(dims)
         self.classes = classes
         self.f0 = dims[0][0]
@@ -66,10 +69,16 @@ class FlatModel:
             shapes += [(fs, h), (fs, h), (2 * h,)]
         shapes += [(2 * dims[-1][1], classes), (classes,)]
         self.shapes = shapes
-        offs, o = [], 0
-        for sh in shapes:
-            offs.append(o)
-            o += (int(np.prod(sh)) + 63) // 64 * 64     # 256-byte aligned views
+        self.matrices = [i for i in range(3 * len(dims)) if i % 3 < 2]
+        order = list(range(len(shapes)))
+        if matrices_first:
+            order = self.matrices + [i for i in order if i not in self.matrices]
+        offs, o, self.tail = [0] * len(shapes), 0, 0
+        for k, i in enumerate(order):
+            if k == len(self.matrices):
+                self.tail = o
+            offs[i] = o
+            o += (int(np.prod(shapes[i])) + 63) // 64 * 64     # 256-byte aligned views
         self.offsets, self.total = offs, o
         d = torch.device(device)
         self.params = torch.zeros(o, dtype=torch.float32, device=d)
@@ -99,6 +108,10 @@ class FlatModel:
         buf = self.params if buf is None else buf
         k = 3 * len(self.dims)
         return self._view(buf, k), self._view(buf, k + 1)
+
+    def matrix_views(self, buf):
+        """The layers' weight matrices in a buffer of this layout, the first layer's at their f_in rows."""
+        return [self._view(buf, i)[:self.f0] if i < 2 else self._view(buf, i) for i in self.matrices]
 
     def padding_rows(self):
         """The first layer's padding rows of W_self and W_neigh (host copies)."""
@@ -149,7 +162,13 @@ class Trainer:
     current stream."""
 
     def __init__(self, tg: "synth.TrainingGraph", dims: List[Tuple[int, int]], cfg: SamplerConfig,
-                 lr: float = 0.01, prec: int = B.GCN_F32, device: str = "cuda", model_seed: int = 0):
+                 lr: float = 0.01, prec: int = B.GCN_F32, device: str = "cuda", model_seed: int = 0,
+                 optimizer: str = "adam"):
+        """optimizer: "adam" for every tensor, or "muon": the layers' weight matrices move along the orthogonalised
+        momentum of their gradients (gcn_muon_update), in steps of about ADAM's size, the biases and the prediction
+        layer by ADAM."""
+        if optimizer not in ("adam", "muon"):
+            raise ValueError(f"optimizer must be 'adam' or 'muon', not {optimizer!r}")
         self.dev = torch.device(device)
         self.cfg = cfg
         self.prec = prec
@@ -165,7 +184,7 @@ class Trainer:
         self.labels_all = torch.from_numpy(tg.labels).to(self.dev)
         self.classes = tg.classes
         self.params = B.gcn_sampler_plan(g.indptr, cfg.m, cfg.n, eta=cfg.eta, cap=cfg.cap, seed=cfg.seed)
-        self.model = FlatModel(dims, tg.classes, self.dev, seed=model_seed)
+        self.model = FlatModel(dims, tg.classes, self.dev, seed=model_seed, matrices_first=optimizer == "muon")
         self.dims = list(dims)
         self.L = len(dims)
         self.orders = [B.gcn_layer_pick_order(f, h, li > 0) for li, (f, h) in enumerate(dims)]
@@ -208,6 +227,12 @@ class Trainer:
         self.fused = B.ModelStep(layers, dict(W_pred=Wp, b_pred=bp, kind=B.GCN_SOFTMAX_CE, labels=self.lab,
                                               targets=None, loss=self.losses[:1], dHL=self.dHL, dW_pred=dWp,
                                               db_pred=dbp), prec)
+        # what ADAM updates: all of the flat buffers, or the tail behind the matrices (whose momenta stand where its
+        # first moments would)
+        self.muon, self.adam = None, (mdl.params, mdl.grads, mdl.m, mdl.v)
+        if optimizer == "muon":
+            self.muon = B.MuonStep(mdl.matrix_views(mdl.params), mdl.matrix_views(mdl.grads), mdl.matrix_views(mdl.m))
+            self.adam = tuple(buf[mdl.tail:] for buf in self.adam)
         self.iteration = 0
         self.subgraph_ids: List[int] = []
         for p in self.pools:
@@ -303,7 +328,9 @@ class Trainer:
         self.fused.set_loss(self.losses[t:t + 1])
         self.fused(A, AT, self.H0, self.ws)
         mdl.step_count += 1
-        B.gcn_adam_update(mdl.params, mdl.grads, mdl.m, mdl.v, self.lr, mdl.step_count)
+        if self.muon is not None:
+            self.muon(self.lr, self.ws)
+        B.gcn_adam_update(*self.adam, self.lr, mdl.step_count)
         self.iteration += 1
         return ns, nnz
 
