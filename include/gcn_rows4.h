@@ -67,7 +67,9 @@ typedef struct {
  *     colsum [f] = sum_i Z[i, :] in float32, or NULL
  * at least one of the three given.  With dY and a layer's output as X and mask, Z
  * is dZ and colsum the bias gradient.  The outputs overlap neither X and mask nor
- * each other. */
+ * each other.  ws is used with colsum alone, and may be NULL without it.  Rows of
+ * no columns and columns of no rows take part in nothing: colsum of no rows is
+ * zeros. */
 size_t gcn_rows4_pack_workspace_bytes(int32_t n, int32_t f);
 int gcn_rows4_pack(const void *X, gcn_rows_type type, int32_t n, int32_t f, int32_t ldx, const void *mask,
                    int32_t ldmask, const gcn_rows4 *out, const gcn_rows4 *outT, float *colsum, void *ws,

@@ -250,18 +250,25 @@ __device__ __forceinline__ f32x4 old_at(const Job &J, const uint8_t *X, int row,
     return v;
 }
 
-// W <- decay W - step O, or out = O, for four consecutive columns of a row of O.
+// v of four consecutive columns of a row to four consecutive rows of a column: lane
+// 4 q + k of a row of 16 gives element e to lane 4 q + e and takes element k of
+// it.  In two exchanges, of single columns and of pairs.
+__device__ __forceinline__ f32x4 turned(f32x4 v) {
+    const bool odd = threadIdx.x & 1, up = threadIdx.x & 2;
+    const float a = __shfl_xor(odd ? v[0] : v[1], 1), b = __shfl_xor(odd ? v[2] : v[3], 1);
+    v = odd ? f32x4{a, v[1], b, v[3]} : f32x4{v[0], a, v[2], b};
+    const float c = __shfl_xor(up ? v[0] : v[2], 2), d = __shfl_xor(up ? v[1] : v[3], 2);
+    return up ? f32x4{c, d, v[2], v[3]} : f32x4{v[0], v[1], c, d};
+}
+
+// W <- decay W - step O, or out = O, for four consecutive columns of a row of O, a
+// wavefront's 16 x 16 at a time.
 __device__ __forceinline__ void apply(const Group &g, const Job &J, int row, int col, f32x4 o) {
     if (J.rows > J.cols) {   // O lies transposed
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (row >= J.cols || col + e >= J.rows) continue;
-            const int64_t at = (int64_t)(col + e) * J.ldw + row;
-            if (J.W) J.W[at] = g.decay * J.W[at] - J.step * o[e];
-            else if (g.out_bf16) ((uint16_t *)J.out)[at] = to_bf16(o[e]);
-            else ((float *)J.out)[at] = o[e];
-        }
-        return;
+        o = turned(o);
+        const int r = col + (row & 3);
+        col = row & ~3;
+        row = r;
     }
     if (row >= J.rows) return;
     const int64_t at = (int64_t)row * J.ldw + col;
@@ -284,17 +291,6 @@ __device__ __forceinline__ void apply(const Group &g, const Job &J, int row, int
         else if (g.out_bf16) ((uint16_t *)J.out)[at + e] = to_bf16(o[e]);
         else ((float *)J.out)[at + e] = o[e];
     }
-}
-
-// v of four consecutive columns of a row to four consecutive rows of a column: lane
-// 4 q + k of a row of 16 gives element e to lane 4 q + e and takes element k of
-// it.  In two exchanges, of single columns and of pairs.
-__device__ __forceinline__ f32x4 turned(f32x4 v) {
-    const bool odd = threadIdx.x & 1, up = threadIdx.x & 2;
-    const float a = __shfl_xor(odd ? v[0] : v[1], 1), b = __shfl_xor(odd ? v[2] : v[3], 1);
-    v = odd ? f32x4{a, v[1], b, v[3]} : f32x4{v[0], a, v[2], b};
-    const float c = __shfl_xor(up ? v[0] : v[2], 2), d = __shfl_xor(up ? v[1] : v[3], 2);
-    return up ? f32x4{c, d, v[2], v[3]} : f32x4{v[0], v[1], c, d};
 }
 
 // Four sums to what the product forms.  mirror: of a tile below the diagonal of A or

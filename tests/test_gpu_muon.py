@@ -285,3 +285,20 @@ def test_captured_update(ws):
         torch.cuda.synchronize()
         for (W, _, M, *_), (w, _, m) in zip(ts, eager):
             assert torch.equal(W, w) and torch.equal(M, m)
+
+
+def test_another_stream(ws):
+    """The calls follow the current stream: both ways of working, with their own workspaces at the same time."""
+    a, b = to_dev(gradient(gen(20), 300, 200)), to_dev(gradient(gen(21), 60, 90))
+    want = [B.gcn_orthogonalise(x, torch.empty_like(x), ws) for x in (a, b)]
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [torch.empty_like(x) for x in (a, b)]
+    spaces = [B.Workspace() for _ in range(2)]
+    for w in spaces:
+        w.get(1 << 24)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, w, x, o in zip(streams, spaces, (a, b), got):
+            with torch.cuda.stream(s):
+                B.gcn_orthogonalise(x, o, w)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))

@@ -281,3 +281,84 @@ def test_products_are_the_layers_gradients(ws):
         dn[k, j] -= h
         diff = ((V(x) @ up) * V(z)).sum() - ((V(x) @ dn) * V(z)).sum()
         assert abs(diff / (2 * h) - V(x)[:, k] @ V(z)[:, j]) < 1e-9
+
+
+def test_another_stream_and_a_captured_graph():
+    """The calls follow the current stream, and replay from a graph with eager work between the replays."""
+    g = gen(9)
+    x, w, dy = (to_dev(g.normal(size=s)) for s in ((300, 200), (150, 200), (300, 9000)))
+    ws = B.Workspace()
+
+    def run(ws):
+        X4, W4, D4T = B.Rows4(300, 200), B.Rows4(150, 200), B.Rows4(9000, 300)
+        X4T, Y, dW, cs = B.Rows4(200, 300), torch.empty((300, 150), device="cuda"), None, torch.empty(9000, device="cuda")
+        B.gcn_rows4_pack(x, ws, out=X4, out_t=X4T)
+        B.gcn_rows4_pack(w, ws, out=W4)
+        B.gcn_rows4_pack(dy, ws, out_t=D4T, mask=dy, colsum=cs)
+        B.gcn_rows4_product(X4, W4, Y, ws, relu=True)
+        L4, M4 = B.Rows4(200, 9000), B.Rows4(120, 9000)      # a long sum in parts
+        B.gcn_rows4_pack(dy[:200], ws, out=L4)
+        B.gcn_rows4_pack(dy[100:220], ws, out=M4)
+        dW = torch.empty((200, 120), device="cuda")
+        B.gcn_rows4_product(L4, M4, dW, ws)
+        v = torch.empty((9000, 300), device="cuda", dtype=torch.bfloat16)
+        B.gcn_rows4_unpack(D4T, v)
+        return Y, cs, dW, v
+
+    want = [t.clone() for t in run(ws)]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = run(B.Workspace())
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    ws2 = B.Workspace()
+    ws2.get(1 << 24)
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        got = run(ws2)
+    for _ in range(4):
+        for t in got:
+            t.zero_()
+        graph.replay()
+        eager = run(ws)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) and torch.equal(a, e) for a, b, e in zip(got, want, eager))
+
+
+def test_rows_past_32_bit_offsets(ws):
+    """More than 2^31 elements, in both orientations: the last rows as packed alone, and a sum over all of them."""
+    n, f, tail = 2_100_032, 1056, 320                         # (n - tail a multiple of 64: whole groups and blocks)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    X = torch.empty((n, f), dtype=torch.bfloat16, device="cuda")
+    part = torch.randn((4096, f), generator=g, device="cuda")
+    for i in range(0, n, 4096):
+        m = min(4096, n - i)
+        X[i:i + m] = part[:m] * 2.0 ** (i // 4096 % 7 - 3)
+    out, out_t = B.Rows4(n, f), B.Rows4(f, n)
+    B.gcn_rows4_pack(X, ws, out=out, out_t=out_t)
+    last, last_t = B.Rows4(tail, f), B.Rows4(f, tail)
+    B.gcn_rows4_pack(X[n - tail:], ws, out=last, out_t=last_t)
+    assert torch.equal(out.values[n - tail:], last.values)
+    assert torch.equal(out.scale[:, (n - tail) // 64:], last.scale)
+    assert torch.equal(out_t.values[:, (n - tail) // 2:n // 2], last_t.values[:, :tail // 2])
+    v, w = torch.empty((n, f), dtype=torch.bfloat16, device="cuda"), torch.empty((tail, f), device="cuda")
+    B.gcn_rows4_unpack(out, v)
+    B.gcn_rows4_unpack(last, w)
+    assert torch.equal(v[n - tail:].float(), w)
+    # X^T X over all rows is the sum of two parts' (whole pieces of 256 each)
+    del v
+    half = n // 512 * 256
+    Y = torch.empty((f, f), device="cuda")
+    B.gcn_rows4_product(out_t, out_t, Y, ws)
+    sums = torch.zeros((f, f), dtype=torch.float64, device="cuda")
+    for a, b in ((0, half), (half, n)):
+        p = B.Rows4.of(out_t.values[:, a // 2:], out_t.scale[a // 256:-(-b // 256)], b - a) if b == n else \
+            B.Rows4.of(out_t.values[:, a // 2:b // 2], out_t.scale[a // 256:b // 256], b - a)
+        y = torch.empty((f, f), device="cuda")
+        B.gcn_rows4_product(p, p, y, ws)
+        sums += y.double()
+    # each is a float32 sum: within sqrt(K / 128) half steps of its size in the 2-norm, and all three far below this
+    assert float((Y.double() - sums).norm() / sums.norm()) < 128 * 2.0 ** -24
