@@ -389,7 +389,7 @@ __device__ __forceinline__ void product_of(const Group &g, const Job &J, const u
 // which waits for its own copies, reads and products in turn.
 template <bool PAIR, int STAGE, int BM, int BN, int WM, int WN, int KG>
 __global__ __launch_bounds__(64 * WM *WN *KG) void muon_kernel(Group g, int odd) {
-    constexpr int TYPE = type_of<PAIR, STAGE>(), FM = BM / WM / 16, FN = BN / WN / 16, kBlocks = FM * FN, kOwn = kBlocks / KG,
+    constexpr int TYPE = type_of<PAIR, STAGE>(), FM = BM / WM / 16, FN = BN / WN / 16, kBlocks = FM * FN, kOwn = kBlocks < KG ? 1 : kBlocks / KG,
                   T = 64 * WM * WN;
     constexpr int kLds = small_lds(TYPE, BM, BN);
     static_assert(KG == 1 || kBlocks * T * 16 <= kLds, "the groups' sums fit where the operands were");
@@ -418,6 +418,7 @@ __global__ __launch_bounds__(64 * WM *WN *KG) void muon_kernel(Group g, int odd)
 #pragma unroll
         for (int u = 0; u < kOwn; ++u) {
             const int b = u * KG + group;
+            if (kBlocks < KG && b >= kBlocks) break;   // (more parts than blocks: a wavefront has none)
             f32x4 v = part[b * KG * T + tid];
 #pragma unroll
             for (int q = 1; q < KG; ++q) v += part[(b * KG + q) * T + tid];
@@ -673,9 +674,10 @@ int product(Group &g, int odd, hipStream_t s) {
         return n;
     };
     double flops = 0.0;
-    bool deep = true;
+    bool deep = true, long_k = false;
     for (int j = 0; j < g.count; ++j) {
         const Job &J = g.job[j];
+        long_k = long_k || J.np >= 16 * (PAIR ? 32 : 64);
         deep = deep && J.mp >= 256 && J.np < (1 << 22);   // (a large tile's row offsets within it: 32 bits)
         const double m = std::min(J.rows, J.cols), n = std::max(J.rows, J.cols);
         flops += STAGE == GRAM ? m * m * n : STAGE == POLY ? m * m * m : 2.0 * m * m * n;
@@ -713,6 +715,7 @@ int product(Group &g, int odd, hipStream_t s) {
         else if (all(64, 64) > 512) GCN_MUON(64, 64, 4, 1, 1);
         else if (all(64, 64) > 256) GCN_MUON(64, 64, 4, 1, 2);
         else if (all(32, 32) > 400) GCN_MUON(64, 64, 4, 1, 4);
+        else if (STAGE == GRAM && all(32, 32) <= 256 && long_k) GCN_MUON(32, 32, 1, 1, 8);
         else GCN_MUON(32, 32, 1, 1, 4);
     } else {
         // The smallest tiles that one round of a workgroup a CU holds: 512 x 512 and 1024 x 512, two each (416 of 32
