@@ -59,6 +59,7 @@ struct alignas(64) Job {
     float *M;                // momentum, or null
     int64_t ldg, ldm;
     double *part;            // sums of squares
+    int32_t slab;            // columns of X a workgroup where there are few rows, else 0
 };
 // A launch's arguments.  The chain of loads from its number to a block's operands is a
 // good part of a small launch: the table of first blocks is one line, read
@@ -522,23 +523,41 @@ __device__ __forceinline__ void block_of(const Resident &P, int pieces, int i0, 
         }
     }
 }
-// A = X X^T, then B in A's place; every wavefront calls it
+// The wavefront's block of an mp x mp matrix, if it has one: rows i0 .., columns j0 ...
 template <int TS>
-__device__ __forceinline__ void gram_and_poly(const Resident &X, const Resident &A, int mp, int np, int lane, int wave) {
-    const int across = mp / (16 * TS), i0 = wave / across * 16 * TS, j0 = wave % across * 16 * TS;
-    const bool mine = wave < across * across;
-    f32x4 acc[TS][TS];
-    const int r0 = i0 + (lane & 15), c0 = j0 + 4 * (lane >> 4);
-    if (mine) {
-        block_of<TS>(X, np / 32, i0, j0, lane, acc);
+struct Block {
+    int i0, j0;
+    bool mine;
+    __device__ __forceinline__ Block(int mp, int wave) {
+        const int across = mp / (16 * TS);
+        i0 = wave / across * 16 * TS;
+        j0 = wave % across * 16 * TS;
+        mine = wave < across * across;
+    }
+};
+// A = X X^T; every wavefront calls it
+template <int TS>
+__device__ __forceinline__ void gram(const Resident &X, const Resident &A, int mp, int np, int lane, int wave) {
+    const Block<TS> b(mp, wave);
+    if (b.mine) {
+        f32x4 acc[TS][TS];
+        block_of<TS>(X, np / 32, b.i0, b.j0, lane, acc);
 #pragma unroll
         for (int i = 0; i < TS; ++i)
 #pragma unroll
-            for (int j = 0; j < TS; ++j) A.put(r0 + 16 * i, c0 + 16 * j, acc[i][j] * two_to(kABits - 2 * kXBits));
+            for (int j = 0; j < TS; ++j)
+                A.put(b.i0 + 16 * i + (lane & 15), b.j0 + 16 * j + 4 * (lane >> 4), acc[i][j] * two_to(kABits - 2 * kXBits));
     }
     __syncthreads();
-    if (mine) {
-        block_of<TS>(A, mp / 32, i0, j0, lane, acc);
+}
+// B in A's place; every wavefront calls it
+template <int TS>
+__device__ __forceinline__ void poly(const Resident &A, int mp, int lane, int wave) {
+    const Block<TS> b(mp, wave);
+    const int r0 = b.i0 + (lane & 15), c0 = b.j0 + 4 * (lane >> 4);
+    f32x4 acc[TS][TS];
+    if (b.mine) {
+        block_of<TS>(A, mp / 32, b.i0, b.j0, lane, acc);
 #pragma unroll
         for (int i = 0; i < TS; ++i)
 #pragma unroll
@@ -547,13 +566,55 @@ __device__ __forceinline__ void gram_and_poly(const Resident &X, const Resident 
                             A.four(r0 + 16 * i, c0 + 16 * j) * (kCoefB * two_to(kBBits - kABits));
     }
     __syncthreads();   // A is read
-    if (mine) {
+    if (b.mine) {
 #pragma unroll
         for (int i = 0; i < TS; ++i)
 #pragma unroll
             for (int j = 0; j < TS; ++j) A.put(r0 + 16 * i, c0 + 16 * j, acc[i][j]);
     }
     __syncthreads();
+}
+// X <- a X + B X in place, or, behind the last step, the update of W; column 0 of X
+// here is column `first` of the matrix's.  Every wavefront calls it.
+__device__ __forceinline__ void move_columns(const Group &g, const Job &J, const Resident &X, const Resident &B, int mp, int np,
+                                             int first, bool last, int lane, int wave) {
+    for (int c0 = 16 * wave; c0 < np; c0 += 16 * (kSmallThreads / 64)) {
+        f32x4 acc[kSmallSide / 16];
+#pragma unroll
+        for (int i = 0; i < kSmallSide / 16; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+        for (int t = 0; t < mp / 32; ++t) {
+            const Frag x = X.columns(t, c0, lane);
+#pragma unroll
+            for (int i = 0; i < kSmallSide / 16; ++i)
+                if (16 * i < mp) mma<TILE_PAIR>(acc[i], B.rows(16 * i, t, lane), x, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kSmallSide / 16; ++i) {
+            if (16 * i >= mp) break;
+            const int row = 16 * i + (lane & 15), col = c0 + 4 * (lane >> 4);
+            const f32x4 v = acc[i] * two_to(-kBBits) + X.four(row, col) * kCoefA;
+            if (last) apply(g, J, row, first + col, v * two_to(-kXBits));
+            else X.put(row, col, v);
+        }
+    }
+    __syncthreads();
+}
+// Zeros to X's pieces.
+__device__ __forceinline__ void clear(const Resident &X, int mp, int np) {
+    for (int i = threadIdx.x; i < mp * np / 4; i += kSmallThreads) *(uint4 *)(X.base + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+}
+// four elements of U times inv to their places in X, whose column 0 is `first`
+__device__ __forceinline__ void place_u(const Resident &X, const Job &J, int r, int c, int first, f32x4 u, double inv) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = (float)((double)u[e] * inv);
+    if (J.rows > J.cols) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < J.cols) X.put_one(c + e, r - first, u[e]);
+    } else {
+        X.put(r, c - first, u);
+    }
 }
 
 __global__ __launch_bounds__(kSmallThreads) void resident_kernel(Group g, int steps) {
@@ -570,53 +631,101 @@ __global__ __launch_bounds__(kSmallThreads) void resident_kernel(Group g, int st
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     double *const red = (double *)lds;   // (A's place)
     if (lane == 0) red[wave] = sum;
-    for (int i = threadIdx.x; i < mp * np / 4; i += kSmallThreads) *(uint4 *)(X.base + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+    clear(X, mp, np);
     __syncthreads();
     sum = 0.0;
 #pragma unroll
     for (int w = 0; w < kSmallThreads / 64; ++w) sum += red[w];
     const double inv = inverse_norm(sum);
-    const bool tall = J.rows > J.cols;
     for (uint32_t i = threadIdx.x; i < total; i += kSmallThreads) {
         const int r = (int)(i / per_row), c = 4 * (int)(i % per_row);
-        f32x4 u = four_of_u<false>(g, J, r, c);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) u[e] = (float)((double)u[e] * inv);
-        if (tall) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (c + e < J.cols) X.put_one(c + e, r, u[e]);
-        } else {
-            X.put(r, c, u);
-        }
+        place_u(X, J, r, c, 0, four_of_u<false>(g, J, r, c), inv);
     }
     __syncthreads();
     for (int k = 0; k < steps; ++k) {
-        if (mp > 64) gram_and_poly<2>(X, A, mp, np, lane, wave);
-        else gram_and_poly<1>(X, A, mp, np, lane, wave);
-        const bool last = k + 1 == steps;
-        for (int c0 = 16 * wave; c0 < np; c0 += 16 * (kSmallThreads / 64)) {
-            f32x4 acc[kSmallSide / 16];
+        if (mp > 64) {
+            gram<2>(X, A, mp, np, lane, wave);
+            poly<2>(A, mp, lane, wave);
+        } else {
+            gram<1>(X, A, mp, np, lane, wave);
+            poly<1>(A, mp, lane, wave);
+        }
+        move_columns(g, J, X, A, mp, np, 0, k + 1 == steps, lane, wave);
+    }
+}
+
+// Few rows and many columns: a workgroup has J.slab of X's columns for one step.  It adds
+// the workgroups' parts of A = X X^T from the step before, in order, forms B by
+// itself, moves its columns, and leaves its part of the next A: one launch a step
+// instead of three, and the sum over the columns in as many parts as there are
+// workgroups.  Its columns go through memory as they lie in LDS.  Parts alternate
+// between two places, since others may still read the old ones.  us, three launches a
+// step / one: 64 x 700 95 / 55, 64 x 2000 109 / 64, 30 x 4000 137 / 52, 16 x 8000 201 / 62,
+// 96 x 700 87 / 84, 96 x 2000 112 / 105, but 128 x 602 90 / 108: B and the part of A are
+// formed by one CU each.
+__global__ __launch_bounds__(kSmallThreads) void slab_kernel(Group g, int step, int steps) {
+    __shared__ __attribute__((aligned(16))) char lds[kSmallLds];
+    const int j = job_of(g, blockIdx.x);
+    const Job &J = g.job[j];
+    const int s = (int)(blockIdx.x - g.first[j]), slabs = (int)((j + 1 < g.count ? g.first[j + 1] : g.total) - g.first[j]);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mp = J.mp, np = J.slab;
+    const int first = s * np;
+    const Resident A{lds, 128 * mp}, X{lds + 4 * mp * mp, 128 * mp};
+    uint4 *const image = (uint4 *)(J.X0 + (int64_t)s * 4 * mp * np);
+    float *const parts = (float *)J.X1;   // [2][slabs][mp x mp]
+    if (step < 0) {
+        double sum = 0.0;
+        for (int i = threadIdx.x; i < J.parts; i += kSmallThreads) sum += J.part[i];
 #pragma unroll
-            for (int i = 0; i < kSmallSide / 16; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 1
-            for (int t = 0; t < mp / 32; ++t) {
-                const Frag x = X.columns(t, c0, lane);
+        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+        double *const red = (double *)lds;   // (A's place)
+        if (lane == 0) red[wave] = sum;
+        clear(X, mp, np);
+        __syncthreads();
+        sum = 0.0;
 #pragma unroll
-                for (int i = 0; i < kSmallSide / 16; ++i)
-                    if (16 * i < mp) mma<TILE_PAIR>(acc[i], A.rows(16 * i, t, lane), x, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < kSmallSide / 16; ++i) {
-                if (16 * i >= mp) break;
-                const int row = 16 * i + (lane & 15), col = c0 + 4 * (lane >> 4);
-                const f32x4 v = acc[i] * two_to(-kBBits) + X.four(row, col) * kCoefA;
-                if (last) apply(g, J, row, col, v * two_to(-kXBits));
-                else X.put(row, col, v);
-            }
+        for (int w = 0; w < kSmallThreads / 64; ++w) sum += red[w];
+        const double inv = inverse_norm(sum);
+        const bool tall = J.rows > J.cols;
+        const int r0 = tall ? first : 0, rows = tall ? min(np, J.rows - first) : J.rows;
+        const int c0 = tall ? 0 : first, fours = tall ? (J.cols + 3) / 4 : (min(np, J.cols - first) + 3) / 4;
+        for (int i = threadIdx.x; i < rows * fours; i += kSmallThreads) {
+            const int r = r0 + i / fours, c = c0 + 4 * (i % fours);
+            place_u(X, J, r, c, first, four_of_u<false>(g, J, r, c), inv);
+        }
+    } else {
+        for (int i = threadIdx.x; i < mp * np / 4; i += kSmallThreads) *(uint4 *)(X.base + i * 16) = image[i];
+        const f32x4 *const p = (const f32x4 *)(parts + (int64_t)(step & 1) * slabs * mp * mp);
+        for (int i = threadIdx.x; i < mp * mp / 4; i += kSmallThreads) {
+            f32x4 v = p[i];
+#pragma unroll 8
+            for (int w = 1; w < slabs; ++w) v += p[(int64_t)w * (mp * mp / 4) + i];
+            A.put(4 * i / mp, 4 * i % mp, v * two_to(kABits - 2 * kXBits));
         }
         __syncthreads();
+        if (mp > 64) poly<2>(A, mp, lane, wave);
+        else poly<1>(A, mp, lane, wave);
+        const bool last = step + 1 == steps;
+        move_columns(g, J, X, A, mp, np, first, last, lane, wave);
+        if (last) return;
     }
+    __syncthreads();
+    for (int i = threadIdx.x; i < mp * np / 4; i += kSmallThreads) image[i] = *(const uint4 *)(X.base + i * 16);
+    float *const mine = parts + ((int64_t)((step + 1) & 1) * slabs + s) * mp * mp;
+    auto leave = [&](auto ts) {
+        constexpr int TS = decltype(ts)::value;
+        const Block<TS> b(mp, wave);
+        if (!b.mine) return;
+        f32x4 acc[TS][TS];
+        block_of<TS>(X, np / 32, b.i0, b.j0, lane, acc);
+#pragma unroll
+        for (int i = 0; i < TS; ++i)
+#pragma unroll
+            for (int k = 0; k < TS; ++k)
+                *(f32x4 *)(mine + (b.i0 + 16 * i + (lane & 15)) * mp + b.j0 + 16 * k + 4 * (lane >> 4)) = acc[i][k];
+    };
+    if (mp > 64) leave(std::integral_constant<int, 2>{});
+    else leave(std::integral_constant<int, 1>{});
 }
 
 // Whether a matrix takes pairs.  GCN_BF16 does so too for matrices with a short side: a
@@ -630,13 +739,24 @@ bool takes_pairs(int32_t rows, int32_t cols, int prec) {
 bool aligned(const void *p, uintptr_t b) { return (uintptr_t)p % b == 0; }
 int32_t up(int32_t x, int32_t to) { return (x + to - 1) / to * to; }
 
+// Columns of a slab: the fewest of 128, 256 and 512 that make at most 16 of them (and fit in LDS).
+constexpr int32_t kSlabSide = 96;
+int32_t slab_of(int32_t mp, int32_t np) {
+    int32_t c = 128;
+    while (c < 512 && np > 16 * c && fits_lds(mp, 2 * c)) c *= 2;
+    return c;
+}
+
 // The job's places in the workspace.
 void plan_job(Job &J, bool pair, Arena &ar) {
     const int32_t unit = pair ? 32 : 64;
     J.mp = up(std::min(J.rows, J.cols), unit);
     J.np = up(std::max(J.rows, J.cols), unit);
-    J.X0 = ar.take<uint8_t>(4 * (size_t)J.mp * J.np);
-    J.X1 = ar.take<uint8_t>(4 * (size_t)J.mp * J.np);
+    // (few rows: X0 takes whole slabs, X1 their parts of A, twice)
+    J.slab = pair && J.mp <= kSlabSide ? slab_of(J.mp, J.np) : 0;
+    const size_t slabs = J.slab ? (size_t)(J.np + J.slab - 1) / J.slab : 0;
+    J.X0 = ar.take<uint8_t>(4 * (size_t)J.mp * std::max((size_t)J.np, slabs * J.slab));
+    J.X1 = ar.take<uint8_t>(4 * (size_t)J.mp * std::max((size_t)J.np, 2 * slabs * J.mp));
     J.A = ar.take<uint8_t>((pair ? 4 : 2) * (size_t)J.mp * J.mp);
     J.B = ar.take<uint8_t>((pair ? 4 : 2) * (size_t)J.mp * J.mp);
     const int64_t total = (int64_t)J.rows * J.cols;
@@ -733,12 +853,13 @@ int product(Group &g, int odd, hipStream_t s) {
 
 template <bool PAIR>
 int run_group(Group &g, int32_t steps, hipStream_t s) {
+    bool small = PAIR, few = PAIR;
+    double flops = 0.0;
     if constexpr (PAIR) {
-        bool small = true;
-        double flops = 0.0;
         for (int j = 0; j < g.count; ++j) {
             const Job &J = g.job[j];
             small = small && fits_lds(J.mp, J.np);
+            few = few && J.slab > 0;
             flops += (3.0 * J.np + J.mp) * J.mp * J.mp * steps;
         }
         if (small) {
@@ -748,14 +869,26 @@ int run_group(Group &g, int32_t steps, hipStream_t s) {
             return GCN_OK;
         }
     }
+    double bytes = 0.0;
+    for (int j = 0; j < g.count; ++j) bytes += 12.0 * g.job[j].rows * g.job[j].cols;
     {
-        double bytes = 0.0;
-        for (int j = 0; j < g.count; ++j) bytes += 12.0 * g.job[j].rows * g.job[j].cols;
         ProfScope prof(K_MUON_PREP, s, 0.0, bytes);
-        dim3 b(blocks_of(g, [](const Job &J) { return (uint64_t)J.parts; }));
+        const dim3 b(blocks_of(g, [](const Job &J) { return (uint64_t)J.parts; }));
         hipLaunchKernelGGL(momentum_kernel, b, dim3(kTB), 0, s, g);
         GCN_LAUNCH_CHECK("momentum_kernel");
-        b = dim3(blocks_of(g, [](const Job &J) { return (uint64_t)tiles(J.mp, J.np, 64, 64); }));
+    }
+    if (PAIR && few) {
+        const dim3 b(blocks_of(g, [](const Job &J) { return (uint64_t)(J.np + J.slab - 1) / J.slab; }));
+        for (int32_t k = -1; k < steps; ++k) {
+            ProfScope prof(K_MUON_SMALL, s, flops / steps, 0.0);
+            hipLaunchKernelGGL(slab_kernel, b, dim3(kSmallThreads), 0, s, g, (int)k, (int)steps);
+            GCN_LAUNCH_CHECK("slab_kernel");
+        }
+        return GCN_OK;
+    }
+    {
+        ProfScope prof(K_MUON_PREP, s, 0.0, bytes);
+        const dim3 b = dim3(blocks_of(g, [](const Job &J) { return (uint64_t)tiles(J.mp, J.np, 64, 64); }));
         hipLaunchKernelGGL(operand_kernel<PAIR>, b, dim3(kTB), 0, s, g);
         GCN_LAUNCH_CHECK("operand_kernel");
     }

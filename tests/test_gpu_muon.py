@@ -64,7 +64,7 @@ def gradient(g, rows, cols, n=500):
 
 
 SHAPES = [(1, 1), (1, 7), (7, 1), (2, 3), (31, 33), (33, 31), (50, 64), (64, 64), (65, 65), (602, 128), (128, 130), (300, 256),
-          (257, 1000), (1000, 40)]
+          (257, 1000), (1000, 40), (64, 2000), (2000, 33), (20, 2081), (1, 6000), (8200, 17)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
