@@ -15,10 +15,11 @@
  * more rows than columns the iteration runs on U^T.
  *
  * prec: GCN_F32 forms the products to float32's precision (float16 pairs on the
- * matrix cores).  GCN_BF16 rounds their operands to float16 but carries X
- * itself to float32's precision: results within 2^-8 in the 2-norm, whatever
- * the singular values, at a third of the matrix work.  (Matrices with a side
- * below 128 take GCN_F32's products in either.)
+ * matrix cores).  GCN_BF16 rounds their operands to float16, but carries X
+ * itself and the diagonals of A and B to float32's precision: results within
+ * about 2^-10 in the 2-norm, less than bfloat16's rounding, whatever the singular
+ * values, at a third of the matrix work.  (Matrices with a side below 128 take
+ * GCN_F32's products in either.)
  *
  * Conventions are those of gcn_layer.h (device pointers owned by the caller,
  * row-major leading dimensions, `stream` a hipStream_t as void*, a 256-byte

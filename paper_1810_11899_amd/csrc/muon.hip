@@ -16,10 +16,18 @@
 //   GCN_BF16  products of the high parts alone; X keeps its low part, for a X.
 //             A direction with a small singular value grows a-fold a step by a X
 //             alone, and a rounding of X would grow with it: so it is not rounded.
-// a X is added to the sums as its own term.  Put on B's diagonal it would be rounded
-// there to B's largest element, which small singular values feel: 8 of 512 directions
-// large, the error against float64 5.4e-5 instead of 2.2e-5 (float32 products
-// throughout: 2.0e-5).
+// The diagonals of A and B are the larger part of them (X's rows are nearly
+// orthogonal after the first steps), and a rounding there moves a whole row alike.
+// So they stay float32, in vectors e and d beside A' and B', which have zeros there:
+//     A = e + A'     A A = e^2 + (e_i + e_j) A' + A' A'     X' = (a + d) X + B' X
+// a apart from the products matters most where singular values are small: on B's
+// diagonal it would be rounded to B's largest element.  Error against float64 (2-norm;
+// float32 products throughout / pairs / pairs and diagonals; single products, the same):
+//     50 x 64        1.1e-6  1.3e-6  7.0e-7    2.1e-3  8.7e-4
+//     512 x 512      2.5e-6  1.6e-6  8.4e-7    1.5e-3  7.0e-4
+//     17 x 900       1.6e-6  2.0e-6  1.4e-6    2.8e-3  9.0e-4
+//     512 x 1024, 8 directions large
+//                    2.0e-5  2.2e-5  2.1e-5 (a on the diagonal: 5.4e-5)    3.3e-4  5.8e-4
 #include <algorithm>
 #include <cmath>
 #include <vector>
@@ -59,6 +67,7 @@ struct alignas(64) Job {
     float *M;                // momentum, or null
     int64_t ldg, ldm;
     double *part;            // sums of squares
+    float *e, *d;            // the diagonals of A and B
     int32_t slab;            // columns of X a workgroup where there are few rows, else 0
 };
 // A launch's arguments.  The chain of loads from its number to a block's operands is a
@@ -235,19 +244,49 @@ __global__ __launch_bounds__(kTB) void operand_kernel(Group g) {
 
 enum Stage { GRAM = 0, POLY = 1, NEXT = 2, LAST = 3 };
 
-// What a product's epilogue reads beside four sums: A's or X's elements at their place.
+// What a product's epilogue reads beside four sums: A's or X's elements at their
+// place, and A's diagonal at their row and columns or B's at their row.
+struct Old {
+    f32x4 v, cols;
+    float row;
+};
 template <bool PAIR, int STAGE>
-__device__ __forceinline__ f32x4 old_at(const Job &J, const uint8_t *X, int row, int col) {
-    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    if constexpr (STAGE == GRAM) return v;
+__device__ __forceinline__ Old old_at(const Job &J, const uint8_t *X, int row, int col) {
+    Old o{f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0.0f};
+    if constexpr (STAGE == GRAM) return o;
     const int32_t cols = STAGE == POLY ? J.mp : J.np;
     if (row < J.mp && col < cols) {
         const uint8_t *p = (STAGE == POLY ? J.A : X) + place<PAIR>(row, row_bytes<PAIR>(cols), col);
-        v = four_of(p);
+        o.v = four_of(p);
         // (A of the single products is its high parts alone)
-        if constexpr (PAIR) v += four_of(p + 64);
-        else if (STAGE != POLY) v += four_of(p + 2 * (int64_t)J.mp * J.np);
+        if constexpr (PAIR) o.v += four_of(p + 64);
+        else if (STAGE != POLY) o.v += four_of(p + 2 * (int64_t)J.mp * J.np);
+        o.row = (STAGE == POLY ? J.e : J.d)[row];
+        if constexpr (STAGE == POLY) o.cols = *(const f32x4 *)(J.e + col);
     }
+    return o;
+}
+// A's four elements at (row, col ..) from their sums, and B's from the sums of A' A';
+// those of the diagonal go to *diagonal and leave zero
+__device__ __forceinline__ f32x4 gram_of(f32x4 sum, int row, int col, float *diagonal) {
+    f32x4 v = sum * two_to(kABits - 2 * kXBits);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (row == col + k) {
+            *diagonal = sum[k] * two_to(-2 * kXBits);
+            v[k] = 0.0f;
+        }
+    return v;
+}
+__device__ __forceinline__ f32x4 poly_of(f32x4 sum, f32x4 a, float e_row, f32x4 e_cols, int row, int col, float *diagonal) {
+    f32x4 v = (sum * two_to(-kABits) + (e_cols + e_row) * a) * (kCoefC * two_to(kBBits - kABits)) +
+              a * (kCoefB * two_to(kBBits - kABits));
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (row == col + k) {
+            *diagonal = kCoefC * (sum[k] * two_to(-2 * kABits) + e_row * e_row) + kCoefB * e_row;
+            v[k] = 0.0f;
+        }
     return v;
 }
 
@@ -297,16 +336,18 @@ __device__ __forceinline__ void apply(const Group &g, const Job &J, int row, int
 // Four sums to what the product forms.  mirror: of a tile below the diagonal of A or
 // B, whose other half they are too.
 template <bool PAIR, int STAGE>
-__device__ __forceinline__ void finish(const Group &g, const Job &J, uint8_t *next, int row, int col, bool mirror, f32x4 old,
-                                       f32x4 v) {
+__device__ __forceinline__ void finish(const Group &g, const Job &J, uint8_t *next, int row, int col, bool mirror,
+                                       const Old &old, f32x4 v) {
     const int32_t cols = STAGE <= POLY ? J.mp : J.np;
     const int64_t bytes = row_bytes<PAIR>(cols);
     // (A and B of the single products are their high parts alone)
     const int64_t low = PAIR ? 64 : STAGE <= POLY ? 0 : 2 * (int64_t)J.mp * J.np;
     const bool in = row < J.mp && col < cols;
     if constexpr (STAGE <= POLY) {
-        if constexpr (STAGE == GRAM) v *= two_to(kABits - 2 * kXBits);
-        else v = v * (kCoefC * two_to(kBBits - 2 * kABits)) + old * (kCoefB * two_to(kBBits - kABits));
+        if (in) {
+            if constexpr (STAGE == GRAM) v = gram_of(v, row, col, J.e + row);
+            else v = poly_of(v, old.v, old.row, old.cols, row, col, J.d + row);
+        }
         uint8_t *const to = STAGE == GRAM ? J.A : J.B;
         if (in) store_parts(to + place<PAIR>(row, bytes, col), low, v);
         if (mirror) {   // (all lanes exchange; mp is a multiple of 32: a block of 16 x 16 is in or out)
@@ -315,7 +356,7 @@ __device__ __forceinline__ void finish(const Group &g, const Job &J, uint8_t *ne
         }
     } else {
         if (!in) return;
-        v = v * two_to(-kBBits) + old * kCoefA;
+        v = v * two_to(-kBBits) + old.v * (kCoefA + old.row);
         if constexpr (STAGE == NEXT) store_parts(next + place<PAIR>(row, bytes, col), low, v);
         else apply(g, J, row, col, v * two_to(-kXBits));
     }
@@ -400,7 +441,7 @@ __global__ __launch_bounds__(64 * WM *WN *KG) void muon_kernel(Group g, int odd)
     const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / T), lane = tid & 63, wave = tid >> 6;
     const int r0 = c.tm * BM + wave / WN * (BM / WM) + (lane & 15), c0 = c.tn * BN + wave % WN * (BN / WN) + 4 * (lane >> 4);
     constexpr bool kAhead = kOwn <= 4;   // (a few registers)
-    f32x4 old[kAhead ? kOwn : 1];
+    Old old[kAhead ? kOwn : 1];
     if constexpr (kAhead) {
 #pragma unroll
         for (int u = 0; u < kOwn; ++u) {
@@ -431,7 +472,7 @@ __global__ __launch_bounds__(64 * WM *WN *KG) void muon_kernel(Group g, int odd)
         for (int i = 0; i < FM; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                const f32x4 o = kAhead ? old[kAhead ? i * FN + j : 0] : old_at<PAIR, STAGE>(J, X, r0 + 16 * i, c0 + 16 * j);
+                const Old o = kAhead ? old[kAhead ? i * FN + j : 0] : old_at<PAIR, STAGE>(J, X, r0 + 16 * i, c0 + 16 * j);
                 finish<PAIR, STAGE>(g, J, next, r0 + 16 * i, c0 + 16 * j, mirror, o, acc[i][j]);
             }
     }
@@ -447,7 +488,7 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
     const int r0 = c.tm * kBigT + (wave >> 2) * 128 + (lane & 15), c0 = c.tn * kBigT + (wave & 3) * 64 + 4 * (lane >> 4);
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {   // (two rows' reads at a time)
-        f32x4 old[2][4];
+        Old old[2][4];
 #pragma unroll
         for (int k = 0; k < 8; ++k) old[k / 4][k % 4] = old_at<PAIR, STAGE>(J, X, r0 + 16 * (i + k / 4), c0 + 16 * (k % 4));
 #pragma unroll
@@ -466,7 +507,7 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
 // other reads, and writes them back in place.  50 x 64: 80 us in launches of their
 // own, 19 here; 64 x 560 102 and 54, 128 x 192 98 and 62, sixteen of 128 x 128 96 and 56.
 constexpr int kSmallLds = 160 << 10, kSmallThreads = 1024, kSmallSide = 128;
-bool fits_lds(int64_t mp, int64_t np) { return mp <= kSmallSide && 4 * mp * (mp + np) <= kSmallLds; }
+bool fits_lds(int64_t mp, int64_t np) { return mp <= kSmallSide && 4 * mp * (mp + np + 2) <= kSmallLds; }
 
 struct Resident {
     char *base;
@@ -537,7 +578,7 @@ struct Block {
 };
 // A = X X^T; every wavefront calls it
 template <int TS>
-__device__ __forceinline__ void gram(const Resident &X, const Resident &A, int mp, int np, int lane, int wave) {
+__device__ __forceinline__ void gram(const Resident &X, const Resident &A, float *e, int mp, int np, int lane, int wave) {
     const Block<TS> b(mp, wave);
     if (b.mine) {
         f32x4 acc[TS][TS];
@@ -545,14 +586,16 @@ __device__ __forceinline__ void gram(const Resident &X, const Resident &A, int m
 #pragma unroll
         for (int i = 0; i < TS; ++i)
 #pragma unroll
-            for (int j = 0; j < TS; ++j)
-                A.put(b.i0 + 16 * i + (lane & 15), b.j0 + 16 * j + 4 * (lane >> 4), acc[i][j] * two_to(kABits - 2 * kXBits));
+            for (int j = 0; j < TS; ++j) {
+                const int row = b.i0 + 16 * i + (lane & 15), col = b.j0 + 16 * j + 4 * (lane >> 4);
+                A.put(row, col, gram_of(acc[i][j], row, col, e + row));
+            }
     }
     __syncthreads();
 }
 // B in A's place; every wavefront calls it
 template <int TS>
-__device__ __forceinline__ void poly(const Resident &A, int mp, int lane, int wave) {
+__device__ __forceinline__ void poly(const Resident &A, const float *e, float *d, int mp, int lane, int wave) {
     const Block<TS> b(mp, wave);
     const int r0 = b.i0 + (lane & 15), c0 = b.j0 + 4 * (lane >> 4);
     f32x4 acc[TS][TS];
@@ -561,9 +604,10 @@ __device__ __forceinline__ void poly(const Resident &A, int mp, int lane, int wa
 #pragma unroll
         for (int i = 0; i < TS; ++i)
 #pragma unroll
-            for (int j = 0; j < TS; ++j)
-                acc[i][j] = acc[i][j] * (kCoefC * two_to(kBBits - 2 * kABits)) +
-                            A.four(r0 + 16 * i, c0 + 16 * j) * (kCoefB * two_to(kBBits - kABits));
+            for (int j = 0; j < TS; ++j) {
+                const int row = r0 + 16 * i, col = c0 + 16 * j;
+                acc[i][j] = poly_of(acc[i][j], A.four(row, col), e[row], *(const f32x4 *)(e + col), row, col, d + row);
+            }
     }
     __syncthreads();   // A is read
     if (b.mine) {
@@ -576,8 +620,8 @@ __device__ __forceinline__ void poly(const Resident &A, int mp, int lane, int wa
 }
 // X <- a X + B X in place, or, behind the last step, the update of W; column 0 of X
 // here is column `first` of the matrix's.  Every wavefront calls it.
-__device__ __forceinline__ void move_columns(const Group &g, const Job &J, const Resident &X, const Resident &B, int mp, int np,
-                                             int first, bool last, int lane, int wave) {
+__device__ __forceinline__ void move_columns(const Group &g, const Job &J, const Resident &X, const Resident &B,
+                                             const float *d, int mp, int np, int first, bool last, int lane, int wave) {
     for (int c0 = 16 * wave; c0 < np; c0 += 16 * (kSmallThreads / 64)) {
         f32x4 acc[kSmallSide / 16];
 #pragma unroll
@@ -593,7 +637,7 @@ __device__ __forceinline__ void move_columns(const Group &g, const Job &J, const
         for (int i = 0; i < kSmallSide / 16; ++i) {
             if (16 * i >= mp) break;
             const int row = 16 * i + (lane & 15), col = c0 + 4 * (lane >> 4);
-            const f32x4 v = acc[i] * two_to(-kBBits) + X.four(row, col) * kCoefA;
+            const f32x4 v = acc[i] * two_to(-kBBits) + X.four(row, col) * (kCoefA + d[row]);
             if (last) apply(g, J, row, first + col, v * two_to(-kXBits));
             else X.put(row, col, v);
         }
@@ -622,6 +666,7 @@ __global__ __launch_bounds__(kSmallThreads) void resident_kernel(Group g, int st
     const Job &J = g.job[blockIdx.x];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mp = J.mp, np = J.np;
     const Resident A{lds, 128 * mp}, X{lds + 4 * mp * mp, 128 * mp};
+    float *const e = (float *)(lds + 4 * mp * (mp + np)), *const d = e + mp;
     // M and the norm, then X, each of a thread's own elements of U both times
     const uint32_t per_row = ((uint32_t)J.cols + 3) / 4, total = (uint32_t)J.rows * per_row;
     double sum = 0.0;
@@ -644,13 +689,13 @@ __global__ __launch_bounds__(kSmallThreads) void resident_kernel(Group g, int st
     __syncthreads();
     for (int k = 0; k < steps; ++k) {
         if (mp > 64) {
-            gram<2>(X, A, mp, np, lane, wave);
-            poly<2>(A, mp, lane, wave);
+            gram<2>(X, A, e, mp, np, lane, wave);
+            poly<2>(A, e, d, mp, lane, wave);
         } else {
-            gram<1>(X, A, mp, np, lane, wave);
-            poly<1>(A, mp, lane, wave);
+            gram<1>(X, A, e, mp, np, lane, wave);
+            poly<1>(A, e, d, mp, lane, wave);
         }
-        move_columns(g, J, X, A, mp, np, 0, k + 1 == steps, lane, wave);
+        move_columns(g, J, X, A, d, mp, np, 0, k + 1 == steps, lane, wave);
     }
 }
 
@@ -671,6 +716,7 @@ __global__ __launch_bounds__(kSmallThreads) void slab_kernel(Group g, int step, 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mp = J.mp, np = J.slab;
     const int first = s * np;
     const Resident A{lds, 128 * mp}, X{lds + 4 * mp * mp, 128 * mp};
+    float *const e = (float *)(lds + 4 * mp * (mp + np)), *const d = e + mp;
     uint4 *const image = (uint4 *)(J.X0 + (int64_t)s * 4 * mp * np);
     float *const parts = (float *)J.X1;   // [2][slabs][mp x mp]
     if (step < 0) {
@@ -700,13 +746,14 @@ __global__ __launch_bounds__(kSmallThreads) void slab_kernel(Group g, int step, 
             f32x4 v = p[i];
 #pragma unroll 8
             for (int w = 1; w < slabs; ++w) v += p[(int64_t)w * (mp * mp / 4) + i];
-            A.put(4 * i / mp, 4 * i % mp, v * two_to(kABits - 2 * kXBits));
+            const int row = 4 * i / mp, col = 4 * i % mp;
+            A.put(row, col, gram_of(v, row, col, e + row));
         }
         __syncthreads();
-        if (mp > 64) poly<2>(A, mp, lane, wave);
-        else poly<1>(A, mp, lane, wave);
+        if (mp > 64) poly<2>(A, e, d, mp, lane, wave);
+        else poly<1>(A, e, d, mp, lane, wave);
         const bool last = step + 1 == steps;
-        move_columns(g, J, X, A, mp, np, first, last, lane, wave);
+        move_columns(g, J, X, A, d, mp, np, first, last, lane, wave);
         if (last) return;
     }
     __syncthreads();
@@ -728,9 +775,8 @@ __global__ __launch_bounds__(kSmallThreads) void slab_kernel(Group g, int step, 
     else leave(std::integral_constant<int, 1>{});
 }
 
-// Whether a matrix takes pairs.  GCN_BF16 does so too for matrices with a short side: a
-// single product's roundings average out over many singular values only (one row:
-// 4e-3 off, 128 rows 1.7e-3), and their time is launches, not products.
+// Whether a matrix takes pairs.  GCN_BF16 does so too for matrices with a short side,
+// whose time is launches, not products.
 constexpr int32_t kSingleSide = 128;
 bool takes_pairs(int32_t rows, int32_t cols, int prec) {
     return prec == GCN_F32 || std::min(rows, cols) < kSingleSide;
@@ -759,6 +805,8 @@ void plan_job(Job &J, bool pair, Arena &ar) {
     J.X1 = ar.take<uint8_t>(4 * (size_t)J.mp * std::max((size_t)J.np, 2 * slabs * J.mp));
     J.A = ar.take<uint8_t>((pair ? 4 : 2) * (size_t)J.mp * J.mp);
     J.B = ar.take<uint8_t>((pair ? 4 : 2) * (size_t)J.mp * J.mp);
+    J.e = ar.take<float>((size_t)J.mp);
+    J.d = ar.take<float>((size_t)J.mp);
     const int64_t total = (int64_t)J.rows * J.cols;
     J.parts = (int32_t)std::min<int64_t>(kMostParts, (total + 4 * kTB - 1) / (4 * kTB));
     J.part = ar.take<double>((size_t)J.parts);
