@@ -251,20 +251,32 @@ struct Old {
     float row;
 };
 template <bool PAIR, int STAGE>
-__device__ __forceinline__ Old old_at(const Job &J, const uint8_t *X, int row, int col) {
-    Old o{f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0.0f};
-    if constexpr (STAGE == GRAM) return o;
+__device__ __forceinline__ f32x4 elements_at(const Job &J, const uint8_t *X, int row, int col) {
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if constexpr (STAGE == GRAM) return v;
     const int32_t cols = STAGE == POLY ? J.mp : J.np;
     if (row < J.mp && col < cols) {
         const uint8_t *p = (STAGE == POLY ? J.A : X) + place<PAIR>(row, row_bytes<PAIR>(cols), col);
-        o.v = four_of(p);
+        v = four_of(p);
         // (A of the single products is its high parts alone)
-        if constexpr (PAIR) o.v += four_of(p + 64);
-        else if (STAGE != POLY) o.v += four_of(p + 2 * (int64_t)J.mp * J.np);
-        o.row = (STAGE == POLY ? J.e : J.d)[row];
-        if constexpr (STAGE == POLY) o.cols = *(const f32x4 *)(J.e + col);
+        if constexpr (PAIR) v += four_of(p + 64);
+        else if (STAGE != POLY) v += four_of(p + 2 * (int64_t)J.mp * J.np);
     }
-    return o;
+    return v;
+}
+template <int STAGE>
+__device__ __forceinline__ float diagonal_at(const Job &J, int row) {
+    if constexpr (STAGE == GRAM) return 0.0f;
+    else return (STAGE == POLY ? J.e : J.d)[min(row, J.mp - 1)];
+}
+template <int STAGE>
+__device__ __forceinline__ f32x4 diagonals_at(const Job &J, int col) {
+    if constexpr (STAGE != POLY) return f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    else return *(const f32x4 *)(J.e + min(col, J.mp - 4));
+}
+template <bool PAIR, int STAGE>
+__device__ __forceinline__ Old old_at(const Job &J, const uint8_t *X, int row, int col) {
+    return Old{elements_at<PAIR, STAGE>(J, X, row, col), diagonals_at<STAGE>(J, col), diagonal_at<STAGE>(J, row)};
 }
 // A's four elements at (row, col ..) from their sums, and B's from the sums of A' A';
 // those of the diagonal go to *diagonal and leave zero
@@ -486,15 +498,21 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
     big_loop<TYPE>(p, c, 0, p.kt, lds, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int r0 = c.tm * kBigT + (wave >> 2) * 128 + (lane & 15), c0 = c.tn * kBigT + (wave & 3) * 64 + 4 * (lane >> 4);
+    f32x4 cols[4];
+    float rows[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) cols[k] = diagonals_at<STAGE>(J, c0 + 16 * k);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rows[i] = diagonal_at<STAGE>(J, r0 + 16 * i);
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {   // (two rows' reads at a time)
-        Old old[2][4];
+        f32x4 old[2][4];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) old[k / 4][k % 4] = old_at<PAIR, STAGE>(J, X, r0 + 16 * (i + k / 4), c0 + 16 * (k % 4));
+        for (int k = 0; k < 8; ++k) old[k / 4][k % 4] = elements_at<PAIR, STAGE>(J, X, r0 + 16 * (i + k / 4), c0 + 16 * (k % 4));
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            finish<PAIR, STAGE>(g, J, next, r0 + 16 * (i + k / 4), c0 + 16 * (k % 4), mirror, old[k / 4][k % 4],
-                                acc[i + k / 4][k % 4]);
+            finish<PAIR, STAGE>(g, J, next, r0 + 16 * (i + k / 4), c0 + 16 * (k % 4), mirror,
+                                Old{old[k / 4][k % 4], cols[k % 4], rows[i + k / 4]}, acc[i + k / 4][k % 4]);
     }
 }
 
