@@ -443,8 +443,8 @@ __device__ __forceinline__ void product_of(const Group &g, const Job &J, const u
 // which waits for its own copies, reads and products in turn.
 template <bool PAIR, int STAGE, int BM, int BN, int WM, int WN, int KG>
 __global__ __launch_bounds__(64 * WM *WN *KG) void muon_kernel(Group g, int odd) {
-    constexpr int TYPE = type_of<PAIR, STAGE>(), FM = BM / WM / 16, FN = BN / WN / 16, kBlocks = FM * FN, kOwn = kBlocks < KG ? 1 : kBlocks / KG,
-                  T = 64 * WM * WN;
+    constexpr int TYPE = type_of<PAIR, STAGE>(), T = 64 * WM * WN;
+    constexpr int FM = BM / WM / 16, FN = BN / WN / 16, kBlocks = FM * FN, kOwn = kBlocks < KG ? 1 : kBlocks / KG;
     constexpr int kLds = small_lds(TYPE, BM, BN);
     static_assert(KG == 1 || kBlocks * T * 16 <= kLds, "the groups' sums fit where the operands were");
     __shared__ __attribute__((aligned(16))) char lds[KG * kLds];
@@ -520,10 +520,11 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
 // A whole update of a matrix whose X and A fit in LDS as pairs, by one workgroup: no
 // launches between the products.  X and A lie as pieces of 32 columns, a
 // row's 128 bytes (high parts, low parts) beside the next row's, chunk c of row r at
-// c ^ (r % 8), so that 16 rows' chunks are on different banks.  B takes A's place.  A and B: a wavefront has one block of
-// 16 TS x 16 TS.  a X + B X: a wavefront has 16 columns of X at a time, which no
-// other reads, and writes them back in place.  50 x 64: 80 us in launches of their
-// own, 19 here; 64 x 560 102 and 54, 128 x 192 98 and 62, sixteen of 128 x 128 96 and 56.
+// c ^ (r % 8), so that 16 rows' chunks are on different banks.  B takes A's place.
+// A and B: a wavefront has one block of 16 TS x 16 TS.  a X + B X: a wavefront has
+// 16 columns of X at a time, which no other reads, and writes them back in place.
+// us, in launches of their own / here: 50 x 64 51 / 20, 64 x 560 62 / 55, 128 x 128
+// 64 / 55, 128 x 160 65 / 62, sixteen of 128 x 128 75 / 58.
 constexpr int kSmallLds = 160 << 10, kSmallThreads = 1024, kSmallSide = 128;
 bool fits_lds(int64_t mp, int64_t np) { return mp <= kSmallSide && 4 * mp * (mp + np + 2) <= kSmallLds; }
 
@@ -723,9 +724,9 @@ __global__ __launch_bounds__(kSmallThreads) void resident_kernel(Group g, int st
 // instead of three, and the sum over the columns in as many parts as there are
 // workgroups.  Its columns go through memory as they lie in LDS.  Parts alternate
 // between two places, since others may still read the old ones.  us, three launches a
-// step / one: 64 x 700 95 / 55, 64 x 2000 109 / 64, 30 x 4000 137 / 52, 16 x 8000 201 / 62,
-// 96 x 700 87 / 84, 96 x 2000 112 / 105, but 128 x 602 90 / 108: B and the part of A are
-// formed by one CU each.
+// step / one: 64 x 700 89 / 56, 64 x 2000 111 / 65, 64 x 65,536 1245 / 191, 30 x 4000 135 / 53,
+// 16 x 8000 201 / 63, 96 x 2000 115 / 105, 96 x 65,536 1222 / 576, but 128 x 1000 101 / 128, 128 x
+// 8192 230 / 270: B and the part of A are formed by one CU each.
 __global__ __launch_bounds__(kSmallThreads) void slab_kernel(Group g, int step, int steps) {
     __shared__ __attribute__((aligned(16))) char lds[kSmallLds];
     const int j = job_of(g, blockIdx.x);
@@ -791,6 +792,74 @@ __global__ __launch_bounds__(kSmallThreads) void slab_kernel(Group g, int step, 
     };
     if (mp > 64) leave(std::integral_constant<int, 2>{});
     else leave(std::integral_constant<int, 1>{});
+}
+
+// B and a X + B X in one launch where A fits in LDS beside the columns of X: 32 rows and
+// 64 columns of the next X to a workgroup, which forms its rows of B from A by itself.
+// Up to twice the products, and A read once a workgroup, against a launch, five of
+// which are 20 us.  For one round of a workgroup a CU (us, apart / so: 602 x 128 and 256 x
+// 128, two each, 96 / 76, 128 x 300 89 / 68, 128 x 4096, 256 workgroups, 159 / 140, but six of
+// 700 x 128, 264, 100 / 109, 128 x 8192 230 / 235).
+constexpr int kStepRows = 32, kStepCols = 64, kStepThreads = 512, kMostSteps = 256;
+__host__ __device__ __forceinline__ int64_t step_blocks(const Job &J) {
+    return (int64_t)(J.mp / kStepRows) * ((J.np + kStepCols - 1) / kStepCols);
+}
+template <int STAGE>
+__global__ __launch_bounds__(kStepThreads) void step_kernel(Group g, int odd) {
+    constexpr int kSide = kSmallSide, kFours = kSide * kSide / 4 / kStepThreads, kXFours = kSide * kStepCols / 4 / kStepThreads;
+    __shared__ __attribute__((aligned(16))) char lds[4 * kSide * (kSide + kStepCols) + 4 * kStepRows * kSide];
+    __shared__ float d[kStepRows];
+    const int j = job_of(g, blockIdx.x);
+    const Job &J = g.job[j];
+    const uint8_t *const from = odd ? J.X1 : J.X0;
+    uint8_t *const next = odd ? J.X0 : J.X1;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mp = J.mp, np = J.np;
+    const int at = (int)(blockIdx.x - g.first[j]), down = mp / kStepRows;
+    const int r0 = at % down * kStepRows, first = at / down * kStepCols, cols = min(kStepCols, np - first);
+    const Resident A{lds, 128 * mp}, X{lds + 4 * mp * mp, 128 * mp}, B{lds + 4 * mp * (mp + kStepCols), 128 * kStepRows};
+    f32x4 a[kFours], x[kXFours];
+    const int per = mp / 4;   // chunks of 16 bytes of a row of A
+#pragma unroll
+    for (int u = 0; u < kFours; ++u) {
+        const int i = u * kStepThreads + threadIdx.x;
+        a[u] = *(const f32x4 *)(J.A + (int64_t)(i < mp * per ? i : 0) * 16);
+    }
+#pragma unroll
+    for (int u = 0; u < kXFours; ++u) {
+        const int i = u * kStepThreads + threadIdx.x, r = i / 16, c = i % 16;
+        x[u] = *(const f32x4 *)(from + (r < mp && 4 * c < cols ? (int64_t)r * 4 * np + 4 * first + c * 16 : 0));
+    }
+    const int br = 16 * (wave & 1), bc = 16 * (wave >> 1);   // the wavefront's first block, of B and of X
+    const int lr = br + (lane & 15), lc = bc + 4 * (lane >> 4);
+    const float e_row = J.e[r0 + lr];
+    const f32x4 e_cols[2] = {diagonals_at<POLY>(J, lc), diagonals_at<POLY>(J, lc + 64)};
+#pragma unroll
+    for (int u = 0; u < kFours; ++u) {
+        const int i = u * kStepThreads + threadIdx.x, r = i / per, c = i - r * per;
+        if (i < mp * per) *(f32x4 *)(A.base + c / 8 * A.step + r * 128 + ((c % 8) ^ (r & 7)) * 16) = a[u];
+    }
+#pragma unroll
+    for (int u = 0; u < kXFours; ++u) {
+        const int i = u * kStepThreads + threadIdx.x, r = i / 16, c = i % 16;
+        if (r < mp && 4 * c < cols) *(f32x4 *)(X.base + c / 8 * X.step + r * 128 + ((c % 8) ^ (r & 7)) * 16) = x[u];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        const int pieces = bc + 64 * u < mp ? mp / 32 : 0;
+#pragma unroll 1
+        for (int t = 0; t < pieces; ++t) mma<TILE_PAIR>(v, A.rows(r0 + br, t, lane), A.rows(bc + 64 * u, t, lane), 0, 0);
+        if (pieces) B.put(lr, lc + 64 * u, poly_of(v, A.four(r0 + lr, lc + 64 * u), e_row, e_cols[u], r0 + lr, lc + 64 * u, d + lr));
+    }
+    __syncthreads();
+    if (bc >= cols) return;
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int t = 0; t < mp / 32; ++t) mma<TILE_PAIR>(v, B.rows(br, t, lane), X.columns(t, bc, lane), 0, 0);
+    v = v * two_to(-kBBits) + X.four(r0 + lr, lc) * (kCoefA + d[lr]);
+    if constexpr (STAGE == NEXT) store_parts(next + place<true>(r0 + lr, row_bytes<true>(np), first + lc), 64, v);
+    else apply(g, J, r0 + lr, first + lc, v * two_to(-kXBits));
 }
 
 // Whether a matrix takes pairs.  GCN_BF16 does so too for matrices with a short side,
@@ -884,9 +953,9 @@ int product(Group &g, int odd, hipStream_t s) {
         const dim3 b = grid(BM, BN);                                                                             \
         hipLaunchKernelGGL((muon_kernel<PAIR, STAGE, BM, BN, WM, WN, KG>), b, dim3(64 * WM * WN * KG), 0, s, g, odd); \
     } while (0)
-    // us a call of five steps, the two ways on either side of each border.  Large tiles for a X + B X: 3000 x 3200
-    // (156 of them) 2185 with 128 x 128 ones, 2121 with large; for A and B 3000 x 3200 (78) 2185 and 2850, 3400 x
-    // 3400 in GCN_BF16 (105) 1099 and 1386.
+    // us a call of five steps, the two ways on either side of each border (taken with the diagonals still within A
+    // and B, 1 to 2 % faster throughout).  Large tiles for a X + B X: 3000 x 3200 (156 of them) 2185 with 128 x 128
+    // ones, 2121 with large; for A and B 3000 x 3200 (78) 2185 and 2850, 3400 x 3400 in GCN_BF16 (105) 1099 and 1386.
     if (deep && all(kBigT, kBigT) >= (STAGE <= POLY ? 120 : 150)) {
         const dim3 b = grid(kBigT, kBigT);
         hipLaunchKernelGGL((muon_big_kernel<PAIR, STAGE>), b, dim3(kBigThreads), 0, s, g, odd);
@@ -919,15 +988,23 @@ int product(Group &g, int odd, hipStream_t s) {
 
 template <bool PAIR>
 int run_group(Group &g, int32_t steps, hipStream_t s) {
-    bool small = PAIR, few = PAIR;
+    bool small = PAIR, few = PAIR, narrow = PAIR;
     double flops = 0.0;
     if constexpr (PAIR) {
+        int64_t blocks = 0;
+        int32_t most = 0;
         for (int j = 0; j < g.count; ++j) {
             const Job &J = g.job[j];
             small = small && fits_lds(J.mp, J.np);
             few = few && J.slab > 0;
             flops += (3.0 * J.np + J.mp) * J.mp * J.mp * steps;
+            blocks += step_blocks(J);
+            most = std::max(most, J.mp);
         }
+        narrow = most <= kSmallSide && blocks <= kMostSteps;
+        // (us, step_kernel / slab_kernel: 96 x 700 67 / 87, 96 x 2000, 96 workgroups of the former, 91 / 105, 96 x 3000,
+        // 141, 111 / 109, 96 x 5000 155 / 119; 64 x 700 62 / 56, 64 x 2000 85 / 65)
+        if (most > 64 && blocks <= kMostSteps / 2) few = false;
         if (small) {
             ProfScope prof(K_MUON_SMALL, s, flops, 0.0);
             hipLaunchKernelGGL(resident_kernel, dim3((unsigned)g.count), dim3(kSmallThreads), 0, s, g, (int)steps);
@@ -961,6 +1038,15 @@ int run_group(Group &g, int32_t steps, hipStream_t s) {
     int rc;
     for (int32_t k = 0; k < steps; ++k) {
         const int odd = k & 1;
+        if (PAIR && narrow) {
+            if ((rc = product<PAIR, GRAM>(g, odd, s))) return rc;
+            ProfScope prof(K_MUON_PRODUCT, s, flops / steps, 0.0);
+            const dim3 b(blocks_of(g, [](const Job &J) { return (uint64_t)step_blocks(J); }));
+            if (k + 1 < steps) hipLaunchKernelGGL(step_kernel<NEXT>, b, dim3(kStepThreads), 0, s, g, odd);
+            else hipLaunchKernelGGL(step_kernel<LAST>, b, dim3(kStepThreads), 0, s, g, odd);
+            GCN_LAUNCH_CHECK("step_kernel");
+            continue;
+        }
         if ((rc = product<PAIR, GRAM>(g, odd, s)) || (rc = product<PAIR, POLY>(g, odd, s))) return rc;
         if ((rc = k + 1 < steps ? product<PAIR, NEXT>(g, odd, s) : product<PAIR, LAST>(g, odd, s))) return rc;
     }

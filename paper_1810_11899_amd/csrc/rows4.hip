@@ -371,7 +371,8 @@ int gcn_rows4_pack(const void *X, gcn_rows_type type, int32_t n, int32_t f, int3
     if (colsum) {
         const int32_t rows = (int32_t)((n + (int64_t)kTile - 1) / kTile);
         ProfScope prof(K_ROWS4_PACK, s, 0.0, 4.0 * rows * f);
-        hipLaunchKernelGGL(colsum4_kernel, dim3((unsigned)std::min<int64_t>((f + 3ll) / 4, 1 << 16)), dim3(kTB), 0, s, rows, f, a.part, colsum);
+        const dim3 b((unsigned)std::min<int64_t>((f + 3ll) / 4, 1 << 16));
+        hipLaunchKernelGGL(colsum4_kernel, b, dim3(kTB), 0, s, rows, f, a.part, colsum);
         GCN_LAUNCH_CHECK("colsum4_kernel");
     }
     return GCN_OK;

@@ -394,7 +394,8 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 if constexpr (TYPE == TILE_FP8_EXACT) asm volatile("" : "+v"(acc[i][j]));
-                else asm volatile("" : "+a"(acc[i][j]));   // (where the products leave them: pinned elsewhere they are moved there and back)
+                // (where the products leave them: pinned elsewhere they are moved there and back)
+                else asm volatile("" : "+a"(acc[i][j]));
             }
     }
     for (int t = nt; t < turns; ++t) turn();

@@ -110,6 +110,20 @@ def test_spectra_that_fall(rows, cols, kind, ws):
     assert rel2(out.cpu().numpy(), want) <= 2.0 ** -8
 
 
+@pytest.mark.parametrize("rows, cols", [(96, 700), (70, 2950), (2500, 96), (90, 20001), (30, 65536), (128, 4070), (4170, 128), (100, 333)])
+def test_few_rows_and_many_columns(rows, cols, ws):
+    """Tens to hundreds of workgroups a step, the last one's columns a part of its share."""
+    u = np.random.default_rng(rows).normal(size=(rows, cols)).astype(np.float32)
+    x = torch.from_numpy(u).cuda()
+    got = B.gcn_orthogonalise(x, torch.empty_like(x), ws)
+    again = B.gcn_orthogonalise(x, torch.empty_like(x), ws)
+    assert torch.equal(got, again)
+    want = O.orthogonalise(u)
+    got = got.cpu().numpy().astype(np.float64)
+    assert np.linalg.norm(got - want) <= O.error_bound(u) + 2.0 ** -24 * np.linalg.norm(want)
+    assert rel2(got, want) <= 4 * rel2(f32_iteration(u), want) + 2.0 ** -21
+
+
 @pytest.mark.parametrize("rows, cols", [(700, 700), (1024, 1100), (1500, 1500), (2300, 1030), (2050, 2300), (2500, 2500),
                                         (3000, 3300), (4096, 2816), (300, 9000), (4096, 4100)])
 @pytest.mark.parametrize("prec", [B.GCN_F32, B.GCN_BF16])

@@ -174,6 +174,15 @@ def test_no_rows(ws):
     assert B.gcn_rows4_product(out, out, torch.empty((0, 0), device="cuda"), ws).numel() == 0
 
 
+@pytest.mark.parametrize("M, N", [(100, 70), (2600, 2700)])
+def test_sums_over_nothing(M, N, ws):
+    """Tiles without a piece."""
+    b = torch.linspace(-1, 1, N, device="cuda")
+    Y = torch.empty((M, N), device="cuda")
+    B.gcn_rows4_product(B.Rows4(M, 0), B.Rows4(N, 0), Y, ws, bias=b)
+    assert torch.equal(Y, b.expand(M, N))
+
+
 # ------------------------------------------------------------------- product
 def sum_bound(K, a, b):
     """Every instruction adds 128 products to a float32 sum, parts and the bias are added after it: each of these
