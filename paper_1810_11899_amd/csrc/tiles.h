@@ -210,9 +210,10 @@ constexpr int kScalePieces = 64;
 constexpr int small_lds(int type, int BM, int BN) {
     return 2 * (BM + BN) * kPiece + (is_fp8(type) ? kScalePieces * (BM + 1) : type == TILE_FP4 ? 16 * (BM + BN) : 0);
 }
-// `lds`: small_lds bytes; behind the loop they are free again.  `tid`: the thread's number among the loop's 64 WM WN, where a workgroup
-// runs several of them side by side, with LDS of their own; then `turns` is the
-// largest nt among them (they share their barriers).
+// `lds`: small_lds bytes; behind the loop they are free again.  `tid`: the thread's
+// number among the loop's 64 WM WN, where a workgroup runs several of them side by
+// side, with LDS of their own; then `turns` is the largest nt among them (they share
+// their barriers).
 template <int TYPE, int BM, int BN, int WM, int WN>
 __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c, int kt0, int nt, char *lds,
                                            f32x4 (&acc)[BM / WM / 16][BN / WN / 16], uint32_t tid, int turns) {
@@ -404,7 +405,14 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
 template <int TYPE, int BM, int BN, int WM, int WN>
 __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c, int kt0, int nt, char *lds,
                                            f32x4 (&acc)[BM / WM / 16][BN / WN / 16]) {
-    small_loop<TYPE, BM, BN, WM, WN>(p, c, kt0, nt, lds, acc, threadIdx.x, nt);
+    // (sums of its own: formed in the caller's array, they are cleared on a path of
+    // their own where there is no piece; 6205 x 512 x 602 of 8-bit rows 12.5 / 12.2 us)
+    f32x4 sum[BM / WM / 16][BN / WN / 16];
+    small_loop<TYPE, BM, BN, WM, WN>(p, c, kt0, nt, lds, sum, threadIdx.x, nt);
+#pragma unroll
+    for (int i = 0; i < BM / WM / 16; ++i)
+#pragma unroll
+        for (int j = 0; j < BN / WN / 16; ++j) acc[i][j] = sum[i][j];
 }
 
 
