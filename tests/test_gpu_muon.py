@@ -301,6 +301,34 @@ def test_captured_update(ws):
             assert torch.equal(W, w) and torch.equal(M, m)
 
 
+@pytest.mark.parametrize("rows, cols", [(602, 128), (64, 2000), (300, 400)])
+def test_captured_in_each_way_of_working(rows, cols):
+    """Two graphs with workspaces of their own, replayed in turn between eager calls of the same matrix."""
+    x = to_dev(gradient(gen(31), rows, cols))
+    ws, outs, graphs, spaces = B.Workspace(), [], [], []
+    want = B.gcn_orthogonalise(x, torch.empty_like(x), ws)
+    for _ in range(2):
+        w, out = B.Workspace(), torch.empty_like(x)
+        w.get(1 << 26)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=s):
+                B.gcn_orthogonalise(x, out, w)
+        outs.append(out)
+        graphs.append(graph)
+        spaces.append(w)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for graph, out in zip(graphs, outs):
+            out.zero_()
+            graph.replay()
+            assert torch.equal(B.gcn_orthogonalise(x, torch.empty_like(x), ws), want)
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
+
+
 def test_another_stream(ws):
     """The calls follow the current stream: both ways of working, with their own workspaces at the same time."""
     a, b = to_dev(gradient(gen(20), 300, 200)), to_dev(gradient(gen(21), 60, 90))
