@@ -287,7 +287,7 @@ int check_rows4(const gcn_rows4 *r, const char *who) {
 // 116 / 67 / 61 / 65; 256 x 256 tiles 363 / 192 / 105 / 63 / 44 and 364 / 193 / 107 / 66 / 54).
 // Few rows take thin4_kernel unless it has few workgroups and a long sum.
 int32_t split4(int32_t M, int32_t N, int32_t kt) {
-    if (kt < 24 || (M <= 64 && N > 2048)) return 1;
+    if (M <= 0 || N <= 0 || kt < 24 || (M <= 64 && N > 2048)) return 1;
     const int64_t t64 = ((M + 63ll) / 64) * ((N + 63ll) / 64), t128 = ((M + 127ll) / 128) * ((N + 127ll) / 128);
     int64_t sp = std::min<int64_t>(512 / t128, kt / 16);
     if (t128 * sp < 192) sp = std::min<int64_t>({(kt < 64 ? 256 : 512) / t64, kt / 8, 32});

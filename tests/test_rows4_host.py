@@ -146,3 +146,18 @@ def test_product_argument_errors(L):
     assert need > 4 * 512 * 512
     a = rows4(n=512, f=65536, ldq=32768)
     assert product(a=a, b=a, ldy=512, wb=need - 1) == B.GCN_EWORKSPACE
+
+
+@pytest.mark.parametrize("M, N", [(0, 50), (50, 0), (0, 0), (0, 1 << 20), (1 << 20, 0)])
+@pytest.mark.parametrize("f", [0, 40, 5888, 5889, 6144, 8000, 65536, 1 << 24])
+def test_operands_of_no_rows_at_any_length_of_the_sum(L, M, N, f):
+    """Nothing to form: no parts, no launch, whatever the sum's length."""
+    assert L.gcn_rows4_product_workspace_bytes(M, N, f) == 256
+    ldq = 128 * -(-f // 256)
+
+    def rows(n):
+        return rows4(n=n, f=f, ldq=ldq, q=0x20000 if n else None, scale=0x30000 if n else None)
+
+    a, b = rows(M), rows(N)
+    assert L.gcn_rows4_product(ctypes.byref(a), ctypes.byref(b), None, 0, None, 0, N, FAKE, 256, None) == B.GCN_OK
+    assert L.gcn_rows4_product(ctypes.byref(a), ctypes.byref(b), None, 0, None, 1, N, FAKE, 255, None) == B.GCN_EWORKSPACE
