@@ -217,10 +217,21 @@ def _stream(stream=None):
     return stream.cuda_stream
 
 
+_MOST = 2 ** 31 - 1   # (ctypes cuts what its 32-bit arguments do not hold, without a word)
+
+
 def _ld(t: torch.Tensor) -> int:
     if t.dim() != 2 or t.stride(1) != 1:
         raise ValueError("expected a row-major 2-D tensor with unit column stride")
-    return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1]))
+    # (a single row's stride says nothing)
+    ld = int(t.stride(0)) if t.shape[0] > 1 else max(min(int(t.stride(0)), _MOST), int(t.shape[1]))
+    if ld > _MOST or t.shape[0] > _MOST:
+        _too_large()
+    return ld
+
+
+def _too_large():
+    raise ValueError("sizes and row strides must fit in 32 bits")
 
 
 def _dev_f32(t: torch.Tensor, name: str):
@@ -630,6 +641,8 @@ def _kept8(rows: int, cols: int, device) -> torch.Tensor:
 def _ld8(t: torch.Tensor, name: str) -> int:
     if t.dim() != 2 or t.dtype != torch.float8_e4m3fn or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
         raise TypeError(f"{name} must be a row-major float8_e4m3fn CUDA/HIP tensor")
+    if max(*t.shape, t.stride(0)) > _MOST:
+        _too_large()
     return int(t.stride(0))
 
 
@@ -813,6 +826,8 @@ class Rows4:
                 raise ValueError("values must have unit column stride")
             if self.n > 1:
                 ld = int(values.stride(0))
+        if max(self.n, self.f, ld) > _MOST:
+            _too_large()
         _want(scale, "scale", torch.uint8, (_pieces4(self.f), (self.n + 63) // 64, 512))
         if not scale.is_contiguous():
             raise ValueError("scale must be contiguous")
