@@ -14,12 +14,15 @@
  * 1.2025 (Newton-Schulz iteration with a quintic; Jordan et al., 2024).  With
  * more rows than columns the iteration runs on U^T.
  *
- * prec: GCN_F32 forms the products to float32's precision (float16 pairs on the
- * matrix cores).  GCN_BF16 rounds their operands to float16, but carries X
- * itself and the diagonals of A and B to float32's precision: results within
- * about 2^-10 in the 2-norm, less than bfloat16's rounding, whatever the singular
- * values, at a third of the matrix work.  (Matrices with a side below 128 take
- * GCN_F32's products in either.)
+ * prec: GCN_F32 forms the products to float32's precision (the last 6 steps with
+ * float16 pairs on the matrix cores, those ahead of them with float32 operands: a pair
+ * ends at 2^-40 |U|_F, and a direction that more steps bring up would carry that
+ * along).  GCN_BF16 rounds the operands of the last 12 steps to float16, but carries X
+ * itself and the diagonals of A and B as pairs: five steps' results within about
+ * 2^-10 in the 2-norm, less than bfloat16's rounding, whatever the singular values, at
+ * a third of the matrix work.  (More steps move what they are off on with the
+ * singular values, by slopes of -1.6 .. 4 between 0.7 and 1.2.  Matrices with a side
+ * below 128 take GCN_F32's products in either.)
  *
  * Conventions are those of gcn_layer.h (device pointers owned by the caller,
  * row-major leading dimensions, `stream` a hipStream_t as void*, a 256-byte

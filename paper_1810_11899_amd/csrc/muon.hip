@@ -16,6 +16,16 @@
 //   GCN_BF16  products of the high parts alone; X keeps its low part, for a X.
 //             A direction with a small singular value grows a-fold a step by a X
 //             alone, and a rounding of X would grow with it: so it is not rounded.
+// One power of two for a whole matrix leaves a floor: half a step of float16's smallest
+// numbers, 2^-40 of |U| for an element of X, 2^-39 and 2^-38 for one of A and B.  A direction of
+// the size s |U| carries it along as it grows, and is 2^-36 / s off at most (rows of unlike
+// sizes, CPU model / float32 products: s = 1e-4, 8 steps 1.5e-7 / 1.3e-7, 1e-6, 13 steps 4.7e-6 /
+// 6e-7, 1e-10, 20 steps 4.4e-2 / 3e-7).  Only many steps bring such directions up, and at
+// the last few of them they are large enough: the steps ahead of the last kPairSteps, or
+// kSingleSteps of GCN_BF16, are
+//   WHOLE     float32 rows and products, on the same tiles (us, ten steps, pairs alone / so: 50 x 64
+//             35 / 110, 602 x 128 137 / 164, 512 x 512 235 / 258, 1024 x 1024 442 / 544, 4096 x
+//             4096 7740 / 15,050).
 // The diagonals of A and B are the larger part of them (X's rows are nearly
 // orthogonal after the first steps), and a rounding there moves a whole row alike.
 // So they stay float32, in vectors e and d beside A' and B', which have zeros there:
@@ -171,11 +181,19 @@ __global__ __launch_bounds__(kTB) void momentum_kernel(Group g) {
 __device__ __forceinline__ uint16_t half_bits(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
 __device__ __forceinline__ float half_value(uint32_t b) { return (float)__builtin_bit_cast(_Float16, (uint16_t)b); }
 
+// What operands are made of: float16, pairs, float32 (see above).
+enum Kind { SINGLE = 0, PAIR = 1, WHOLE = 2 };
+// The last steps, with pairs or GCN_BF16's operands.  Half of the rows a twentieth of what so many steps bring to one,
+// how far they are off (model; pairs for the last 8 / 7 / 6 / 5 steps / float32 products): 20 x 3000 4.7e-6 / 1.4e-6 /
+// 4.2e-7 / 1.8e-7 / 1.5e-7, 100 x 300 3.4e-6 / 1.0e-6 / 3.4e-7 / 2.0e-7 / 3.7e-7, 400 x 700 1.0e-5 / 3.0e-6 / 9.0e-7 /
+// 3.6e-7 / 7.6e-7.  2^-36 3.4445^12 is a twentieth of what GCN_BF16 leaves, 2^-10.
+constexpr int32_t kPairSteps = 6, kSingleSteps = 12;
+
 // Four consecutive elements (column a multiple of 4) of an operand, and back.  `low`:
 // bytes from the high parts to the low ones.  bytes: of a row.
-template <bool PAIR>
+template <int KIND>
 __device__ __forceinline__ int64_t place(int64_t row, int64_t bytes, int64_t col) {
-    return row * bytes + (PAIR ? pair_place(col) : 2 * col);
+    return row * bytes + (KIND == PAIR ? pair_place(col) : (KIND == WHOLE ? 4 : 2) * col);
 }
 __device__ __forceinline__ f32x4 four_of(const uint8_t *p) {
     const uint2 h = *(const uint2 *)p;
@@ -194,12 +212,17 @@ __device__ __forceinline__ void store_parts(uint8_t *p, int64_t low, f32x4 v) {
         *(uint2 *)(p + low) = four_halves(v - hi);
     }
 }
-template <bool PAIR>
-__device__ __forceinline__ int64_t row_bytes(int32_t cols) { return (int64_t)cols * (PAIR ? 4 : 2); }
+template <int KIND>
+__device__ __forceinline__ void store_four(uint8_t *p, int64_t low, f32x4 v) {
+    if constexpr (KIND == WHOLE) *(f32x4 *)p = v;
+    else store_parts(p, low, v);
+}
+template <int KIND>
+__device__ __forceinline__ int64_t row_bytes(int32_t cols) { return (int64_t)cols * (KIND == SINGLE ? 2 : 4); }
 
 // X0 = U / |U|, 64 x 64 elements to a block, zeros past U's sides, through LDS
 // where U is laid out transposed.
-template <bool PAIR>
+template <int KIND>
 __global__ __launch_bounds__(kTB) void operand_kernel(Group g) {
     __shared__ float tile[64][65];
     __shared__ double red[kTB / 64];
@@ -235,14 +258,15 @@ __global__ __launch_bounds__(kTB) void operand_kernel(Group g) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) u[k][e] = tile[16 * k + tr][tc + e];
     }
-    const int64_t bytes = row_bytes<PAIR>(J.np), low = PAIR ? 64 : 2 * (int64_t)J.mp * J.np;
+    const int64_t bytes = row_bytes<KIND>(J.np), low = KIND == PAIR ? 64 : 2 * (int64_t)J.mp * J.np;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
         if (i0 + 16 * k + tr < J.mp && j0 + tc < J.np)
-            store_parts(J.X0 + place<PAIR>(i0 + 16 * k + tr, bytes, j0 + tc), low, u[k]);
+            store_four<KIND>(J.X0 + place<KIND>(i0 + 16 * k + tr, bytes, j0 + tc), low, u[k]);
 }
 
-enum Stage { GRAM = 0, POLY = 1, NEXT = 2, LAST = 3 };
+// (TO_PAIR, TO_SINGLE: the next X of float32 products in the layout of the steps behind them)
+enum Stage { GRAM = 0, POLY = 1, NEXT = 2, LAST = 3, TO_PAIR = 4, TO_SINGLE = 5 };
 
 // What a product's epilogue reads beside four sums: A's or X's elements at their
 // place, and A's diagonal at their row and columns or B's at their row.
@@ -250,16 +274,17 @@ struct Old {
     f32x4 v, cols;
     float row;
 };
-template <bool PAIR, int STAGE>
+template <int KIND, int STAGE>
 __device__ __forceinline__ f32x4 elements_at(const Job &J, const uint8_t *X, int row, int col) {
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
     if constexpr (STAGE == GRAM) return v;
     const int32_t cols = STAGE == POLY ? J.mp : J.np;
     if (row < J.mp && col < cols) {
-        const uint8_t *p = (STAGE == POLY ? J.A : X) + place<PAIR>(row, row_bytes<PAIR>(cols), col);
+        const uint8_t *p = (STAGE == POLY ? J.A : X) + place<KIND>(row, row_bytes<KIND>(cols), col);
+        if constexpr (KIND == WHOLE) return *(const f32x4 *)p;
         v = four_of(p);
         // (A of the single products is its high parts alone)
-        if constexpr (PAIR) v += four_of(p + 64);
+        if constexpr (KIND == PAIR) v += four_of(p + 64);
         else if (STAGE != POLY) v += four_of(p + 2 * (int64_t)J.mp * J.np);
     }
     return v;
@@ -274,9 +299,9 @@ __device__ __forceinline__ f32x4 diagonals_at(const Job &J, int col) {
     if constexpr (STAGE != POLY) return f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     else return *(const f32x4 *)(J.e + min(col, J.mp - 4));
 }
-template <bool PAIR, int STAGE>
+template <int KIND, int STAGE>
 __device__ __forceinline__ Old old_at(const Job &J, const uint8_t *X, int row, int col) {
-    return Old{elements_at<PAIR, STAGE>(J, X, row, col), diagonals_at<STAGE>(J, col), diagonal_at<STAGE>(J, row)};
+    return Old{elements_at<KIND, STAGE>(J, X, row, col), diagonals_at<STAGE>(J, col), diagonal_at<STAGE>(J, row)};
 }
 // A's four elements at (row, col ..) from their sums, and B's from the sums of A' A';
 // those of the diagonal go to *diagonal and leave zero
@@ -347,13 +372,14 @@ __device__ __forceinline__ void apply(const Group &g, const Job &J, int row, int
 
 // Four sums to what the product forms.  mirror: of a tile below the diagonal of A or
 // B, whose other half they are too.
-template <bool PAIR, int STAGE>
+template <int KIND, int STAGE>
 __device__ __forceinline__ void finish(const Group &g, const Job &J, uint8_t *next, int row, int col, bool mirror,
                                        const Old &old, f32x4 v) {
+    constexpr int TO = STAGE == TO_PAIR ? PAIR : STAGE == TO_SINGLE ? SINGLE : KIND;
     const int32_t cols = STAGE <= POLY ? J.mp : J.np;
-    const int64_t bytes = row_bytes<PAIR>(cols);
+    const int64_t bytes = row_bytes<TO>(cols);
     // (A and B of the single products are their high parts alone)
-    const int64_t low = PAIR ? 64 : STAGE <= POLY ? 0 : 2 * (int64_t)J.mp * J.np;
+    const int64_t low = TO == PAIR ? 64 : STAGE <= POLY ? 0 : 2 * (int64_t)J.mp * J.np;
     const bool in = row < J.mp && col < cols;
     if constexpr (STAGE <= POLY) {
         if (in) {
@@ -361,48 +387,49 @@ __device__ __forceinline__ void finish(const Group &g, const Job &J, uint8_t *ne
             else v = poly_of(v, old.v, old.row, old.cols, row, col, J.d + row);
         }
         uint8_t *const to = STAGE == GRAM ? J.A : J.B;
-        if (in) store_parts(to + place<PAIR>(row, bytes, col), low, v);
+        if (in) store_four<TO>(to + place<TO>(row, bytes, col), low, v);
         if (mirror) {   // (all lanes exchange; mp is a multiple of 32: a block of 16 x 16 is in or out)
             v = turned(v);
-            if (in) store_parts(to + place<PAIR>(col + (row & 3), bytes, row & ~3), low, v);
+            if (in) store_four<TO>(to + place<TO>(col + (row & 3), bytes, row & ~3), low, v);
         }
     } else {
         if (!in) return;
         v = v * two_to(-kBBits) + old.v * (kCoefA + old.row);
-        if constexpr (STAGE == NEXT) store_parts(next + place<PAIR>(row, bytes, col), low, v);
+        if constexpr (STAGE != LAST) store_four<TO>(next + place<TO>(row, bytes, col), low, v);
         else apply(g, J, row, col, v * two_to(-kXBits));
     }
 }
 
-template <bool PAIR, int STAGE>
+template <int KIND, int STAGE>
 constexpr int type_of() {
-    return STAGE <= POLY ? (PAIR ? TILE_PAIR : TILE_F16) : (PAIR ? TILE_PAIR_NN : TILE_F16_NN);
+    if (KIND == WHOLE) return STAGE <= POLY ? TILE_F32 : TILE_F32_NN;
+    return STAGE <= POLY ? (KIND == PAIR ? TILE_PAIR : TILE_F16) : (KIND == PAIR ? TILE_PAIR_NN : TILE_F16_NN);
 }
 
 // A tile of a product of one of the group's matrices.  odd: X is in X1.  The
 // group's tiles are numbered matrix by matrix and dealt to the XCDs in eight
 // runs, so that a matrix is read by as few L2s as can be; within a matrix in
 // bands of `band` row tiles (A and B: tiles on and below the diagonal, row by row).
-template <bool PAIR, int STAGE, int BM, int BN>
+template <int KIND, int STAGE, int BM, int BN>
 __device__ __forceinline__ void product_of(const Group &g, const Job &J, const uint8_t *X, uint32_t at, TileProduct &p,
                                            Coord &c) {
-    constexpr int kUnit = PAIR ? 32 : 64;   // columns of a piece
+    constexpr int kUnit = KIND == SINGLE ? 64 : 32;   // columns of a piece
     p.M = J.mp;
     if constexpr (STAGE == GRAM) {
         p.A = p.B = X;
-        p.lda = p.ldb = row_bytes<PAIR>(J.np);
+        p.lda = p.ldb = row_bytes<KIND>(J.np);
         p.N = J.mp;
         p.kt = J.np / kUnit;
     } else if constexpr (STAGE == POLY) {
         p.A = p.B = J.A;
-        p.lda = p.ldb = row_bytes<PAIR>(J.mp);
+        p.lda = p.ldb = row_bytes<KIND>(J.mp);
         p.N = J.mp;
         p.kt = J.mp / kUnit;
     } else {
         p.A = J.B;
-        p.lda = row_bytes<PAIR>(J.mp);
+        p.lda = row_bytes<KIND>(J.mp);
         p.B = X;
-        p.ldb = row_bytes<PAIR>(J.np);
+        p.ldb = row_bytes<KIND>(J.np);
         p.N = J.np;
         p.kt = J.mp / kUnit;
     }
@@ -435,15 +462,15 @@ __device__ __forceinline__ void product_of(const Group &g, const Job &J, const u
     uint8_t *const next = odd ? J.X0 : J.X1;                                   \
     TileProduct p{};                                                           \
     Coord c;                                                                   \
-    product_of<PAIR, STAGE, BM, BN>(g, J, X, L - g.first[job], p, c);          \
+    product_of<KIND, STAGE, BM, BN>(g, J, X, L - g.first[job], p, c);          \
     const bool mirror = STAGE <= POLY && !g.full && c.tm != c.tn
 
 // KG groups of WM x WN wavefronts take a KG-th of the sum each, and share the tile's
 // epilogue: a launch of fewer tiles than CUs has one wavefront a SIMD and group,
 // which waits for its own copies, reads and products in turn.
-template <bool PAIR, int STAGE, int BM, int BN, int WM, int WN, int KG>
+template <int KIND, int STAGE, int BM, int BN, int WM, int WN, int KG>
 __global__ __launch_bounds__(64 * WM *WN *KG) void muon_kernel(Group g, int odd) {
-    constexpr int TYPE = type_of<PAIR, STAGE>(), T = 64 * WM * WN;
+    constexpr int TYPE = type_of<KIND, STAGE>(), T = 64 * WM * WN;
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16, kBlocks = FM * FN, kOwn = kBlocks < KG ? 1 : kBlocks / KG;
     constexpr int kLds = small_lds(TYPE, BM, BN);
     static_assert(KG == 1 || kBlocks * T * 16 <= kLds, "the groups' sums fit where the operands were");
@@ -458,7 +485,7 @@ __global__ __launch_bounds__(64 * WM *WN *KG) void muon_kernel(Group g, int odd)
 #pragma unroll
         for (int u = 0; u < kOwn; ++u) {
             const int b = u * KG + group;
-            old[u] = old_at<PAIR, STAGE>(J, X, r0 + 16 * (b / FN), c0 + 16 * (b % FN));
+            old[u] = old_at<KIND, STAGE>(J, X, r0 + 16 * (b / FN), c0 + 16 * (b % FN));
         }
     }
     f32x4 acc[FM][FN];
@@ -476,22 +503,22 @@ __global__ __launch_bounds__(64 * WM *WN *KG) void muon_kernel(Group g, int odd)
             f32x4 v = part[b * KG * T + tid];
 #pragma unroll
             for (int q = 1; q < KG; ++q) v += part[(b * KG + q) * T + tid];
-            finish<PAIR, STAGE>(g, J, next, r0 + 16 * (b / FN), c0 + 16 * (b % FN), mirror,
-                                kAhead ? old[kAhead ? u : 0] : old_at<PAIR, STAGE>(J, X, r0 + 16 * (b / FN), c0 + 16 * (b % FN)), v);
+            finish<KIND, STAGE>(g, J, next, r0 + 16 * (b / FN), c0 + 16 * (b % FN), mirror,
+                                kAhead ? old[kAhead ? u : 0] : old_at<KIND, STAGE>(J, X, r0 + 16 * (b / FN), c0 + 16 * (b % FN)), v);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                const Old o = kAhead ? old[kAhead ? i * FN + j : 0] : old_at<PAIR, STAGE>(J, X, r0 + 16 * i, c0 + 16 * j);
-                finish<PAIR, STAGE>(g, J, next, r0 + 16 * i, c0 + 16 * j, mirror, o, acc[i][j]);
+                const Old o = kAhead ? old[kAhead ? i * FN + j : 0] : old_at<KIND, STAGE>(J, X, r0 + 16 * i, c0 + 16 * j);
+                finish<KIND, STAGE>(g, J, next, r0 + 16 * i, c0 + 16 * j, mirror, o, acc[i][j]);
             }
     }
 }
-template <bool PAIR, int STAGE>
+template <int KIND, int STAGE>
 __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void muon_big_kernel(Group g, int odd) {
-    constexpr int TYPE = type_of<PAIR, STAGE>();
+    constexpr int TYPE = type_of<KIND, STAGE>();
     __shared__ __attribute__((aligned(16))) char lds[big_lds(TYPE)];
     GCN_MUON_TILE(kBigT, kBigT);
     f32x4 acc[8][4];
@@ -508,10 +535,10 @@ __global__ __launch_bounds__(kBigThreads) __attribute__((amdgpu_waves_per_eu(2, 
     for (int i = 0; i < 8; i += 2) {   // (two rows' reads at a time)
         f32x4 old[2][4];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) old[k / 4][k % 4] = elements_at<PAIR, STAGE>(J, X, r0 + 16 * (i + k / 4), c0 + 16 * (k % 4));
+        for (int k = 0; k < 8; ++k) old[k / 4][k % 4] = elements_at<KIND, STAGE>(J, X, r0 + 16 * (i + k / 4), c0 + 16 * (k % 4));
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            finish<PAIR, STAGE>(g, J, next, r0 + 16 * (i + k / 4), c0 + 16 * (k % 4), mirror,
+            finish<KIND, STAGE>(g, J, next, r0 + 16 * (i + k / 4), c0 + 16 * (k % 4), mirror,
                                 Old{old[k / 4][k % 4], cols[k % 4], rows[i + k / 4]}, acc[i + k / 4][k % 4]);
     }
 }
@@ -858,7 +885,7 @@ __global__ __launch_bounds__(kStepThreads) void step_kernel(Group g, int odd) {
 #pragma unroll 1
     for (int t = 0; t < mp / 32; ++t) mma<TILE_PAIR>(v, B.rows(br, t, lane), X.columns(t, bc, lane), 0, 0);
     v = v * two_to(-kBBits) + X.four(r0 + lr, lc) * (kCoefA + d[lr]);
-    if constexpr (STAGE == NEXT) store_parts(next + place<true>(r0 + lr, row_bytes<true>(np), first + lc), 64, v);
+    if constexpr (STAGE == NEXT) store_parts(next + place<PAIR>(r0 + lr, row_bytes<PAIR>(np), first + lc), 64, v);
     else apply(g, J, r0 + lr, first + lc, v * two_to(-kXBits));
 }
 
@@ -890,8 +917,8 @@ void plan_job(Job &J, bool pair, Arena &ar) {
     const size_t slabs = J.slab ? (size_t)(J.np + J.slab - 1) / J.slab : 0;
     J.X0 = ar.take<uint8_t>(4 * (size_t)J.mp * std::max((size_t)J.np, slabs * J.slab));
     J.X1 = ar.take<uint8_t>(4 * (size_t)J.mp * std::max((size_t)J.np, 2 * slabs * J.mp));
-    J.A = ar.take<uint8_t>((pair ? 4 : 2) * (size_t)J.mp * J.mp);
-    J.B = ar.take<uint8_t>((pair ? 4 : 2) * (size_t)J.mp * J.mp);
+    J.A = ar.take<uint8_t>(4 * (size_t)J.mp * J.mp);   // (of floats after many steps, whatever the precision)
+    J.B = ar.take<uint8_t>(4 * (size_t)J.mp * J.mp);
     J.e = ar.take<float>((size_t)J.mp);
     J.d = ar.take<float>((size_t)J.mp);
     const int64_t total = (int64_t)J.rows * J.cols;
@@ -916,7 +943,7 @@ int64_t tiles(int32_t m, int32_t n, int32_t tm, int32_t tn) {
     return (((int64_t)m + tm - 1) / tm) * (((int64_t)n + tn - 1) / tn);
 }
 
-template <bool PAIR, int STAGE>
+template <int KIND, int STAGE>
 int product(Group &g, int odd, hipStream_t s) {
     auto cols = [](const Job &J) { return STAGE <= POLY ? J.mp : J.np; };
     auto count = [&](const Job &J, int32_t tm, int32_t tn) {
@@ -932,7 +959,7 @@ int product(Group &g, int odd, hipStream_t s) {
     bool deep = true, long_k = false;
     for (int j = 0; j < g.count; ++j) {
         const Job &J = g.job[j];
-        long_k = long_k || J.np >= 16 * (PAIR ? 32 : 64);
+        long_k = long_k || J.np >= 16 * (KIND == SINGLE ? 64 : 32);
         deep = deep && J.mp >= 256 && J.np < (1 << 22);   // (a large tile's row offsets within it: 32 bits)
         const double m = std::min(J.rows, J.cols), n = std::max(J.rows, J.cols);
         flops += STAGE == GRAM ? m * m * n : STAGE == POLY ? m * m * m : 2.0 * m * m * n;
@@ -951,14 +978,14 @@ int product(Group &g, int odd, hipStream_t s) {
 #define GCN_MUON(BM, BN, WM, WN, KG)                                                                             \
     do {                                                                                                         \
         const dim3 b = grid(BM, BN);                                                                             \
-        hipLaunchKernelGGL((muon_kernel<PAIR, STAGE, BM, BN, WM, WN, KG>), b, dim3(64 * WM * WN * KG), 0, s, g, odd); \
+        hipLaunchKernelGGL((muon_kernel<KIND, STAGE, BM, BN, WM, WN, KG>), b, dim3(64 * WM * WN * KG), 0, s, g, odd); \
     } while (0)
     // us a call of five steps, the two ways on either side of each border (taken with the diagonals still within A
     // and B, 1 to 2 % faster throughout).  Large tiles for a X + B X: 3000 x 3200 (156 of them) 2185 with 128 x 128
     // ones, 2121 with large; for A and B 3000 x 3200 (78) 2185 and 2850, 3400 x 3400 in GCN_BF16 (105) 1099 and 1386.
-    if (deep && all(kBigT, kBigT) >= (STAGE <= POLY ? 120 : 150)) {
+    if (KIND != WHOLE && deep && all(kBigT, kBigT) >= (STAGE <= POLY ? 120 : 150)) {
         const dim3 b = grid(kBigT, kBigT);
-        hipLaunchKernelGGL((muon_big_kernel<PAIR, STAGE>), b, dim3(kBigThreads), 0, s, g, odd);
+        if constexpr (KIND != WHOLE) hipLaunchKernelGGL((muon_big_kernel<KIND, STAGE>), b, dim3(kBigThreads), 0, s, g, odd);
     } else if constexpr (STAGE <= POLY) {
         // 32 x 32 tiles while they are few: a CU's own path to its L2 carries 64 bytes a cycle, and few tiles leave
         // most of the CUs, and their paths, idle (four of 602 x 128 and 256 x 128: 118 with 64 x 64 ones, 93 so; 700 x
@@ -986,11 +1013,12 @@ int product(Group &g, int odd, hipStream_t s) {
     return GCN_OK;
 }
 
-template <bool PAIR>
-int run_group(Group &g, int32_t steps, hipStream_t s) {
-    bool small = PAIR, few = PAIR, narrow = PAIR;
+// `ahead`: the first steps, in float32.
+template <int KIND>
+int run_group(Group &g, int32_t steps, int32_t ahead, hipStream_t s) {
+    bool small = KIND == PAIR && ahead == 0, few = small, narrow = KIND == PAIR;
     double flops = 0.0;
-    if constexpr (PAIR) {
+    if constexpr (KIND == PAIR) {
         int64_t blocks = 0;
         int32_t most = 0;
         for (int j = 0; j < g.count; ++j) {
@@ -1020,7 +1048,7 @@ int run_group(Group &g, int32_t steps, hipStream_t s) {
         hipLaunchKernelGGL(momentum_kernel, b, dim3(kTB), 0, s, g);
         GCN_LAUNCH_CHECK("momentum_kernel");
     }
-    if (PAIR && few) {
+    if (KIND == PAIR && few) {
         const dim3 b(blocks_of(g, [](const Job &J) { return (uint64_t)(J.np + J.slab - 1) / J.slab; }));
         for (int32_t k = -1; k < steps; ++k) {
             ProfScope prof(K_MUON_SMALL, s, flops / steps, 0.0);
@@ -1032,14 +1060,21 @@ int run_group(Group &g, int32_t steps, hipStream_t s) {
     {
         ProfScope prof(K_MUON_PREP, s, 0.0, bytes);
         const dim3 b = dim3(blocks_of(g, [](const Job &J) { return (uint64_t)tiles(J.mp, J.np, 64, 64); }));
-        hipLaunchKernelGGL(operand_kernel<PAIR>, b, dim3(kTB), 0, s, g);
+        if (ahead) hipLaunchKernelGGL(operand_kernel<WHOLE>, b, dim3(kTB), 0, s, g);
+        else hipLaunchKernelGGL(operand_kernel<KIND>, b, dim3(kTB), 0, s, g);
         GCN_LAUNCH_CHECK("operand_kernel");
     }
     int rc;
     for (int32_t k = 0; k < steps; ++k) {
         const int odd = k & 1;
-        if (PAIR && narrow) {
-            if ((rc = product<PAIR, GRAM>(g, odd, s))) return rc;
+        if (k < ahead) {
+            if ((rc = product<WHOLE, GRAM>(g, odd, s)) || (rc = product<WHOLE, POLY>(g, odd, s))) return rc;
+            constexpr int TO = KIND == PAIR ? TO_PAIR : TO_SINGLE;
+            if ((rc = k + 1 < ahead ? product<WHOLE, NEXT>(g, odd, s) : product<WHOLE, TO>(g, odd, s))) return rc;
+            continue;
+        }
+        if (KIND == PAIR && narrow) {
+            if ((rc = product<KIND, GRAM>(g, odd, s))) return rc;
             ProfScope prof(K_MUON_PRODUCT, s, flops / steps, 0.0);
             const dim3 b(blocks_of(g, [](const Job &J) { return (uint64_t)step_blocks(J); }));
             if (k + 1 < steps) hipLaunchKernelGGL(step_kernel<NEXT>, b, dim3(kStepThreads), 0, s, g, odd);
@@ -1047,14 +1082,15 @@ int run_group(Group &g, int32_t steps, hipStream_t s) {
             GCN_LAUNCH_CHECK("step_kernel");
             continue;
         }
-        if ((rc = product<PAIR, GRAM>(g, odd, s)) || (rc = product<PAIR, POLY>(g, odd, s))) return rc;
-        if ((rc = k + 1 < steps ? product<PAIR, NEXT>(g, odd, s) : product<PAIR, LAST>(g, odd, s))) return rc;
+        if ((rc = product<KIND, GRAM>(g, odd, s)) || (rc = product<KIND, POLY>(g, odd, s))) return rc;
+        if ((rc = k + 1 < steps ? product<KIND, NEXT>(g, odd, s) : product<KIND, LAST>(g, odd, s))) return rc;
     }
     return GCN_OK;
 }
-int run_group(Group &g, int32_t steps, bool pairs, hipStream_t s) {
+int run_group(Group &g, int32_t steps, int prec, bool pairs, hipStream_t s) {
     if (g.count == 0) return GCN_OK;
-    return pairs ? run_group<true>(g, steps, s) : run_group<false>(g, steps, s);
+    const int32_t ahead = std::max(0, steps - (prec == GCN_F32 ? kPairSteps : kSingleSteps));
+    return pairs ? run_group<PAIR>(g, steps, ahead, s) : run_group<SINGLE>(g, steps, ahead, s);
 }
 
 constexpr int32_t kMostSide = 65536;   // (tile counts and row offsets of a launch within 32 bits)
@@ -1141,7 +1177,7 @@ int gcn_orthogonalise(const void *X, gcn_rows_type type, int32_t rows, int32_t c
     plan_job(J, pairs, ar);
     g.count = 1;
     g.grad_bf16 = g.out_bf16 = type == GCN_ROWS_BF16;
-    return run_group(g, steps, pairs, (hipStream_t)stream);
+    return run_group(g, steps, prec, pairs, (hipStream_t)stream);
 }
 
 size_t gcn_muon_workspace_bytes(int32_t count, const gcn_muon_matrix *mats, int prec) {
@@ -1231,7 +1267,7 @@ int gcn_muon_update(int32_t count, const gcn_muon_matrix *mats, gcn_rows_type gr
         g.decay = (float)(1.0 - lr * weight_decay);
         g.nesterov = nesterov != 0;
         g.grad_bf16 = grad_type == GCN_ROWS_BF16;
-        if ((rc = run_group(g, steps, pairs, (hipStream_t)stream))) return rc;
+        if ((rc = run_group(g, steps, prec, pairs, (hipStream_t)stream))) return rc;
     }
     return GCN_OK;
 }
