@@ -68,7 +68,9 @@ typedef struct {
  *     M <- momentum M + G;   U = G + momentum M with nesterov != 0, else M
  *     W <- (1 - lr weight_decay) W - lr scale orthogonalised(U)
  * The coefficients are formed in double and rounded once.  No W or M overlaps
- * another matrix of the call. */
+ * another matrix of the call.  Up to 16 matrices share their launches, whose tiles and
+ * parts of sums go by all of them: a call repeats its bits, but a matrix's last
+ * bits can depend on what else is updated with it. */
 size_t gcn_muon_workspace_bytes(int32_t count, const gcn_muon_matrix *mats, int prec);
 int gcn_muon_update(int32_t count, const gcn_muon_matrix *mats, gcn_rows_type grad_type, double lr, double momentum,
                     int nesterov, double weight_decay, int32_t steps, int prec, void *ws, size_t ws_bytes,
