@@ -50,7 +50,9 @@ extern "C" {
  * A block with the largest magnitude a = m 2^k (1 <= m < 2) gets the scale 2^e,
  * e = k - 2 where m <= 1.5, else k - 1 (so that no value is beyond 6), held
  * within -126 .. 127 (a = 0: e = 0), and the values are x 2^-e rounded to the
- * nearest e2m1, ties to even.  A block with a value that is not finite gets s = 255
+ * nearest e2m1, ties to even.  (Other writers of such rows take 2^(k - 2) throughout
+ * and let what is beyond 6 saturate: theirs multiply and read back as they stand
+ * for, but are not the same bits.)  A block with a value that is not finite gets s = 255
  * and stands for NaN throughout: four bits have no NaN. */
 typedef struct {
     int32_t n, f;

@@ -341,8 +341,7 @@ __device__ __forceinline__ void small_loop(const TileProduct &p, const Coord &c,
                 const Frag fa = frag(ta, wm * (BM / WM) + 16 * i.value, false);
                 static_for<FN>([&](auto j) { mma4<i.value, j.value>(acc[i.value][j.value], fa, fb[j.value], a4, b4); });
             });
-        } else
-        if constexpr (TYPE == TILE_FP8_EXACT) {
+        } else if constexpr (TYPE == TILE_FP8_EXACT) {
             bf16v8 wb[FN][4];
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
@@ -565,19 +564,20 @@ __device__ __forceinline__ void big_loop(const TileProduct &p, const Coord &c, i
     auto quarter = [&](auto hh, auto kk, const Frag (&b)[2]) {   // rows half h, columns half k
         constexpr int h = decltype(hh)::value, k = decltype(kk)::value;
         __builtin_amdgcn_s_setprio(1);
-        if constexpr (TYPE == TILE_FP4)
+        if constexpr (TYPE == TILE_FP4) {
             static_for<2>([&](auto j) {
                 static_for<4>([&](auto i) {
                     mma4<i.value, 2 * k + j.value>(acc[4 * h + i.value][2 * k + j.value], fa[i.value], b[j.value], a4[h], b4);
                 });
             });
-        else
+        } else {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            mma_big<TYPE, 0>(acc[4 * h + 0][2 * k + j], fa[0], b[j], sa[h], sb);
-            mma_big<TYPE, 1>(acc[4 * h + 1][2 * k + j], fa[1], b[j], sa[h], sb);
-            mma_big<TYPE, 2>(acc[4 * h + 2][2 * k + j], fa[2], b[j], sa[h], sb);
-            mma_big<TYPE, 3>(acc[4 * h + 3][2 * k + j], fa[3], b[j], sa[h], sb);
+            for (int j = 0; j < 2; ++j) {
+                mma_big<TYPE, 0>(acc[4 * h + 0][2 * k + j], fa[0], b[j], sa[h], sb);
+                mma_big<TYPE, 1>(acc[4 * h + 1][2 * k + j], fa[1], b[j], sa[h], sb);
+                mma_big<TYPE, 2>(acc[4 * h + 2][2 * k + j], fa[2], b[j], sa[h], sb);
+                mma_big<TYPE, 3>(acc[4 * h + 3][2 * k + j], fa[3], b[j], sa[h], sb);
+            }
         }
         // (the sums are pinned here, or the compiler moves the products past the barriers)
         asm volatile("" : "+v"(acc[4 * h][2 * k]), "+v"(acc[4 * h + 1][2 * k]), "+v"(acc[4 * h + 2][2 * k]),
