@@ -70,7 +70,8 @@ typedef struct {
  * The coefficients are formed in double and rounded once.  No W or M overlaps
  * another matrix of the call.  Up to 16 matrices share their launches, whose tiles and
  * parts of sums go by all of them: a call repeats its bits, but a matrix's last
- * bits can depend on what else is updated with it. */
+ * bits can depend on what else is updated with it, and one of thousands of rows and
+ * columns is faster in a call without small ones. */
 size_t gcn_muon_workspace_bytes(int32_t count, const gcn_muon_matrix *mats, int prec);
 int gcn_muon_update(int32_t count, const gcn_muon_matrix *mats, gcn_rows_type grad_type, double lr, double momentum,
                     int nesterov, double weight_decay, int32_t steps, int prec, void *ws, size_t ws_bytes,

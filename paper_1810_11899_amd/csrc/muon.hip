@@ -49,7 +49,10 @@ namespace gcn {
 namespace {
 
 constexpr int kTB = 256;
-constexpr int kGroup = 16;        // matrices of a launch
+// Matrices of a launch.  Which way of working and which tiles it takes goes by all of them: one with a short side takes
+// the 256 x 256 tiles from a wide one (us, 4096 x 4096 and 602 x 128 in one call 4590, in two 3900 + 75; GCN_BF16 2150,
+// 1750 + 85), while of like ones the launches are shared (602 x 128 and 50 x 64 75, 75 + 21).
+constexpr int kGroup = 16;
 constexpr int kMostParts = 1024;  // of a matrix's sum of squares
 constexpr int kXBits = 15, kABits = 14, kBBits = 13;   // what X, A and B are scaled by
 constexpr float kCoefA = 3.4445f, kCoefB = -4.7750f, kCoefC = 2.0315f;

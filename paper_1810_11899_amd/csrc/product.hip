@@ -573,9 +573,10 @@ TileShape tile_shape(TileType type, const TileProduct &p) {
         if (splits > 1) return t128 * splits >= 192 && per >= 16 ? TileShape{128, 128} : TileShape{64, 64};   // (split4)
         // (us, few rows / 64 x 64: 64 x 4096 x 4096 7.3 / 7.8, 32 rows 6.5 / 7.8; 64 x 512 x 1024 6.5 / 6.6)
         if (p.M <= kThin) return TileShape{kThin, 16};
-        // us, 64 x 64 / 128 x 128 / 256 x 256 (the first two 0.3 less since): 6205 x 512 x 602 6.6 / 7.0 / 12.0, 8000 x
-        // 512 x 1024 7.4 / 7.7 / 13.5, 2000 x 2048 x 2048 11.2 / 10.5 / 19.7, 16,384 x 512 x 512 9.8 / 8.7 / 11.9, 4000 x
-        // 4096 x 1024 23.4 / 19.3 / 18.2, float32 results 24.4 / 31 / 25; 8000 x 2048 x 2048 float32 38 / 36 / 29
+        // us, 64 x 64 / 128 x 128 / 256 x 256, bfloat16 results (the first two 0.3 less since): 6205 x 512 x 602 6.6 / 7.0 /
+        // 12.0, 8000 x 512 x 1024 7.4 / 7.7 / 13.5, 2000 x 2048 x 2048 11.2 / 10.5 / 19.7, 16,384 x 512 x 512 9.8 / 8.7 /
+        // 11.9, 4000 x 4096 x 1024 23.4 / 19.3 / 18.2; float32 results 24.4 / 31 / 25, 8000 x 2048 x 2048 38 / 36 / 29 (as
+        // chosen, 6205 x 512 x 602 7.9, 8000 x 512 x 1024 9.3, 2000 x 2048 x 2048 11.7, 16,384 x 512 x 512 11.3)
         if (tiles_of(p.M, p.N, kBigT) >= 160 && per >= 4 && std::max(p.lda, p.ldb) < (1 << 24)) return TileShape{kBigT, kBigT};
         return t128 < 256 ? TileShape{64, 64} : TileShape{128, 128};
     }

@@ -280,7 +280,8 @@ int check_rows4(const gcn_rows4 *r, const char *who) {
 // Parts of a product's sum, for products with few tiles and long sums (weight
 // gradients): 128 x 128 tiles, two a CU and 16 pieces a part or more, where they fill the
 // CUs, else 64 x 64 ones of 8 pieces.  Parts are written and read again, which
-// costs about 3 us and 0.4 us a megabyte (us, in 1 / 2 / 4 / 8 / 16 parts, float32 results;
+// costs about 3 us and 0.4 us a megabyte (us, in 1 / 2 / 4 / 8 / 16 parts, float32 results, the
+// operands in the caches; 1024 x 512 x 65,536 is 36 where they are others every call;
 // 64 x 64: 1024 x 512 x 8000 12.6 / 12.0 / 13.3, 512 x 256 x 8000 12.2 / 9.9 / 9.5 / 9.7,
 // 256 x 256 x 32,000 38 / 22 / 14.5 / 11.7 / 11.5, 1024 x 1024 x 8192 13.3 / 16.4; 128 x 128:
 // 1024 x 512 x 65,536 151 / 84 / 48 / 32 / 33, 1024 x 1024 x 65,536 156 / 85 / 52 / 45 / 61, 64 x 64
