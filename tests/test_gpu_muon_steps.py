@@ -170,3 +170,29 @@ def test_large_sides_of_many_steps(rows, cols, ws):
         # (GCN_BF16: twelve steps in float16, each within 2^-9; a step carries that on by -1.58 at the fixed point 0.868, by
         # 1.2 around the cycle 0.70, 1.11: 1.45 taken.  A lost part or a wrong index is off by about one.)
         assert err <= (4 * plain + 2.0 ** -21 if prec == B.GCN_F32 else 2.0 ** -9 * sum(1.45 ** k for k in range(12))), prec
+
+
+@pytest.mark.parametrize("rows, cols", [(40, 70), (300, 200)])
+@pytest.mark.parametrize("prec, steps", [(B.GCN_F32, 7), (B.GCN_BF16, 13), (B.GCN_F32, 64)])
+def test_zeros_and_values_that_are_not_finite(rows, cols, prec, steps, ws):
+    x = torch.zeros((rows, cols), device="cuda")
+    out = torch.full_like(x, 5.0)
+    B.gcn_orthogonalise(x, out, ws, steps=steps, prec=prec)
+    assert not out.any()
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        x = torch.randn((rows, cols), device="cuda")
+        x[7, 9] = bad
+        B.gcn_orthogonalise(x, out, ws, steps=steps, prec=prec)
+        assert bool(torch.isnan(out).all())
+
+
+@pytest.mark.parametrize("rows, cols", [(70, 90), (300, 200)])
+def test_scale_does_not_matter(rows, cols, ws):
+    """A power of two changes no bit; the matrix may be its own result; bfloat16 results are float32's, rounded."""
+    x = torch.randn((rows, cols), generator=torch.Generator().manual_seed(rows)).bfloat16().float().cuda()
+    base = B.gcn_orthogonalise(x, torch.empty_like(x), ws, steps=10)
+    for k in (-100, -20, 60, 120):
+        assert torch.equal(B.gcn_orthogonalise(x * 2.0 ** k, torch.empty_like(x), ws, steps=10), base), k
+    half = x.bfloat16()
+    assert torch.equal(B.gcn_orthogonalise(half, half, ws, steps=10), base.bfloat16())
+    assert torch.equal(B.gcn_orthogonalise(x, x, ws, steps=10), base)
