@@ -196,3 +196,27 @@ def test_scale_does_not_matter(rows, cols, ws):
     half = x.bfloat16()
     assert torch.equal(B.gcn_orthogonalise(half, half, ws, steps=10), base.bfloat16())
     assert torch.equal(B.gcn_orthogonalise(x, x, ws, steps=10), base)
+
+
+@pytest.mark.parametrize("tall", [False, True])
+@pytest.mark.parametrize("prec, steps", [(B.GCN_F32, 2), (B.GCN_BF16, 2), (B.GCN_F32, 7)])
+def test_matrices_past_32_bit_offsets(prec, steps, tall, ws):
+    """More than 2^31 elements, one in each row: what every row comes to is known, and everything else is zero."""
+    rows, cols = 36_000, 60_000
+    i = torch.arange(rows, device="cuda")
+    at = i * 5 // 3
+    s = torch.logspace(0, -2, rows, dtype=torch.float64, device="cuda")[i * 7 % rows].float()
+    u = torch.zeros((cols, rows) if tall else (rows, cols), device="cuda")
+    place = (at, i) if tall else (i, at)
+    u[place] = s
+    out = torch.full_like(u, 5.0)
+    B.gcn_orthogonalise(u, out, ws, steps=steps, prec=prec)
+    x = s.double() / s.double().norm()
+    for _ in range(steps):
+        x = polynomial(x)
+    # A step's few roundings of 2^-22 (float16's of e, 2^-10 of a term below 2^-9 of the factor, x being below 0.02 at the
+    # start): below 2^-20, and not larger in the next, where |x p'(x) / p(x)| < 1 up to 0.7.  Beyond, which more than
+    # three steps reach, it is below 5: three such steps 2^7
+    assert float(((out[place].double() - x) / x).abs().max()) < 2.0 ** (-17 if steps == 2 else -13)
+    out[place] = 0.0
+    assert not out.any()
